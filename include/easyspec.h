@@ -11,6 +11,10 @@
  *   - easyspec_greedy_accept  acceptance of drafted tokens at temperature 0 (paper Alg. 3)
  *   - easyspec_accept         acceptance by speculative sampling at a temperature > 0
  *                             (paper Alg. 3, bonus distribution of Sec. 2.1)
+ *   - easyspec_beam_select, easyspec_kv_reorder   the best continuations of a group of beams, and the
+ *                             beams' caches in the order of their parents
+ *   - easyspec_attn_weights, easyspec_kv_evict    the attention weight that cached slots receive, and a
+ *                             cache thinned by it
  *
  * Model function: pre-norm decoder with RMSNorm, rotary embedding (pairs i, i + head_dim/2),
  * grouped-query attention (query head j reads KV head j / (n_q_heads/n_kv_heads)), SwiGLU MLP,
@@ -252,6 +256,101 @@ int easyspec_accept_static(const int32_t *draft, const float *draft_logits, cons
                            const float *u, int32_t batch, int32_t gamma, int32_t vocab, float temperature,
                            int32_t *accept_len, int32_t *bonus, void *hip_stream);
 int64_t easyspec_accept_static_max_bytes(void);
+
+/* ---- Drafting with beams ------------------------------------------------------------------------------------ */
+
+#define EASYSPEC_MAX_BEAMS 64        /* beams of one group */
+#define EASYSPEC_MAX_SELECT 64       /* continuations one easyspec_beam_select call picks per group */
+#define EASYSPEC_MAX_BEAM_VOCAB 1048576
+
+/* The n_select best continuations of every group of beams, over all its beams and the whole vocabulary:
+ *   score(w, v) = scores[w] + logits[w][v] / temperature - log sum_u exp(logits[w][u] / temperature)
+ * in descending order; of equal scores the lowest beam comes first, of one beam's candidates the highest logit, of equal
+ * logits the lowest token.  Scores are compared in double precision.
+ *   logits      dev [groups][beams][vocab]  fp32, as easyspec_draft_step and easyspec_draft_tree_step write them
+ *   scores      dev [groups][beams]         fp32, cumulative log-probability of the beam; a beam of minus infinity (or NaN) offers
+ *                                           no continuation and its logits are not read
+ *   ended       dev [groups][beams] or NULL nonzero: the beam has ended; it offers one continuation, end_token, at its own
+ *                                           score, and its logits are not read
+ *   tokens_out  dev [groups][n_select]      the token; -1 where a group has fewer continuations than n_select
+ *   parents_out dev [groups][n_select]      the beam it continues, 0..beams-1, or -1
+ *   scores_out  dev [groups][n_select]      fp32, or minus infinity; may be `scores` if n_select == beams
+ *   workspace   dev, easyspec_beam_select_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ *   hip_stream  the hipStream_t to launch on (NULL = the null stream); nothing is synchronised
+ * Logits of minus infinity and NaN are no continuations and add nothing to the sum; a beam with a logit of plus infinity, or
+ * with none that is finite, offers nothing.  A beam selection over sequences 0..beams-1 of a context takes the logits of a
+ * draft step as they are; over the nodes of a tree level, beams is EASYSPEC_MAX_TREE_WIDTH and the scores of unused rows are
+ * minus infinity.  EASYSPEC_EINVAL for NULL pointers, groups or vocab < 1, groups * beams > 65535, beams, n_select or vocab
+ * beyond the limits above, an end_token outside the vocabulary if `ended` is given, a temperature that is not positive and
+ * finite, or outputs that are not device memory. */
+int easyspec_beam_select(const float *logits, const float *scores, const int32_t *ended, int32_t groups, int32_t beams, int32_t vocab,
+                         int32_t n_select, float temperature, int32_t end_token, int32_t *tokens_out, int32_t *parents_out,
+                         float *scores_out, void *workspace, void *hip_stream);
+int64_t easyspec_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_select); /* -1 for bad arguments */
+
+/* Caches of the caller, as a context holds them: K and V apart, [n_layers][n_seqs][n_kv_heads][max_slots][head_dim] in dtype,
+ * contiguous, 16-byte aligned. */
+typedef struct easyspec_kv_layout {
+  int32_t n_layers;
+  int32_t n_seqs;     /* 1..EASYSPEC_MAX_BATCH */
+  int32_t n_kv_heads;
+  int32_t max_slots;  /* 1..65536 */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t dtype;      /* EASYSPEC_DTYPE_* */
+} easyspec_kv_layout;
+
+/* Beams' caches in the order of their parents.  The sequences are groups of `beams` (which divides n_seqs); in every layer and
+ * KV head, sequence i of k_out, v_out receives the slots [from_slot, to_slot) of sequence
+ * i - i % beams + parents[i] of k, v.  A parent outside 0..beams-1 (easyspec_beam_select's -1) stands for the sequence itself.
+ *   k, v, k_out, v_out  dev  k_out == k and v_out == v (in place) or arrays apart from both
+ *   parents             dev [n_seqs]
+ * Other slots of k_out, v_out are left as they were.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for
+ * NULL pointers, a bad layout or slot range, beams that do not divide n_seqs, arrays that overlap in part or are not 16-byte
+ * aligned, or outputs that are not device memory. */
+int easyspec_kv_reorder(const void *k, const void *v, const easyspec_kv_layout *layout, const int32_t *parents, int32_t beams,
+                        int32_t from_slot, int32_t to_slot, void *k_out, void *v_out, void *hip_stream);
+
+/* ---- Bounded caches ----------------------------------------------------------------------------------------- */
+
+/* The attention weight that cached slots receive from new tokens: in every layer and KV head,
+ *   weights_out[s] = weights_in[s] + sum over the sequence's new tokens and the query heads of the KV head of
+ *                    softmax_s(q . k_s / sqrt(head_dim))
+ * The new tokens of sequence b, n_tokens[b] of them, are its last: token t sits in slot lens[b] - n_tokens[b] + t and attends
+ * to the slots up to its own (causal, as a calibration).
+ *   q            dev fp32 [n_layers][sum of n_tokens][n_q_heads][head_dim]  rotated queries, sequences in index order
+ *   k            dev      layout (keys with the new tokens' among them)
+ *   n_tokens     host [n_seqs]  0..EASYSPEC_MAX_CALIB_TOKENS; 0: the sequence is left alone
+ *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots
+ *   n_q_heads    n_kv_heads times 1, 2, 4, 7 or 8
+ *   weights_in   dev fp32 [n_layers][n_seqs][n_kv_heads][max_slots], read up to the new tokens' slots, which start from zero;
+ *                NULL: zeros
+ *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
+ *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
+ * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers, a bad layout, counts or lengths, arrays
+ * that are not 16-byte aligned (weights: 4), or weights_out that is not device memory. */
+int easyspec_attn_weights(const float *q, const void *k, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
+                          int32_t n_q_heads, const float *weights_in, float *weights_out, void *workspace, void *hip_stream);
+int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
+                                              int32_t n_q_heads); /* -1 for bad arguments */
+
+/* A cache thinned: of sequence b min(keep[b], lens[b]) slots stay, in every layer and KV head its own: the last
+ * min(recent, keep[b]) and, of the slots before them, the heaviest (of equal weights the lowest slot; a NaN is lighter than any
+ * number).  They keep their order: slot j of the result is the j-th of the slots that stayed.
+ *   k, v         dev layout
+ *   weights      dev fp32 [n_layers][n_seqs][n_kv_heads][max_slots]
+ *   lens, keep   host [n_seqs], 0..max_slots and >= 0; nothing is done for a sequence of which nothing stays
+ *   out_slots    max_slots of the results, 1..65536
+ *   k_out, v_out dev, the layout with out_slots; k_out == k, v_out == v and weights_out == weights with
+ *                out_slots == max_slots (in place), or arrays apart from all inputs
+ *   weights_out  dev fp32 [n_layers][n_seqs][n_kv_heads][out_slots]  the weights of the slots that stayed
+ *   slots_out    dev [n_layers][n_seqs][n_kv_heads][out_slots]       which they were
+ * Results from a sequence's last slot on are left as they were.  Keys keep the rotary positions that they were written with.
+ * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers, a bad layout or lengths, more slots to
+ * stay than out_slots, arrays that overlap in part or are not 16-byte aligned (weights, slots: 4), or outputs that are not
+ * device memory. */
+int easyspec_kv_evict(const void *k, const void *v, const float *weights, const easyspec_kv_layout *layout, const int32_t *lens,
+                      const int32_t *keep, int32_t recent, int32_t out_slots, void *k_out, void *v_out, float *weights_out,
+                      int32_t *slots_out, void *hip_stream);
 
 /* Host copies of the per-sequence lengths; each of precise, fuzzy: host [max_batch] or NULL. */
 int easyspec_get_lens(const easyspec_ctx *ctx, int32_t *precise, int32_t *fuzzy);

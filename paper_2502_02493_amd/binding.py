@@ -18,12 +18,15 @@ EASYSPEC_MAX_BATCH, EASYSPEC_MAX_CALIB_TOKENS, EASYSPEC_MAX_SET = 16, 16, 8
 EASYSPEC_MAX_TREE_WIDTH, EASYSPEC_MAX_TREE_NODES = 16, 64
 EASYSPEC_MAX_CHUNKS = 64
 EASYSPEC_PARALLEL_ATTENTION, EASYSPEC_PARALLEL_FULL_LAYER = 0, 1
+EASYSPEC_MAX_BEAMS, EASYSPEC_MAX_SELECT, EASYSPEC_MAX_BEAM_VOCAB = 64, 64, 1048576
 
 EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easyspec_set_groups",
            "easyspec_default_groups", "easyspec_draft_step", "easyspec_calibrate", "easyspec_greedy_accept", "easyspec_greedy_accept_host",
            "easyspec_accept", "easyspec_accept_give_up", "easyspec_accept_workspace_bytes", "easyspec_accept_static", "easyspec_accept_static_max_bytes", "easyspec_draft_tree_step", "easyspec_set_parallel_mode", "easyspec_stream_read", "easyspec_stream_read_sink_floats", "easyspec_attention_cut", "easyspec_attention_route", "easyspec_weight_walk", "easyspec_wide_walk", "easyspec_attention_stage_walk",
            "easyspec_get_lens", "easyspec_truncate", "easyspec_kv_import", "easyspec_kv_export",
            "easyspec_get_hidden", "easyspec_poison_workspaces", "easyspec_force_give_up", "easyspec_step_bytes", "easyspec_profile_begin", "easyspec_profile_end",
+           "easyspec_beam_select", "easyspec_beam_select_workspace_bytes", "easyspec_kv_reorder",
+           "easyspec_attn_weights", "easyspec_attn_weights_workspace_bytes", "easyspec_kv_evict",
            "easyspec_last_error"]
 EASYSPEC_OP_QKV, EASYSPEC_OP_ATTN, EASYSPEC_OP_OPROJ, EASYSPEC_OP_GATEUP, EASYSPEC_OP_DOWN, EASYSPEC_OP_HEAD, EASYSPEC_OP_ALL = range(7)
 
@@ -48,6 +51,10 @@ class easyspec_layer_weights(C.Structure):
 class easyspec_weights(C.Structure):
     _fields_ = [("layers", C.POINTER(easyspec_layer_weights)), ("embed", C.c_void_p), ("lm_head", C.c_void_p),
                 ("g_final", C.c_void_p)]
+
+
+class easyspec_kv_layout(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seqs", "n_kv_heads", "max_slots", "head_dim", "dtype")]
 
 
 _lib = None
@@ -80,6 +87,15 @@ def load_library():
         L.easyspec_accept_static_max_bytes.restype = C.c_int64
         L.easyspec_accept_workspace_bytes.argtypes = [i32, i32, i32]
         L.easyspec_accept_workspace_bytes.restype = C.c_int64
+        kvl = C.POINTER(easyspec_kv_layout)
+        L.easyspec_beam_select.argtypes = [vp, vp, vp, i32, i32, i32, i32, C.c_float, i32, vp, vp, vp, vp, vp]
+        L.easyspec_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.easyspec_beam_select_workspace_bytes.restype = C.c_int64
+        L.easyspec_kv_reorder.argtypes = [vp, vp, kvl, vp, i32, i32, i32, vp, vp, vp]
+        L.easyspec_attn_weights.argtypes = [vp, vp, kvl, vp, vp, i32, vp, vp, vp, vp]
+        L.easyspec_attn_weights_workspace_bytes.argtypes = [kvl, vp, vp, i32]
+        L.easyspec_attn_weights_workspace_bytes.restype = C.c_int64
+        L.easyspec_kv_evict.argtypes = [vp, vp, vp, kvl, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         L.easyspec_get_lens.argtypes = [vp, vp, vp]
         L.easyspec_truncate.argtypes = [vp, i32, i32]
         L.easyspec_kv_import.argtypes = [vp, i32, vp, vp, i32]
@@ -232,6 +248,46 @@ def easyspec_accept_static_max_bytes() -> int:
 
 def easyspec_accept_workspace_bytes(batch: int, gamma: int, vocab: int) -> int:
     return int(load_library().easyspec_accept_workspace_bytes(batch, gamma, vocab))
+
+
+def easyspec_beam_select(logits, scores, ended, groups, beams, vocab, n_select, temperature, end_token, tokens_out, parents_out,
+                         scores_out, workspace, hip_stream=None):
+    _check(load_library().easyspec_beam_select(_ptr(logits), _ptr(scores), _ptr(ended), groups, beams, vocab, n_select,
+                                               float(temperature), end_token, _ptr(tokens_out), _ptr(parents_out), _ptr(scores_out),
+                                               _ptr(workspace), _ptr(hip_stream)), None)
+
+
+def easyspec_beam_select_workspace_bytes(groups: int, beams: int, vocab: int, n_select: int) -> int:
+    return int(load_library().easyspec_beam_select_workspace_bytes(groups, beams, vocab, n_select))
+
+
+def _host_ints(x, n):
+    a = np.ascontiguousarray(x, dtype=np.int32)
+    assert a.size == n
+    return a
+
+
+def easyspec_kv_reorder(k, v, layout: easyspec_kv_layout, parents, beams, from_slot, to_slot, k_out, v_out, hip_stream=None):
+    _check(load_library().easyspec_kv_reorder(_ptr(k), _ptr(v), C.byref(layout), _ptr(parents), beams, from_slot, to_slot, _ptr(k_out),
+                                              _ptr(v_out), _ptr(hip_stream)), None)
+
+
+def easyspec_attn_weights(q, k, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, weights_in, weights_out, workspace, hip_stream=None):
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    _check(load_library().easyspec_attn_weights(_ptr(q), _ptr(k), C.byref(layout), _ptr(n), _ptr(s), n_q_heads, _ptr(weights_in),
+                                                _ptr(weights_out), _ptr(workspace), _ptr(hip_stream)), None)
+
+
+def easyspec_attn_weights_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads) -> int:
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    return int(load_library().easyspec_attn_weights_workspace_bytes(C.byref(layout), _ptr(n), _ptr(s), n_q_heads))
+
+
+def easyspec_kv_evict(k, v, weights, layout: easyspec_kv_layout, lens, keep, recent, out_slots, k_out, v_out, weights_out, slots_out,
+                      hip_stream=None):
+    n, s = _host_ints(lens, layout.n_seqs), _host_ints(keep, layout.n_seqs)
+    _check(load_library().easyspec_kv_evict(_ptr(k), _ptr(v), _ptr(weights), C.byref(layout), _ptr(n), _ptr(s), recent, out_slots,
+                                            _ptr(k_out), _ptr(v_out), _ptr(weights_out), _ptr(slots_out), _ptr(hip_stream)), None)
 
 
 def easyspec_stream_read(buf, nbytes: int, sink, hip_stream=None):

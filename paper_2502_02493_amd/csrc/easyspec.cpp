@@ -1,6 +1,6 @@
 // Host side of the EasySpec C ABI (include/easyspec.h): argument checks, the per-sequence
 // precise / fuzzy length state machine, weight repacking, and the launch sequence of one
-// forward pass.  All arithmetic of the method runs in the kernels of gemv.hip, attention.hip and accept.hip.
+// forward pass.  All arithmetic of the method runs in the kernels of the .hip files.
 #include "../../include/easyspec.h"
 #include "../../include/easyspec_instrument.h"
 
@@ -12,6 +12,7 @@
 #include <unistd.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -717,7 +718,7 @@ extern "C" int easyspec_calibrate(easyspec_ctx* ctx, const int32_t* tokens, cons
 }
 
 // ---------------------------------------------------------------------------------------------
-// acceptance, lengths, cache access
+// acceptance
 // ---------------------------------------------------------------------------------------------
 
 static int check_greedy_args(const int32_t* draft, const int32_t* target, int32_t batch, int32_t gamma, int32_t* accept_len,
@@ -820,6 +821,195 @@ extern "C" int easyspec_accept_static(const int32_t* draft, const float* draft_l
   HIPCHK(nullptr, hipGetLastError());
   return EASYSPEC_OK;
 }
+
+// ---------------------------------------------------------------------------------------------
+// beams and bounded caches: operators on the caller's arrays
+// ---------------------------------------------------------------------------------------------
+
+// The arrays that a launch writes have to be device memory of the current device: anything else (a host array, memory of another
+// device) would be written through an address that the kernel does not have.
+static int check_outputs(const char* what, std::initializer_list<const void*> outs) {
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return fail(nullptr, EASYSPEC_EHIP, "%s: no HIP device available (this library has no CPU path)", what);
+  for (const void* p : outs) {
+    hipPointerAttribute_t attr;
+    const bool ok = hipPointerGetAttributes(&attr, p) == hipSuccess &&
+                    (attr.type == hipMemoryTypeManaged || (attr.type == hipMemoryTypeDevice && attr.device == dev));
+    if (!ok) {
+      (void)hipGetLastError();
+      return fail(nullptr, EASYSPEC_EINVAL, "%s: an output or the workspace is not memory of the current device", what);
+    }
+  }
+  return EASYSPEC_OK;
+}
+
+static bool misaligned(std::initializer_list<const void*> ps, uintptr_t to) {
+  for (const void* p : ps)
+    if ((uintptr_t)p % to) return true;
+  return false;
+}
+
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+static bool beam_sizes_ok(int32_t groups, int32_t beams, int32_t vocab, int32_t n_select) {
+  return groups >= 1 && beams >= 1 && beams <= EASYSPEC_MAX_BEAMS && (int64_t)groups * beams <= 65535 && vocab >= 1 &&
+         vocab <= EASYSPEC_MAX_BEAM_VOCAB && n_select >= 1 && n_select <= EASYSPEC_MAX_SELECT;
+}
+
+extern "C" int64_t easyspec_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_select) {
+  if (!beam_sizes_ok(groups, beams, vocab, n_select)) return -1;
+  return (int64_t)beam_select_workspace_bytes(groups, beams, vocab, n_select);
+}
+
+extern "C" int easyspec_beam_select(const float* logits, const float* scores, const int32_t* ended, int32_t groups, int32_t beams, int32_t vocab,
+                                    int32_t n_select, float temperature, int32_t end_token, int32_t* tokens_out, int32_t* parents_out,
+                                    float* scores_out, void* workspace, void* hip_stream) {
+  if (!logits || !scores || !tokens_out || !parents_out || !scores_out || !workspace) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: NULL argument");
+  if (!beam_sizes_ok(groups, beams, vocab, n_select))
+    return fail(nullptr, EASYSPEC_EINVAL, "beam_select: need groups >= 1, 1 <= beams <= %d, groups * beams <= 65535, 1 <= vocab <= %d, 1 <= n_select <= %d",
+                EASYSPEC_MAX_BEAMS, EASYSPEC_MAX_BEAM_VOCAB, EASYSPEC_MAX_SELECT);
+  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: temperature must be positive and finite");
+  if (ended && (end_token < 0 || end_token >= vocab)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: end_token %d outside the vocabulary", end_token);
+  if (misaligned({workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: workspace must be 16-byte aligned");
+  const int rc = check_outputs("beam_select", {tokens_out, parents_out, scores_out, workspace});
+  if (rc != EASYSPEC_OK) return rc;
+  launch_beam_select(logits, scores, ended, groups, beams, vocab, n_select, (double)temperature, end_token, tokens_out, parents_out, scores_out,
+                     workspace, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+static int check_layout(const char* what, const easyspec_kv_layout* g) {
+  if (!g) return fail(nullptr, EASYSPEC_EINVAL, "%s: layout is NULL", what);
+  if (g->n_layers < 1 || g->n_layers > 65535 || g->n_seqs < 1 || g->n_seqs > EASYSPEC_MAX_BATCH || g->n_kv_heads < 1 || g->n_kv_heads > 65535 ||
+      (int64_t)g->n_layers * g->n_seqs * g->n_kv_heads > INT32_MAX || g->max_slots < 1 || g->max_slots > kMaxEvictSlots ||
+      (g->head_dim != 64 && g->head_dim != 128) || (g->dtype != EASYSPEC_DTYPE_F32 && g->dtype != EASYSPEC_DTYPE_BF16))
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: bad cache layout", what);
+  return EASYSPEC_OK;
+}
+static size_t layout_rows(const easyspec_kv_layout* g) { return (size_t)g->n_layers * g->n_seqs * g->n_kv_heads; }
+static int slot_bytes(const easyspec_kv_layout* g) { return g->head_dim * (g->dtype == EASYSPEC_DTYPE_BF16 ? 2 : 4); }
+
+// Outputs of `out_bytes` each that may be the inputs of `in_bytes` themselves or lie apart from both inputs and each other.
+static int check_in_place(const char* what, const void* k, const void* v, size_t in_bytes, const void* k_out, const void* v_out, size_t out_bytes) {
+  const bool same = k_out == k && v_out == v;
+  if ((!same && (overlap(k_out, out_bytes, k, in_bytes) || overlap(k_out, out_bytes, v, in_bytes) || overlap(v_out, out_bytes, k, in_bytes) ||
+                 overlap(v_out, out_bytes, v, in_bytes))) ||
+      overlap(k_out, out_bytes, v_out, out_bytes))
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: arrays overlap (in place: k_out == k and v_out == v)", what);
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_kv_reorder(const void* k, const void* v, const easyspec_kv_layout* layout, const int32_t* parents, int32_t beams,
+                                   int32_t from_slot, int32_t to_slot, void* k_out, void* v_out, void* hip_stream) {
+  if (!k || !v || !parents || !k_out || !v_out) return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: NULL argument");
+  int rc = check_layout("kv_reorder", layout);
+  if (rc != EASYSPEC_OK) return rc;
+  if (beams < 1 || layout->n_seqs % beams) return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: %d sequences are no groups of %d beams", layout->n_seqs, beams);
+  if (from_slot < 0 || to_slot < from_slot || to_slot > layout->max_slots)
+    return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: slots %d..%d outside 0..%d", from_slot, to_slot, layout->max_slots);
+  if (misaligned({k, v, k_out, v_out}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: arrays must be 16-byte aligned");
+  const size_t bytes = layout_rows(layout) * layout->max_slots * slot_bytes(layout);
+  rc = check_in_place("kv_reorder", k, v, bytes, k_out, v_out, bytes);
+  if (rc == EASYSPEC_OK) rc = check_outputs("kv_reorder", {k_out, v_out});
+  if (rc != EASYSPEC_OK) return rc;
+  const KvLayout g = {layout->n_layers, layout->n_seqs, layout->n_kv_heads, layout->max_slots};
+  launch_kv_reorder(k, v, k_out, v_out, g, slot_bytes(layout), parents, 0, 0, layout->n_seqs, beams, from_slot, to_slot, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+static int weigh_args(const char* what, const easyspec_kv_layout* g, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads, WeighArgs& a) {
+  const int rc = check_layout(what, g);
+  if (rc != EASYSPEC_OK) return rc;
+  if (!n_tokens || !lens) return fail(nullptr, EASYSPEC_EINVAL, "%s: NULL argument", what);
+  const int group = n_q_heads > 0 && n_q_heads % g->n_kv_heads == 0 ? n_q_heads / g->n_kv_heads : 0;
+  if (group != 1 && group != 2 && group != 4 && group != 7 && group != 8)
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: %d query heads on %d KV heads: not 1, 2, 4, 7 or 8 each", what, n_q_heads, g->n_kv_heads);
+  memset(&a, 0, sizeof a);
+  int q_first = 0;
+  for (int b = 0; b < g->n_seqs; ++b) {
+    const int n = n_tokens[b];
+    if (n < 0 || n > EASYSPEC_MAX_CALIB_TOKENS) return fail(nullptr, EASYSPEC_EINVAL, "%s: n_tokens[%d] = %d outside 0..%d", what, b, n, EASYSPEC_MAX_CALIB_TOKENS);
+    if (n == 0) continue;
+    if (lens[b] < n || lens[b] > g->max_slots) return fail(nullptr, EASYSPEC_EINVAL, "%s: lens[%d] = %d outside %d..%d", what, b, lens[b], n, g->max_slots);
+    WeighEntry& e = a.entry[a.n_entries++];
+    e.seq = b; e.n = n; e.len = lens[b]; e.q_first = q_first;
+    q_first += n;
+  }
+  a.n_seqs = g->n_seqs; a.heads = g->n_kv_heads; a.Hq = n_q_heads; a.group = group; a.max_slots = g->max_slots;
+  a.q_layer_pitch = (size_t)q_first * n_q_heads * g->head_dim;
+  a.scale = 1.f / sqrtf((float)g->head_dim);
+  weigh_plan(a, g->n_layers);
+  return EASYSPEC_OK;
+}
+
+extern "C" int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads) {
+  WeighArgs a;
+  if (weigh_args("attn_weights_workspace_bytes", layout, n_tokens, lens, n_q_heads, a) != EASYSPEC_OK) return -1;
+  return (int64_t)weigh_workspace_bytes(a, layout->n_layers);
+}
+
+extern "C" int easyspec_attn_weights(const float* q, const void* k, const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens,
+                                     int32_t n_q_heads, const float* weights_in, float* weights_out, void* workspace, void* hip_stream) {
+  if (!q || !k || !weights_out || !workspace) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: NULL argument");
+  WeighArgs a;
+  int rc = weigh_args("attn_weights", layout, n_tokens, lens, n_q_heads, a);
+  if (rc != EASYSPEC_OK) return rc;
+  if (misaligned({q, k, workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: q, k and workspace must be 16-byte aligned");
+  if (misaligned({weights_in, weights_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights must be 4-byte aligned");
+  const size_t bytes = layout_rows(layout) * layout->max_slots * sizeof(float);
+  if (weights_in && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes))
+    return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights_in and weights_out overlap in part");
+  rc = check_outputs("attn_weights", {weights_out, workspace});
+  if (rc != EASYSPEC_OK) return rc;
+  a.q = q; a.k = k; a.w_in = weights_in; a.w_out = weights_out; a.stats = (float2*)workspace;
+  launch_weigh(a, layout->n_layers, layout->dtype, layout->head_dim, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_kv_evict(const void* k, const void* v, const float* weights, const easyspec_kv_layout* layout, const int32_t* lens,
+                                 const int32_t* keep, int32_t recent, int32_t out_slots, void* k_out, void* v_out, float* weights_out,
+                                 int32_t* slots_out, void* hip_stream) {
+  if (!k || !v || !weights || !lens || !keep || !k_out || !v_out || !weights_out || !slots_out) return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: NULL argument");
+  int rc = check_layout("kv_evict", layout);
+  if (rc != EASYSPEC_OK) return rc;
+  if (recent < 0 || out_slots < 1 || out_slots > kMaxEvictSlots) return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: bad recent or out_slots");
+  EvictArgs a;
+  memset(&a, 0, sizeof a);
+  a.recent = recent;
+  a.out_slots = out_slots;
+  for (int b = 0; b < layout->n_seqs; ++b) {
+    if (lens[b] < 0 || lens[b] > layout->max_slots || keep[b] < 0)
+      return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: sequence %d: %d slots of %d, %d to stay", b, lens[b], layout->max_slots, keep[b]);
+    a.len[b] = lens[b];
+    a.keep[b] = std::min(keep[b], lens[b]);
+    if (a.keep[b] > out_slots) return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: %d slots of sequence %d stay, the results hold %d", a.keep[b], b, out_slots);
+  }
+  if (misaligned({k, v, k_out, v_out}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: caches must be 16-byte aligned");
+  if (misaligned({weights, weights_out, slots_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: weights and slots must be 4-byte aligned");
+  const size_t rows = layout_rows(layout), in_bytes = rows * layout->max_slots * slot_bytes(layout), out_bytes = rows * out_slots * slot_bytes(layout);
+  const size_t w_in = rows * layout->max_slots * sizeof(float), w_out = rows * out_slots * sizeof(float);
+  const bool same = k_out == k && v_out == v;
+  rc = check_in_place("kv_evict", k, v, in_bytes, k_out, v_out, out_bytes);
+  if (rc != EASYSPEC_OK) return rc;
+  if (same != (weights_out == weights) || (same && out_slots != layout->max_slots) || (!same && overlap(weights, w_in, weights_out, w_out)) ||
+      overlap(slots_out, w_out, weights, w_in) || overlap(slots_out, w_out, weights_out, w_out))
+    return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: arrays overlap (in place: all three of them, with out_slots == max_slots)");
+  rc = check_outputs("kv_evict", {k_out, v_out, weights_out, slots_out});
+  if (rc != EASYSPEC_OK) return rc;
+  const KvLayout g = {layout->n_layers, layout->n_seqs, layout->n_kv_heads, layout->max_slots};
+  launch_kv_evict(k, v, weights, k_out, v_out, weights_out, slots_out, g, slot_bytes(layout), a, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// lengths, cache access
+// ---------------------------------------------------------------------------------------------
 
 extern "C" int easyspec_get_lens(const easyspec_ctx* ctx, int32_t* precise, int32_t* fuzzy) {
   if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
@@ -993,6 +1183,9 @@ extern "C" int easyspec_stream_read(const void* buf, int64_t bytes, float* sink,
 
 extern "C" int32_t easyspec_stream_read_sink_floats(void) { return stream_read_sink_floats(); }
 
+static_assert(EASYSPEC_MAX_BEAMS == kMaxBeams && EASYSPEC_MAX_SELECT == kMaxSelect && EASYSPEC_MAX_BEAM_VOCAB == kMaxBeamVocab,
+              "header and kernels disagree on the limits of a beam selection");
+static_assert(EASYSPEC_MAX_BATCH == kMaxCols, "per-sequence arrays of the cache operators hold kMaxCols entries");
 static_assert(EASYSPEC_MAX_CHUNKS == kMaxChunks, "header and kernels disagree on the chunk limit");
 
 extern "C" int easyspec_attention_route(const easyspec_config* cfg, const int32_t* ctx_lens, const int32_t* seqs, int32_t n_cols,

@@ -1,5 +1,6 @@
 // Internal interface between the host state machine (easyspec.cpp) and the gfx950 kernels
-// (gemv.hip, attention.hip, wide.hip, resident.hip, util.hip, accept.hip).  Plain structs and launch functions; no device code in this header.
+// (gemv.hip, attention.hip, wide.hip, resident.hip, util.hip, accept.hip, beam.hip, weigh.hip,
+// cache_ops.hip).  Plain structs and launch functions; no device code in this header.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -244,6 +245,56 @@ void launch_sample_accept(const int32_t* draft, const float* draft_logits, const
 // address on the current device (resolved at the first call there) and its size.  Allocates nothing.
 hipError_t sample_accept_static_workspace(double** out);
 size_t sample_accept_static_capacity_bytes();
+// Selection over beams and vocabulary; ws: beam_select_workspace_bytes() of scratch, 16-byte aligned.
+constexpr int kMaxBeams = 64, kMaxSelect = 64, kMaxBeamVocab = 1 << 20;
+size_t beam_select_workspace_bytes(int groups, int beams, int V, int n_select);
+void launch_beam_select(const float* logits, const float* scores, const int32_t* ended, int groups, int beams, int V, int n_select,
+                        double T, int end_token, int32_t* tokens_out, int32_t* parents_out, float* scores_out, void* ws, hipStream_t st);
+
+// Caches [layer][sequence][KV head][slot] of slots of so many bytes.
+struct KvLayout {
+  int n_layers, n_seqs, n_heads, max_slots;
+};
+struct ReorderArgs {
+  const int32_t* parents;  // [n] of the n sequences from `first` on, inside their group of `beams`; null: all from `source`
+  int source, first, n, beams, heads, in_place;
+  size_t run, offset, head_pitch, seq_pitch, layer_pitch;  // pieces
+};
+// v may be null (a single array).  slot_bytes: a multiple of 4; of 16 with 16-byte aligned arrays.
+void launch_kv_reorder(const void* k, const void* v, void* k_out, void* v_out, const KvLayout& g, int slot_bytes, const int32_t* parents, int source,
+                       int first, int n, int beams, int from, int to, hipStream_t st);
+struct EvictArgs {
+  int len[kMaxCols], keep[kMaxCols];  // per sequence; keep 0: left alone
+  int recent, out_slots;
+  int heads, n_seqs, max_slots, row0, log2_ppr;  // set by the launch
+};
+constexpr int kMaxEvictSlots = 65536;
+// k_out == k (then v_out == v, weights_out == weights and out_slots == max_slots): inside the same arrays.
+void launch_kv_evict(const void* k, const void* v, const float* weights, void* k_out, void* v_out, float* weights_out, int32_t* slots_out,
+                     const KvLayout& g, int slot_bytes, const EvictArgs& plan, hipStream_t st);
+
+// Attention weight of cached slots.  An entry: a sequence with new tokens.
+struct WeighEntry {
+  int seq, n, len, q_first;  // its new tokens, its slots with them, its first row of tokens in q
+  int chunks, first_wg;      // set by weigh_plan
+  size_t first_stat;
+};
+constexpr int kWeighMaxChunk = 1024;
+struct WeighArgs {
+  const float* q;     // [layer][token][Hq][hd]
+  const void* k;      // cache, T
+  const float* w_in;  // [layer][sequence][KV head][slot]; null: zeros
+  float* w_out;
+  float2* stats;
+  size_t q_layer_pitch, stats_pitch;
+  int n_seqs, heads, Hq, group, max_slots, chunk, n_entries, n_wgs;
+  float scale;
+  WeighEntry entry[kMaxCols];
+};
+void weigh_plan(WeighArgs& a, int n_layers);
+size_t weigh_workspace_bytes(const WeighArgs& a, int n_layers);
+void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
+
 // Reads `bytes` (multiple of 16) of buf once; sink: stream_read_sink_floats() floats.
 void launch_stream_read(const void* buf, size_t bytes, float* sink, hipStream_t st);
 int stream_read_sink_floats();

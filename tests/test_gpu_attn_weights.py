@@ -1,0 +1,134 @@
+"""Accumulated attention weights (easyspec_attn_weights) against a 64-bit evaluation, within the bound that operator_ref derives."""
+import numpy as np
+import pytest
+
+import operator_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def es():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a HIP device; none is visible")
+    import paper_2502_02493_amd as es
+    return es
+
+
+def setup(es, seed, L, heads, hd, dtype, n, lens, slots, q_std=1.5, beyond=float("nan")):
+    """Everything on the device; slots from a sequence's length on hold NaN."""
+    import torch
+    Hq, H = heads
+    B = len(lens)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    k = torch.empty(L, B, H, slots, hd, device="cuda", dtype=dt).normal_(generator=g)
+    w = torch.rand(L, B, H, slots, device="cuda", generator=g)
+    for b in range(B):
+        k[:, b, :, lens[b]:] = beyond
+        w[:, b, :, lens[b] - n[b]:] = float("nan")     # not read
+    q = torch.empty(L, sum(n), Hq, hd, device="cuda").normal_(0, q_std, generator=g)
+    layout = es.easyspec_kv_layout(L, B, H, slots, hd, es.EASYSPEC_DTYPE_BF16 if dtype == "bf16" else es.EASYSPEC_DTYPE_F32)
+    return q, k, w, layout
+
+
+def call(es, q, k, w, layout, n, lens, Hq, out=None, stream=None):
+    import torch
+    out = torch.full(tuple(k.shape[:4]), -3.0, device="cuda") if out is None else out
+    nb = es.easyspec_attn_weights_workspace_bytes(layout, n, lens, Hq)
+    assert nb >= 0
+    ws = torch.full((nb // 4 + 4,), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    es.easyspec_attn_weights(q, k, layout, n, lens, Hq, w, out, ws, (stream or torch.cuda.current_stream()).cuda_stream)
+    torch.cuda.synchronize()
+    return out
+
+
+def check(q, k, w, n, lens, out):
+    want, tol = ref.attn_weights(q.double().cpu().numpy(), k.double().cpu().numpy(), n, lens, None if w is None else w.double().cpu().numpy())
+    got = out.double().cpu().numpy()
+    there = ~np.isnan(want)
+    assert np.all(got[~there] == -3.0), "slots that are not the call's"
+    assert np.all(np.isfinite(got[there]))
+    err = np.abs(got - want)[there]
+    assert np.all(err <= tol[there]), float((err / tol[there]).max())
+
+
+@pytest.mark.parametrize("L,heads,hd,dtype,n,lens,slots", [
+    (1, (1, 1), 64, "fp32", [1], [1], 1),                     # one token that sees itself
+    (1, (1, 1), 64, "bf16", [1], [1], 5),
+    (1, (4, 2), 64, "fp32", [1], [128], 130),
+    (2, (7, 1), 64, "fp32", [5], [61], 64),
+    (1, (32, 8), 128, "bf16", [1], [777], 800),
+    (1, (32, 8), 128, "bf16", [6], [63], 64),
+    (2, (28, 4), 128, "bf16", [16], [65], 65),                # 112 rows a KV head
+    (1, (28, 4), 128, "fp32", [11], [333], 340),
+    (1, (8, 1), 128, "bf16", [16], [16], 16),                 # nothing but the new tokens, 128 rows
+    (1, (8, 1), 64, "bf16", [16], [1500], 1501),
+    (3, (4, 4), 64, "bf16", [3, 0, 16, 1], [3, 50, 700, 129], 700),   # ragged; one sequence left alone
+    (1, (16, 2), 128, "bf16", [2, 9], [1025, 2049], 2100),
+    (1, (2, 1), 64, "bf16", [1] * 16, list(range(1, 17)), 20),
+    (2, (32, 8), 128, "bf16", [6, 2, 1], [1111, 300, 1], 1200),
+])
+def test_sizes(es, L, heads, hd, dtype, n, lens, slots):
+    q, k, w, layout = setup(es, sum(lens), L, heads, hd, dtype, n, lens, slots)
+    check(q, k, w, n, lens, call(es, q, k, w, layout, n, lens, heads[0]))
+
+
+def test_without_earlier_weights_in_place_and_on_another_stream(es):
+    import torch
+    n, lens = [4, 1], [200, 77]
+    q, k, w, layout = setup(es, 5, 2, (8, 2), 128, "bf16", n, lens, 210)
+    check(q, k, None, n, lens, call(es, q, k, None, layout, n, lens, 8))
+    a = call(es, q, k, w, layout, n, lens, 8, stream=torch.cuda.Stream())
+    inside = w.clone()
+    inside[:, 0, :, 200:], inside[:, 1, :, 77:] = -3.0, -3.0
+    b = call(es, q, k, inside, layout, n, lens, 8, out=inside)
+    assert torch.equal(a, b)
+    check(q, k, w, n, lens, b)
+
+
+def test_the_same_bits_again_and_alone(es):
+    """No atomics: a call repeats bit for bit; a sequence's weights do not depend on the others'."""
+    import torch
+    n, lens = [6, 6], [3000, 2000]
+    q, k, w, layout = setup(es, 6, 1, (32, 8), 128, "bf16", n, lens, 3001)
+    a = call(es, q, k, w, layout, n, lens, 32)
+    assert torch.equal(a, call(es, q, k, w, layout, n, lens, 32))
+
+
+def test_sharp_and_flat_scores(es):
+    for std in (0.0, 40.0):
+        n, lens = [2], [500]
+        q, k, w, layout = setup(es, 7, 1, (4, 1), 128, "bf16", n, lens, 512, q_std=std)
+        check(q, k, w, n, lens, call(es, q, k, w, layout, n, lens, 4))
+
+
+def test_sums_over_slots_are_the_rows(es):
+    """Every row gives a weight of one in all: 48 rows per KV head here, at a long context."""
+    n, lens = [6], [32768]
+    q, k, w, layout = setup(es, 8, 1, (32, 4), 128, "bf16", n, lens, 32832)
+    out = call(es, q, k, None, layout, n, lens, 32)
+    total = out[0, 0, :, :32768].double().sum(-1).cpu().numpy()
+    assert np.all(np.abs(total - 48) < 48 * 8192 * 2.0 ** -24)     # a running sum adds at most a quarter of the slots
+
+
+def test_graph_replays(es):
+    import torch
+    n, lens = [3], [700]
+    q, k, w, layout = setup(es, 9, 1, (8, 2), 64, "bf16", n, lens, 704)
+    out = torch.full((1, 1, 2, 704), -3.0, device="cuda")
+    ws = torch.zeros(es.easyspec_attn_weights_workspace_bytes(layout, n, lens, 8) // 4 + 4, device="cuda")
+    run = lambda: es.easyspec_attn_weights(q, k, layout, n, lens, 8, w, out, ws, torch.cuda.current_stream().cuda_stream)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in range(3):
+        q.normal_(0, 1.5, generator=torch.Generator(device="cuda").manual_seed(seed))
+        out.fill_(-3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(q, k, w, n, lens, out)

@@ -1,0 +1,125 @@
+"""What the operators on beams and bounded caches refuse, on the host, before anything is launched."""
+import numpy as np
+import pytest
+
+import paper_2502_02493_amd as es
+
+X = 1 << 20      # stands for an array: never looked at, since the arguments are refused first
+
+
+def refused(f, *args):
+    with pytest.raises(es.EasySpecError) as e:
+        f(*args)
+    assert e.value.code == es.EASYSPEC_EINVAL, str(e.value)
+
+
+def beam(**change):
+    a = dict(logits=X, scores=X, ended=None, groups=1, beams=4, vocab=100, n_select=4, temperature=1.0, end_token=0, tokens_out=X, parents_out=X,
+             scores_out=X, workspace=X)
+    a.update(change)
+    return lambda: es.easyspec_beam_select(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(logits=None), dict(scores=None), dict(tokens_out=None), dict(parents_out=None), dict(scores_out=None), dict(workspace=None),
+    dict(groups=0), dict(groups=-1), dict(beams=0), dict(beams=65), dict(groups=16384, beams=4), dict(vocab=0), dict(vocab=(1 << 20) + 1),
+    dict(n_select=0), dict(n_select=65), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("inf")),
+    dict(temperature=float("nan")), dict(ended=X, end_token=-1), dict(ended=X, end_token=100), dict(workspace=X + 8),
+])
+def test_beam_select(change):
+    refused(beam(**change))
+
+
+def test_beam_select_workspace_bytes():
+    assert es.easyspec_beam_select_workspace_bytes(1, 4, 1000, 4) > 0
+    for bad in ((0, 4, 10, 4), (1, 0, 10, 4), (1, 65, 10, 4), (1, 4, 0, 4), (1, 4, 10, 0), (1, 4, 10, 65), (65535, 2, 10, 1)):
+        assert es.easyspec_beam_select_workspace_bytes(*bad) == -1
+
+
+def layout(**change):
+    a = dict(n_layers=2, n_seqs=4, n_kv_heads=2, max_slots=32, head_dim=64, dtype=es.EASYSPEC_DTYPE_BF16)
+    a.update(change)
+    return es.easyspec_kv_layout(*a.values())
+
+
+BAD_LAYOUTS = [dict(n_layers=0), dict(n_layers=65536), dict(n_seqs=0), dict(n_seqs=20), dict(n_kv_heads=0), dict(max_slots=0), dict(max_slots=65537),
+               dict(head_dim=96), dict(head_dim=0), dict(dtype=2), dict(n_layers=65535, n_kv_heads=65535)]
+
+
+def far(i):
+    return X + (i << 24)
+
+
+def reorder(lay=None, **change):
+    a = dict(k=far(0), v=far(1), layout=lay or layout(), parents=X, beams=2, a=0, z=32, k_out=far(2), v_out=far(3))
+    a.update(change)
+    return lambda: es.easyspec_kv_reorder(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(k=None), dict(v=None), dict(parents=None), dict(k_out=None), dict(v_out=None), dict(beams=0), dict(beams=3), dict(beams=8), dict(a=-1),
+    dict(a=5, z=4), dict(z=33), dict(k=far(0) + 8), dict(v_out=far(3) + 4),
+    dict(k_out=far(0) + 64), dict(k_out=far(1)), dict(v_out=far(2)), dict(k_out=far(0)), dict(v_out=far(1)), dict(k_out=far(1), v_out=far(0)),
+])
+def test_kv_reorder(change):
+    refused(reorder(**change))
+
+
+@pytest.mark.parametrize("bad", BAD_LAYOUTS)
+def test_layouts(bad):
+    refused(reorder(layout(**bad)))
+    n = layout(**bad).n_seqs
+    assert es.easyspec_attn_weights_workspace_bytes(layout(**bad), [1] * n, [8] * n, 4) == -1
+    refused(lambda: es.easyspec_kv_evict(far(0), far(1), far(2), layout(**bad), [8] * n, [4] * n, 1, 8, far(3), far(4), far(5), far(6), None))
+
+
+def weigh(lay=None, **change):
+    a = dict(q=far(0), k=far(1), layout=lay or layout(), n_tokens=[1, 2, 0, 16], lens=[1, 32, 0, 20], n_q_heads=4, w_in=far(2), w_out=far(3), ws=far(4))
+    a.update(change)
+    return lambda: es.easyspec_attn_weights(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=None), dict(k=None), dict(w_out=None), dict(ws=None), dict(n_tokens=[-1, 1, 1, 1]), dict(n_tokens=[17, 0, 0, 0], lens=[30, 1, 1, 1]),
+    dict(lens=[0, 32, 0, 20]), dict(lens=[1, 33, 0, 20]), dict(lens=[1, 32, 0, 15]), dict(n_q_heads=0), dict(n_q_heads=3), dict(n_q_heads=6),
+    dict(n_q_heads=32), dict(q=far(0) + 4), dict(k=far(1) + 8), dict(ws=far(4) + 8), dict(w_out=far(2) + 4), dict(w_out=far(3) + 2),
+])
+def test_attn_weights(change):
+    refused(weigh(**change))
+
+
+def test_attn_weights_workspace_bytes():
+    assert es.easyspec_attn_weights_workspace_bytes(layout(), [0] * 4, [0] * 4, 4) == 0
+    assert es.easyspec_attn_weights_workspace_bytes(layout(), [1, 0, 0, 0], [32, 0, 0, 0], 4) > 0
+    assert es.easyspec_attn_weights_workspace_bytes(layout(), [1, 0, 0, 0], [33, 0, 0, 0], 4) == -1
+
+
+def evict(lay=None, **change):
+    a = dict(k=far(0), v=far(1), w=far(2), layout=lay or layout(), lens=[32, 0, 5, 20], keep=[8, 8, 8, 8], recent=2, out_slots=8, k_out=far(3),
+             v_out=far(4), w_out=far(5), slots=far(6))
+    a.update(change)
+    return lambda: es.easyspec_kv_evict(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(k=None), dict(v=None), dict(w=None), dict(k_out=None), dict(v_out=None), dict(w_out=None), dict(slots=None), dict(lens=[33, 0, 0, 0]),
+    dict(lens=[-1, 0, 0, 0]), dict(keep=[-1, 8, 8, 8]), dict(recent=-1), dict(out_slots=0), dict(out_slots=7), dict(out_slots=65537),
+    dict(k=far(0) + 4), dict(k_out=far(3) + 8), dict(w=far(2) + 1), dict(slots=far(6) + 2),
+    dict(k_out=far(0), v_out=far(1), w_out=far(2)),                            # in place, but results of another pitch
+    dict(k_out=far(0), v_out=far(1), out_slots=32),                            # in place, but for the weights
+    dict(w_out=far(2), out_slots=32), dict(k_out=far(0), out_slots=32), dict(k_out=far(1)), dict(v_out=far(3)), dict(slots=far(2)), dict(slots=far(5)),
+])
+def test_kv_evict(change):
+    refused(evict(**change))
+
+
+def test_outputs_that_are_host_arrays_are_refused():
+    """Without a device the calls end with EHIP, with one with EINVAL; nothing is written either way."""
+    logits, scores = np.zeros((1, 2, 8), np.float32), np.zeros((1, 2), np.float32)
+    tok, par, out = np.full(2, 5, np.int32), np.full(2, 5, np.int32), np.full(2, 5, np.float32)
+    ws = np.zeros(64, np.complex128)
+    ws = ws if ws.ctypes.data % 16 == 0 else ws[1:]
+    with pytest.raises(es.EasySpecError) as e:
+        es.easyspec_beam_select(logits, scores, None, 1, 2, 8, 2, 1.0, 0, tok, par, out, ws, None)
+    assert e.value.code in (es.EASYSPEC_EHIP, es.EASYSPEC_EINVAL)
+    assert np.all(tok == 5) and np.all(par == 5) and np.all(out == 5)

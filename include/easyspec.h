@@ -310,6 +310,17 @@ typedef struct easyspec_kv_layout {
 int easyspec_kv_reorder(const void *k, const void *v, const easyspec_kv_layout *layout, const int32_t *parents, int32_t beams,
                         int32_t from_slot, int32_t to_slot, void *k_out, void *v_out, void *hip_stream);
 
+/* The same on a context whose sequences are beams.
+ * easyspec_beam_fork: sequences first .. first + count - 1 become copies of sequence `source` (which may be one of them): cache,
+ * lengths, token tree, tracked weights.  One prompt is calibrated once and forked into its beams.  EASYSPEC_ESTATE if `source` is idle.
+ * easyspec_beam_reorder: sequence first + i takes the slots from from_slot on of sequence first + parents[i]; parents: dev
+ * [count], as easyspec_beam_select writes them for one group, -1 (or anything outside 0..count-1) = its own.  The slots below
+ * from_slot are taken to be common to the beams: their precise length, as a rule, after which only drafted slots move.  The
+ * sequences have to be of one length, precise and fuzzy, and without token trees: EASYSPEC_ESTATE otherwise.  Works in place.
+ * Neither synchronises: draft step, selection and reordering of one beam search need no look at the host in between. */
+int easyspec_beam_fork(easyspec_ctx *ctx, int32_t source, int32_t first, int32_t count);
+int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const int32_t *parents, int32_t from_slot);
+
 /* ---- Bounded caches ----------------------------------------------------------------------------------------- */
 
 /* The attention weight that cached slots receive from new tokens: in every layer and KV head,
@@ -352,11 +363,32 @@ int easyspec_kv_evict(const void *k, const void *v, const float *weights, const 
                       const int32_t *keep, int32_t recent, int32_t out_slots, void *k_out, void *v_out, float *weights_out,
                       int32_t *slots_out, void *hip_stream);
 
+/* The same on a context: drafting with a cache of bounded length.
+ * easyspec_track_attention: from now on every calibration adds the attention weights of its tokens (easyspec_attn_weights; fuzzy
+ * forwards add none) to the context's, one per layer, sequence, KV head and precise slot; slots filled before, by
+ * easyspec_kv_import or by a calibration, start from zero.  Passes of such calibrations are separate launches also where a
+ * small model's would be one.  max_positions: how far sequences may get, evicted slots counted (max_ctx ..
+ * EASYSPEC_MAX_POSITIONS; max_ctx without this call).  Synchronous; EASYSPEC_ESTATE the second time.
+ * easyspec_evict: of every sequence with 0 < keep[b] < precise[b] (keep: host [max_batch]; -1 leaves a sequence alone) keep[b]
+ * precise slots stay, chosen as easyspec_kv_evict does in every layer and KV head, and move together; its fuzzy slots are dropped.
+ * Afterwards precise[b] = keep[b].  Later tokens take the next free slots and go on at the next positions.  In place, on the
+ * context's stream, not synchronised.  EASYSPEC_ESTATE if attention is not tracked.
+ * easyspec_truncate refuses (EASYSPEC_ESTATE) to cut into the slots below the run of most recent ones that an eviction kept.
+ * easyspec_get_evicted: host [max_batch], the slots of each sequence evicted so far (precise + fuzzy + evicted = its position).
+ * easyspec_get_attn_weights: the weights of the first n_slots precise slots of sequence b, host|dev fp32
+ * [n_layers][n_kv_heads][n_slots].  Synchronous. */
+#define EASYSPEC_MAX_POSITIONS 1048576
+int easyspec_track_attention(easyspec_ctx *ctx, int32_t max_positions);
+int easyspec_evict(easyspec_ctx *ctx, const int32_t *keep, int32_t recent);
+int easyspec_get_evicted(const easyspec_ctx *ctx, int32_t *evicted);
+int easyspec_get_attn_weights(easyspec_ctx *ctx, int32_t b, float *out, int32_t n_slots);
+
 /* Host copies of the per-sequence lengths; each of precise, fuzzy: host [max_batch] or NULL. */
 int easyspec_get_lens(const easyspec_ctx *ctx, int32_t *precise, int32_t *fuzzy);
 
 /* Shorten sequence b to new_precise_len precise slots and no fuzzy ones (base-model rollback
- * after verification; 0 makes the sequence idle).  Host state only. */
+ * after verification; 0 makes the sequence idle).  Host state only.  EASYSPEC_ESTATE if that cuts into what an eviction
+ * left of the sequence's older slots (easyspec_evict). */
 int easyspec_truncate(easyspec_ctx *ctx, int32_t b, int32_t new_precise_len);
 
 /* Replace the cache of sequence b by n_slots precise entries.  k, v: host|dev

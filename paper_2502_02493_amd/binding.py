@@ -19,6 +19,7 @@ EASYSPEC_MAX_TREE_WIDTH, EASYSPEC_MAX_TREE_NODES = 16, 64
 EASYSPEC_MAX_CHUNKS = 64
 EASYSPEC_PARALLEL_ATTENTION, EASYSPEC_PARALLEL_FULL_LAYER = 0, 1
 EASYSPEC_MAX_BEAMS, EASYSPEC_MAX_SELECT, EASYSPEC_MAX_BEAM_VOCAB = 64, 64, 1048576
+EASYSPEC_MAX_POSITIONS = 1048576
 
 EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easyspec_set_groups",
            "easyspec_default_groups", "easyspec_draft_step", "easyspec_calibrate", "easyspec_greedy_accept", "easyspec_greedy_accept_host",
@@ -27,6 +28,8 @@ EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easy
            "easyspec_get_hidden", "easyspec_poison_workspaces", "easyspec_force_give_up", "easyspec_step_bytes", "easyspec_profile_begin", "easyspec_profile_end",
            "easyspec_beam_select", "easyspec_beam_select_workspace_bytes", "easyspec_kv_reorder",
            "easyspec_attn_weights", "easyspec_attn_weights_workspace_bytes", "easyspec_kv_evict",
+           "easyspec_beam_fork", "easyspec_beam_reorder", "easyspec_track_attention", "easyspec_evict", "easyspec_get_evicted",
+           "easyspec_get_attn_weights",
            "easyspec_last_error"]
 EASYSPEC_OP_QKV, EASYSPEC_OP_ATTN, EASYSPEC_OP_OPROJ, EASYSPEC_OP_GATEUP, EASYSPEC_OP_DOWN, EASYSPEC_OP_HEAD, EASYSPEC_OP_ALL = range(7)
 
@@ -96,6 +99,12 @@ def load_library():
         L.easyspec_attn_weights_workspace_bytes.argtypes = [kvl, vp, vp, i32]
         L.easyspec_attn_weights_workspace_bytes.restype = C.c_int64
         L.easyspec_kv_evict.argtypes = [vp, vp, vp, kvl, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        L.easyspec_beam_fork.argtypes = [vp, i32, i32, i32]
+        L.easyspec_beam_reorder.argtypes = [vp, i32, i32, vp, i32]
+        L.easyspec_track_attention.argtypes = [vp, i32]
+        L.easyspec_evict.argtypes = [vp, vp, i32]
+        L.easyspec_get_evicted.argtypes = [vp, vp]
+        L.easyspec_get_attn_weights.argtypes = [vp, i32, vp, i32]
         L.easyspec_get_lens.argtypes = [vp, vp, vp]
         L.easyspec_truncate.argtypes = [vp, i32, i32]
         L.easyspec_kv_import.argtypes = [vp, i32, vp, vp, i32]
@@ -288,6 +297,33 @@ def easyspec_kv_evict(k, v, weights, layout: easyspec_kv_layout, lens, keep, rec
     n, s = _host_ints(lens, layout.n_seqs), _host_ints(keep, layout.n_seqs)
     _check(load_library().easyspec_kv_evict(_ptr(k), _ptr(v), _ptr(weights), C.byref(layout), _ptr(n), _ptr(s), recent, out_slots,
                                             _ptr(k_out), _ptr(v_out), _ptr(weights_out), _ptr(slots_out), _ptr(hip_stream)), None)
+
+
+def easyspec_beam_fork(ctx, source: int, first: int, count: int):
+    _check(load_library().easyspec_beam_fork(ctx, source, first, count), ctx)
+
+
+def easyspec_beam_reorder(ctx, first: int, count: int, parents, from_slot: int):
+    _check(load_library().easyspec_beam_reorder(ctx, first, count, _ptr(parents), from_slot), ctx)
+
+
+def easyspec_track_attention(ctx, max_positions: int):
+    _check(load_library().easyspec_track_attention(ctx, max_positions), ctx)
+
+
+def easyspec_evict(ctx, keep, recent: int):
+    k = np.ascontiguousarray(keep, dtype=np.int32)
+    _check(load_library().easyspec_evict(ctx, _ptr(k), recent), ctx)
+
+
+def easyspec_get_evicted(ctx, max_batch: int):
+    n = np.zeros(max_batch, np.int32)
+    _check(load_library().easyspec_get_evicted(ctx, _ptr(n)), ctx)
+    return n
+
+
+def easyspec_get_attn_weights(ctx, b: int, out, n_slots: int):
+    _check(load_library().easyspec_get_attn_weights(ctx, b, _ptr(out), n_slots), ctx)
 
 
 def easyspec_stream_read(buf, nbytes: int, sink, hip_stream=None):

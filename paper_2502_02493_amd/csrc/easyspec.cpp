@@ -40,6 +40,15 @@ struct easyspec_ctx {
     uint64_t line[EASYSPEC_MAX_TREE_NODES];  // bit a set: node a is the node itself or an ancestor
   };
   std::vector<Tree> tree;
+  // bounded caches: what easyspec_track_attention allocated (weights == null: nothing is tracked)
+  struct Tracked {
+    float* weights = nullptr;   // [L][B][Hkv][max_ctx]
+    int32_t* kept = nullptr;    // the same shape: an eviction's list of slots
+    float2* stats = nullptr;    // workspace of launch_weigh
+    int32_t max_positions = 0;  // rows of the rotary table
+    std::vector<int32_t> gone;  // slots evicted so far: slot s of sequence b is at rotary position s + gone[b] from firm[b] on;
+    std::vector<int32_t> firm;  // the slots below come from anywhere before
+  } track;
   std::vector<int32_t> bounds;  // current layer-parallel strategy
   std::vector<int32_t> single;  // every layer alone (Alg. 1 order)
   std::vector<void*> allocs;
@@ -138,6 +147,25 @@ static void shape_of(const easyspec_config* cfg, Shape& s) {
   s.R_qkv = qkv_tile_rows(s.RQKV / 2);
 }
 
+// rotary table in double precision: angle(pos, i) = pos * theta^(-2 i / hd), a few thousand positions at a time
+static hipError_t fill_rope(const easyspec_config& cfg, float2* rope, int n_pos) {
+  const int half = cfg.head_dim / 2, most = std::min(n_pos, 4096);
+  std::vector<float2> tab((size_t)most * half);
+  std::vector<double> freq(half);
+  for (int i = 0; i < half; ++i) freq[i] = pow((double)cfg.rope_theta, -2.0 * (double)i / (double)cfg.head_dim);
+  for (int p0 = 0; p0 < n_pos; p0 += most) {
+    const int n = std::min(most, n_pos - p0);
+    for (int p = 0; p < n; ++p)
+      for (int i = 0; i < half; ++i) {
+        const double ang = (double)(p0 + p) * freq[i];
+        tab[(size_t)p * half + i] = make_float2((float)cos(ang), (float)sin(ang));
+      }
+    const hipError_t e = hipMemcpy(rope + (size_t)p0 * half, tab.data(), (size_t)n * half * sizeof(float2), hipMemcpyHostToDevice);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 extern "C" int easyspec_create(const easyspec_config* cfg, void* hip_stream, easyspec_ctx** out) {
   if (!out) return fail(nullptr, EASYSPEC_EINVAL, "out is NULL");
   *out = nullptr;
@@ -164,6 +192,9 @@ extern "C" int easyspec_create(const easyspec_config* cfg, void* hip_stream, eas
   ctx->precise.assign(s.B, 0);
   ctx->fuzzy.assign(s.B, 0);
   ctx->tree.assign(s.B, easyspec_ctx::Tree());
+  ctx->track.max_positions = s.max_ctx;
+  ctx->track.gone.assign(s.B, 0);
+  ctx->track.firm.assign(s.B, 0);
   for (int i = 0; i <= s.L; ++i) ctx->single.push_back(i);
   ctx->bounds = ctx->single;
 
@@ -256,17 +287,7 @@ extern "C" int easyspec_create(const easyspec_config* cfg, void* hip_stream, eas
     HIPCHK(ctx, hipMemsetAsync(b.kc, 0, kv_bytes, ctx->stream));
     HIPCHK(ctx, hipMemsetAsync(b.vc, 0, kv_bytes, ctx->stream));
 
-    // rotary table in double precision: angle(pos, i) = pos * theta^(-2 i / hd)
-    const int half = s.hd / 2;
-    std::vector<float2> tab((size_t)s.max_ctx * half);
-    std::vector<double> freq(half);
-    for (int i = 0; i < half; ++i) freq[i] = pow((double)cfg->rope_theta, -2.0 * (double)i / (double)s.hd);
-    for (int p = 0; p < s.max_ctx; ++p)
-      for (int i = 0; i < half; ++i) {
-        const double ang = (double)p * freq[i];
-        tab[(size_t)p * half + i] = make_float2((float)cos(ang), (float)sin(ang));
-      }
-    HIPCHK(ctx, hipMemcpy(b.rope, tab.data(), tab.size() * sizeof(float2), hipMemcpyHostToDevice));
+    HIPCHK(ctx, fill_rope(ctx->cfg, b.rope, s.max_ctx));
     HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
     return EASYSPEC_OK;
   };
@@ -443,10 +464,54 @@ static bool resident_takes(const easyspec_ctx* ctx, const Cols& c, const std::ve
   return ctx->r.ctl && ctx->prof_op < 0 && resident_pass(ctx->s, c, bounds.data(), (int)bounds.size() - 1) && !launches_forced();
 }
 
+// The entries of a calibration's columns (those of a sequence lie together) and of a wide pass's, for launch_weigh.
+static void weigh_begin(const easyspec_ctx* ctx, const float* q, WeighArgs& a) {
+  const Shape& s = ctx->s;
+  memset(&a, 0, sizeof a);
+  a.q = q;
+  a.stats = ctx->track.stats;
+  a.n_seqs = s.B; a.heads = s.Hkv; a.Hq = s.Hq; a.group = s.Hq / s.Hkv; a.max_slots = s.max_ctx;
+  a.scale = 1.f / sqrtf((float)s.hd);
+}
+static void weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q, WeighArgs& a) {
+  weigh_begin(ctx, q, a);
+  for (int i = 0; i < c.n; ++i) {
+    if (i == 0 || c.seq[i] != c.seq[i - 1]) {
+      WeighEntry& e = a.entry[a.n_entries++];
+      e.seq = c.seq[i];
+      e.q_first = i;
+    }
+    WeighEntry& e = a.entry[a.n_entries - 1];
+    e.n += 1;
+    e.len = c.pos[i] + 1;
+  }
+  weigh_plan(a, 1);
+}
+static void weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q, WeighArgs& a) {
+  weigh_begin(ctx, q, a);
+  for (int i = 0; i < sp.n_seq; ++i) {
+    WeighEntry& e = a.entry[a.n_entries++];
+    e.seq = sp.seq[i];
+    e.q_first = sp.first[i];
+    e.n = sp.first[i + 1] - sp.first[i];
+    e.len = sp.pos0[i] + e.n;
+  }
+  weigh_plan(a, 1);
+}
+static void weigh_layer(const easyspec_ctx* ctx, WeighArgs& a, int layer) {
+  const Shape& s = ctx->s;
+  const size_t slots = (size_t)layer * s.B * s.Hkv * s.max_ctx;
+  a.k = (const char*)ctx->b.kc + slots * s.hd * esize(s);
+  a.w_out = ctx->track.weights + slots;
+  a.w_in = a.w_out;
+  launch_weigh(a, 1, s.dtype, s.hd, ctx->stream);
+}
+
 // c2: a second pass of as many columns run together with the first (sets of one layer only: a calibration); the
 // weight kernels then serve both passes in one launch each, embedding, attention and argmax run per pass.
+// weigh: the attention weights of the pass's queries are added to the context's (a calibration of a context that tracks them).
 static int forward(easyspec_ctx* ctx, const Cols& c, const int32_t* tokens, const std::vector<int32_t>& bounds,
-                   bool full_layer, float* logits_out, int32_t* tokens_out, const Cols* c2 = nullptr) {
+                   bool full_layer, float* logits_out, int32_t* tokens_out, const Cols* c2 = nullptr, bool weigh = false) {
   const Shape& s = ctx->s;
   const Buffers& b = ctx->b;
   const Buffers* b2 = c2 ? &ctx->b2 : nullptr;
@@ -454,7 +519,10 @@ static int forward(easyspec_ctx* ctx, const Cols& c, const int32_t* tokens, cons
   const int n_sets = (int)bounds.size() - 1;
   if (c2 && (full_layer || !ctx->has_b2 || c2->n != c.n || n_sets != s.L))
     return fail(ctx, EASYSPEC_EINVAL, "internal: two passes together need equal column counts and sets of one layer");
-  if (!c2 && !full_layer && resident_takes(ctx, c, bounds)) {
+  WeighArgs wa, wa2;
+  if (weigh) weigh_columns(ctx, c, b.Q, wa);
+  if (weigh && c2) weigh_columns(ctx, *c2, b2->Q, wa2);
+  if (!c2 && !full_layer && !weigh && resident_takes(ctx, c, bounds)) {
     launch_resident(s, b, ctx->r, c, tokens, bounds.data(), n_sets, logits_out, tokens_out, st);
     HIPCHK(ctx, hipGetLastError());
     ctx->last_rows = c.n;
@@ -470,6 +538,8 @@ static int forward(easyspec_ctx* ctx, const Cols& c, const int32_t* tokens, cons
     { ProfScope p(ctx, EASYSPEC_OP_QKV); launch_qkv(s, b, c, lo, k, st, b2, c2); }
     { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_attn(s, b, c, lo, k, cut, st); }
     if (c2) { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_attn(s, *b2, *c2, lo, k, attn_cut(s, *c2, k), st); }
+    if (weigh) weigh_layer(ctx, wa, lo);
+    if (weigh && c2) weigh_layer(ctx, wa2, lo);
     if (full_layer && k > 1) {
       // App. B ablation: the MLPs of the set also work from the set's input, each behind its own
       // layer's attention; one launch per operation for the whole set
@@ -509,10 +579,13 @@ static int wide_forward(easyspec_ctx* ctx, const Spans& sp, const int32_t* token
   hipStream_t st = ctx->stream;
   { ProfScope p(ctx, EASYSPEC_OP_ALL); launch_wide_embed(s, b, w, sp, tokens, st); }
   const bool wide_head = all_rows && logits_out;
+  WeighArgs wa;
+  if (ctx->track.weights) weigh_spans(ctx, sp, w.Q, wa);
   for (int l = 0; l < s.L; ++l) {
     const bool last = l + 1 == s.L;
     { ProfScope p(ctx, EASYSPEC_OP_QKV); launch_wide_qkv(s, b, w, sp, l, st); }
     { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_wide_attn(s, b, w, sp, l, st); }
+    if (ctx->track.weights) weigh_layer(ctx, wa, l);
     { ProfScope p(ctx, EASYSPEC_OP_OPROJ); launch_wide_proj(s, b, w, sp, l, false, b.g_mlp + (size_t)l * s.d, false, st); }
     { ProfScope p(ctx, EASYSPEC_OP_GATEUP); launch_wide_gateup(s, b, w, sp, l, st); }
     ProfScope p(ctx, EASYSPEC_OP_DOWN);
@@ -555,9 +628,11 @@ extern "C" int easyspec_draft_step(easyspec_ctx* ctx, const int32_t* tokens_in, 
     if (ctx->precise[b] == 0) continue;
     const int pos = ctx->precise[b] + ctx->fuzzy[b];
     if (pos + 1 > s.max_ctx) return fail(ctx, EASYSPEC_ECAPACITY, "draft_step: sequence %d is full (%d slots)", b, s.max_ctx);
+    if (pos + ctx->track.gone[b] >= ctx->track.max_positions)
+      return fail(ctx, EASYSPEC_ECAPACITY, "draft_step: sequence %d has reached its last position (%d)", b, ctx->track.max_positions);
     if (ctx->tree[b].n > 0) return fail(ctx, EASYSPEC_ESTATE, "draft_step: sequence %d holds a token tree (continue it with easyspec_draft_tree_step)", b);
     c.seq[c.n] = b; c.pos[c.n] = pos; c.tok_idx[c.n] = b; c.logit_row[c.n] = b; c.out_idx[c.n] = b;
-    c.rope_pos[c.n] = pos; c.vis_base[c.n] = pos + 1;  // causal: every earlier slot is visible
+    c.rope_pos[c.n] = pos + ctx->track.gone[b]; c.vis_base[c.n] = pos + 1;  // causal: every earlier slot is visible
     ++c.n;
   }
   if (c.n == 0) return fail(ctx, EASYSPEC_ESTATE, "draft_step: no live sequence (calibrate a prompt first)");
@@ -594,7 +669,9 @@ extern "C" int easyspec_draft_tree_step(easyspec_ctx* ctx, const int32_t* tokens
       const int depth = par < 0 ? 0 : t.depth[par] + 1;
       c.seq[c.n] = b;
       c.pos[c.n] = ctx->precise[b] + node;
-      c.rope_pos[c.n] = ctx->precise[b] + depth;
+      c.rope_pos[c.n] = ctx->precise[b] + ctx->track.gone[b] + depth;
+      if (c.rope_pos[c.n] >= ctx->track.max_positions)
+        return fail(ctx, EASYSPEC_ECAPACITY, "draft_tree_step: sequence %d has reached its last position (%d)", b, ctx->track.max_positions);
       c.vis_base[c.n] = ctx->precise[b];
       c.vis_mask[c.n] = (par < 0 ? 0ull : t.line[par]) | (1ull << node);
       c.tok_idx[c.n] = b * W + j; c.logit_row[c.n] = b * W + j; c.out_idx[c.n] = b * W + j;
@@ -607,7 +684,7 @@ extern "C" int easyspec_draft_tree_step(easyspec_ctx* ctx, const int32_t* tokens
   for (int i = 0; i < c.n; ++i) {
     easyspec_ctx::Tree& t = ctx->tree[c.seq[i]];
     const int node = c.pos[i] - ctx->precise[c.seq[i]];
-    t.depth[node] = c.rope_pos[i] - ctx->precise[c.seq[i]];
+    t.depth[node] = c.rope_pos[i] - ctx->track.gone[c.seq[i]] - ctx->precise[c.seq[i]];
     t.line[node] = c.vis_mask[i];
   }
   for (int b = 0; b < s.B; ++b) {
@@ -632,6 +709,8 @@ extern "C" int easyspec_calibrate(easyspec_ctx* ctx, const int32_t* tokens, cons
     if (n < 0 || n > mc) return fail(ctx, EASYSPEC_ECAPACITY, "calibrate: n_tokens[%d] = %d outside 0..%d", b, n, mc);
     if (n > 0 && ctx->precise[b] + n > s.max_ctx)
       return fail(ctx, EASYSPEC_ECAPACITY, "calibrate: sequence %d would hold %d > %d slots", b, ctx->precise[b] + n, s.max_ctx);
+    if (n > 0 && ctx->precise[b] + n + ctx->track.gone[b] > ctx->track.max_positions)
+      return fail(ctx, EASYSPEC_ECAPACITY, "calibrate: sequence %d would pass its last position (%d)", b, ctx->track.max_positions);
     total += n;
   }
   if (total == 0) return fail(ctx, EASYSPEC_EINVAL, "calibrate: no tokens");
@@ -658,6 +737,7 @@ extern "C" int easyspec_calibrate(easyspec_ctx* ctx, const int32_t* tokens, cons
       sp.first[e] = sp.n;
       sp.seq[e] = q;
       sp.pos0[e] = ctx->precise[q];  // fuzzy slots are dropped: positions restart at the precise length
+      sp.ahead[e] = ctx->track.gone[q];
       sp.n += n;
     }
     sp.first[sp.n_seq] = sp.n;
@@ -667,7 +747,7 @@ extern "C" int easyspec_calibrate(easyspec_ctx* ctx, const int32_t* tokens, cons
     ctx->last_H = ctx->w.H + (size_t)pass_first * s.d;
     b = s.B;
   }
-  auto run = [&](const Cols& c, const Cols* partner) { return forward(ctx, c, tokens, ctx->single, false, logits_out, next_token_out, partner); };
+  auto run = [&](const Cols& c, const Cols* partner) { return forward(ctx, c, tokens, ctx->single, false, logits_out, next_token_out, partner, ctx->track.weights != nullptr); };
   while (b < s.B) {
     Cols c;
     memset(&c, 0, sizeof c);
@@ -677,7 +757,7 @@ extern "C" int easyspec_calibrate(easyspec_ctx* ctx, const int32_t* tokens, cons
         const bool last = r == n - 1;
         c.seq[c.n] = b;
         c.pos[c.n] = ctx->precise[b] + r;  // fuzzy slots are dropped: positions restart at the precise length
-        c.rope_pos[c.n] = c.pos[c.n];
+        c.rope_pos[c.n] = c.pos[c.n] + ctx->track.gone[b];
         c.vis_base[c.n] = c.pos[c.n] + 1;  // causal among the tokens of the pass
         c.tok_idx[c.n] = b * mc + r;
         c.logit_row[c.n] = logits_rows ? b * mc + r : (last ? b : -1);
@@ -1008,6 +1088,140 @@ extern "C" int easyspec_kv_evict(const void* k, const void* v, const float* weig
 }
 
 // ---------------------------------------------------------------------------------------------
+// beams and bounded caches: the same operators on a context
+// ---------------------------------------------------------------------------------------------
+
+extern "C" int easyspec_beam_fork(easyspec_ctx* ctx, int32_t source, int32_t first, int32_t count) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  CHECK_PASSES(ctx);
+  const Shape& s = ctx->s;
+  if (source < 0 || source >= s.B || first < 0 || count < 1 || count > s.B - first)
+    return fail(ctx, EASYSPEC_EINVAL, "beam_fork: sequence %d into %d from %d on: out of range", source, count, first);
+  const int len = ctx->precise[source] + ctx->fuzzy[source], slot = s.hd * (int)esize(s);
+  if (ctx->precise[source] == 0) return fail(ctx, EASYSPEC_ESTATE, "beam_fork: sequence %d has no context (calibrate a prompt first)", source);
+  const KvLayout g = {s.L, s.B, s.Hkv, s.max_ctx};
+  launch_kv_reorder(ctx->b.kc, ctx->b.vc, ctx->b.kc, ctx->b.vc, g, slot, nullptr, source, first, count, 1, 0, len, ctx->stream);
+  float* w = ctx->track.weights;
+  if (w) launch_kv_reorder(w, nullptr, w, nullptr, g, sizeof(float), nullptr, source, first, count, 1, 0, ctx->precise[source], ctx->stream);
+  HIPCHK(ctx, hipGetLastError());
+  for (int b = first; b < first + count; ++b) {
+    ctx->precise[b] = ctx->precise[source];
+    ctx->fuzzy[b] = ctx->fuzzy[source];
+    ctx->tree[b] = ctx->tree[source];
+    ctx->track.gone[b] = ctx->track.gone[source];
+    ctx->track.firm[b] = ctx->track.firm[source];
+  }
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_beam_reorder(easyspec_ctx* ctx, int32_t first, int32_t count, const int32_t* parents, int32_t from_slot) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  CHECK_PASSES(ctx);
+  if (!parents) return fail(ctx, EASYSPEC_EINVAL, "beam_reorder: NULL argument");
+  const Shape& s = ctx->s;
+  if (first < 0 || count < 1 || count > s.B - first) return fail(ctx, EASYSPEC_EINVAL, "beam_reorder: sequences %d .. %d out of range", first, first + count - 1);
+  const int precise = ctx->precise[first], len = precise + ctx->fuzzy[first], slot = s.hd * (int)esize(s);
+  for (int b = first; b < first + count; ++b) {
+    if (ctx->precise[b] == 0) return fail(ctx, EASYSPEC_ESTATE, "beam_reorder: sequence %d has no context (calibrate a prompt first)", b);
+    // which caches move is known to the device alone: the lengths have to be the same whatever it decides
+    if (ctx->precise[b] != precise || ctx->fuzzy[b] != ctx->fuzzy[first] || ctx->track.gone[b] != ctx->track.gone[first] || ctx->track.firm[b] != ctx->track.firm[first])
+      return fail(ctx, EASYSPEC_ESTATE, "beam_reorder: sequences %d and %d differ in length", first, b);
+    if (ctx->tree[b].n > 0) return fail(ctx, EASYSPEC_ESTATE, "beam_reorder: sequence %d holds a token tree", b);
+  }
+  if (from_slot < 0 || from_slot > len) return fail(ctx, EASYSPEC_EINVAL, "beam_reorder: from_slot %d outside 0..%d", from_slot, len);
+  const KvLayout g = {s.L, s.B, s.Hkv, s.max_ctx};
+  launch_kv_reorder(ctx->b.kc, ctx->b.vc, ctx->b.kc, ctx->b.vc, g, slot, parents, 0, first, count, count, from_slot, len, ctx->stream);
+  float* w = ctx->track.weights;
+  if (w) launch_kv_reorder(w, nullptr, w, nullptr, g, sizeof(float), parents, 0, first, count, count, from_slot, precise, ctx->stream);
+  HIPCHK(ctx, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_track_attention(easyspec_ctx* ctx, int32_t max_positions) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  CHECK_PASSES(ctx);
+  const Shape& s = ctx->s;
+  if (max_positions < s.max_ctx || max_positions > EASYSPEC_MAX_POSITIONS)
+    return fail(ctx, EASYSPEC_EINVAL, "track_attention: max_positions must be max_ctx (%d) .. %d", s.max_ctx, EASYSPEC_MAX_POSITIONS);
+  if (ctx->track.weights) return fail(ctx, EASYSPEC_ESTATE, "track_attention: attention is tracked already");
+  const size_t n = (size_t)s.L * s.B * s.Hkv * s.max_ctx;
+  float *weights = nullptr, *rope = nullptr;
+  ALLOC(ctx, weights, n * sizeof(float));
+  ALLOC(ctx, ctx->track.kept, n * sizeof(int32_t));
+  ALLOC(ctx, ctx->track.stats, weigh_workspace_limit(ctx->cfg.max_calib_tokens, s.B, s.Hkv, s.Hq / s.Hkv, s.max_ctx));
+  HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
+  if (max_positions > s.max_ctx) {
+    ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));
+    HIPCHK(ctx, fill_rope(ctx->cfg, (float2*)rope, max_positions));
+  }
+  HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
+  if (rope) ctx->b.rope = ctx->b2.rope = (float2*)rope;  // the shorter table stays: a captured pass may read it
+  ctx->track.max_positions = max_positions;
+  ctx->track.weights = weights;
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_evict(easyspec_ctx* ctx, const int32_t* keep, int32_t recent) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  CHECK_PASSES(ctx);
+  if (!keep) return fail(ctx, EASYSPEC_EINVAL, "evict: NULL argument");
+  if (recent < 0) return fail(ctx, EASYSPEC_EINVAL, "evict: recent must be >= 0");
+  if (!ctx->track.weights) return fail(ctx, EASYSPEC_ESTATE, "evict: attention is not tracked (easyspec_track_attention)");
+  const Shape& s = ctx->s;
+  EvictArgs a;
+  memset(&a, 0, sizeof a);
+  a.recent = recent;
+  a.out_slots = s.max_ctx;
+  bool any = false;
+  for (int b = 0; b < s.B; ++b) {
+    if (keep[b] == 0) return fail(ctx, EASYSPEC_EINVAL, "evict: nothing of sequence %d would stay (easyspec_truncate makes it idle)", b);
+    if (keep[b] < 0 || keep[b] >= ctx->precise[b]) continue;
+    a.len[b] = ctx->precise[b];
+    a.keep[b] = keep[b];
+    any = true;
+  }
+  if (!any) return EASYSPEC_OK;
+  const KvLayout g = {s.L, s.B, s.Hkv, s.max_ctx};
+  launch_kv_evict(ctx->b.kc, ctx->b.vc, ctx->track.weights, ctx->b.kc, ctx->b.vc, ctx->track.weights, ctx->track.kept, g, s.hd * (int)esize(s), a, ctx->stream);
+  HIPCHK(ctx, hipGetLastError());
+  for (int b = 0; b < s.B; ++b)
+    if (a.keep[b] > 0) {
+      // the slots that stay as a run of positions: the last `recent`, as far as they were one before
+      const int run = std::min(std::min(recent, a.keep[b]), ctx->precise[b] - ctx->track.firm[b]);
+      ctx->track.gone[b] += ctx->precise[b] - a.keep[b];
+      ctx->track.firm[b] = a.keep[b] - run;
+      ctx->precise[b] = a.keep[b];
+      ctx->fuzzy[b] = 0;
+      ctx->tree[b].n = 0;
+    }
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_get_evicted(const easyspec_ctx* ctx, int32_t* evicted) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  if (!evicted) return fail(const_cast<easyspec_ctx*>(ctx), EASYSPEC_EINVAL, "get_evicted: NULL argument");
+  for (int b = 0; b < ctx->s.B; ++b) evicted[b] = ctx->track.gone[b];
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_get_attn_weights(easyspec_ctx* ctx, int32_t b, float* out, int32_t n_slots) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  CHECK_PASSES(ctx);
+  const Shape& s = ctx->s;
+  if (!ctx->track.weights) return fail(ctx, EASYSPEC_ESTATE, "get_attn_weights: attention is not tracked (easyspec_track_attention)");
+  if (b < 0 || b >= s.B) return fail(ctx, EASYSPEC_EINVAL, "get_attn_weights: sequence %d out of range", b);
+  if (n_slots < 0 || n_slots > ctx->precise[b]) return fail(ctx, EASYSPEC_EINVAL, "get_attn_weights: %d slots outside 0..%d", n_slots, ctx->precise[b]);
+  if (n_slots == 0) return EASYSPEC_OK;
+  if (!out) return fail(ctx, EASYSPEC_EINVAL, "get_attn_weights: NULL argument");
+  const size_t width = n_slots * sizeof(float);
+  for (int l = 0; l < s.L; ++l)
+    HIPCHK(ctx, hipMemcpy2DAsync(out + (size_t)l * s.Hkv * n_slots, width, ctx->track.weights + ((size_t)l * s.B + b) * s.Hkv * s.max_ctx,
+                                 s.max_ctx * sizeof(float), width, s.Hkv, hipMemcpyDefault, ctx->stream));
+  HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
+  return check_passes(ctx);
+}
+
+// ---------------------------------------------------------------------------------------------
 // lengths, cache access
 // ---------------------------------------------------------------------------------------------
 
@@ -1026,6 +1240,9 @@ extern "C" int easyspec_truncate(easyspec_ctx* ctx, int32_t b, int32_t new_len) 
   CHECK_PASSES(ctx);
   if (b < 0 || b >= ctx->s.B) return fail(ctx, EASYSPEC_EINVAL, "truncate: sequence %d out of range", b);
   if (new_len < 0 || new_len > ctx->precise[b]) return fail(ctx, EASYSPEC_EINVAL, "truncate: length %d outside 0..%d", new_len, ctx->precise[b]);
+  if (new_len > 0 && new_len < ctx->track.firm[b])
+    return fail(ctx, EASYSPEC_ESTATE, "truncate: sequence %d was thinned; its first %d slots are not the first of its tokens", b, ctx->track.firm[b]);
+  if (new_len == 0) ctx->track.gone[b] = ctx->track.firm[b] = 0;
   ctx->precise[b] = new_len;
   ctx->fuzzy[b] = 0;
   ctx->tree[b].n = 0;
@@ -1094,8 +1311,14 @@ extern "C" int easyspec_kv_import(easyspec_ctx* ctx, int32_t b, const void* k, c
   if (b < 0 || b >= ctx->s.B) return fail(ctx, EASYSPEC_EINVAL, "kv_import: sequence %d out of range", b);
   if (n_slots < 0 || n_slots > ctx->s.max_ctx) return fail(ctx, EASYSPEC_ECAPACITY, "kv_import: %d slots exceed max_ctx %d", n_slots, ctx->s.max_ctx);
   if (n_slots > 0 && (!k || !v)) return fail(ctx, EASYSPEC_EINVAL, "kv_import: NULL argument");
+  const Shape& s = ctx->s;
+  const size_t pitch = (size_t)s.max_ctx * sizeof(float);
+  if (ctx->track.weights && n_slots > 0)  // nothing is known of them
+    for (int l = 0; l < s.L; ++l)
+      HIPCHK(ctx, hipMemset2DAsync(ctx->track.weights + ((size_t)l * s.B + b) * s.Hkv * s.max_ctx, pitch, 0, n_slots * sizeof(float), s.Hkv, ctx->stream));
   const int rc = kv_xfer(ctx, b, const_cast<void*>(k), const_cast<void*>(v), n_slots, 1);
   if (rc != EASYSPEC_OK) return rc;
+  ctx->track.gone[b] = ctx->track.firm[b] = 0;
   ctx->precise[b] = n_slots;
   ctx->fuzzy[b] = 0;
   ctx->tree[b].n = 0;

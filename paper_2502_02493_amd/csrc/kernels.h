@@ -15,7 +15,7 @@ struct Cols {
   int32_t n;
   int32_t seq[kMaxCols];
   int32_t pos[kMaxCols];        // slot the column writes; the highest slot it attends to
-  int32_t rope_pos[kMaxCols];   // its rotary position (= pos except for the nodes of a token tree)
+  int32_t rope_pos[kMaxCols];   // its rotary position (= pos except for the nodes of a token tree and after an eviction)
   // Visibility of slots 0..pos: every slot below vis_base, and slot vis_base + i iff bit i of
   // vis_mask (pos < vis_base + 64).  Causal columns: vis_base = pos + 1.
   int32_t vis_base[kMaxCols];
@@ -26,14 +26,14 @@ struct Cols {
 };
 
 // The columns of a wide pass: a calibration of more than kMaxCols columns in one pass.  Entry e is a sequence with
-// columns first[e] .. first[e + 1] - 1, its tokens in order from position pos0[e] on (causal).
+// columns first[e] .. first[e + 1] - 1, its tokens in order from slot pos0[e] on (causal); rotary positions lie ahead[e] further.
 constexpr int kWideCols = 256;  // 16 sequences of 16 tokens
 constexpr int kWideSeqs = 16;
 struct Spans {
   int32_t n, n_seq;
   int32_t tok_pitch;  // the token of column i of entry e: tokens[seq[e] * tok_pitch + i - first[e]]
   int32_t first[kWideSeqs + 1];
-  int32_t seq[kWideSeqs], pos0[kWideSeqs];
+  int32_t seq[kWideSeqs], pos0[kWideSeqs], ahead[kWideSeqs];
 };
 
 struct Shape {
@@ -57,7 +57,7 @@ struct Buffers {
   void *embed;                           // plain [V][d] T
   float *bqkv;                           // [L][RQKV] or null
   float *g_attn, *g_mlp, *g_final;       // [L][d], [L][d], [d]
-  float2 *rope;                          // [max_ctx][hd/2] (cos, sin)
+  float2 *rope;                          // [positions][hd/2] (cos, sin); positions: max_ctx, or what easyspec_track_attention asked for
   // cache
   void *kc, *vc;  // [L][B][Hkv][max_ctx][hd] T
   // workspaces (per forward pass).  fp32 arrays are [.][kMaxCols][width].  Arrays in T are operands of
@@ -293,6 +293,7 @@ struct WeighArgs {
 };
 void weigh_plan(WeighArgs& a, int n_layers);
 size_t weigh_workspace_bytes(const WeighArgs& a, int n_layers);
+size_t weigh_workspace_limit(int max_tokens, int B, int heads, int group, int max_slots);  // of any call of one layer
 void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
 
 // Reads `bytes` (multiple of 16) of buf once; sink: stream_read_sink_floats() floats.

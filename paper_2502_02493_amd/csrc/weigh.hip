@@ -258,13 +258,15 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_add_kernel(WeighArgs a) {
   }
 }
 
+constexpr long kWeighMostWgs = 2048;
+
 // Chunks: short enough that the workgroups fill the chip several times over, from one tile per wave up.
 static int weigh_chunk(const WeighArgs& a, int n_layers) {
   int chunk = 64;
   for (; chunk < kWeighMaxChunk; chunk *= 2) {
     long wgs = 0;
     for (int i = 0; i < a.n_entries; ++i) wgs += (a.entry[i].len + chunk - 1) / chunk;
-    if (wgs * a.heads * n_layers <= 2048) break;
+    if (wgs * a.heads * n_layers <= kWeighMostWgs) break;
   }
   return chunk;
 }
@@ -291,6 +293,11 @@ void weigh_plan(WeighArgs& a, int n_layers) {
   a.stats_pitch = stat;
 }
 size_t weigh_workspace_bytes(const WeighArgs& a, int n_layers) { return a.stats_pitch * a.heads * n_layers * sizeof(float2); }
+
+size_t weigh_workspace_limit(int max_tokens, int B, int heads, int group, int max_slots) {
+  const size_t wgs = std::max((size_t)kWeighMostWgs, (size_t)B * heads * ((max_slots + kWeighMaxChunk - 1) / kWeighMaxChunk));
+  return wgs * max_tokens * group * sizeof(float2);
+}
 
 void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st) {
   if (a.n_entries == 0) return;

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void wide_qkv_finish_kernel(WideQkvArgs a, Spa
     b_hi = *reinterpret_cast<const f32x4*>(a.bias + head * a.hd + e0 + half);
   }
   if (head < a.Hq + a.Hkv) {
-    const f32x4* rp = reinterpret_cast<const f32x4*>(a.rope + (size_t)pos * half + e0);
+    const f32x4* rp = reinterpret_cast<const f32x4*>(a.rope + (size_t)(pos + sp.ahead[en]) * half + e0);
     cs0 = rp[0];
     cs1 = rp[1];
   }

@@ -14,6 +14,7 @@
 namespace es {
 
 constexpr int kSliceThreads = 512, kSliceRegs = 8, kSliceMax = kSliceThreads * kSliceRegs;
+constexpr int kListMax = 1024;  // candidates ranked in LDS
 constexpr int kPickThreads = 1024;
 
 // A candidate of (1): logit and token as one number whose order is that of the candidates of a beam.  0: none.
@@ -21,6 +22,10 @@ typedef unsigned long long cand_t;
 __device__ __forceinline__ uint32_t ordered_bits(float f) {  // order-preserving; not 0 for anything but a NaN of all ones
   const uint32_t u = __float_as_uint(f + 0.f);               // -0 and 0 are one logit
   return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long ordered_bits(double f) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, f + 0.0);
+  return u >> 63 ? ~u : u | 1ull << 63;
 }
 __device__ __forceinline__ cand_t make_cand(float logit, int token) {
   if (!(logit > -INFINITY)) return 0;  // minus infinity and NaN are no candidates
@@ -63,7 +68,8 @@ __global__ __launch_bounds__(kSliceThreads) void beam_slice_kernel(BeamArgs a) {
   constexpr int NW = kSliceThreads / 64;
   __shared__ double sh_d[NW];
   __shared__ float sh_f[NW];
-  __shared__ cand_t sh_c[NW];
+  __shared__ cand_t s_list[kListMax];
+  __shared__ int s_n, s_wave[NW];
   const int slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (!(a.scores[row] > -INFINITY) || (a.ended && a.ended[row])) return;  // (2) looks at neither
   const float* l_row = a.logits + (size_t)row * a.V;
@@ -90,24 +96,62 @@ __global__ __launch_bounds__(kSliceThreads) void beam_slice_kernel(BeamArgs a) {
     a.stats[2 * at] = (double)mx;
     a.stats[2 * at + 1] = z;
   }
-  // the n_select highest, one after the other
-  cand_t c[kSliceRegs];
+  // The n_select highest.  A bound from below: of at least n_select groups of threads the lowest maximum, which as many logits
+  // reach.  Few more do: with 16 groups of 256 logits some 50 of 4096.
+  const int lanes = a.n_select <= NW ? 64 : a.n_select <= 2 * NW ? 32 : a.n_select <= 4 * NW ? 16 : 8;
+  float own = l[0];
 #pragma unroll
-  for (int i = 0; i < kSliceRegs; ++i) c[i] = v0 + i * kSliceThreads + tid < v1 ? make_cand(l[i], v0 + i * kSliceThreads + tid) : 0;
-  for (int k = 0; k < a.n_select; ++k) {
-    cand_t best = 0;
+  for (int i = 1; i < kSliceRegs; ++i) own = fmaxf(own, l[i]);
+  own = lanes_max(own, lanes);
+  for (int off = lanes; off < 64; off <<= 1) own = fminf(own, __shfl_xor(own, off, 64));
+  if (lane == 0) sh_f[wave] = own;
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  float bound = sh_f[0];
 #pragma unroll
-    for (int i = 0; i < kSliceRegs; ++i) best = max(best, c[i]);
-    for (int off = 32; off > 0; off >>= 1) best = max(best, (cand_t)__shfl_xor((unsigned long long)best, off, 64));
+  for (int w = 1; w < NW; ++w) bound = fminf(bound, sh_f[w]);
+  auto cand = [&](int i) { return make_cand(l[i], v0 + i * kSliceThreads + tid); };  // none past the slice: minus infinity
+  auto collect = [&](auto&& reaches) {
+#pragma unroll
+    for (int i = 0; i < kSliceRegs; ++i)
+      if (reaches(i)) {
+        const int at_n = atomicAdd(&s_n, 1);
+        if (at_n < kListMax) s_list[at_n] = cand(i);
+      }
     __syncthreads();
-    if (lane == 0) sh_c[wave] = best;
+  };
+  collect([&](int i) { return l[i] >= bound && l[i] > -INFINITY; });
+  if (s_n > kListMax) {
+    // Many equal logits, or groups that a mask empties: the n_select-th candidate itself, bit by bit
+    cand_t least = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const cand_t t = least | (cand_t)1 << bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kSliceRegs; ++i) n += __popcll(__ballot(cand(i) >= t));
+      __syncthreads();
+      if (lane == 0) s_wave[wave] = n;
+      __syncthreads();
+      n = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) n += s_wave[w];
+      if (n >= a.n_select) least = t;
+    }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NW; ++w) best = max(best, sh_c[w]);
-    if (tid == 0) a.cands[at * a.n_select + k] = best;
-#pragma unroll
-    for (int i = 0; i < kSliceRegs; ++i) c[i] = c[i] == best ? 0 : c[i];
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    collect([&](int i) { return cand(i) >= least && cand(i) != 0; });
   }
+  // in order: a candidate's place is the number of those above it
+  const int n = s_n;
+  cand_t* list = a.cands + at * a.n_select;
+  for (int i = tid; i < n; i += kSliceThreads) {
+    const cand_t c = s_list[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += s_list[j] > c;
+    if (above < a.n_select) list[above] = c;
+  }
+  if (tid >= n && tid < a.n_select) list[tid] = 0;
 }
 
 // A candidate of (2).  Order: score, then beam, then what (1) goes by.
@@ -120,11 +164,13 @@ __device__ __forceinline__ bool before(const Pick& a, const Pick& b) {
   return a.score != b.score ? a.score > b.score : a.beam != b.beam ? a.beam < b.beam : a.cand > b.cand;
 }
 
-// grid (groups): the slices' lists merged, the best head at a time.
+// grid (groups)
 __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
   constexpr int NW = kPickThreads / 64;
   __shared__ double s_top[kMaxBeams], s_log[kMaxBeams], s_cum[kMaxBeams];
-  __shared__ Pick s_best[NW];
+  __shared__ Pick s_list[kListMax];
+  __shared__ unsigned long long s_bound[kMaxSelect];
+  __shared__ int s_n;
   __shared__ int s_kind[kMaxBeams];  // 0 no candidates, 1 its lists, 2 the end token alone
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.slices, K = a.n_select;
   for (int w = wave; w < a.beams; w += NW) {
@@ -148,47 +194,85 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
       s_cum[w] = (double)cum;
     }
   }
+  if (tid < kMaxSelect) s_bound[tid] = 0;
+  if (tid == 0) s_n = 0;
   __syncthreads();
-  const Pick none = {-INFINITY, 0, kMaxBeams};
-  // a list: (beam, slice); an ended beam is a list of one.  The thread's lists: tid, tid + kPickThreads, ...
+  // a list: (beam, slice); an ended beam is one of a single candidate
   const int lists = a.beams * S;
+  const cand_t* cands = a.cands + (size_t)g * lists * K;
+  auto entry = [&](int i, int j, Pick& p) {  // the j-th candidate of list i; false: there is none
+    const int w = i / S, s = i - w * S;
+    p.beam = w;
+    if (s_kind[w] == 1) {
+      p.cand = j < K ? cands[(size_t)i * K + j] : 0;
+      p.score = s_cum[w] + (((double)cand_logit(p.cand) - s_top[w]) * a.inv_T - s_log[w]);
+      return p.cand != 0 && p.score > -INFINITY;  // a beam without a distribution offers nothing
+    }
+    p.cand = (cand_t)1 << 63 | (uint32_t)~a.end_token;
+    p.score = s_cum[w];
+    return s_kind[w] == 2 && s == 0 && j == 0;
+  };
+  // As in (1): the lists' first candidates dealt to at least n_select groups, and the lowest of the groups' maxima.
+  const int groups = K <= 16 ? 16 : K <= 32 ? 32 : 64;
+  const int depth = min(K, (2 * groups + lists - 1) / lists);
+  for (int i = tid; i < lists; i += kPickThreads)
+    for (int j = 0; j < depth; ++j) {
+      Pick p;
+      if (!entry(i, j, p)) break;
+      atomicMax(&s_bound[(i * depth + j) & (groups - 1)], ordered_bits(p.score));
+    }
+  __syncthreads();
+  unsigned long long bound = ~0ull;
+  for (int i = 0; i < groups; ++i) bound = min(bound, s_bound[i]);
+  for (int i = tid; i < lists; i += kPickThreads)
+    for (int j = 0; j < K; ++j) {
+      Pick p;
+      if (!entry(i, j, p) || ordered_bits(p.score) < bound) break;
+      const int at = atomicAdd(&s_n, 1);
+      if (at < kListMax) s_list[at] = p;
+    }
+  __syncthreads();
+  const int n = s_n;
+  auto write = [&](int k, const Pick& p) {
+    a.tokens_out[(size_t)g * K + k] = cand_token(p.cand);
+    a.parents_out[(size_t)g * K + k] = p.beam;
+    a.scores_out[(size_t)g * K + k] = (float)p.score;
+  };
+  if (n <= kListMax) {
+    for (int i = tid; i < n; i += kPickThreads) {
+      const Pick p = s_list[i];
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += before(s_list[j], p);
+      if (above < K) write(above, p);
+    }
+    if (tid >= n && tid < K) {
+      a.tokens_out[(size_t)g * K + tid] = a.parents_out[(size_t)g * K + tid] = -1;
+      a.scores_out[(size_t)g * K + tid] = -INFINITY;
+    }
+    return;
+  }
+  // Many equal scores: the best head of the lists, K times (there are more than K candidates)
   Pick taken = {INFINITY, 0, -1};  // everything that comes before it has been handed out
   for (int k = 0; k < K; ++k) {
-    Pick best = none;
-    for (int i = tid; i < lists; i += kPickThreads) {
-      const int w = i / S, s = i - w * S;
-      if (s_kind[w] == 0 || (s_kind[w] == 2 && s > 0)) continue;
-      if (s_kind[w] == 2) {
-        const Pick p = {s_cum[w], (cand_t)1 << 63 | (uint32_t)~a.end_token, w};
-        if (before(taken, p) && before(p, best)) best = p;
-        continue;
-      }
-      const cand_t* list = a.cands + ((size_t)(g * a.beams + w) * S + s) * K;
+    Pick best = {-INFINITY, 0, kMaxBeams};
+    for (int i = tid; i < lists; i += kPickThreads)
       for (int j = 0; j < K; ++j) {
-        const cand_t c = list[j];
-        if (!c) break;
-        const Pick p = {s_cum[w] + (((double)cand_logit(c) - s_top[w]) * a.inv_T - s_log[w]), c, w};
-        if (!(p.score > -INFINITY)) break;  // a beam without a distribution
+        Pick p;
+        if (!entry(i, j, p)) break;
         if (!before(taken, p)) continue;
         if (before(p, best)) best = p;
         break;
       }
-    }
     for (int off = 32; off > 0; off >>= 1) {
       const Pick o = {__shfl_xor(best.score, off, 64), (cand_t)__shfl_xor((unsigned long long)best.cand, off, 64), __shfl_xor(best.beam, off, 64)};
       if (before(o, best)) best = o;
     }
     __syncthreads();
-    if (lane == 0) s_best[wave] = best;
+    if (lane == 0) s_list[wave] = best;
     __syncthreads();
     for (int w = 0; w < NW; ++w)
-      if (before(s_best[w], best)) best = s_best[w];
-    if (tid == 0) {
-      const bool any = best.beam < kMaxBeams;
-      a.tokens_out[(size_t)g * K + k] = any ? cand_token(best.cand) : -1;
-      a.parents_out[(size_t)g * K + k] = any ? best.beam : -1;
-      a.scores_out[(size_t)g * K + k] = any ? (float)best.score : -INFINITY;
-    }
+      if (before(s_list[w], best)) best = s_list[w];
+    if (tid == 0) write(k, best);
     taken = best;
   }
 }

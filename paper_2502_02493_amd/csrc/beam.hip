@@ -8,14 +8,13 @@
 //   (1) beam_slice_kernel  per beam and vocabulary slice: slice maximum and sum of exp((l - max) / T), and the slice's n_select
 //                          highest logits in order.  A thread holds its logits in registers: the slice is read once.
 //   (2) beam_pick_kernel   per group: the beams' sums from their slices', then the best of the slices' lists.
-#include "kernels.h"
+#include "launch_common.hpp"
 #include "lane_ops.hpp"
 
 namespace es {
 
-constexpr int kSliceThreads = 512, kSliceRegs = 8, kSliceMax = kSliceThreads * kSliceRegs;
+constexpr int kSliceThreads = 256, kSliceRegs = 16, kSliceMax = kSliceThreads * kSliceRegs;
 constexpr int kListMax = 1024;  // candidates ranked in LDS
-constexpr int kPickThreads = 1024;
 
 // A candidate of (1): logit and token as one number whose order is that of the candidates of a beam.  0: none.
 typedef unsigned long long cand_t;
@@ -55,7 +54,7 @@ struct BeamArgs {
   const float* scores;
   const int32_t* ended;
   int beams, V, n_select, slices, end_token;
-  double inv_T;
+  double inv_T, log2e_T;
   double* stats;
   cand_t* cands;
   int32_t* tokens_out;
@@ -63,187 +62,325 @@ struct BeamArgs {
   float* scores_out;
 };
 
+// exp2(u) for -1000 <= u <= 0 in double precision: the whole part goes into the exponent, the rest through the series of
+// exp(f ln 2) up to f^10 (|f| <= 1/2: off by 0.347^11 / 11! = 2.2e-13 at most).  The launch of (1) is bound by instructions: the
+// library's exponential, which serves arguments that do not occur here, takes more than twice as many.
+__device__ __forceinline__ double scalar_operand(double c) {  // the compiler would copy a literal into a vector register at every use
+  asm("" : "+s"(c));
+  return c;
+}
+__device__ __forceinline__ double exp2_below(double u) {
+  const double n = __builtin_rint(u), f = u - n;
+  double p = 7.054911620801121e-09;  // ln2^10 / 10!
+  p = fma(p, f, scalar_operand(1.0178086009239696e-07));
+  p = fma(p, f, scalar_operand(1.3215486790144305e-06));
+  p = fma(p, f, scalar_operand(1.5252733804059838e-05));
+  p = fma(p, f, scalar_operand(1.5403530393381606e-04));
+  p = fma(p, f, scalar_operand(1.3333558146428441e-03));
+  p = fma(p, f, scalar_operand(9.618129107628477e-03));
+  p = fma(p, f, scalar_operand(5.5504108664821576e-02));
+  p = fma(p, f, scalar_operand(2.402265069591007e-01));
+  p = fma(p, f, scalar_operand(6.931471805599453e-01));
+  p = fma(p, f, 1.0);
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, p);
+  return __builtin_bit_cast(double, (unsigned long long)((uint32_t)(b >> 32) + ((uint32_t)(int)n << 20)) << 32 | (uint32_t)b);
+}
+// A slice's sum on top of another maximum: sum exp((m - top) / T), top >= m.  Nothing where nothing is finite.
+__device__ __forceinline__ double rescaled(double sum, double m, double top, double log2e_T) {
+  const double u = (m - top) * log2e_T;
+  return u > -1000.0 ? sum * exp2_below(u) : 0.0;
+}
+
 // grid (slices, rows)
 __global__ __launch_bounds__(kSliceThreads) void beam_slice_kernel(BeamArgs a) {
-  constexpr int NW = kSliceThreads / 64;
-  __shared__ double sh_d[NW];
-  __shared__ float sh_f[NW];
-  __shared__ cand_t s_list[kListMax];
-  __shared__ int s_n, s_wave[NW];
-  const int slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int NW = kSliceThreads / 64, kWaveList = kListMax / NW;
+  __shared__ u32x2 s_list[NW][kWaveList];  // (token, logit); later the candidates of all waves
+  __shared__ int s_above[NW][64];
+  __shared__ double s_sum[NW];
+  __shared__ float s_max[NW], s_bound[NW];
+  __shared__ int s_count[NW];
+  const int slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (!(a.scores[row] > -INFINITY) || (a.ended && a.ended[row])) return;  // (2) looks at neither
   const float* l_row = a.logits + (size_t)row * a.V;
   const int per = (a.V + a.slices - 1) / a.slices, v0 = min(a.V, slice * per), v1 = min(a.V, v0 + per);
   float l[kSliceRegs];
 #pragma unroll
-  for (int i = 0; i < kSliceRegs; ++i) {
-    const int v = v0 + i * kSliceThreads + tid;
-    l[i] = v < v1 ? l_row[v] : -INFINITY;
-    l[i] = l[i] == l[i] ? l[i] : -INFINITY;
-  }
-  float mx = -INFINITY;
+  for (int i = 0; i < kSliceRegs; ++i) l[i] = l_row[min(v0 + i * kSliceThreads + tid, a.V - 1)];
 #pragma unroll
-  for (int i = 0; i < kSliceRegs; ++i) mx = fmaxf(mx, l[i]);
-  mx = block_max<NW>(mx, sh_f);
-  const double ref = mx == -INFINITY ? 0.0 : (double)mx;
+  for (int i = 0; i < kSliceRegs; ++i) l[i] = v0 + i * kSliceThreads + tid < v1 ? l[i] : -INFINITY;
+  float half_max[2] = {-INFINITY, -INFINITY};  // of the thread's two halves of the slice; a maximum passes over NaNs
+#pragma unroll
+  for (int i = 0; i < kSliceRegs; ++i) half_max[2 * i / kSliceRegs] = fmaxf(half_max[2 * i / kSliceRegs], l[i]);
+  const float own = fmaxf(half_max[0], half_max[1]);
+  // A bound of the n_select highest from below: of at least n_select groups of threads (of halves of them, for more than 32) the
+  // lowest maximum, which as many logits reach.  Few more do: with 16 groups of 256 logits some 50 of 4096.
+  const int lanes = a.n_select <= NW ? 64 : a.n_select <= 2 * NW ? 32 : a.n_select <= 4 * NW ? 16 : 8;
+  const float top = lanes_max(own, 64);
+  float least_max = groups_min(lanes_max(a.n_select <= 8 * NW ? own : half_max[0], lanes), lanes);
+  if (a.n_select > 8 * NW) least_max = fminf(least_max, groups_min(lanes_max(half_max[1], lanes), lanes));
+  // Every wave's sum on top of its own maximum: no wait for the others'.  What lies 1000 powers of two below, minus infinities and
+  // NaNs among it, counts as 2^-1000.
+  const double ref = top == -INFINITY ? 0.0 : (double)top;
   double z = 0.0;
 #pragma unroll
-  for (int i = 0; i < kSliceRegs; ++i)
-    if (v0 + i * kSliceThreads < v1) z += exp(((double)l[i] - ref) * a.inv_T);  // uniform; slots past the end add 0
-  z = block_sum<NW>(z, sh_d);
-  const size_t at = (size_t)row * a.slices + slice;
-  if (tid == 0) {
-    a.stats[2 * at] = (double)mx;
-    a.stats[2 * at + 1] = z;
+  for (int i = 0; i < kSliceRegs; ++i) z += exp2_below(fmax(((double)l[i] - ref) * a.log2e_T, -1000.0));
+  z = lanes_sum(z, 64);
+  if (lane == 0) {
+    s_max[wave] = top;
+    s_bound[wave] = least_max;
+    s_sum[wave] = z;
   }
-  // The n_select highest.  A bound from below: of at least n_select groups of threads the lowest maximum, which as many logits
-  // reach.  Few more do: with 16 groups of 256 logits some 50 of 4096.
-  const int lanes = a.n_select <= NW ? 64 : a.n_select <= 2 * NW ? 32 : a.n_select <= 4 * NW ? 16 : 8;
-  float own = l[0];
-#pragma unroll
-  for (int i = 1; i < kSliceRegs; ++i) own = fmaxf(own, l[i]);
-  own = lanes_max(own, lanes);
-  for (int off = lanes; off < 64; off <<= 1) own = fminf(own, __shfl_xor(own, off, 64));
-  if (lane == 0) sh_f[wave] = own;
-  if (tid == 0) s_n = 0;
   __syncthreads();
-  float bound = sh_f[0];
+  const size_t at = (size_t)row * a.slices + slice;
+  float bound = s_bound[0];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) bound = fminf(bound, sh_f[w]);
-  auto cand = [&](int i) { return make_cand(l[i], v0 + i * kSliceThreads + tid); };  // none past the slice: minus infinity
-  auto collect = [&](auto&& reaches) {
+  for (int w = 1; w < NW; ++w) bound = fminf(bound, s_bound[w]);
+  bound = fmaxf(bound, -3.4028235e38f);  // minus infinity is no candidate
+  auto cand = [&](int i) { return make_cand(l[i], v0 + i * kSliceThreads + tid); };
+  // every wave lists its own: no counter, and as a rule a comparison is all there is to do
+  int mine = 0;
 #pragma unroll
-    for (int i = 0; i < kSliceRegs; ++i)
-      if (reaches(i)) {
-        const int at_n = atomicAdd(&s_n, 1);
-        if (at_n < kListMax) s_list[at_n] = cand(i);
-      }
-    __syncthreads();
-  };
-  collect([&](int i) { return l[i] >= bound && l[i] > -INFINITY; });
-  if (s_n > kListMax) {
-    // Many equal logits, or groups that a mask empties: the n_select-th candidate itself, bit by bit
-    cand_t least = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const cand_t t = least | (cand_t)1 << bit;
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < kSliceRegs; ++i) n += __popcll(__ballot(cand(i) >= t));
-      __syncthreads();
-      if (lane == 0) s_wave[wave] = n;
-      __syncthreads();
-      n = 0;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) n += s_wave[w];
-      if (n >= a.n_select) least = t;
+  for (int i = 0; i < kSliceRegs; ++i) {
+    const unsigned long long who = __ballot(l[i] >= bound);
+    if (who) {
+      const int place = mine + __popcll(who & ((1ull << lane) - 1));
+      if ((who >> lane & 1) && place < kWaveList) s_list[wave][place] = u32x2{(uint32_t)(v0 + i * kSliceThreads + tid), __float_as_uint(l[i])};
+      mine += __popcll(who);
     }
-    __syncthreads();
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-    collect([&](int i) { return cand(i) >= least && cand(i) != 0; });
   }
-  // in order: a candidate's place is the number of those above it
-  const int n = s_n;
+  if (lane == 0) s_count[wave] = mine;
+  __syncthreads();
+  int count[NW], n = 0;
+  bool fits = true;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    count[w] = s_count[w];
+    fits = fits && count[w] <= kWaveList;
+    n += count[w];
+  }
   cand_t* list = a.cands + at * a.n_select;
-  for (int i = tid; i < n; i += kSliceThreads) {
-    const cand_t c = s_list[i];
-    int above = 0;
-    for (int j = 0; j < n; ++j) above += s_list[j] > c;
-    if (above < a.n_select) list[above] = c;
+  if (wave == NW - 1) {  // the slice's maximum and sum
+    float all = s_max[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) all = fmaxf(all, s_max[w]);
+    double sum = 0.0;
+    for (int w = 0; w < NW; ++w) sum += rescaled(s_sum[w], s_max[w], all, a.log2e_T);
+    if (lane == 0) {
+      a.stats[2 * at] = (double)all;
+      a.stats[2 * at + 1] = all == INFINITY ? __builtin_nan("") : all == -INFINITY ? 0.0 : sum;
+    }
   }
-  if (tid >= n && tid < a.n_select) list[tid] = 0;
+  auto entry = [&](int i) {  // of the waves' lists, one after the other
+    int w = 0;
+#pragma unroll
+    for (int k = 0; k < NW - 1; ++k) {
+      const bool next = w == k && i >= count[k];
+      i -= next ? count[k] : 0;
+      w += next;
+    }
+    const u32x2 c = s_list[w][max(i, 0)];
+    return make_cand(__uint_as_float(c[1]), (int)c[0]);
+  };
+  // in order: a candidate's place is the number of those above it
+  if (n <= 64) {  // as a rule: a lane's candidate each, the others handed round by a quarter of them to a wave
+    const cand_t own_c = entry(min(lane, n - 1)), c = lane < n ? own_c : 0;
+    int above = 0;
+    for (int i = 4 * wave; i < n; i += 4 * NW)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const cand_t o = (cand_t)(uint32_t)__builtin_amdgcn_readlane((int)(c >> 32), i + k) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)c, i + k);
+        above += o > c;
+      }
+    s_above[wave][lane] = above;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < NW; ++w) above += s_above[w][lane];
+    if (lane < n && above < a.n_select) list[above] = c;
+    if (lane >= n && lane < a.n_select) list[lane] = 0;
+    return;
+  }
+  cand_t* s_flat = reinterpret_cast<cand_t*>(&s_list[0][0]);
+  if (fits) {
+    cand_t all[kListMax / kSliceThreads];
+#pragma unroll
+    for (int k = 0; k < kListMax / kSliceThreads; ++k) all[k] = entry(min(tid + k * kSliceThreads, n - 1));
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kListMax / kSliceThreads; ++k)
+      if (tid + k * kSliceThreads < n) s_flat[tid + k * kSliceThreads] = all[k];
+    __syncthreads();
+    for (int i = tid; i < n; i += kSliceThreads) {
+      const cand_t c = s_flat[i];
+      int above = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) above += s_flat[j] > c;
+      if (above < a.n_select) list[above] = c;
+    }
+    return;
+  }
+  // Many equal logits, or groups that a mask empties: the n_select-th candidate itself, bit by bit, then those from it on
+  cand_t last = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const cand_t t = last | (cand_t)1 << bit;
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < kSliceRegs; ++i) reach += __popcll(__ballot(cand(i) >= t));
+    __syncthreads();
+    if (lane == 0) s_count[wave] = reach;
+    __syncthreads();
+    reach = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) reach += s_count[w];
+    if (reach >= a.n_select) last = t;
+  }
+  __syncthreads();
+  if (tid == 0) s_count[0] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSliceRegs; ++i)
+    if (cand(i) >= last && cand(i) != 0) s_flat[atomicAdd(&s_count[0], 1)] = cand(i);  // n_select of them: candidates are all different
+  __syncthreads();
+  n = s_count[0];
+  if (tid < n) {
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += s_flat[j] > s_flat[tid];
+    list[above] = s_flat[tid];
+  }
 }
 
-// A candidate of (2).  Order: score, then beam, then what (1) goes by.
-struct Pick {
-  double score;
-  cand_t cand;
-  int beam;
+// A candidate of (2) as two numbers whose order is that of the candidates: its score, then beam (the lowest first), logit and token.
+static_assert(kMaxBeams <= 64 && kMaxBeamVocab <= 1 << 20, "beam, logit and token share 64 bits");
+struct alignas(16) Pick {
+  uint64_t score, tie;
 };
+__device__ __forceinline__ Pick make_pick(double score, int beam, uint32_t logit_bits, int token) {
+  return Pick{ordered_bits(score), (uint64_t)(63 - beam) << 52 | (uint64_t)logit_bits << 20 | (uint32_t)(0xFFFFF - token)};
+}
 __device__ __forceinline__ bool before(const Pick& a, const Pick& b) {
-  return a.score != b.score ? a.score > b.score : a.beam != b.beam ? a.beam < b.beam : a.cand > b.cand;
+  return (int)(a.score > b.score) | ((int)(a.score == b.score) & (int)(a.tie > b.tie));
 }
 
-// grid (groups)
-__global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
-  constexpr int NW = kPickThreads / 64;
+// grid (groups).  A thread takes a list: (beam, slice); the lists are sorted, and few reach far.
+constexpr int kHead = 4;  // candidates of a list that are looked at side by side
+template <int NT>
+__global__ __launch_bounds__(NT) void beam_pick_kernel(BeamArgs a) {
+  constexpr int NW = NT / 64;
   __shared__ double s_top[kMaxBeams], s_log[kMaxBeams], s_cum[kMaxBeams];
+  __shared__ int s_kind[kMaxBeams];  // 0 no candidates, 1 its lists, 2 the end token alone
   __shared__ Pick s_list[kListMax];
   __shared__ unsigned long long s_bound[kMaxSelect];
-  __shared__ int s_n;
-  __shared__ int s_kind[kMaxBeams];  // 0 no candidates, 1 its lists, 2 the end token alone
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.slices, K = a.n_select;
+  __shared__ int s_n, s_rank[kListMax];
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), S = a.slices, K = a.n_select;
+  const int lists = a.beams * S;
+  const cand_t* cands = a.cands + (size_t)g * lists * K;
+  cand_t c[kHead];
+  auto load_head = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) c[j] = cands[(size_t)min(i, lists - 1) * K + min(j, K - 1)];
+  };
+  load_head(tid);
   for (int w = wave; w < a.beams; w += NW) {
     const int row = g * a.beams + w;
+    const double* st = a.stats + (size_t)row * S * 2;
+    const int s0 = min(lane, S - 1);
+    const double m0 = st[2 * s0], z0 = st[2 * s0 + 1];  // of a beam without candidates: whatever is there
     const float cum = a.scores[row];
-    const int kind = !(cum > -INFINITY) ? 0 : a.ended && a.ended[row] ? 2 : 1;
-    double top = -INFINITY, sum = 0.0;
-    if (kind == 1) {
-      const double* st = a.stats + (size_t)row * S * 2;
-      float m = -INFINITY;
-      for (int s = lane; s < S; s += 64) m = fmaxf(m, (float)st[2 * s]);
+    const int ended = a.ended ? a.ended[row] : 0;
+    float m = (float)m0;
+    double top = (double)lanes_max(m, 64), sum = lane < S ? rescaled(z0, m0, top, a.log2e_T) : 0.0;
+    if (S > 64) {
+      for (int s = lane + 64; s < S; s += 64) m = fmaxf(m, (float)st[2 * s]);
       top = (double)lanes_max(m, 64);
-      for (int s = lane; s < S; s += 64)
-        if (st[2 * s] > -INFINITY) sum += st[2 * s + 1] * exp((st[2 * s] - top) * a.inv_T);
-      sum = lanes_sum(sum, 64);
+      sum = rescaled(z0, m0, top, a.log2e_T);
+      for (int s = lane + 64; s < S; s += 64) sum += rescaled(st[2 * s + 1], st[2 * s], top, a.log2e_T);
     }
+    sum = lanes_sum(sum, 64);
     if (lane == 0) {
-      s_kind[w] = kind;
+      s_kind[w] = !(cum > -INFINITY) ? 0 : ended ? 2 : 1;
       s_top[w] = top;
-      s_log[w] = kind == 1 ? log(sum) : 0.0;
+      s_log[w] = log(sum);
       s_cum[w] = (double)cum;
     }
   }
+  for (int i = tid; i < kListMax; i += NT) s_rank[i] = 0;
   if (tid < kMaxSelect) s_bound[tid] = 0;
   if (tid == 0) s_n = 0;
   __syncthreads();
-  // a list: (beam, slice); an ended beam is one of a single candidate
-  const int lists = a.beams * S;
-  const cand_t* cands = a.cands + (size_t)g * lists * K;
-  auto entry = [&](int i, int j, Pick& p) {  // the j-th candidate of list i; false: there is none
-    const int w = i / S, s = i - w * S;
-    p.beam = w;
+  auto entry = [&](int w, int s, int j, cand_t cand, Pick& p) {  // the j-th candidate of list (w, s); false: there is none
     if (s_kind[w] == 1) {
-      p.cand = j < K ? cands[(size_t)i * K + j] : 0;
-      p.score = s_cum[w] + (((double)cand_logit(p.cand) - s_top[w]) * a.inv_T - s_log[w]);
-      return p.cand != 0 && p.score > -INFINITY;  // a beam without a distribution offers nothing
+      const double score = s_cum[w] + (((double)cand_logit(cand) - s_top[w]) * a.inv_T - s_log[w]);
+      p = make_pick(score, w, (uint32_t)(cand >> 32), cand_token(cand));
+      return (int)(j < K) & (int)(cand != 0) & (int)(score > -INFINITY);  // a beam without a distribution offers nothing
     }
-    p.cand = (cand_t)1 << 63 | (uint32_t)~a.end_token;
-    p.score = s_cum[w];
-    return s_kind[w] == 2 && s == 0 && j == 0;
+    p = make_pick(s_cum[w], w, 0, a.end_token);
+    return (int)(s_kind[w] == 2) & (int)(s == 0) & (int)(j == 0);
   };
-  // As in (1): the lists' first candidates dealt to at least n_select groups, and the lowest of the groups' maxima.
-  const int groups = K <= 16 ? 16 : K <= 32 ? 32 : 64;
-  const int depth = min(K, (2 * groups + lists - 1) / lists);
-  for (int i = tid; i < lists; i += kPickThreads)
-    for (int j = 0; j < depth; ++j) {
+  // As in (1): the heads of the live beams' lists dealt to at least n_select groups, and the lowest of the groups' maxima.  Where
+  // these lists are few, the first candidates of each; a group that stays empty then means that there are fewer than
+  // groups / kHead lists, and all their candidates fit.
+  const int groups = K <= 8 ? 8 : K <= 16 ? 16 : K <= 32 ? 32 : 64;
+  const unsigned long long live = __ballot(lane < a.beams && s_kind[min(lane, a.beams - 1)] == 1);
+  const bool heads_do = __popcll(live) * S >= 4 * groups;
+  for (int i = tid; i < lists; i += NT) {
+    if (i >= NT) load_head(i);
+    const int w = i / S, s = i - w * S, number = __popcll(live & ((1ull << w) - 1)) * S + s;
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) {
       Pick p;
-      if (!entry(i, j, p)) break;
-      atomicMax(&s_bound[(i * depth + j) & (groups - 1)], ordered_bits(p.score));
+      if (entry(w, s, j, c[j], p)) atomicMax(&s_bound[(heads_do ? number : number * kHead + j) & (groups - 1)], (unsigned long long)p.score);
+      if (heads_do) break;
     }
+  }
   __syncthreads();
-  unsigned long long bound = ~0ull;
-  for (int i = 0; i < groups; ++i) bound = min(bound, s_bound[i]);
-  for (int i = tid; i < lists; i += kPickThreads)
-    for (int j = 0; j < K; ++j) {
-      Pick p;
-      if (!entry(i, j, p) || ordered_bits(p.score) < bound) break;
-      const int at = atomicAdd(&s_n, 1);
-      if (at < kListMax) s_list[at] = p;
+  const uint64_t bound = lanes_fold((uint64_t)s_bound[lane & (groups - 1)], groups, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+  for (int i = tid; i < lists; i += NT) {
+    if (lists > NT) load_head(i);
+    const int w = i / S, s = i - w * S;
+    Pick p[kHead];
+    int reach = 0;
+    bool in = true;
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) {
+      in = (int)in & entry(w, s, j, c[j], p[j]) & (int)(p[j].score >= bound);
+      reach += in;
     }
+    if (reach) {
+      int at = atomicAdd(&s_n, reach);
+#pragma unroll
+      for (int j = 0; j < kHead; ++j, ++at)
+        if (j < reach && at < kListMax) s_list[at] = p[j];
+    }
+    for (int j = kHead; j < K && in; ++j) {
+      Pick q;
+      in = (int)entry(w, s, j, cands[(size_t)i * K + j], q) & (int)(q.score >= bound);
+      if (in) {
+        const int at = atomicAdd(&s_n, 1);
+        if (at < kListMax) s_list[at] = q;
+      }
+    }
+  }
   __syncthreads();
   const int n = s_n;
   auto write = [&](int k, const Pick& p) {
-    a.tokens_out[(size_t)g * K + k] = cand_token(p.cand);
-    a.parents_out[(size_t)g * K + k] = p.beam;
-    a.scores_out[(size_t)g * K + k] = (float)p.score;
+    const uint64_t u = p.score >> 63 ? p.score & ~(1ull << 63) : ~p.score;
+    a.tokens_out[(size_t)g * K + k] = 0xFFFFF - (int)(p.tie & 0xFFFFF);
+    a.parents_out[(size_t)g * K + k] = 63 - (int)(p.tie >> 52);
+    a.scores_out[(size_t)g * K + k] = (float)__builtin_bit_cast(double, u);
   };
   if (n <= kListMax) {
-    for (int i = tid; i < n; i += kPickThreads) {
-      const Pick p = s_list[i];
+    // A candidate's place is the number of those before it: a lane takes one and the waves share out the others.
+    for (int j0 = 0; j0 < n; j0 += 64) {
+      const Pick own = s_list[min(j0 + lane, n - 1)];
       int above = 0;
-      for (int j = 0; j < n; ++j) above += before(s_list[j], p);
-      if (above < K) write(above, p);
+#pragma unroll 4
+      for (int i = wave; i < n; i += NW) above += before(s_list[i], own);
+      if (j0 + lane < n && above) atomicAdd(&s_rank[j0 + lane], above);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) {
+      const int above = s_rank[i];
+      if (above < K) write(above, s_list[i]);
     }
     if (tid >= n && tid < K) {
       a.tokens_out[(size_t)g * K + tid] = a.parents_out[(size_t)g * K + tid] = -1;
@@ -251,20 +388,20 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
     }
     return;
   }
-  // Many equal scores: the best head of the lists, K times (there are more than K candidates)
-  Pick taken = {INFINITY, 0, -1};  // everything that comes before it has been handed out
+  // Many equal scores: the best of the lists, K times (there are more than K candidates)
+  Pick taken = {~0ull, ~0ull};  // everything that comes before it has been handed out
   for (int k = 0; k < K; ++k) {
-    Pick best = {-INFINITY, 0, kMaxBeams};
-    for (int i = tid; i < lists; i += kPickThreads)
+    Pick best = {0, 0};
+    for (int i = tid; i < lists; i += NT)
       for (int j = 0; j < K; ++j) {
         Pick p;
-        if (!entry(i, j, p)) break;
+        if (!entry(i / S, i % S, j, cands[(size_t)i * K + j], p)) break;
         if (!before(taken, p)) continue;
         if (before(p, best)) best = p;
         break;
       }
     for (int off = 32; off > 0; off >>= 1) {
-      const Pick o = {__shfl_xor(best.score, off, 64), (cand_t)__shfl_xor((unsigned long long)best.cand, off, 64), __shfl_xor(best.beam, off, 64)};
+      const Pick o = {(uint64_t)__shfl_xor((unsigned long long)best.score, off, 64), (uint64_t)__shfl_xor((unsigned long long)best.tie, off, 64)};
       if (before(o, best)) best = o;
     }
     __syncthreads();
@@ -284,11 +421,13 @@ void launch_beam_select(const float* logits, const float* scores, const int32_t*
   a.logits = logits; a.scores = scores; a.ended = ended; a.beams = beams; a.V = V; a.n_select = n_select; a.end_token = end_token;
   a.slices = beam_slices(rows, V);
   a.inv_T = 1.0 / T;
+  a.log2e_T = 1.4426950408889634 / T;
   a.stats = (double*)ws;
   a.cands = (cand_t*)(a.stats + (size_t)rows * a.slices * 2);
   a.tokens_out = tokens_out; a.parents_out = parents_out; a.scores_out = scores_out;
   hipLaunchKernelGGL(beam_slice_kernel, dim3(a.slices, (unsigned)rows), dim3(kSliceThreads), 0, st, a);
-  hipLaunchKernelGGL(beam_pick_kernel, dim3(groups), dim3(kPickThreads), 0, st, a);
+  if ((long)beams * a.slices <= 256) hipLaunchKernelGGL(beam_pick_kernel<256>, dim3(groups), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(beam_pick_kernel<1024>, dim3(groups), dim3(1024), 0, st, a);
 }
 
 }  // namespace es

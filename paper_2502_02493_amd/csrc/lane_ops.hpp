@@ -13,11 +13,14 @@ __device__ __forceinline__ float dpp(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 template <int CTRL>
-__device__ __forceinline__ double dpp(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+__device__ __forceinline__ uint64_t dpp(uint64_t u) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, true);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
-  return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+  return (uint64_t)lo | ((uint64_t)hi << 32);
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  return __builtin_bit_cast(double, dpp<CTRL>(__builtin_bit_cast(uint64_t, v)));
 }
 // f of the values of lanes l and l ^ 16 (l ^ 32)
 template <bool HALF, class F>
@@ -27,12 +30,16 @@ __device__ __forceinline__ float across(float v, const F& f) {
   return f(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1]));
 }
 template <bool HALF, class F>
-__device__ __forceinline__ double across(double v, const F& f) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+__device__ __forceinline__ uint64_t across(uint64_t u, const F& f) {
   const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32);
   const auto l = HALF ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
   const auto h = HALF ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
-  return f(__builtin_bit_cast(double, (uint64_t)l[0] | ((uint64_t)h[0] << 32)), __builtin_bit_cast(double, (uint64_t)l[1] | ((uint64_t)h[1] << 32)));
+  return f((uint64_t)l[0] | ((uint64_t)h[0] << 32), (uint64_t)l[1] | ((uint64_t)h[1] << 32));
+}
+template <bool HALF, class F>
+__device__ __forceinline__ double across(double v, const F& f) {
+  const auto g = [&](uint64_t a, uint64_t b) { return __builtin_bit_cast(uint64_t, f(__builtin_bit_cast(double, a), __builtin_bit_cast(double, b))); };
+  return __builtin_bit_cast(double, across<HALF>(__builtin_bit_cast(uint64_t, v), g));
 }
 template <typename V, class F>
 __device__ __forceinline__ V lanes_fold(V v, int n, const F& f) {
@@ -50,6 +57,15 @@ __device__ __forceinline__ V lanes_sum(V v, int n) {
 }
 __device__ __forceinline__ float lanes_max(float v, int n) {
   return lanes_fold(v, n, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The lowest of the wave's values, which are the same in every lane of each group of n (8, 16, 32 or 64) neighbours.
+__device__ __forceinline__ float groups_min(float v, int n) {
+  const auto f = [](float a, float b) { return fminf(a, b); };
+  if (n <= 8) v = f(v, dpp<0x140>(v));  // row_mirror
+  if (n <= 16) v = across<false>(v, f);
+  if (n <= 32) v = across<true>(v, f);
+  return v;
 }
 
 // Over the workgroup of NW waves: the waves' results in order, the same bits in every thread.

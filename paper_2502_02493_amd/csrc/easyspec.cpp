@@ -464,6 +464,8 @@ static bool resident_takes(const easyspec_ctx* ctx, const Cols& c, const std::ve
   return ctx->r.ctl && ctx->prof_op < 0 && resident_pass(ctx->s, c, bounds.data(), (int)bounds.size() - 1) && !launches_forced();
 }
 
+static float weigh_scale(int hd) { return (float)(1.4426950408889634 / sqrt((double)hd)); }
+
 // The entries of a calibration's columns (those of a sequence lie together) and of a wide pass's, for launch_weigh.
 static void weigh_begin(const easyspec_ctx* ctx, const float* q, WeighArgs& a) {
   const Shape& s = ctx->s;
@@ -471,9 +473,10 @@ static void weigh_begin(const easyspec_ctx* ctx, const float* q, WeighArgs& a) {
   a.q = q;
   a.stats = ctx->track.stats;
   a.n_seqs = s.B; a.heads = s.Hkv; a.Hq = s.Hq; a.group = s.Hq / s.Hkv; a.max_slots = s.max_ctx;
-  a.scale = 1.f / sqrtf((float)s.hd);
+  a.scale = weigh_scale(s.hd);
 }
 static void weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q, WeighArgs& a) {
+  const Shape& s = ctx->s;
   weigh_begin(ctx, q, a);
   for (int i = 0; i < c.n; ++i) {
     if (i == 0 || c.seq[i] != c.seq[i - 1]) {
@@ -485,9 +488,10 @@ static void weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q
     e.n += 1;
     e.len = c.pos[i] + 1;
   }
-  weigh_plan(a, 1);
+  weigh_plan(a, 1, s.dtype);
 }
 static void weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q, WeighArgs& a) {
+  const Shape& s = ctx->s;
   weigh_begin(ctx, q, a);
   for (int i = 0; i < sp.n_seq; ++i) {
     WeighEntry& e = a.entry[a.n_entries++];
@@ -496,7 +500,7 @@ static void weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q
     e.n = sp.first[i + 1] - sp.first[i];
     e.len = sp.pos0[i] + e.n;
   }
-  weigh_plan(a, 1);
+  weigh_plan(a, 1, s.dtype);
 }
 static void weigh_layer(const easyspec_ctx* ctx, WeighArgs& a, int layer) {
   const Shape& s = ctx->s;
@@ -1021,8 +1025,8 @@ static int weigh_args(const char* what, const easyspec_kv_layout* g, const int32
   }
   a.n_seqs = g->n_seqs; a.heads = g->n_kv_heads; a.Hq = n_q_heads; a.group = group; a.max_slots = g->max_slots;
   a.q_layer_pitch = (size_t)q_first * n_q_heads * g->head_dim;
-  a.scale = 1.f / sqrtf((float)g->head_dim);
-  weigh_plan(a, g->n_layers);
+  a.scale = weigh_scale(g->head_dim);
+  weigh_plan(a, g->n_layers, g->dtype);
   return EASYSPEC_OK;
 }
 
@@ -1148,7 +1152,7 @@ extern "C" int easyspec_track_attention(easyspec_ctx* ctx, int32_t max_positions
   float *weights = nullptr, *rope = nullptr;
   ALLOC(ctx, weights, n * sizeof(float));
   ALLOC(ctx, ctx->track.kept, n * sizeof(int32_t));
-  ALLOC(ctx, ctx->track.stats, weigh_workspace_limit(ctx->cfg.max_calib_tokens, s.B, s.Hkv, s.Hq / s.Hkv, s.max_ctx));
+  ALLOC(ctx, ctx->track.stats, weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx));
   HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
   if (max_positions > s.max_ctx) {
     ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));

@@ -276,10 +276,9 @@ void launch_kv_evict(const void* k, const void* v, const float* weights, void* k
 // Attention weight of cached slots.  An entry: a sequence with new tokens.
 struct WeighEntry {
   int seq, n, len, q_first;  // its new tokens, its slots with them, its first row of tokens in q
-  int chunks, first_wg;      // set by weigh_plan
+  int chunks;                // set by weigh_plan
   size_t first_stat;
 };
-constexpr int kWeighMaxChunk = 1024;
 struct WeighArgs {
   const float* q;     // [layer][token][Hq][hd]
   const void* k;      // cache, T
@@ -288,12 +287,13 @@ struct WeighArgs {
   float2* stats;
   size_t q_layer_pitch, stats_pitch;
   int n_seqs, heads, Hq, group, max_slots, chunk, n_entries, n_wgs;
-  float scale;
+  float scale, inv_group;  // log2(e) / sqrt(hd); 1 / group
+  int first_wg[kMaxCols];  // set by weigh_plan: an entry's first workgroup of a KV head
   WeighEntry entry[kMaxCols];
 };
-void weigh_plan(WeighArgs& a, int n_layers);
+void weigh_plan(WeighArgs& a, int n_layers, int dtype);
 size_t weigh_workspace_bytes(const WeighArgs& a, int n_layers);
-size_t weigh_workspace_limit(int max_tokens, int B, int heads, int group, int max_slots);  // of any call of one layer
+size_t weigh_workspace_limit(int B, int heads, int group, int max_tokens, int max_slots);  // of any call of one layer
 void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
 
 // Reads `bytes` (multiple of 16) of buf once; sink: stream_read_sink_floats() floats.

@@ -1,6 +1,7 @@
 // Operators on KV caches [layer][sequence][KV head][slot][head_dim] (gfx950): the beams' slots put in the order of their parents,
 // and the lightest slots dropped.  Bytes are moved, nothing is computed but which.
 #include "launch_common.hpp"
+#include "lane_ops.hpp"
 
 namespace es {
 
@@ -74,11 +75,16 @@ void launch_kv_reorder(const void* k, const void* v, void* k_out, void* v_out, c
 
 // ------------------------------------------------------------------------------------------
 // Evict: of every (layer, sequence, KV head) the last `recent` slots and the heaviest of the others stay, in slot order.
-//   (1) evict_select_kernel  a workgroup per (layer, sequence, KV head) holds its weights in registers, finds the weight of the
-//                            last heavy slot bit by bit, and writes the list of kept slots and their weights;
+//   (1) evict_select_kernel  a workgroup per (layer, sequence, KV head) finds the weight of the last heavy slot by counting, and
+//                            writes the list of kept slots and their weights;
 //   (2) evict_move_kernel    the kept rows of K and V, elsewhere; or evict_shift_kernel, down inside the same cache.
+// Where few rows stay, (1) moves them itself.
+// The weight is found digit by digit: a histogram of the highest eleven bits of all weights, then of the next eleven of those that
+// share these, then of the last ten.  (Bit by bit, every step counting all weights again, 256 rows of up to 32768 took 88 us.)
 // ------------------------------------------------------------------------------------------
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kBins = 2048;
+constexpr int kFewKept = 256;          // rows that (1) moves itself: at most so many ...
+constexpr int kFewBytes = 32 * 1024;   // ... and so many bytes of K
 
 // The order of weights as unsigned numbers: NaN below everything, the two zeros alike.  0 is no weight.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -86,101 +92,186 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return w == w ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 1u;
 }
 
-// grid (layers x sequences x KV heads); NR: weights a thread holds.  weights_out may be weights.
-template <int NR>
-__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const float* weights, float* weights_out, int32_t* slots_out, EvictArgs a) {
-  __shared__ int s_count[2][kSelWaves];
-  __shared__ int s_gt[NR * kSelWaves], s_eq[NR * kSelWaves];
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// Running sums of two numbers over the threads of a workgroup of NW waves, in front of the thread; all: the whole sums.  sh: 2 NW
+// numbers, which nobody reads any more.
+struct Pair {
+  int x, y;
+};
+template <int NW>
+__device__ __forceinline__ Pair sum_before(Pair v, Pair* sh, Pair& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Pair s = {(int)lanes_running_sum(v.x), (int)lanes_running_sum(v.y)};
+  if (lane == 63) sh[wave] = s;
+  __syncthreads();
+  Pair before = {s.x - v.x, s.y - v.y};
+  all = Pair{0, 0};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const Pair o = sh[w];
+    before.x += w < wave ? o.x : 0;
+    before.y += w < wave ? o.y : 0;
+    all.x += o.x;
+    all.y += o.y;
+  }
+  return before;
+}
+
+// The rows of a list of n slots, moved by a workgroup of NT threads to the front of dst, which may be src: the list ascends, so the
+// rows of later rounds lie above everything that a round writes, and inside a round every load is done before the first store.
+template <int NT, class Slot>
+__device__ __forceinline__ void move_rows(const u32x4* src, u32x4* dst, int n, int log2_ppr, const Slot& slot_of) {
+  constexpr int kPieces = 4;
+  const int pieces = n << log2_ppr, mask = (1 << log2_ppr) - 1;
+  for (int base = 0; base < pieces; base += NT * kPieces) {
+    u32x4 x[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = min(base + j * NT + (int)threadIdx.x, pieces - 1);
+      x[j] = src[((size_t)slot_of(i >> log2_ppr) << log2_ppr) + (i & mask)];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads are done when their values are here: the barrier alone does not wait for them
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = base + j * NT + threadIdx.x;
+      if (i < pieces) dst[i] = x[j];
+    }
+  }
+}
+
+// grid (layers x sequences x KV heads).  A thread takes NR neighbouring slots of every run of NT * NR; weights are read again for every
+// digit (a row of 65536 is 256 KB, which the L2 holds).  weights_out may be weights.
+template <int NT, bool MOVE>
+__global__ __launch_bounds__(NT) void evict_select_kernel(const float* weights, float* weights_out, int32_t* slots_out, EvictArgs a, const u32x4* k,
+                                                          const u32x4* v, u32x4* k_out, u32x4* v_out) {
+  constexpr int NW = NT / 64, NR = 8, kRun = NT * NR;
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  __shared__ i32x4 s_hist[kBins / 4];  // the highest bin first
+  __shared__ Pair s_scan[2][NW];
+  __shared__ int s_bin, s_over, s_in;
+  __shared__ int s_kept[MOVE ? kFewKept : 1];
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int b = row / a.heads % a.n_seqs;
   const int n = a.len[b], keep = min(a.keep[b], n), recent = min(a.recent, keep), m = n - recent, need = keep - recent;
   if (keep <= 0) return;
   const float* w_row = weights + (size_t)row * a.max_slots;
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows need not lie on 16 bytes
   float w[NR];
+  auto load = [&](int first) {
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int s = r * kSelThreads + tid;
-    w[r] = s < n ? w_row[s] : 0.f;
-  }
-  auto key = [&](int r) { return r * kSelThreads + tid < m ? weight_key(w[r]) : 0u; };
-  int phase = 0;
-  auto count = [&](uint32_t least) {  // keys >= least, over the workgroup
-    int c = 0;
+    for (int r = 0; r < NR; r += 4) {
+      if (first + r + 3 < n) {
+        const f32x4_any x = *reinterpret_cast<const f32x4_any*>(w_row + first + r);
 #pragma unroll
-    for (int r = 0; r < NR; ++r) c += __popcll(__ballot(key(r) >= least));
-    if (lane == 0) s_count[phase][wave] = c;
-    __syncthreads();
-    int all = 0;
+        for (int j = 0; j < 4; ++j) w[r + j] = x[j];
+      } else {
 #pragma unroll
-    for (int i = 0; i < kSelWaves; ++i) all += s_count[phase][i];
-    phase ^= 1;
-    return all;
-  };
-  // The need-th largest key, from the highest bit down.  above: keys over it that all stay; equal ones stay up to `need`.
-  uint32_t t = 0, above;
-  int ties;
-  bool whole = need == 0;  // keys > above are exactly the ones that stay
-  if (!whole) {
-    for (int bit = 31; bit >= 0 && !whole; --bit) {
-      const uint32_t c = t | 1u << bit;
-      const int k = count(c);
-      if (k >= need) t = c;
-      whole = k == need;
-    }
-  }
-  if (need == 0) {
-    above = 0xFFFFFFFFu;
-    ties = 0;
-  } else if (whole) {
-    above = t - 1;
-    ties = 0;
-  } else {
-    above = t;
-    ties = need - (t == 0xFFFFFFFFu ? 0 : count(t + 1));
-  }
-  auto stays = [&](int r) {
-    const int s = r * kSelThreads + tid;
-    return s < m ? key(r) > above : s < n;
-  };
-  auto tied = [&](int r) { return ties > 0 && r * kSelThreads + tid < m && key(r) == above; };
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int gt = __popcll(__ballot(stays(r))), eq = __popcll(__ballot(tied(r)));
-    if (lane == 0) {
-      s_gt[r * kSelWaves + wave] = gt;
-      s_eq[r * kSelWaves + wave] = eq;
-    }
-  }
-  __syncthreads();
-  // running sums over (r, wave), the order of the slots
-  if (wave == 0) {
-    int base_gt = 0, base_eq = 0;
-    for (int i0 = 0; i0 < NR * kSelWaves; i0 += 64) {
-      const int i = i0 + lane;
-      const int gt = s_gt[i], eq = s_eq[i];
-      int sg = gt, se = eq;
-      for (int off = 1; off < 64; off <<= 1) {
-        const int og = __shfl_up(sg, off, 64), oe = __shfl_up(se, off, 64);
-        if (lane >= off) sg += og, se += oe;
+        for (int j = 0; j < 4; ++j) w[r + j] = first + r + j < n ? w_row[first + r + j] : 0.f;
       }
-      s_gt[i] = base_gt + sg - gt;
-      s_eq[i] = base_eq + se - eq;
-      base_gt += __shfl(sg, 63, 64);
-      base_eq += __shfl(se, 63, 64);
+    }
+  };
+  load(tid * NR);  // a row of one run stays in registers
+  // Keys over `above` stay, and of those equal to `tie` the first `ties`.
+  uint32_t above = 0xFFFFFFFFu, tie = 0;
+  int ties = 0;
+  if (need > 0) {
+    uint32_t prefix = 0;
+    int left = need;
+    for (int digit = 0; digit < 3; ++digit) {
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+      for (int i = tid; i < kBins / 4; i += NT) s_hist[i] = i32x4{0, 0, 0, 0};
+      __syncthreads();
+      int* hist = reinterpret_cast<int*>(s_hist);
+      for (int run = 0; run < m; run += kRun) {
+        const int first = run + tid * NR;
+        if (n > kRun) load(first);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const uint32_t key = weight_key(w[r]);
+          const bool counts = first + r < m && (digit == 0 || key >> (shift + bits) == prefix);
+          const int bin = kBins - 1 - (int)((key >> shift) & ((1u << bits) - 1));
+          const unsigned long long who = __ballot(counts);
+          if (!who) continue;
+          // many equal weights are common (slots that nothing has attended to have none): those of the first lane's bin at once
+          const int lead = __ffsll((long long)who) - 1, lead_bin = __builtin_amdgcn_readlane(bin, lead);
+          const unsigned long long same = __ballot(counts && bin == lead_bin);
+          if (counts && (bin != lead_bin || lane == lead)) atomicAdd(&hist[bin], bin == lead_bin ? __popcll(same) : 1);
+        }
+      }
+      __syncthreads();
+      // the bin that the left-th highest lies in
+      constexpr int kPer = kBins / NT;
+      int in[kPer], own = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) own += in[i] = hist[tid * kPer + i];
+      Pair all;
+      int over = sum_before<NW>(Pair{own, 0}, s_scan[digit & 1], all).x;
+      if (over < left && left <= over + own) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (over < left && left <= over + in[i]) {
+            s_bin = kBins - 1 - (tid * kPer + i);
+            s_over = over;
+            s_in = in[i];
+          }
+          over += in[i];
+        }
+      }
+      __syncthreads();
+      prefix = prefix << bits | (uint32_t)s_bin;
+      left -= s_over;
+      const bool whole = s_in == left;  // everything with this prefix stays
+      if (whole || digit == 2) {
+        tie = prefix << shift;
+        above = whole ? (tie ? tie - 1 : 0) : tie;
+        ties = whole ? 0 : left;
+        break;
+      }
     }
   }
+  // Slots that stay: their places are running sums over the threads, in the order of the slots.  A place lies below its slot, in
+  // runs that have been read.
+  int32_t* list = slots_out + (size_t)row * a.out_slots;
+  float* w_list = weights_out + (size_t)row * a.out_slots;
+  Pair so_far = {0, 0};  // sure to stay, and equal to `tie`
   __syncthreads();
-  const unsigned long long below = (1ull << lane) - 1;
+  int turn = 0;
+  for (int run = 0; run < n; run += kRun, turn ^= 1) {
+    const int first = run + tid * NR;
+    if (n > kRun) load(first);
+    auto stays = [&](int r) { return first + r < m ? weight_key(w[r]) > above : first + r < n; };
+    auto tied = [&](int r) { return ties > 0 && first + r < m && weight_key(w[r]) == tie; };
+    Pair own = {0, 0}, all;
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const bool st = stays(r), eq = tied(r);
-    const int gt_before = s_gt[r * kSelWaves + wave] + __popcll(__ballot(st) & below);
-    const int eq_before = s_eq[r * kSelWaves + wave] + __popcll(__ballot(eq) & below);
-    if (st || (eq && eq_before < ties)) {
-      const size_t at = (size_t)row * a.out_slots + gt_before + min(eq_before, ties);
-      slots_out[at] = r * kSelThreads + tid;
-      weights_out[at] = w[r];
+    for (int r = 0; r < NR; ++r) {
+      own.x += stays(r);
+      own.y += tied(r);
     }
+    Pair before = sum_before<NW>(own, s_scan[turn], all);
+    before.x += so_far.x;
+    before.y += so_far.y;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const bool s = stays(r), t = tied(r);
+      if (s || (t && before.y < ties)) {
+        const int at = before.x + min(before.y, ties);
+        list[at] = first + r;
+        w_list[at] = w[r];
+        if (MOVE) s_kept[at] = first + r;
+      }
+      before.x += s;
+      before.y += t;
+    }
+    so_far.x += all.x;
+    so_far.y += all.y;
+  }
+  if (MOVE) {
+    if (k == k_out && keep == n) return;
+    __syncthreads();
+    const size_t in = (size_t)row * a.max_slots << a.log2_ppr, out = (size_t)row * a.out_slots << a.log2_ppr;
+    const auto slot = [&](int j) { return s_kept[j]; };
+    move_rows<NT>(k + in, k_out + out, keep, a.log2_ppr, slot);
+    move_rows<NT>(v + in, v_out + out, keep, a.log2_ppr, slot);
   }
 }
 
@@ -207,33 +298,15 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const u32x4* k
   }
 }
 
-// The same inside one cache: a workgroup per (layer, sequence, KV head) and K or V walks the list upwards.  A kept row moves to a
-// lower slot or stays, so the rows of later rounds lie above everything that this round writes; inside a round every load is done
-// before the first store.
-constexpr int kShiftThreads = 512, kShiftPieces = 4;
+// The same inside one cache: a workgroup per (layer, sequence, KV head) and K or V.
+constexpr int kShiftThreads = 512;
 __global__ __launch_bounds__(kShiftThreads) void evict_shift_kernel(u32x4* k, u32x4* v, const int32_t* __restrict__ slots, EvictArgs a) {
   const int row = blockIdx.x, b = row / a.heads % a.n_seqs;
-  const int kept = min(a.keep[b], a.len[b]), log2_ppr = a.log2_ppr;
+  const int kept = min(a.keep[b], a.len[b]);
   if (kept == a.len[b]) return;
-  u32x4* rows = (blockIdx.y ? v : k) + ((size_t)row * a.max_slots << log2_ppr);
+  u32x4* rows = (blockIdx.y ? v : k) + ((size_t)row * a.max_slots << a.log2_ppr);
   const int32_t* list = slots + (size_t)row * a.out_slots;
-  const int n = kept << log2_ppr;
-  for (int base = 0; base < n; base += kShiftThreads * kShiftPieces) {
-    u32x4 x[kShiftPieces];
-#pragma unroll
-    for (int j = 0; j < kShiftPieces; ++j) {
-      const int i = base + j * kShiftThreads + threadIdx.x;
-      if (i < n) x[j] = rows[((size_t)list[i >> log2_ppr] << log2_ppr) + (i & ((1 << log2_ppr) - 1))];
-    }
-    // the loads are done when their values are here: the barrier alone does not wait for them
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kShiftPieces; ++j) {
-      const int i = base + j * kShiftThreads + threadIdx.x;
-      if (i < n) rows[i] = x[j];
-    }
-  }
+  move_rows<kShiftThreads>(rows, rows, kept, a.log2_ppr, [&](int j) { return list[j]; });
 }
 
 void launch_kv_evict(const void* k, const void* v, const float* weights, void* k_out, void* v_out, float* weights_out, int32_t* slots_out,
@@ -246,11 +319,16 @@ void launch_kv_evict(const void* k, const void* v, const float* weights, void* k
     if (a.keep[b] > 0) longest = std::max(longest, a.len[b]), most = std::max(most, std::min(a.keep[b], a.len[b]));
   if (most == 0) return;
   const int rows = g.n_layers * g.n_seqs * g.n_heads;
-  auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(kSelThreads), 0, st, weights, weights_out, slots_out, a); };
-  if (longest <= 4 * kSelThreads) select(evict_select_kernel<4>);
-  else if (longest <= 16 * kSelThreads) select(evict_select_kernel<16>);
-  else if (longest <= 32 * kSelThreads) select(evict_select_kernel<32>);
-  else select(evict_select_kernel<64>);
+  const bool move = most <= kFewKept && most * slot_bytes <= kFewBytes;
+  auto select = [&](int threads, auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, st, weights, weights_out, slots_out, a, (const u32x4*)k, (const u32x4*)v,
+                       (u32x4*)k_out, (u32x4*)v_out);
+  };
+  if (longest <= 2048 && move) select(256, evict_select_kernel<256, true>);
+  else if (longest <= 2048) select(256, evict_select_kernel<256, false>);
+  else if (move) select(1024, evict_select_kernel<1024, true>);
+  else select(1024, evict_select_kernel<1024, false>);
+  if (move) return;
   if (k == k_out) {
     hipLaunchKernelGGL(evict_shift_kernel, dim3(rows, 2), dim3(kShiftThreads), 0, st, (u32x4*)k_out, (u32x4*)v_out, slots_out, a);
     return;

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace es {
 
 // Reductions over 8, 16, 32 or 64 neighbouring lanes (n, uniform) by operand swizzles, every lane receiving the result; a shuffle
@@ -57,6 +59,19 @@ __device__ __forceinline__ V lanes_sum(V v, int n) {
 }
 __device__ __forceinline__ float lanes_max(float v, int n) {
   return lanes_fold(v, n, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// Running sum over the wave's lanes, the own one included.
+__device__ __forceinline__ uint32_t lanes_running_sum(uint32_t v) {
+  const auto moved = [](uint32_t x, auto ctrl, auto rows) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+  typedef std::integral_constant<int, 0xF> All;
+  v += moved(v, std::integral_constant<int, 0x111>{}, All{});  // row_shr by 1, 2, 4, 8: zeros come in
+  v += moved(v, std::integral_constant<int, 0x112>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x114>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x118>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});  // row_bcast15: the rows' ends to the second and fourth
+  v += moved(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});  // row_bcast31: the second's to the upper two
+  return v;
 }
 
 // The lowest of the wave's values, which are the same in every lane of each group of n (8, 16, 32 or 64) neighbours.

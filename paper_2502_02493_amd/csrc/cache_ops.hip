@@ -88,8 +88,14 @@ constexpr int kFewBytes = 32 * 1024;   // ... and so many bytes of K
 
 // The order of weights as unsigned numbers: NaN below everything, the two zeros alike.  0 is no weight.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  const uint32_t u = __float_as_uint(w + 0.f);
-  return w == w ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 1u;
+  const uint32_t u = __float_as_uint(w + 0.f), key = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+  return w == w ? key : 1u;
+}
+// The number of a key of at least minus infinity's.  Between the zeros there is none: the one below them for -0.
+constexpr uint32_t kLowestKey = 0x007FFFFFu;
+__device__ __forceinline__ float weight_of(uint32_t key) {
+  key -= key == 0x7FFFFFFFu;
+  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
 // Running sums of two numbers over the threads of a workgroup of NW waves, in front of the thread; all: the whole sums.  sh: 2 NW
@@ -150,27 +156,38 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const float* weights, 
   __shared__ Pair s_scan[2][NW];
   __shared__ int s_bin, s_over, s_in;
   __shared__ int s_kept[MOVE ? kFewKept : 1];
+  __shared__ int s_slot[kRun];      // what stays of a run, on its way out: scattered stores of single words took longer than
+  __shared__ float s_weight[kRun];  // everything else there
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int b = row / a.heads % a.n_seqs;
   const int n = a.len[b], keep = min(a.keep[b], n), recent = min(a.recent, keep), m = n - recent, need = keep - recent;
   if (keep <= 0) return;
   const float* w_row = weights + (size_t)row * a.max_slots;
   typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows need not lie on 16 bytes
-  float w[NR];
-  auto load = [&](int first) {
+  float w[NR], next[NR];
+  auto load = [&](float (&to)[NR], int first) {
 #pragma unroll
     for (int r = 0; r < NR; r += 4) {
       if (first + r + 3 < n) {
         const f32x4_any x = *reinterpret_cast<const f32x4_any*>(w_row + first + r);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[r + j] = x[j];
+        for (int j = 0; j < 4; ++j) to[r + j] = x[j];
       } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[r + j] = first + r + j < n ? w_row[first + r + j] : 0.f;
+        for (int j = 0; j < 4; ++j) to[r + j] = first + r + j < n ? w_row[first + r + j] : 0.f;
       }
     }
   };
-  load(tid * NR);  // a row of one run stays in registers
+  // A row of one run stays in registers; of a longer one the next run (after the last, the first) is on its way while one is used.
+  load(w, tid * NR);
+  auto request = [&](int run) {
+    if (n > kRun) load(next, (run + kRun < n ? run + kRun : 0) + tid * NR);
+  };
+  auto advance = [&] {
+    if (n > kRun)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) w[r] = next[r];
+  };
   // Keys over `above` stay, and of those equal to `tie` the first `ties`.
   uint32_t above = 0xFFFFFFFFu, tie = 0;
   int ties = 0;
@@ -182,21 +199,28 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const float* weights, 
       for (int i = tid; i < kBins / 4; i += NT) s_hist[i] = i32x4{0, 0, 0, 0};
       __syncthreads();
       int* hist = reinterpret_cast<int*>(s_hist);
-      for (int run = 0; run < m; run += kRun) {
+      for (int run = 0; run < n; run += kRun) {
         const int first = run + tid * NR;
-        if (n > kRun) load(first);
+        request(run);
+        auto count = [&](auto whole_run) {
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const uint32_t key = weight_key(w[r]);
-          const bool counts = first + r < m && (digit == 0 || key >> (shift + bits) == prefix);
-          const int bin = kBins - 1 - (int)((key >> shift) & ((1u << bits) - 1));
-          const unsigned long long who = __ballot(counts);
-          if (!who) continue;
-          // many equal weights are common (slots that nothing has attended to have none): those of the first lane's bin at once
-          const int lead = __ffsll((long long)who) - 1, lead_bin = __builtin_amdgcn_readlane(bin, lead);
-          const unsigned long long same = __ballot(counts && bin == lead_bin);
-          if (counts && (bin != lead_bin || lane == lead)) atomicAdd(&hist[bin], bin == lead_bin ? __popcll(same) : 1);
-        }
+          for (int r = 0; r < NR; ++r) {
+            const uint32_t key = weight_key(w[r]);
+            const bool counts = (int)(decltype(whole_run)::value || first + r < m) & (int)(digit == 0 || key >> (shift + bits) == prefix);
+            if (!decltype(whole_run)::value || digit > 0) {
+              if (!__ballot(counts)) continue;
+            }
+            const int bin = kBins - 1 - (int)((key >> shift) & ((1u << bits) - 1));
+            // many equal weights are common (slots that nothing has attended to have none): those of the first lane's bin at once
+            const int lead_bin = __builtin_amdgcn_readfirstlane(bin);
+            const unsigned long long same = __ballot(counts && bin == lead_bin);
+            if (counts && bin != lead_bin) atomicAdd(&hist[bin], 1);
+            if (lane == 0) atomicAdd(&hist[lead_bin], __popcll(same));
+          }
+        };
+        if (run + kRun <= m) count(std::true_type{});
+        else count(std::false_type{});
+        advance();
       }
       __syncthreads();
       // the bin that the left-th highest lies in
@@ -234,36 +258,54 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const float* weights, 
   int32_t* list = slots_out + (size_t)row * a.out_slots;
   float* w_list = weights_out + (size_t)row * a.out_slots;
   Pair so_far = {0, 0};  // sure to stay, and equal to `tie`
+  const bool numbers = ties == 0 && above >= kLowestKey;
+  const float over = weight_of(above);  // 0xFFFFFFFF: a NaN, which nothing is over
   __syncthreads();
   int turn = 0;
   for (int run = 0; run < n; run += kRun, turn ^= 1) {
     const int first = run + tid * NR;
-    if (n > kRun) load(first);
-    auto stays = [&](int r) { return first + r < m ? weight_key(w[r]) > above : first + r < n; };
-    auto tied = [&](int r) { return ties > 0 && first + r < m && weight_key(w[r]) == tie; };
-    Pair own = {0, 0}, all;
+    request(run);
+    int base = 0, end = 0;
+    // plain: a slot stays if its weight is over a number, which as a rule is all there is to it
+    auto emit = [&](auto plain, auto whole_run) {
+      constexpr bool P = decltype(plain)::value, W = decltype(whole_run)::value;
+      auto stays = [&](int r) { return W || first + r < m ? (P ? w[r] > over : weight_key(w[r]) > above) : first + r < n; };
+      auto tied = [&](int r) { return !P && ties > 0 && first + r < m && weight_key(w[r]) == tie; };
+      Pair own = {0, 0}, all;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      own.x += stays(r);
-      own.y += tied(r);
-    }
-    Pair before = sum_before<NW>(own, s_scan[turn], all);
-    before.x += so_far.x;
-    before.y += so_far.y;
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      const bool s = stays(r), t = tied(r);
-      if (s || (t && before.y < ties)) {
-        const int at = before.x + min(before.y, ties);
-        list[at] = first + r;
-        w_list[at] = w[r];
-        if (MOVE) s_kept[at] = first + r;
+      for (int r = 0; r < NR; ++r) {
+        own.x += stays(r);
+        if (!P) own.y += tied(r);
       }
-      before.x += s;
-      before.y += t;
+      Pair before = sum_before<NW>(own, s_scan[turn], all);
+      base = so_far.x + min(so_far.y, ties);
+      before.x += so_far.x - base;
+      before.y += so_far.y;
+      so_far.x += all.x;
+      so_far.y += all.y;
+      end = so_far.x + min(so_far.y, ties);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const bool s = stays(r), t = tied(r);
+        if (s || (!P && t && before.y < ties)) {
+          const int at = before.x + (P ? 0 : min(before.y, ties));
+          s_slot[at] = first + r;
+          s_weight[at] = w[r];
+        }
+        before.x += s;
+        if (!P) before.y += t;
+      }
+    };
+    if (!numbers) emit(std::false_type{}, std::false_type{});
+    else if (run + kRun <= m) emit(std::true_type{}, std::true_type{});
+    else emit(std::true_type{}, std::false_type{});
+    __syncthreads();
+    for (int i = tid; i < end - base; i += NT) {
+      list[base + i] = s_slot[i];
+      w_list[base + i] = s_weight[i];
+      if (MOVE) s_kept[base + i] = s_slot[i];
     }
-    so_far.x += all.x;
-    so_far.y += all.y;
+    advance();
   }
   if (MOVE) {
     if (k == k_out && keep == n) return;

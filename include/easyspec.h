@@ -282,7 +282,8 @@ int64_t easyspec_accept_static_max_bytes(void);
  * draft step as they are; over the nodes of a tree level, beams is EASYSPEC_MAX_TREE_WIDTH and the scores of unused rows are
  * minus infinity.  EASYSPEC_EINVAL for NULL pointers, groups or vocab < 1, groups * beams > 65535, beams, n_select or vocab
  * beyond the limits above, an end_token outside the vocabulary if `ended` is given, a temperature that is not positive and
- * finite, or outputs that are not device memory. */
+ * finite, or arrays that are not memory of the
+ * current device. */
 int easyspec_beam_select(const float *logits, const float *scores, const int32_t *ended, int32_t groups, int32_t beams, int32_t vocab,
                          int32_t n_select, float temperature, int32_t end_token, int32_t *tokens_out, int32_t *parents_out,
                          float *scores_out, void *workspace, void *hip_stream);
@@ -306,7 +307,8 @@ typedef struct easyspec_kv_layout {
  *   parents             dev [n_seqs]
  * Other slots of k_out, v_out are left as they were.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for
  * NULL pointers, a bad layout or slot range, beams that do not divide n_seqs, arrays that overlap in part or are not 16-byte
- * aligned, or outputs that are not device memory. */
+ * aligned, or arrays that are not memory of the
+ * current device. */
 int easyspec_kv_reorder(const void *k, const void *v, const easyspec_kv_layout *layout, const int32_t *parents, int32_t beams,
                         int32_t from_slot, int32_t to_slot, void *k_out, void *v_out, void *hip_stream);
 
@@ -338,7 +340,7 @@ int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const
  *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
  *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
  * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers, a bad layout, counts or lengths, arrays
- * that are not 16-byte aligned (weights: 4), or weights_out that is not device memory. */
+ * that are not 16-byte aligned (weights: 4) or not memory of the current device. */
 int easyspec_attn_weights(const float *q, const void *k, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
                           int32_t n_q_heads, const float *weights_in, float *weights_out, void *workspace, void *hip_stream);
 int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
@@ -357,8 +359,8 @@ int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout *layout, 
  *   slots_out    dev [n_layers][n_seqs][n_kv_heads][out_slots]       which they were
  * Results from a sequence's last slot on are left as they were.  Keys keep the rotary positions that they were written with.
  * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers, a bad layout or lengths, more slots to
- * stay than out_slots, arrays that overlap in part or are not 16-byte aligned (weights, slots: 4), or outputs that are not
- * device memory. */
+ * stay than out_slots, arrays that overlap in part or are not 16-byte aligned (weights, slots: 4), or not memory of the
+ * current device. */
 int easyspec_kv_evict(const void *k, const void *v, const float *weights, const easyspec_kv_layout *layout, const int32_t *lens,
                       const int32_t *keep, int32_t recent, int32_t out_slots, void *k_out, void *v_out, float *weights_out,
                       int32_t *slots_out, void *hip_stream);

@@ -137,7 +137,7 @@ def _ptr(x):
         return x
     if isinstance(x, np.ndarray):
         assert x.flags["C_CONTIGUOUS"]
-        return x.ctypes.data
+        return x.__array_interface__["data"][0]  # x.ctypes.data, at a third of its time
     if hasattr(x, "data_ptr"):
         assert x.is_contiguous()
         return x.data_ptr()

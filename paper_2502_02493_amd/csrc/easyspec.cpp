@@ -45,6 +45,7 @@ struct easyspec_ctx {
     float* weights = nullptr;   // [L][B][Hkv][max_ctx]
     int32_t* kept = nullptr;    // the same shape: an eviction's list of slots
     float2* stats = nullptr;    // workspace of launch_weigh
+    size_t stats_bytes = 0;
     int32_t max_positions = 0;  // rows of the rotary table
     std::vector<int32_t> gone;  // slots evicted so far: slot s of sequence b is at rotary position s + gone[b] from firm[b] on;
     std::vector<int32_t> firm;  // the slots below come from anywhere before
@@ -466,7 +467,8 @@ static bool resident_takes(const easyspec_ctx* ctx, const Cols& c, const std::ve
 
 static float weigh_scale(int hd) { return (float)(1.4426950408889634 / sqrt((double)hd)); }
 
-// The entries of a calibration's columns (those of a sequence lie together) and of a wide pass's, for launch_weigh.
+// The entries of a calibration's columns (those of a sequence lie together) and of a wide pass's, for launch_weigh; false: the
+// workspace is too small for them.
 static void weigh_begin(const easyspec_ctx* ctx, const float* q, WeighArgs& a) {
   const Shape& s = ctx->s;
   memset(&a, 0, sizeof a);
@@ -475,7 +477,7 @@ static void weigh_begin(const easyspec_ctx* ctx, const float* q, WeighArgs& a) {
   a.n_seqs = s.B; a.heads = s.Hkv; a.Hq = s.Hq; a.group = s.Hq / s.Hkv; a.max_slots = s.max_ctx;
   a.scale = weigh_scale(s.hd);
 }
-static void weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q, WeighArgs& a) {
+static bool weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q, WeighArgs& a) {
   const Shape& s = ctx->s;
   weigh_begin(ctx, q, a);
   for (int i = 0; i < c.n; ++i) {
@@ -489,8 +491,9 @@ static void weigh_columns(const easyspec_ctx* ctx, const Cols& c, const float* q
     e.len = c.pos[i] + 1;
   }
   weigh_plan(a, 1, s.dtype);
+  return weigh_workspace_bytes(a, 1) <= ctx->track.stats_bytes;
 }
-static void weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q, WeighArgs& a) {
+static bool weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q, WeighArgs& a) {
   const Shape& s = ctx->s;
   weigh_begin(ctx, q, a);
   for (int i = 0; i < sp.n_seq; ++i) {
@@ -501,6 +504,7 @@ static void weigh_spans(const easyspec_ctx* ctx, const Spans& sp, const float* q
     e.len = sp.pos0[i] + e.n;
   }
   weigh_plan(a, 1, s.dtype);
+  return weigh_workspace_bytes(a, 1) <= ctx->track.stats_bytes;
 }
 static void weigh_layer(const easyspec_ctx* ctx, WeighArgs& a, int layer) {
   const Shape& s = ctx->s;
@@ -524,8 +528,8 @@ static int forward(easyspec_ctx* ctx, const Cols& c, const int32_t* tokens, cons
   if (c2 && (full_layer || !ctx->has_b2 || c2->n != c.n || n_sets != s.L))
     return fail(ctx, EASYSPEC_EINVAL, "internal: two passes together need equal column counts and sets of one layer");
   WeighArgs wa, wa2;
-  if (weigh) weigh_columns(ctx, c, b.Q, wa);
-  if (weigh && c2) weigh_columns(ctx, *c2, b2->Q, wa2);
+  if ((weigh && !weigh_columns(ctx, c, b.Q, wa)) || (weigh && c2 && !weigh_columns(ctx, *c2, b2->Q, wa2)))
+    return fail(ctx, EASYSPEC_EINVAL, "internal: attention weights need more workspace than there is");
   if (!c2 && !full_layer && !weigh && resident_takes(ctx, c, bounds)) {
     launch_resident(s, b, ctx->r, c, tokens, bounds.data(), n_sets, logits_out, tokens_out, st);
     HIPCHK(ctx, hipGetLastError());
@@ -584,7 +588,7 @@ static int wide_forward(easyspec_ctx* ctx, const Spans& sp, const int32_t* token
   { ProfScope p(ctx, EASYSPEC_OP_ALL); launch_wide_embed(s, b, w, sp, tokens, st); }
   const bool wide_head = all_rows && logits_out;
   WeighArgs wa;
-  if (ctx->track.weights) weigh_spans(ctx, sp, w.Q, wa);
+  if (ctx->track.weights && !weigh_spans(ctx, sp, w.Q, wa)) return fail(ctx, EASYSPEC_EINVAL, "internal: attention weights need more workspace than there is");
   for (int l = 0; l < s.L; ++l) {
     const bool last = l + 1 == s.L;
     { ProfScope p(ctx, EASYSPEC_OP_QKV); launch_wide_qkv(s, b, w, sp, l, st); }
@@ -910,20 +914,23 @@ extern "C" int easyspec_accept_static(const int32_t* draft, const float* draft_l
 // beams and bounded caches: operators on the caller's arrays
 // ---------------------------------------------------------------------------------------------
 
-// The arrays that a launch writes have to be device memory of the current device: anything else (a host array, memory of another
-// device) would be written through an address that the kernel does not have.
-static int check_outputs(const char* what, std::initializer_list<const void*> outs) {
+// The arrays of a launch have to be memory of the current device (those that it only reads may be pinned host memory): anything else,
+// a host array or memory of another device, would be reached through an address that the kernel does not have.  NULL is passed over.
+static int check_arrays(easyspec_ctx* ctx, const char* what, std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
   int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess) return fail(nullptr, EASYSPEC_EHIP, "%s: no HIP device available (this library has no CPU path)", what);
-  for (const void* p : outs) {
+  if (hipGetDevice(&dev) != hipSuccess) return fail(ctx, EASYSPEC_EHIP, "%s: no HIP device available (this library has no CPU path)", what);
+  auto reachable = [&](const void* p, bool only_read) {
     hipPointerAttribute_t attr;
-    const bool ok = hipPointerGetAttributes(&attr, p) == hipSuccess &&
-                    (attr.type == hipMemoryTypeManaged || (attr.type == hipMemoryTypeDevice && attr.device == dev));
-    if (!ok) {
+    if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
       (void)hipGetLastError();
-      return fail(nullptr, EASYSPEC_EINVAL, "%s: an output or the workspace is not memory of the current device", what);
+      return false;
     }
-  }
+    return attr.type == hipMemoryTypeManaged || (attr.type == hipMemoryTypeDevice && attr.device == dev) || (only_read && attr.type == hipMemoryTypeHost);
+  };
+  for (const void* p : written)
+    if (p && !reachable(p, false)) return fail(ctx, EASYSPEC_EINVAL, "%s: an output or the workspace is not memory of the current device", what);
+  for (const void* p : read)
+    if (p && !reachable(p, true)) return fail(ctx, EASYSPEC_EINVAL, "%s: an input is not memory of the current device", what);
   return EASYSPEC_OK;
 }
 
@@ -957,7 +964,7 @@ extern "C" int easyspec_beam_select(const float* logits, const float* scores, co
   if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: temperature must be positive and finite");
   if (ended && (end_token < 0 || end_token >= vocab)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: end_token %d outside the vocabulary", end_token);
   if (misaligned({workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: workspace must be 16-byte aligned");
-  const int rc = check_outputs("beam_select", {tokens_out, parents_out, scores_out, workspace});
+  const int rc = check_arrays(nullptr, "beam_select", {tokens_out, parents_out, scores_out, workspace}, {logits, scores, ended});
   if (rc != EASYSPEC_OK) return rc;
   launch_beam_select(logits, scores, ended, groups, beams, vocab, n_select, (double)temperature, end_token, tokens_out, parents_out, scores_out,
                      workspace, (hipStream_t)hip_stream);
@@ -997,7 +1004,7 @@ extern "C" int easyspec_kv_reorder(const void* k, const void* v, const easyspec_
   if (misaligned({k, v, k_out, v_out}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: arrays must be 16-byte aligned");
   const size_t bytes = layout_rows(layout) * layout->max_slots * slot_bytes(layout);
   rc = check_in_place("kv_reorder", k, v, bytes, k_out, v_out, bytes);
-  if (rc == EASYSPEC_OK) rc = check_outputs("kv_reorder", {k_out, v_out});
+  if (rc == EASYSPEC_OK) rc = check_arrays(nullptr, "kv_reorder", {k_out, v_out}, {k, v, parents});
   if (rc != EASYSPEC_OK) return rc;
   const KvLayout g = {layout->n_layers, layout->n_seqs, layout->n_kv_heads, layout->max_slots};
   launch_kv_reorder(k, v, k_out, v_out, g, slot_bytes(layout), parents, 0, 0, layout->n_seqs, beams, from_slot, to_slot, (hipStream_t)hip_stream);
@@ -1047,7 +1054,7 @@ extern "C" int easyspec_attn_weights(const float* q, const void* k, const easysp
   const size_t bytes = layout_rows(layout) * layout->max_slots * sizeof(float);
   if (weights_in && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes))
     return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights_in and weights_out overlap in part");
-  rc = check_outputs("attn_weights", {weights_out, workspace});
+  rc = check_arrays(nullptr, "attn_weights", {weights_out, workspace}, {q, k, weights_in});
   if (rc != EASYSPEC_OK) return rc;
   a.q = q; a.k = k; a.w_in = weights_in; a.w_out = weights_out; a.stats = (float2*)workspace;
   launch_weigh(a, layout->n_layers, layout->dtype, layout->head_dim, (hipStream_t)hip_stream);
@@ -1083,7 +1090,7 @@ extern "C" int easyspec_kv_evict(const void* k, const void* v, const float* weig
   if (same != (weights_out == weights) || (same && out_slots != layout->max_slots) || (!same && overlap(weights, w_in, weights_out, w_out)) ||
       overlap(slots_out, w_out, weights, w_in) || overlap(slots_out, w_out, weights_out, w_out))
     return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: arrays overlap (in place: all three of them, with out_slots == max_slots)");
-  rc = check_outputs("kv_evict", {k_out, v_out, weights_out, slots_out});
+  rc = check_arrays(nullptr, "kv_evict", {k_out, v_out, weights_out, slots_out}, {k, v, weights});
   if (rc != EASYSPEC_OK) return rc;
   const KvLayout g = {layout->n_layers, layout->n_seqs, layout->n_kv_heads, layout->max_slots};
   launch_kv_evict(k, v, weights, k_out, v_out, weights_out, slots_out, g, slot_bytes(layout), a, (hipStream_t)hip_stream);
@@ -1133,6 +1140,8 @@ extern "C" int easyspec_beam_reorder(easyspec_ctx* ctx, int32_t first, int32_t c
     if (ctx->tree[b].n > 0) return fail(ctx, EASYSPEC_ESTATE, "beam_reorder: sequence %d holds a token tree", b);
   }
   if (from_slot < 0 || from_slot > len) return fail(ctx, EASYSPEC_EINVAL, "beam_reorder: from_slot %d outside 0..%d", from_slot, len);
+  const int rc = check_arrays(ctx, "beam_reorder", {}, {parents});
+  if (rc != EASYSPEC_OK) return rc;
   const KvLayout g = {s.L, s.B, s.Hkv, s.max_ctx};
   launch_kv_reorder(ctx->b.kc, ctx->b.vc, ctx->b.kc, ctx->b.vc, g, slot, parents, 0, first, count, count, from_slot, len, ctx->stream);
   float* w = ctx->track.weights;
@@ -1152,7 +1161,8 @@ extern "C" int easyspec_track_attention(easyspec_ctx* ctx, int32_t max_positions
   float *weights = nullptr, *rope = nullptr;
   ALLOC(ctx, weights, n * sizeof(float));
   ALLOC(ctx, ctx->track.kept, n * sizeof(int32_t));
-  ALLOC(ctx, ctx->track.stats, weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx));
+  ctx->track.stats_bytes = weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx);
+  ALLOC(ctx, ctx->track.stats, ctx->track.stats_bytes);
   HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
   if (max_positions > s.max_ctx) {
     ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));

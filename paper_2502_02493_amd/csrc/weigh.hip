@@ -9,6 +9,11 @@
 // each other, so they are kept to fp32.  Two launches, since a row's sum is known only at the end of its context:
 //   (1) weigh_stats_kernel   per chunk of the context: every row's maximum and sum of exp(score - maximum);
 //   (2) weigh_add_kernel     the scores once more, their probabilities, the sums over the rows.
+// (Keeping the scores between the two would take four bytes a row and slot, up to 512 beside the 256 of a key.)  Contexts of a
+// few hundred slots are one launch, weigh_short_kernel.
+// Long contexts are bound by the keys, which are read twice: 61 440 slots of 8 KV heads, 126 MB, 23 us a launch (5.4 TB/s).  Many
+// rows are bound by what a wave does with a tile of scores: 16 sequences of 16 tokens and 800 slots, 112 rows a KV head, 10 us a launch, of
+// which the keys alone would be 3.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -61,6 +66,9 @@ struct WeighPlace {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     group = wave & (groups - 1);
     split = wave >> log2_groups;
+  }
+  __device__ __forceinline__ size_t cache_row(const WeighArgs& a) const {  // the first slot of the (layer, sequence, KV head)
+    return (((size_t)l * a.n_seqs + a.entry[e].seq) * a.heads + h) * (size_t)a.max_slots;
   }
   __device__ __forceinline__ int token_of(const WeighArgs& a, int row) const { return (int)(((float)row + 0.5f) * a.inv_group); }  // row < 128: off by far less than half a step
   __device__ __forceinline__ int seen_by(const WeighArgs& a, int row) const { return old + token_of(a, row) + 1; }  // slots that a row attends to
@@ -218,18 +226,11 @@ __device__ __forceinline__ void join(float& m, float& l, float om, float ol) {
   m = top;
 }
 
-// grid (chunks of all entries, KV heads, layers)
+// Every row's maximum and sum over the workgroup's chunk: thread r returns those of row r.
 template <typename T, int HD, int NW>
-__global__ __launch_bounds__(NW * 64) void weigh_stats_kernel(WeighArgs a) {
-  __shared__ u32x4 s_space[weigh_space<T, HD, NW>()];
-  __shared__ float s_m[NW][16], s_l[NW][16];
-  const WeighPlace<NW> p(a);
+__device__ __forceinline__ float2 chunk_stats(const WeighArgs& a, const WeighPlace<NW>& p, const T* k_row, const WeighQueries<T, HD, NW>& Q,
+                                              WeighKeys<T, HD>& first, u32x4* s_space, float (&s_m)[NW][16], float (&s_l)[NW][16]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const T* k_row = reinterpret_cast<const T*>(a.k) + (((size_t)p.l * a.n_seqs + a.entry[p.e].seq) * a.heads + p.h) * (size_t)a.max_slots * HD;
-  WeighKeys<T, HD> first;
-  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
-  WeighQueries<T, HD, NW> Q;
-  Q.load(a, p, s_space);
   const int row = p.group * 16 + (lane & 15), seen = row < p.rows ? p.seen_by(a, row) : 0;
   float m = kLowest, l = 0.f;
   each_tile<T, HD, NW>(k_row, p, first, s_space, [&](auto n, const int* s, const WeighKeys<T, HD>* kf) {
@@ -259,54 +260,27 @@ __global__ __launch_bounds__(NW * 64) void weigh_stats_kernel(WeighArgs a) {
     s_l[wave][lane] = l;
   }
   __syncthreads();
-  const int r = threadIdx.x;  // there are at least as many threads as rows
-  if (r < p.rows) {
-    const WeighEntry& e = a.entry[p.e];
-    float top = s_m[r / 16][r % 16], sum = s_l[r / 16][r % 16];
-    for (int w = 1; w < p.splits; ++w) join(top, sum, s_m[w * p.groups + r / 16][r % 16], s_l[w * p.groups + r / 16][r % 16]);
-    a.stats[((size_t)p.l * a.heads + p.h) * a.stats_pitch + e.first_stat + (size_t)r * e.chunks + p.c] = make_float2(top, sum);
-  }
+  const int r = min((int)threadIdx.x, p.rows - 1);  // there are at least as many threads as rows
+  float top = s_m[r / 16][r % 16], sum = s_l[r / 16][r % 16];
+  for (int w = 1; w < p.splits; ++w) join(top, sum, s_m[w * p.groups + r / 16][r % 16], s_l[w * p.groups + r / 16][r % 16]);
+  return make_float2(top, sum);
 }
 
-// grid as above
+// The chunk's probabilities, added up over the rows and to the weights.  s_row: every row's maximum and 1 / sum over its context.
 template <typename T, int HD, int NW>
-__global__ __launch_bounds__(NW * 64) void weigh_add_kernel(WeighArgs a) {
-  constexpr int NT = NW * 64;
-  __shared__ u32x4 s_space[weigh_space<T, HD, NW>()];
-  __shared__ f32x4 s_sums[kWeighSums / 4];
-  __shared__ float s_m[kWeighMaxTiles * 16], s_inv[kWeighMaxTiles * 16];
-  const WeighPlace<NW> p(a);
+__device__ __forceinline__ void chunk_add(const WeighArgs& a, const WeighPlace<NW>& p, const T* k_row, size_t row_at, const WeighQueries<T, HD, NW>& Q,
+                                          WeighKeys<T, HD>& first, u32x4* s_space, const float2* s_row, float* sums) {
   const int lane = threadIdx.x & 63;
-  const WeighEntry& e = a.entry[p.e];
-  const size_t row_at = (((size_t)p.l * a.n_seqs + e.seq) * a.heads + p.h) * (size_t)a.max_slots;
-  const T* k_row = reinterpret_cast<const T*>(a.k) + row_at * HD;
-  WeighKeys<T, HD> first;
-  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
-  // the rows' maxima and sums over all chunks: as many lanes to a row as there are threads for each, one to four rows' worth
-  const float2* st0 = a.stats + ((size_t)p.l * a.heads + p.h) * a.stats_pitch + e.first_stat;
-  const int log2_per_row = p.rows <= NT / 64 ? 6 : p.rows <= NT / 32 ? 5 : p.rows <= NT / 16 ? 4 : p.rows <= NT / 8 ? 3 : 2;  // rows <= NT / 4
-  const int r = threadIdx.x >> log2_per_row, c0 = threadIdx.x & ((1 << log2_per_row) - 1);
-  const float2* st = st0 + (size_t)min(r, p.rows - 1) * e.chunks;
-  const float2 x0 = st[min(c0, e.chunks - 1)];
-  WeighQueries<T, HD, NW> Q;
-  Q.load(a, p, s_space);
-  float rm = c0 < e.chunks ? x0.x : kLowest, rl = c0 < e.chunks ? x0.y : 0.f;
-  for (int c = c0 + (1 << log2_per_row); c < e.chunks; c += 1 << log2_per_row) join(rm, rl, st[c].x, st[c].y);
-  for (int off = 1; off < 1 << log2_per_row; off <<= 1) join(rm, rl, __shfl_xor(rm, off, 64), __shfl_xor(rl, off, 64));
-  if (r < p.rows && c0 == 0) {
-    s_m[r] = rm;
-    s_inv[r] = 1.f / rl;
-  }
-  __syncthreads();
-  float* s_sum = reinterpret_cast<float*>(s_sums) + p.group * a.chunk;
+  float* s_sum = sums + p.group * a.chunk;
   // the lane's four rows; those past the last give nothing
   float m[4], inv[4];
   int seen[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = p.group * 16 + 4 * (lane >> 4) + i;
-    m[i] = s_m[min(row, p.rows - 1)];
-    inv[i] = s_inv[min(row, p.rows - 1)];
+    const float2 x = s_row[min(row, p.rows - 1)];
+    m[i] = x.x;
+    inv[i] = x.y;
     seen[i] = row < p.rows ? p.seen_by(a, row) : 0;
   }
   const bool full = p.group * 16 + 16 <= p.rows;
@@ -328,14 +302,85 @@ __global__ __launch_bounds__(NW * 64) void weigh_add_kernel(WeighArgs a) {
     }
   });
   __syncthreads();
-  const float* sums = reinterpret_cast<const float*>(s_sums);
-  for (int i = threadIdx.x; i < p.s1 - p.s0; i += NT) {
+  for (int i = threadIdx.x; i < p.s1 - p.s0; i += NW * 64) {
     float sum = sums[i];
     for (int g = 1; g < p.tiles; ++g) sum += sums[g * a.chunk + i];
     const int s = p.s0 + i;
     const float before = a.w_in && s < p.old ? a.w_in[row_at + s] : 0.f;  // the new tokens' slots start from nothing
     a.w_out[row_at + s] = before + sum;
   }
+}
+
+// grid (chunks of all entries, KV heads, layers), as the others'
+template <typename T, int HD, int NW>
+__global__ __launch_bounds__(NW * 64) void weigh_stats_kernel(WeighArgs a) {
+  __shared__ u32x4 s_space[weigh_space<T, HD, NW>()];
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  const WeighPlace<NW> p(a);
+  const WeighEntry& e = a.entry[p.e];
+  const T* k_row = reinterpret_cast<const T*>(a.k) + p.cache_row(a) * HD;
+  WeighKeys<T, HD> first;
+  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
+  WeighQueries<T, HD, NW> Q;
+  Q.load(a, p, s_space);
+  const float2 mine = chunk_stats<T, HD, NW>(a, p, k_row, Q, first, s_space, s_m, s_l);
+  const int r = threadIdx.x;
+  if (r < p.rows) a.stats[((size_t)p.l * a.heads + p.h) * a.stats_pitch + e.first_stat + (size_t)r * e.chunks + p.c] = mine;
+}
+
+template <typename T, int HD, int NW>
+__global__ __launch_bounds__(NW * 64) void weigh_add_kernel(WeighArgs a) {
+  constexpr int NT = NW * 64;
+  __shared__ u32x4 s_space[weigh_space<T, HD, NW>()];
+  __shared__ f32x4 s_sums[kWeighSums / 4];
+  __shared__ float2 s_row[kWeighMaxTiles * 16];
+  const WeighPlace<NW> p(a);
+  const WeighEntry& e = a.entry[p.e];
+  const size_t row_at = p.cache_row(a);
+  const T* k_row = reinterpret_cast<const T*>(a.k) + row_at * HD;
+  WeighKeys<T, HD> first;
+  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
+  // the rows' maxima and sums over all chunks: as many lanes to a row as there are threads for each, one to four rows' worth
+  const float2* st0 = a.stats + ((size_t)p.l * a.heads + p.h) * a.stats_pitch + e.first_stat;
+  const int log2_per_row = p.rows <= NT / 64 ? 6 : p.rows <= NT / 32 ? 5 : p.rows <= NT / 16 ? 4 : p.rows <= NT / 8 ? 3 : 2;  // rows <= NT / 4
+  const int r = threadIdx.x >> log2_per_row, c0 = threadIdx.x & ((1 << log2_per_row) - 1);
+  const float2* st = st0 + (size_t)min(r, p.rows - 1) * e.chunks;
+  constexpr int kAhead = 4;  // requested in front of the queries
+  float2 ahead[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) ahead[i] = st[min(c0 + (i << log2_per_row), e.chunks - 1)];
+  WeighQueries<T, HD, NW> Q;
+  Q.load(a, p, s_space);
+  float rm = kLowest, rl = 0.f;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (c0 + (i << log2_per_row) < e.chunks) join(rm, rl, ahead[i].x, ahead[i].y);
+  for (int c = c0 + (kAhead << log2_per_row); c < e.chunks; c += 1 << log2_per_row) join(rm, rl, st[c].x, st[c].y);
+  for (int off = 1; off < 1 << log2_per_row; off <<= 1) join(rm, rl, __shfl_xor(rm, off, 64), __shfl_xor(rl, off, 64));
+  if (r < p.rows && c0 == 0) s_row[r] = make_float2(rm, 1.f / rl);
+  __syncthreads();
+  chunk_add<T, HD, NW>(a, p, k_row, row_at, Q, first, s_space, s_row, reinterpret_cast<float*>(s_sums));
+}
+
+// Contexts of one chunk each: both in one launch.
+template <typename T, int HD, int NW>
+__global__ __launch_bounds__(NW * 64) void weigh_short_kernel(WeighArgs a) {
+  __shared__ u32x4 s_space[weigh_space<T, HD, NW>()];
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ f32x4 s_sums[kWeighSums / 4];
+  __shared__ float2 s_row[kWeighMaxTiles * 16];
+  const WeighPlace<NW> p(a);
+  const size_t row_at = p.cache_row(a);
+  const T* k_row = reinterpret_cast<const T*>(a.k) + row_at * HD;
+  WeighKeys<T, HD> first;
+  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
+  WeighQueries<T, HD, NW> Q;
+  Q.load(a, p, s_space);
+  const float2 mine = chunk_stats<T, HD, NW>(a, p, k_row, Q, first, s_space, s_m, s_l);
+  first.load(k_row, p.s0 + 16 * (threadIdx.x >> 6), p.len);
+  if ((int)threadIdx.x < p.rows) s_row[threadIdx.x] = make_float2(mine.x, 1.f / mine.y);
+  __syncthreads();
+  chunk_add<T, HD, NW>(a, p, k_row, row_at, Q, first, s_space, s_row, reinterpret_cast<float*>(s_sums));
 }
 
 // How the contexts are cut: workgroups of four waves where no entry has more than one row tile, else of eight; chunks of a multiple
@@ -351,9 +396,17 @@ static int most_rows(const WeighArgs& a) {
   for (int i = 0; i < a.n_entries; ++i) rows = std::max(rows, a.entry[i].n * a.group);
   return rows;
 }
+// Contexts that a workgroup goes through twice sooner than a second launch has done its part.  us a call in a graph, 32 query heads on
+// 8 KV heads, two launches and one: one token at 128, 256, 512 slots 7.9, 8.0, 8.1 and 6.0, 7.7, 11.2, six 10.3, 10.5, 10.7 and
+// 7.1, 9.4, 13.4, sixteen sequences of six 10.9, 14.6, 15.7 and 7.4, 9.8, 14.0; but one in fp32 9.3, 9.4 and 8.7, 12.3, sixteen with
+// 28 heads on 4 14.0, 14.2 and 11.6, 17.3.
+static int weigh_short(int rows, int dtype) { return rows <= 32 && dtype == 1 ? 256 : 128; }
 static int weigh_chunk(const WeighArgs& a, int n_layers, int dtype) {
   const int rows = most_rows(a), groups = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
   const long wgs_most = groups == 2 && dtype == 1 ? 2 * kWeighCus : kWeighCus;
+  int longest = 0;
+  for (int i = 0; i < a.n_entries; ++i) longest = std::max(longest, a.entry[i].len);
+  if (longest <= weigh_short(rows, dtype)) return (longest + 63) / 64 * 64;
   int chunk = 64;
   for (; chunk < kWeighSums / groups; chunk += 64) {
     long wgs = 0;
@@ -393,16 +446,25 @@ size_t weigh_workspace_limit(int B, int heads, int group, int max_tokens, int ma
 void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st) {
   if (a.n_entries == 0) return;
   const dim3 grid(a.n_wgs, a.heads, n_layers);
-  auto go = [&](auto stats, auto add, int waves) {
-    hipLaunchKernelGGL(stats, grid, dim3(waves * 64), 0, st, a);
-    hipLaunchKernelGGL(add, grid, dim3(waves * 64), 0, st, a);
+  bool one_chunk = true;
+  for (int i = 0; i < a.n_entries; ++i) one_chunk = one_chunk && a.entry[i].chunks == 1;
+  auto go = [&](auto waves, auto stats, auto add, auto both) {
+    const dim3 block(decltype(waves)::value * 64);
+    if (one_chunk) {
+      hipLaunchKernelGGL(both, grid, block, 0, st, a);
+      return;
+    }
+    hipLaunchKernelGGL(stats, grid, block, 0, st, a);
+    hipLaunchKernelGGL(add, grid, block, 0, st, a);
   };
+  typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 8> Eight;
   const bool narrow = most_rows(a) <= 16;
   DISPATCH_T(dtype, {
-    if (hd == 128 && narrow) go(weigh_stats_kernel<T, 128, 4>, weigh_add_kernel<T, 128, 4>, 4);
-    else if (hd == 128) go(weigh_stats_kernel<T, 128, 8>, weigh_add_kernel<T, 128, 8>, 8);
-    else if (narrow) go(weigh_stats_kernel<T, 64, 4>, weigh_add_kernel<T, 64, 4>, 4);
-    else go(weigh_stats_kernel<T, 64, 8>, weigh_add_kernel<T, 64, 8>, 8);
+    if (hd == 128 && narrow) go(Four{}, weigh_stats_kernel<T, 128, 4>, weigh_add_kernel<T, 128, 4>, weigh_short_kernel<T, 128, 4>);
+    else if (hd == 128) go(Eight{}, weigh_stats_kernel<T, 128, 8>, weigh_add_kernel<T, 128, 8>, weigh_short_kernel<T, 128, 8>);
+    else if (narrow) go(Four{}, weigh_stats_kernel<T, 64, 4>, weigh_add_kernel<T, 64, 4>, weigh_short_kernel<T, 64, 4>);
+    else go(Eight{}, weigh_stats_kernel<T, 64, 8>, weigh_add_kernel<T, 64, 8>, weigh_short_kernel<T, 64, 8>);
   });
 }
 

@@ -279,14 +279,23 @@ __global__ __launch_bounds__(NT) void beam_pick_kernel(BeamArgs a) {
 #pragma unroll
     for (int j = 0; j < kHead; ++j) c[j] = cands[(size_t)min(i, lists - 1) * K + min(j, K - 1)];
   };
+  // A wave takes a beam's sums at a time; the first one's are requested in front of the lists, which are needed behind them.
+  double m0, z0;
+  float cum;
+  int ended;
+  auto load_beam = [&](int w) {
+    const int row = g * a.beams + min(w, a.beams - 1), s0 = min(lane, S - 1);
+    m0 = a.stats[((size_t)row * S + s0) * 2];  // of a beam without candidates: whatever is there
+    z0 = a.stats[((size_t)row * S + s0) * 2 + 1];
+    cum = a.scores[row];
+    ended = a.ended ? a.ended[row] : 0;
+  };
+  load_beam(wave);
+  asm volatile("" ::: "memory");
   load_head(tid);
   for (int w = wave; w < a.beams; w += NW) {
-    const int row = g * a.beams + w;
-    const double* st = a.stats + (size_t)row * S * 2;
-    const int s0 = min(lane, S - 1);
-    const double m0 = st[2 * s0], z0 = st[2 * s0 + 1];  // of a beam without candidates: whatever is there
-    const float cum = a.scores[row];
-    const int ended = a.ended ? a.ended[row] : 0;
+    const double* st = a.stats + (size_t)(g * a.beams + w) * S * 2;
+    if (w != wave) load_beam(w);
     float m = (float)m0;
     double top = (double)lanes_max(m, 64), sum = lane < S ? rescaled(z0, m0, top, a.log2e_T) : 0.0;
     if (S > 64) {
@@ -322,38 +331,50 @@ __global__ __launch_bounds__(NT) void beam_pick_kernel(BeamArgs a) {
   const int groups = K <= 8 ? 8 : K <= 16 ? 16 : K <= 32 ? 32 : 64;
   const unsigned long long live = __ballot(lane < a.beams && s_kind[min(lane, a.beams - 1)] == 1);
   const bool heads_do = __popcll(live) * S >= 4 * groups;
-  for (int i = tid; i < lists; i += NT) {
-    if (i >= NT) load_head(i);
-    const int w = i / S, s = i - w * S, number = __popcll(live & ((1ull << w) - 1)) * S + s;
+  // a thread's (last) list: its beam and the scores of its first candidates, as many as there are
+  int list_w = 0;
+  Pick head[kHead];
+  int there = 0;
+  auto look_at = [&](int i) {
+    list_w = i / S;
+    there = 0;
+    bool in = true;
 #pragma unroll
     for (int j = 0; j < kHead; ++j) {
-      Pick p;
-      if (entry(w, s, j, c[j], p)) atomicMax(&s_bound[(heads_do ? number : number * kHead + j) & (groups - 1)], (unsigned long long)p.score);
+      in = (int)in & (int)entry(list_w, i - list_w * S, j, c[j], head[j]);
+      there += in;
+    }
+  };
+  for (int i = tid; i < lists; i += NT) {
+    if (i >= NT) load_head(i);
+    look_at(i);
+    const int number = __popcll(live & ((1ull << list_w) - 1)) * S + i - list_w * S;
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) {
+      if (j < there) atomicMax(&s_bound[(heads_do ? number : number * kHead + j) & (groups - 1)], (unsigned long long)head[j].score);
       if (heads_do) break;
     }
   }
   __syncthreads();
   const uint64_t bound = lanes_fold((uint64_t)s_bound[lane & (groups - 1)], groups, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
   for (int i = tid; i < lists; i += NT) {
-    if (lists > NT) load_head(i);
-    const int w = i / S, s = i - w * S;
-    Pick p[kHead];
-    int reach = 0;
-    bool in = true;
-#pragma unroll
-    for (int j = 0; j < kHead; ++j) {
-      in = (int)in & entry(w, s, j, c[j], p[j]) & (int)(p[j].score >= bound);
-      reach += in;
+    if (lists > NT) {
+      load_head(i);
+      look_at(i);
     }
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) reach += j < there && head[j].score >= bound;  // sorted: the first ones
     if (reach) {
       int at = atomicAdd(&s_n, reach);
 #pragma unroll
       for (int j = 0; j < kHead; ++j, ++at)
-        if (j < reach && at < kListMax) s_list[at] = p[j];
+        if (j < reach && at < kListMax) s_list[at] = head[j];
     }
+    bool in = reach == kHead;
     for (int j = kHead; j < K && in; ++j) {
       Pick q;
-      in = (int)entry(w, s, j, cands[(size_t)i * K + j], q) & (int)(q.score >= bound);
+      in = (int)entry(list_w, 0, j, cands[(size_t)i * K + j], q) & (int)(q.score >= bound);
       if (in) {
         const int at = atomicAdd(&s_n, 1);
         if (at < kListMax) s_list[at] = q;

@@ -76,6 +76,51 @@ def test_sizes(es, L, heads, hd, dtype, n, lens, slots):
     check(q, k, w, n, lens, call(es, q, k, w, layout, n, lens, heads[0]))
 
 
+@pytest.mark.parametrize("L,heads,hd,dtype,n,lens,slots", [
+    (4, (32, 8), 128, "bf16", [6], [2000], 2010),             # chunks of several rounds of keys
+    (8, (8, 8), 64, "fp32", [9], [1500], 1500),
+    (64, (4, 4), 64, "bf16", [1], [4200], 4200),              # the longest chunk, and a short last one
+    (64, (8, 4), 64, "bf16", [11], [2100], 2100),             # ... of two row tiles
+    (64, (16, 4), 64, "bf16", [12], [1100], 1100),            # ... of four
+    (96, (8, 1), 64, "bf16", [16], [1030], 1030),             # ... of eight
+    (1, (7, 1), 128, "fp32", [16], [2500], 2500),
+    (1, (4, 1), 128, "bf16", [2, 4, 1], [256, 129, 64], 256),  # short contexts, one launch
+    (1, (4, 1), 128, "bf16", [2, 4, 1], [257, 129, 64], 257),
+    (3, (8, 1), 64, "fp32", [16, 5], [128, 17], 130),
+    (1, (2, 2), 64, "bf16", [1], [65536], 65536),
+])
+def test_cuts(es, L, heads, hd, dtype, n, lens, slots):
+    q, k, w, layout = setup(es, sum(lens) + L, L, heads, hd, dtype, n, lens, slots)
+    check(q, k, w, n, lens, call(es, q, k, w, layout, n, lens, heads[0]))
+
+
+def test_stays_inside_its_workspace(es):
+    import torch
+    for heads, hd, n, lens in (((32, 8), 128, [6, 16], [900, 2000]), ((4, 2), 64, [1, 1], [3000, 70]), ((28, 4), 128, [16, 2], [100, 90])):
+        q, k, w, layout = setup(es, 3, 1, heads, hd, "bf16", n, lens, max(lens))
+        nb = es.easyspec_attn_weights_workspace_bytes(layout, n, lens, heads[0])
+        ws = torch.full((nb + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        out = torch.full(tuple(k.shape[:4]), -3.0, device="cuda")
+        es.easyspec_attn_weights(q, k, layout, n, lens, heads[0], w, out, ws, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert bool((ws[nb:] == 0xA5).all())
+        check(q, k, w, n, lens, out)
+
+
+def test_values_that_are_not_finite_stay_with_their_head(es):
+    import torch
+    n, lens = [2], [300]
+    q, k, w, layout = setup(es, 12, 1, (4, 2), 64, "bf16", n, lens, 310)
+    k[0, 0, 1, 17, 3] = float("nan")
+    out = call(es, q, k, w, layout, n, lens, 4)
+    assert bool(torch.isnan(out[0, 0, 1, :300]).all()) and bool(torch.isfinite(out[0, 0, 0, :300]).all())
+    k[0, 0, 1, 17, 3] = 1.0
+    k[0, 0, 1, 299, 3] = float("inf")            # seen by the second token alone
+    q[0, 0, 2:] = 0.25
+    first = call(es, q[:, :1].contiguous(), k, w, layout, [1], [299], 4)
+    assert bool(torch.isfinite(first[0, 0, 1, :299]).all())
+
+
 def test_without_earlier_weights_in_place_and_on_another_stream(es):
     import torch
     n, lens = [4, 1], [200, 77]

@@ -157,3 +157,37 @@ def test_scores_out_may_be_scores_other_stream_and_graph(es):
         for g in range(G):
             w_tok, w_par, _ = ref.beam_select(fresh[g], s[g], None, K, 1.0, 0)
             assert np.array_equal(tok[g].cpu().numpy(), w_tok) and np.array_equal(par[g].cpu().numpy(), w_par)
+
+
+@pytest.mark.parametrize("live,K", [(1, 64), (1, 16), (3, 64), (16, 1)])
+def test_few_live_beams_of_many(es, live, K):
+    """The first step of a search, and a level of few nodes in rows for sixteen; whatever the dead rows hold."""
+    logits, scores = rows(live * K, 2, 16, 40000)
+    scores[:, live:] = -np.inf
+    scores[1] = np.roll(scores[1], 5)
+    logits[scores == -np.inf] = np.nan
+    check(es, logits, scores, None, K)
+
+
+def test_more_lists_than_threads(es):
+    logits, scores = rows(21, 1, 64, 80000)
+    check(es, logits, scores, None, 64)
+    logits[0, :, ::7] = 9.0                      # thousands of equal logits, in equal beams
+    logits[0, 1:] = logits[0, :1]
+    check(es, logits, np.zeros((1, 64), np.float32), None, 64)
+
+
+def test_stays_inside_its_workspace_and_outputs(es):
+    import torch
+    dev = torch.device("cuda:0")
+    for G, W, V, K in ((1, 4, 1000, 4), (3, 5, 9001, 64), (2, 16, 30000, 16)):
+        logits, scores = rows(G + V, G, W, V)
+        n = es.easyspec_beam_select_workspace_bytes(G, W, V, K)
+        ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device=dev)
+        out = [torch.full((G * K + 64,), 77, dtype=t, device=dev) for t in (torch.int32, torch.int32, torch.float32)]
+        es.easyspec_beam_select(torch.from_numpy(logits).to(dev), torch.from_numpy(scores).to(dev), None, G, W, V, K, 1.0, 0, *out, ws,
+                                torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert bool((ws[n:] == 0xA5).all()) and all(bool((o[G * K:] == 77).all()) for o in out)
+        for g in range(G):
+            assert np.array_equal(out[0][g * K: g * K + K].cpu().numpy(), ref.beam_select(logits[g], scores[g], None, K, 1.0, 0)[0])

@@ -125,3 +125,22 @@ def test_weights_of_whole_model_and_graph(es):
         torch.cuda.synchronize()
         for l, b, h in rows:
             assert np.array_equal(so[l, b, h].cpu().numpy(), ref.kept_slots(w[l, b, h].cpu().numpy(), 2048, 1024, 128))
+
+
+def test_more_rows_than_a_grid_extent(es):
+    """72 000 (layer, sequence, KV head) rows: the moving launch goes in pieces."""
+    L, B, H, S, hd = 4500, 2, 8, 6, 64
+    k, v, w = make(9, L, B, H, S, hd, "bf16")
+    rows = [(0, 0, 0), (4095, 1, 7), (4096, 0, 0), (4499, 1, 7), (2500, 0, 3)]
+    check(es, k, v, w, [6, 5], [4, 2], 1, 4, rows=rows)
+    check(es, k, v, w, [6, 5], [4, 2], 1, in_place=True, rows=rows)
+
+
+def test_rows_that_the_selecting_workgroup_moves_and_those_it_does_not(es):
+    """Up to 256 rows and 32 KB of K a list is moved at once; one row more is another launch."""
+    for hd, dtype, most in ((64, "bf16", 256), (64, "fp32", 128), (128, "bf16", 128), (128, "fp32", 64)):
+        for S in (700, 3000):
+            k, v, w = make(S + most, 2, 2, 1, S, hd, dtype)
+            for keep in (most, most + 1):
+                check(es, k, v, w, [S, S - 1], [keep, keep - 3], 7, keep)
+                check(es, k, v, w, [S, S - 1], [keep, keep - 3], 7, in_place=True)

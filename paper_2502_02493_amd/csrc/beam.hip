@@ -8,6 +8,13 @@
 //   (1) beam_slice_kernel  per beam and vocabulary slice: slice maximum and sum of exp((l - max) / T), and the slice's n_select
 //                          highest logits in order.  A thread holds its logits in registers: the slice is read once.
 //   (2) beam_pick_kernel   per group: the beams' sums from their slices', then the best of the slices' lists.
+// Neither sorts: a bound from below that at least n_select candidates reach (the lowest maximum of as many disjoint groups) leaves
+// some n_select ln(n_select) of them, whose places are counted.  Taking the best n_select times over, one workgroup-wide maximum
+// after the other, was 78 us a call (128 256 words, sixteen beams, the sixteen best), this is 15.1; 64 beams in sixteen groups of
+// 152 064 words 66 and 19.4.
+// Bound by the chain of dependent steps: of 15 us the loads take 1.3, the exponentials 1.0, bound and candidates 1.1, their places 1.2,
+// in (2) statistics and logarithm 2.4, bound 0.8, selection and places 1.9, the two launches the rest; 29 MB of logits (48 rows that count)
+// arrive in 8 us, and the steps behind them follow.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -36,7 +43,8 @@ __device__ __forceinline__ float cand_logit(cand_t c) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-// Slices of a row: as many as it takes for a thread to hold kSliceRegs logits, more while the workgroups are fewer than the CUs.
+// Slices of a row: as many as it takes for a thread to hold kSliceRegs logits, more while the workgroups are fewer than the CUs and a
+// thread keeps more than one.
 static int beam_slices(long rows, int V) {
   int slices = (V + kSliceMax - 1) / kSliceMax;
   while (rows * slices < 256 && V >= 2 * slices * kSliceThreads) slices *= 2;
@@ -92,7 +100,7 @@ __device__ __forceinline__ double rescaled(double sum, double m, double top, dou
 }
 
 // grid (slices, rows)
-__global__ __launch_bounds__(kSliceThreads) void beam_slice_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kSliceThreads) __attribute__((amdgpu_waves_per_eu(8))) void beam_slice_kernel(BeamArgs a) {
   constexpr int NW = kSliceThreads / 64, kWaveList = kListMax / NW;
   __shared__ u32x2 s_list[NW][kWaveList];  // (token, logit); later the candidates of all waves
   __shared__ int s_above[NW][64];
@@ -326,8 +334,8 @@ __global__ __launch_bounds__(NT) void beam_pick_kernel(BeamArgs a) {
     return (int)(s_kind[w] == 2) & (int)(s == 0) & (int)(j == 0);
   };
   // As in (1): the heads of the live beams' lists dealt to at least n_select groups, and the lowest of the groups' maxima.  Where
-  // these lists are few, the first candidates of each; a group that stays empty then means that there are fewer than
-  // groups / kHead lists, and all their candidates fit.
+  // these lists are few, the first candidates of each.  A group that stays empty bounds nothing: then there are few lists (all
+  // their candidates fit), or lists that masks have emptied.
   const int groups = K <= 8 ? 8 : K <= 16 ? 16 : K <= 32 ? 32 : 64;
   const unsigned long long live = __ballot(lane < a.beams && s_kind[min(lane, a.beams - 1)] == 1);
   const bool heads_do = __popcll(live) * S >= 4 * groups;

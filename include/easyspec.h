@@ -282,15 +282,15 @@ int64_t easyspec_accept_static_max_bytes(void);
  * draft step as they are; over the nodes of a tree level, beams is EASYSPEC_MAX_TREE_WIDTH and the scores of unused rows are
  * minus infinity.  EASYSPEC_EINVAL for NULL pointers, groups or vocab < 1, groups * beams > 65535, beams, n_select or vocab
  * beyond the limits above, an end_token outside the vocabulary if `ended` is given, a temperature that is not positive and
- * finite, or arrays that are not memory of the
- * current device. */
+ * finite, scores and scores_out that overlap otherwise, or arrays that are not memory of the current device. */
 int easyspec_beam_select(const float *logits, const float *scores, const int32_t *ended, int32_t groups, int32_t beams, int32_t vocab,
                          int32_t n_select, float temperature, int32_t end_token, int32_t *tokens_out, int32_t *parents_out,
                          float *scores_out, void *workspace, void *hip_stream);
 int64_t easyspec_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_select); /* -1 for bad arguments */
 
 /* Caches of the caller, as a context holds them: K and V apart, [n_layers][n_seqs][n_kv_heads][max_slots][head_dim] in dtype,
- * contiguous, 16-byte aligned. */
+ * contiguous, 16-byte aligned; n_layers * n_seqs * n_kv_heads < EASYSPEC_MAX_CACHE_ROWS. */
+#define EASYSPEC_MAX_CACHE_ROWS 4194304
 typedef struct easyspec_kv_layout {
   int32_t n_layers;
   int32_t n_seqs;     /* 1..EASYSPEC_MAX_BATCH */
@@ -339,8 +339,9 @@ int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const
  *                NULL: zeros
  *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
  *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
- * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers, a bad layout, counts or lengths, arrays
- * that are not 16-byte aligned (weights: 4) or not memory of the current device. */
+ * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q and workspace may be NULL if no sequence
+ * has new tokens), a bad layout, counts or lengths, arrays that are not 16-byte aligned (weights: 4) or not memory of the current
+ * device. */
 int easyspec_attn_weights(const float *q, const void *k, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
                           int32_t n_q_heads, const float *weights_in, float *weights_out, void *workspace, void *hip_stream);
 int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
@@ -394,7 +395,8 @@ int easyspec_get_lens(const easyspec_ctx *ctx, int32_t *precise, int32_t *fuzzy)
 int easyspec_truncate(easyspec_ctx *ctx, int32_t b, int32_t new_precise_len);
 
 /* Replace the cache of sequence b by n_slots precise entries.  k, v: host|dev
- * [n_layers][n_kv_heads][n_slots][head_dim] in the storage dtype.  Synchronous. */
+ * [n_layers][n_kv_heads][n_slots][head_dim] in the storage dtype.  Synchronous.  The sequence goes on at position n_slots; its
+ * slots have no tracked weights and count as never evicted from (a thinned cache that was exported goes on nearer to its slots). */
 int easyspec_kv_import(easyspec_ctx *ctx, int32_t b, const void *k, const void *v, int32_t n_slots);
 
 /* Copy slots [0, n_slots) of sequence b out (same layout as import; fuzzy slots included if

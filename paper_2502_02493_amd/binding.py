@@ -19,7 +19,7 @@ EASYSPEC_MAX_TREE_WIDTH, EASYSPEC_MAX_TREE_NODES = 16, 64
 EASYSPEC_MAX_CHUNKS = 64
 EASYSPEC_PARALLEL_ATTENTION, EASYSPEC_PARALLEL_FULL_LAYER = 0, 1
 EASYSPEC_MAX_BEAMS, EASYSPEC_MAX_SELECT, EASYSPEC_MAX_BEAM_VOCAB = 64, 64, 1048576
-EASYSPEC_MAX_POSITIONS = 1048576
+EASYSPEC_MAX_POSITIONS, EASYSPEC_MAX_CACHE_ROWS = 1048576, 4194304
 
 EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easyspec_set_groups",
            "easyspec_default_groups", "easyspec_draft_step", "easyspec_calibrate", "easyspec_greedy_accept", "easyspec_greedy_accept_host",

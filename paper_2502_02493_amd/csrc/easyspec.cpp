@@ -964,6 +964,9 @@ extern "C" int easyspec_beam_select(const float* logits, const float* scores, co
   if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: temperature must be positive and finite");
   if (ended && (end_token < 0 || end_token >= vocab)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: end_token %d outside the vocabulary", end_token);
   if (misaligned({workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: workspace must be 16-byte aligned");
+  if (!(scores_out == scores && n_select == beams) &&
+      overlap(scores, (size_t)groups * beams * sizeof(float), scores_out, (size_t)groups * n_select * sizeof(float)))
+    return fail(nullptr, EASYSPEC_EINVAL, "beam_select: scores and scores_out overlap (they may be one array if n_select == beams)");
   const int rc = check_arrays(nullptr, "beam_select", {tokens_out, parents_out, scores_out, workspace}, {logits, scores, ended});
   if (rc != EASYSPEC_OK) return rc;
   launch_beam_select(logits, scores, ended, groups, beams, vocab, n_select, (double)temperature, end_token, tokens_out, parents_out, scores_out,
@@ -975,7 +978,7 @@ extern "C" int easyspec_beam_select(const float* logits, const float* scores, co
 static int check_layout(const char* what, const easyspec_kv_layout* g) {
   if (!g) return fail(nullptr, EASYSPEC_EINVAL, "%s: layout is NULL", what);
   if (g->n_layers < 1 || g->n_layers > 65535 || g->n_seqs < 1 || g->n_seqs > EASYSPEC_MAX_BATCH || g->n_kv_heads < 1 || g->n_kv_heads > 65535 ||
-      (int64_t)g->n_layers * g->n_seqs * g->n_kv_heads > INT32_MAX || g->max_slots < 1 || g->max_slots > kMaxEvictSlots ||
+      (int64_t)g->n_layers * g->n_seqs * g->n_kv_heads >= EASYSPEC_MAX_CACHE_ROWS || g->max_slots < 1 || g->max_slots > kMaxEvictSlots ||
       (g->head_dim != 64 && g->head_dim != 128) || (g->dtype != EASYSPEC_DTYPE_F32 && g->dtype != EASYSPEC_DTYPE_BF16))
     return fail(nullptr, EASYSPEC_EINVAL, "%s: bad cache layout", what);
   return EASYSPEC_OK;
@@ -1045,10 +1048,12 @@ extern "C" int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layou
 
 extern "C" int easyspec_attn_weights(const float* q, const void* k, const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens,
                                      int32_t n_q_heads, const float* weights_in, float* weights_out, void* workspace, void* hip_stream) {
-  if (!q || !k || !weights_out || !workspace) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: NULL argument");
+  if (!k || !weights_out) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: NULL argument");
   WeighArgs a;
   int rc = weigh_args("attn_weights", layout, n_tokens, lens, n_q_heads, a);
   if (rc != EASYSPEC_OK) return rc;
+  if (a.n_entries == 0) return EASYSPEC_OK;  // no query and no workspace either
+  if (!q || !workspace) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: NULL argument");
   if (misaligned({q, k, workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: q, k and workspace must be 16-byte aligned");
   if (misaligned({weights_in, weights_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights must be 4-byte aligned");
   const size_t bytes = layout_rows(layout) * layout->max_slots * sizeof(float);
@@ -1087,8 +1092,15 @@ extern "C" int easyspec_kv_evict(const void* k, const void* v, const float* weig
   const bool same = k_out == k && v_out == v;
   rc = check_in_place("kv_evict", k, v, in_bytes, k_out, v_out, out_bytes);
   if (rc != EASYSPEC_OK) return rc;
+  auto apart = [&](const void* p, std::initializer_list<const void*> caches, size_t bytes) {
+    for (const void* c : caches)
+      if (overlap(p, w_out, c, bytes)) return false;
+    return true;
+  };
   if (same != (weights_out == weights) || (same && out_slots != layout->max_slots) || (!same && overlap(weights, w_in, weights_out, w_out)) ||
-      overlap(slots_out, w_out, weights, w_in) || overlap(slots_out, w_out, weights_out, w_out))
+      overlap(slots_out, w_out, weights, w_in) || overlap(slots_out, w_out, weights_out, w_out) || !apart(slots_out, {k, v}, in_bytes) ||
+      !apart(slots_out, {k_out, v_out}, out_bytes) || !apart(weights_out, {k, v}, in_bytes) || !apart(weights_out, {k_out, v_out}, out_bytes) ||
+      overlap(weights, w_in, k_out, out_bytes) || overlap(weights, w_in, v_out, out_bytes))
     return fail(nullptr, EASYSPEC_EINVAL, "kv_evict: arrays overlap (in place: all three of them, with out_slots == max_slots)");
   rc = check_arrays(nullptr, "kv_evict", {k_out, v_out, weights_out, slots_out}, {k, v, weights});
   if (rc != EASYSPEC_OK) return rc;
@@ -1163,6 +1175,7 @@ extern "C" int easyspec_track_attention(easyspec_ctx* ctx, int32_t max_positions
   ALLOC(ctx, ctx->track.kept, n * sizeof(int32_t));
   ctx->track.stats_bytes = weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx);
   ALLOC(ctx, ctx->track.stats, ctx->track.stats_bytes);
+  ctx->work.push_back({ctx->track.stats, ctx->track.stats_bytes});
   HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
   if (max_positions > s.max_ctx) {
     ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));
@@ -1325,13 +1338,13 @@ extern "C" int easyspec_kv_import(easyspec_ctx* ctx, int32_t b, const void* k, c
   if (b < 0 || b >= ctx->s.B) return fail(ctx, EASYSPEC_EINVAL, "kv_import: sequence %d out of range", b);
   if (n_slots < 0 || n_slots > ctx->s.max_ctx) return fail(ctx, EASYSPEC_ECAPACITY, "kv_import: %d slots exceed max_ctx %d", n_slots, ctx->s.max_ctx);
   if (n_slots > 0 && (!k || !v)) return fail(ctx, EASYSPEC_EINVAL, "kv_import: NULL argument");
-  const Shape& s = ctx->s;
-  const size_t pitch = (size_t)s.max_ctx * sizeof(float);
-  if (ctx->track.weights && n_slots > 0)  // nothing is known of them
-    for (int l = 0; l < s.L; ++l)
-      HIPCHK(ctx, hipMemset2DAsync(ctx->track.weights + ((size_t)l * s.B + b) * s.Hkv * s.max_ctx, pitch, 0, n_slots * sizeof(float), s.Hkv, ctx->stream));
   const int rc = kv_xfer(ctx, b, const_cast<void*>(k), const_cast<void*>(v), n_slots, 1);
   if (rc != EASYSPEC_OK) return rc;
+  const Shape& s = ctx->s;
+  if (ctx->track.weights && n_slots > 0)  // nothing is known of these slots
+    for (int l = 0; l < s.L; ++l)
+      HIPCHK(ctx, hipMemset2DAsync(ctx->track.weights + ((size_t)l * s.B + b) * s.Hkv * s.max_ctx, (size_t)s.max_ctx * sizeof(float), 0,
+                                   n_slots * sizeof(float), s.Hkv, ctx->stream));
   ctx->track.gone[b] = ctx->track.firm[b] = 0;
   ctx->precise[b] = n_slots;
   ctx->fuzzy[b] = 0;
@@ -1422,6 +1435,7 @@ extern "C" int32_t easyspec_stream_read_sink_floats(void) { return stream_read_s
 
 static_assert(EASYSPEC_MAX_BEAMS == kMaxBeams && EASYSPEC_MAX_SELECT == kMaxSelect && EASYSPEC_MAX_BEAM_VOCAB == kMaxBeamVocab,
               "header and kernels disagree on the limits of a beam selection");
+static_assert((uint64_t)EASYSPEC_MAX_CACHE_ROWS * 1024 <= 1ull << 32, "a grid holds 2^32 - 1 threads in a row, a workgroup of 1024 to every row of a cache");
 static_assert(EASYSPEC_MAX_BATCH == kMaxCols, "per-sequence arrays of the cache operators hold kMaxCols entries");
 static_assert(EASYSPEC_MAX_CHUNKS == kMaxChunks, "header and kernels disagree on the chunk limit");
 

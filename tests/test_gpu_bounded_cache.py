@@ -346,3 +346,21 @@ def test_reorder_moves_drafted_slots_of_one_group_alone(gpu):
             assert np.array_equal(w[:, :, :3], ws[b][:, :, :3]) and np.array_equal(w[:, :, 3:], ws[src][:, :, 3:]), b
     finally:
         g.close()
+
+
+@pytest.mark.parametrize("name,over", SHAPES)
+def test_weights_take_nothing_from_workspaces(gpu, name, over):
+    """The same calibrations with every workspace filled with NaNs in front of each: the same bits."""
+    def run(poison):
+        g, _ = model(gpu, name, 36, track=400, max_batch=3, max_ctx=400, **over)
+        try:
+            rng = np.random.default_rng(9)
+            for sizes in ((16, 16, 16),) * 20 + ((6, 1, 0), (0, 16, 3), (1, 1, 1)):
+                if poison:
+                    gpu.es.easyspec_poison_workspaces(g.ctx)
+                g.calibrate({b: list(rng.integers(0, g.cfg["vocab"], n)) for b, n in enumerate(sizes) if n})
+            return [weights_of(gpu, g, b, 320) for b in range(3)]
+        finally:
+            g.close()
+    for a, b in zip(run(False), run(True)):
+        assert np.array_equal(a, b) and np.all(np.isfinite(a))

@@ -123,3 +123,32 @@ def test_outputs_that_are_host_arrays_are_refused():
         es.easyspec_beam_select(logits, scores, None, 1, 2, 8, 2, 1.0, 0, tok, par, out, ws, None)
     assert e.value.code in (es.EASYSPEC_EHIP, es.EASYSPEC_EINVAL)
     assert np.all(tok == 5) and np.all(par == 5) and np.all(out == 5)
+
+
+def test_beam_select_scores_that_overlap():
+    refused(beam(scores_out=X, n_select=3, tokens_out=far(1), parents_out=far(2), workspace=far(3)))
+    refused(beam(scores_out=X + 8, tokens_out=far(1), parents_out=far(2), workspace=far(3)))
+    refused(beam(scores_out=X - 8, n_select=3, tokens_out=far(1), parents_out=far(2), workspace=far(3)))
+
+
+@pytest.mark.parametrize("change", [
+    dict(slots=far(0) + 64), dict(slots=far(1)), dict(slots=far(3)), dict(slots=far(4) + 64), dict(w_out=far(0)), dict(w_out=far(1) + 64),
+    dict(w_out=far(3) + 64), dict(w_out=far(4)), dict(w=far(3)), dict(w=far(4) + 64),
+])
+def test_kv_evict_weights_or_slots_in_a_cache(change):
+    refused(evict(**change))
+
+
+def test_layout_of_too_many_rows():
+    """A workgroup of 1024 threads to every (layer, sequence, KV head): 2^22 of them would pass a grid's 2^32 - 1 threads."""
+    many = layout(n_layers=65535, n_seqs=16, n_kv_heads=4, max_slots=1)       # 2^22 - 64 rows
+    assert es.easyspec_attn_weights_workspace_bytes(many, [1] + [0] * 15, [1] + [0] * 15, 4) > 0
+    more = layout(n_layers=32768, n_seqs=16, n_kv_heads=8, max_slots=1)       # 2^22
+    assert es.easyspec_attn_weights_workspace_bytes(more, [1] + [0] * 15, [1] + [0] * 15, 8) == -1
+    refused(lambda: es.easyspec_kv_evict(far(0), far(1), far(2), more, [1] * 16, [1] * 16, 1, 1, 1 << 40, 1 << 41, 1 << 42, 1 << 43, None))
+
+
+def test_attn_weights_of_no_new_tokens_need_neither_queries_nor_workspace():
+    es.easyspec_attn_weights(None, far(1), layout(), [0] * 4, [3, 0, 32, 1], 4, far(2), far(3), None, None)
+    refused(weigh(n_tokens=[0, 0, 0, 0], w_out=None))
+    refused(weigh(n_tokens=[0, 0, 0, -1]))

@@ -83,8 +83,8 @@ void launch_kv_reorder(const void* k, const void* v, void* k_out, void* v_out, c
 // apart and in one: 8 lists of 64, 128, 256 and 512 rows of 128 bytes 11.5, 12.3, 12.2, 12.0 and 9.1, 9.5, 9.9, 12.8; 256 lists
 // of 64, 128, 256, 512 and 1024 rows of 256 bytes 12.1, 15.0, 20.4, 29.3, 58.5 and 9.5, 12.8, 18.6, 28.4, 63.5; in place the same to
 // 1 us but for the last, 52 and 48.
-// (2) is bound by memory: 268 MB (1024 rows of 256 lists) in 48 us, 5.6 TB/s.  (1) is bound by its chain of steps for short rows, 256 of
-// 2048 weights 9.7 us, and by instructions for long ones, 256 of up to 32768 34 us.
+// (2) is bound by memory: 268 MB (1024 rows of 256 lists) in 49 us, 5.5 TB/s.  (1) is bound by its chain of steps for short rows, 256 of
+// 2048 weights 9.1 us, and by instructions for long ones, 256 of up to 32768 34 us.
 // The weight is found digit by digit: a histogram of the highest eleven bits of all weights, then of the next eleven of those that
 // share these, then of the last ten.  (Bit by bit, every step counting all weights again, 256 rows of up to 32768 took 88 us.)
 // ------------------------------------------------------------------------------------------

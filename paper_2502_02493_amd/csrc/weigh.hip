@@ -11,9 +11,9 @@
 //   (2) weigh_add_kernel     the scores once more, their probabilities, the sums over the rows.
 // (Keeping the scores between the two would take four bytes a row and slot, up to 512 beside the 256 of a key.)  Contexts of a
 // few hundred slots are one launch, weigh_short_kernel.
-// Long contexts are bound by the keys, which are read twice: 61 440 slots of 8 KV heads, 126 MB, 23 us a launch (5.4 TB/s).  Many
-// rows are bound by what a wave does with a tile of scores: 16 sequences of 16 tokens and 800 slots, 112 rows a KV head, 10 us a launch, of
-// which the keys alone would be 3.
+// Long contexts are bound by the keys, which are read twice: 61 440 slots of 8 KV heads, 126 MB, 23.5 and 25.4 us (5.2 TB/s).  Many
+// rows are bound by what a wave does with a tile of scores: 16 sequences of 16 tokens and 800 slots, 112 rows a KV head, 12.6 and
+// 12.9 us, of which the keys alone would be 3.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -163,7 +163,8 @@ __device__ __forceinline__ f32x4 scores_of(const WeighKeys<T, HD>& kf, const Wei
 // Four waves (one row tile): every wave loads its own tiles, the next one's keys requested before the present one's are used.
 // Eight: the waves need the same keys.  Each loads one tile of a round of eight, they meet in LDS in the order of the operand, and
 // the next round's are on their way while the scores are worked out.  (Every wave loading all the keys that it needs has few
-// different ones under way: sixteen sequences of 16 tokens, 112 rows, 35 us a call, and 25 so.)
+// different ones under way: sixteen sequences of 16 tokens, 112 rows, 35 us a call, and 24 so.
+// Keys of two rounds ahead in registers: 144 of them, one workgroup to a CU, and 52.7 us for these 126 MB instead of 49.8.)
 template <typename T, int HD, int NW>
 constexpr int weigh_keys() {
   return NW == 4 ? 0 : NW * WeighGeom<T, HD>::NKT * 64;

@@ -34,7 +34,8 @@
  *     wait is bounded; a pass that waited some seconds in vain (a device that stopped advancing it)
  *     ends, but its results and cache entries are wrong, and the call that enqueued it has long
  *     returned.  Once such a pass has ended, draft steps, calibrations, easyspec_get_lens, _truncate,
- *     _kv_import, _kv_export and _get_hidden return EASYSPEC_EHIP on that context and keep doing so:
+ *     _kv_import, _kv_export, _get_hidden, _beam_fork, _beam_reorder, _track_attention, _evict and
+ *     _get_attn_weights return EASYSPEC_EHIP on that context and keep doing so:
  *     destroy it.  The import and export look again after their synchronisation; a program that wants
  *     to know earlier, or replays captured passes without calling the library, synchronises its
  *     stream and calls easyspec_get_lens before it uses results.

@@ -177,3 +177,20 @@ def test_graph_replays(es):
         graph.replay()
         torch.cuda.synchronize()
         check(q, k, w, n, lens, out)
+
+
+def test_offsets_beyond_32_bits(es):
+    """A cache of more than 2^31 elements and 4 GiB: the last rows, of a long sequence and a short one."""
+    import torch
+    L, B, H, S, hd = 2, 16, 17, 65536, 64
+    n, lens = [0] * 14 + [1, 16], [0] * 14 + [5, S]
+    k = torch.zeros(L, B, H, S, hd, dtype=torch.bfloat16, device="cuda")
+    assert k.numel() > 1 << 31
+    w = torch.zeros(L, B, H, S, device="cuda")
+    q, few, before, _ = setup(es, 71, 1, (H, H), hd, "bf16", [1, 16], [5, S], S)
+    k[-1, 14:], w[-1, 14:] = few[0], before[0]
+    layout = es.easyspec_kv_layout(L, B, H, S, hd, es.EASYSPEC_DTYPE_BF16)
+    out = call(es, torch.cat([torch.ones_like(q), q]), k, w, layout, n, lens, H)
+    for h in (0, H - 1):
+        check(q[:, :, h:h + 1], few[:, :, h:h + 1], before[:, :, h:h + 1], [1, 16], [5, S], out[-1:, 14:, h:h + 1])
+    assert torch.all(out[:, :14] == -3.0)

@@ -191,3 +191,49 @@ def test_stays_inside_its_workspace_and_outputs(es):
         assert bool((ws[n:] == 0xA5).all()) and all(bool((o[G * K:] == 77).all()) for o in out)
         for g in range(G):
             assert np.array_equal(out[0][g * K: g * K + K].cpu().numpy(), ref.beam_select(logits[g], scores[g], None, K, 1.0, 0)[0])
+
+
+def test_offsets_beyond_32_bits(es):
+    """More than 2^31 logits: two beams of the last group alone are live, the others' logits and lists are not read."""
+    import torch
+    dev = torch.device("cuda:0")
+    G, W, V, K = 33, 64, 1 << 20, 64
+    logits, scores = rows(22, 1, 2, V)
+    d_l = torch.full((G, W, V), float("nan"), device=dev)
+    assert d_l.numel() > 1 << 31
+    d_s = torch.full((G, W), -float("inf"), device=dev)
+    d_l[-1, 62:], d_s[-1, 62:] = torch.from_numpy(logits[0]).to(dev), torch.from_numpy(scores[0]).to(dev)
+    n = es.easyspec_beam_select_workspace_bytes(G, W, V, K)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=dev)
+    tok, par = (torch.full((G, K), -7, dtype=torch.int32, device=dev) for _ in range(2))
+    out = torch.full((G, K), 7.0, device=dev)
+    torch.cuda.synchronize()
+    es.easyspec_beam_select(d_l, d_s, None, G, W, V, K, 1.0, 0, tok, par, out, ws, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    w_tok, w_par, w_out = ref.beam_select(logits[0], scores[0], None, K, 1.0, 0)
+    assert np.array_equal(tok[-1].cpu().numpy(), w_tok) and np.array_equal(par[-1].cpu().numpy(), w_par + 62)
+    assert np.all(np.abs(out[-1].cpu().numpy() - w_out) <= np.abs(w_out) * 2.0 ** -24 * 1.001 + 1e-11)
+    assert torch.all(tok[:-1] == -1) and torch.all(par[:-1] == -1) and torch.all(out[:-1] == -float("inf"))
+
+
+def test_two_calls_at_once(es):
+    """Two streams, each with its own workspace: the same results as one after the other."""
+    import torch
+    dev = torch.device("cuda:0")
+    sets = []
+    for seed, (G, W, V, K) in ((23, (1, 16, 128256, 16)), (24, (7, 5, 50000, 9))):
+        logits, scores = rows(seed, G, W, V)
+        t = [torch.from_numpy(x).to(dev) for x in (logits, scores)]
+        outs = [[torch.zeros((G, K), dtype=d, device=dev) for d in (torch.int32, torch.int32, torch.float32)] for _ in range(2)]
+        ws = torch.zeros(es.easyspec_beam_select_workspace_bytes(G, W, V, K), dtype=torch.uint8, device=dev)
+        sets.append((t, outs, ws, (G, W, V, K), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for (l, s), outs, ws, size, _ in sets:
+        es.easyspec_beam_select(l, s, None, *size, 0.9, 0, *outs[0], ws, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for (l, s), outs, ws, size, st in sets:
+            es.easyspec_beam_select(l, s, None, *size, 0.9, 0, *outs[1], ws, st.cuda_stream)
+    torch.cuda.synchronize()
+    for _, (a, b), _, _, _ in sets:
+        assert all(torch.equal(x, y) for x, y in zip(a, b))

@@ -126,3 +126,22 @@ def test_models_without_such_a_kernel(gpu, over):
         assert int(g.lens()[0][0]) == 3
     finally:
         g.close()
+
+
+def test_calls_on_beams_and_bounded_caches_refuse(pair):
+    import torch
+    import paper_2502_02493_amd as es
+    a, b, st = pair
+    parents = torch.zeros(1, dtype=torch.int32, device="cuda")
+    w = np.zeros((a.cfg["n_layers"], a.cfg["n_kv_heads"], 1), np.float32)
+    torch.cuda.synchronize()
+    es.easyspec_track_attention(a.ctx, 4096)
+    es.easyspec_force_give_up(a.ctx, 1)
+    es.easyspec_draft_step(a.ctx, a.tok_in, a.tok_out, a.logits)
+    refuses(es.easyspec_get_attn_weights, a.ctx, 0, w, 1)         # no synchronisation before it: it looks again after its own
+    refuses(es.easyspec_get_attn_weights, a.ctx, 0, w, 1)
+    refuses(es.easyspec_beam_fork, a.ctx, 0, 1, 1)
+    refuses(es.easyspec_beam_reorder, a.ctx, 0, 1, parents, 0)
+    refuses(es.easyspec_evict, a.ctx, [1, -1], 0)
+    refuses(es.easyspec_track_attention, a.ctx, 4096)
+    es.easyspec_beam_fork(b.ctx, 0, 1, 1)                         # the other context goes on

@@ -144,3 +144,31 @@ def test_rows_that_the_selecting_workgroup_moves_and_those_it_does_not(es):
             for keep in (most, most + 1):
                 check(es, k, v, w, [S, S - 1], [keep, keep - 3], 7, keep)
                 check(es, k, v, w, [S, S - 1], [keep, keep - 3], 7, in_place=True)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_offsets_beyond_32_bits(es, in_place):
+    """Caches of more than 2^31 elements and 4 GiB: the last rows, of a long sequence and a short one."""
+    import torch
+    L, B, H, S, hd = 2, 16, 17, 65536, 64
+    k, v = (torch.zeros(L, B, H, S, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 31
+    w = torch.zeros(L, B, H, S, device="cuda")
+    few = make(70, 1, 2, H, S, hd, "bf16")
+    for whole, part in zip((k, v, w), few):
+        whole[-1, 14:] = part[0]
+    lens, keep, So = [0] * 14 + [70, S], [8] * 14 + [50, 1000], S if in_place else 1000
+    layout = es.easyspec_kv_layout(L, B, H, S, hd, es.EASYSPEC_DTYPE_BF16)
+    slots = torch.full((L, B, H, So), -9, dtype=torch.int32, device="cuda")
+    ko, vo, wo = (k, v, w) if in_place else (torch.zeros(L, B, H, So, *x, dtype=t, device="cuda") for x, t in (((hd,), k.dtype), ((hd,), k.dtype), ((), w.dtype)))
+    torch.cuda.synchronize()
+    es.easyspec_kv_evict(k, v, w, layout, lens, keep, 30, So, ko, vo, wo, slots, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for b in (0, 1):
+        for h in (0, H - 1):
+            kept = ref.kept_slots(few[2][0, b, h].cpu().numpy(), lens[14 + b], keep[14 + b], 30)
+            assert np.array_equal(slots[-1, 14 + b, h, :len(kept)].cpu().numpy(), kept) and torch.all(slots[-1, 14 + b, h, len(kept):] == -9)
+            at = torch.from_numpy(kept.astype(np.int64)).cuda()
+            for got, was in zip((ko, vo, wo), few):
+                assert torch.equal(got[-1, 14 + b, h, :len(kept)], was[0, b, h].index_select(0, at))
+    assert torch.all(slots[:, :14] == -9) and not bool(ko[:, :14].any()) and not bool(vo[:, :14].any()) and not bool(wo[:, :14].any())

@@ -341,8 +341,9 @@ int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const
  *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
  *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
  * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q and workspace may be NULL if no sequence
- * has new tokens), a bad layout, counts or lengths, arrays that are not 16-byte aligned (weights: 4) or not memory of the current
- * device. */
+ * has new tokens), a bad layout, counts or lengths, weights_in and weights_out that overlap in part, weights_out or a workspace that
+ * overlaps q, k or each other, a workspace that overlaps weights_in, arrays that are not 16-byte aligned (weights: 4) or not memory
+ * of the current device. */
 int easyspec_attn_weights(const float *q, const void *k, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
                           int32_t n_q_heads, const float *weights_in, float *weights_out, void *workspace, void *hip_stream);
 int64_t easyspec_attn_weights_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,

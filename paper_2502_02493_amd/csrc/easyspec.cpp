@@ -943,6 +943,21 @@ static bool misaligned(std::initializer_list<const void*> ps, uintptr_t to) {
 static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
+// Does an array that a call writes reach into one that it reads, or into another that it writes?  NULL and empty ones do not.
+struct Extent {
+  const void* p;
+  size_t bytes;
+};
+static bool writes_into(std::initializer_list<Extent> written, std::initializer_list<Extent> read) {
+  auto meet = [](const Extent& a, const Extent& b) { return a.p && b.p && a.bytes && b.bytes && overlap(a.p, a.bytes, b.p, b.bytes); };
+  for (const Extent* w = written.begin(); w != written.end(); ++w) {
+    for (const Extent* o = w + 1; o != written.end(); ++o)
+      if (meet(*w, *o)) return true;
+    for (const Extent& r : read)
+      if (meet(*w, r)) return true;
+  }
+  return false;
+}
 
 static bool beam_sizes_ok(int32_t groups, int32_t beams, int32_t vocab, int32_t n_select) {
   return groups >= 1 && beams >= 1 && beams <= EASYSPEC_MAX_BEAMS && (int64_t)groups * beams <= 65535 && vocab >= 1 &&
@@ -1059,6 +1074,11 @@ extern "C" int easyspec_attn_weights(const float* q, const void* k, const easysp
   const size_t bytes = layout_rows(layout) * layout->max_slots * sizeof(float);
   if (weights_in && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes))
     return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights_in and weights_out overlap in part");
+  // workgroups read queries, keys and statistics while others write weights already
+  const Extent out = {weights_out, bytes}, ws = {workspace, weigh_workspace_bytes(a, layout->n_layers)};
+  const Extent rows = {q, a.q_layer_pitch * layout->n_layers * sizeof(float)}, keys = {k, layout_rows(layout) * layout->max_slots * slot_bytes(layout)};
+  if (writes_into({out, ws}, {rows, keys}) || writes_into({ws}, {{weights_in, bytes}}))
+    return fail(nullptr, EASYSPEC_EINVAL, "attn_weights: weights_out or the workspace overlaps another array");
   rc = check_arrays(nullptr, "attn_weights", {weights_out, workspace}, {q, k, weights_in});
   if (rc != EASYSPEC_OK) return rc;
   a.q = q; a.k = k; a.w_in = weights_in; a.w_out = weights_out; a.stats = (float2*)workspace;

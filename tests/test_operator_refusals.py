@@ -152,3 +152,22 @@ def test_attn_weights_of_no_new_tokens_need_neither_queries_nor_workspace():
     es.easyspec_attn_weights(None, far(1), layout(), [0] * 4, [3, 0, 32, 1], 4, far(2), far(3), None, None)
     refused(weigh(n_tokens=[0, 0, 0, 0], w_out=None))
     refused(weigh(n_tokens=[0, 0, 0, -1]))
+
+
+@pytest.mark.parametrize("change", [
+    dict(w_out=far(0)), dict(w_out=far(0) + 23 * 1024), dict(w_out=far(1)), dict(w_out=far(1) + 64 * 1024 - 16), dict(w_out=far(4)),   # q, k, workspace
+    dict(ws=far(0) + 16), dict(ws=far(0) - 16), dict(ws=far(1)), dict(ws=far(2)), dict(ws=far(2) + 2048 - 16), dict(ws=far(3) - 16),
+    dict(w_in=None, w_out=far(1) + 16), dict(w_in=far(3), ws=far(3)),
+])
+def test_attn_weights_that_overlap_what_others_still_read(change):
+    """weights: 2 x 4 x 2 x 32 floats, 2 KiB; k 64 KiB; q: 2 layers x 19 tokens x 4 heads x 64 floats, 38 KiB."""
+    refused(weigh(**change))
+
+
+def test_attn_weights_whose_arrays_touch():
+    """Arrays behind one another are apart: what refuses the call is that these addresses are no memory."""
+    ws = es.easyspec_attn_weights_workspace_bytes(layout(), [1, 2, 0, 16], [1, 32, 0, 20], 4)
+    q, k, w_in, w_out = far(0), far(0) + 38 * 1024, far(0) + 102 * 1024, far(0) + 104 * 1024
+    with pytest.raises(es.EasySpecError) as e:
+        weigh(q=q, k=k, w_in=w_in, w_out=w_out, ws=far(0) - (ws + 15) // 16 * 16)()
+    assert "overlap" not in str(e.value)

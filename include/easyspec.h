@@ -283,7 +283,8 @@ int64_t easyspec_accept_static_max_bytes(void);
  * draft step as they are; over the nodes of a tree level, beams is EASYSPEC_MAX_TREE_WIDTH and the scores of unused rows are
  * minus infinity.  EASYSPEC_EINVAL for NULL pointers, groups or vocab < 1, groups * beams > 65535, beams, n_select or vocab
  * beyond the limits above, an end_token outside the vocabulary if `ended` is given, a temperature that is not positive and
- * finite, scores and scores_out that overlap otherwise, or arrays that are not memory of the current device. */
+ * finite, scores and scores_out that overlap otherwise, outputs or a workspace that overlap an input or each other, or arrays that
+ * are not memory of the current device. */
 int easyspec_beam_select(const float *logits, const float *scores, const int32_t *ended, int32_t groups, int32_t beams, int32_t vocab,
                          int32_t n_select, float temperature, int32_t end_token, int32_t *tokens_out, int32_t *parents_out,
                          float *scores_out, void *workspace, void *hip_stream);

@@ -979,9 +979,15 @@ extern "C" int easyspec_beam_select(const float* logits, const float* scores, co
   if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: temperature must be positive and finite");
   if (ended && (end_token < 0 || end_token >= vocab)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: end_token %d outside the vocabulary", end_token);
   if (misaligned({workspace}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "beam_select: workspace must be 16-byte aligned");
-  if (!(scores_out == scores && n_select == beams) &&
-      overlap(scores, (size_t)groups * beams * sizeof(float), scores_out, (size_t)groups * n_select * sizeof(float)))
+  const size_t rows = (size_t)groups * beams, picks = (size_t)groups * n_select * sizeof(int32_t);
+  const Extent tokens = {tokens_out, picks}, parents = {parents_out, picks}, sums = {scores_out, picks}, cums = {scores, rows * sizeof(float)};
+  const Extent ws = {workspace, beam_select_workspace_bytes(groups, beams, vocab, n_select)};
+  const Extent rows_in = {logits, rows * vocab * sizeof(float)}, ends = {ended, rows * sizeof(int32_t)};
+  if (!(scores_out == scores && n_select == beams) && writes_into({sums}, {cums}))
     return fail(nullptr, EASYSPEC_EINVAL, "beam_select: scores and scores_out overlap (they may be one array if n_select == beams)");
+  // a group is picked while others' logits, scores and ends are still read
+  if (writes_into({tokens, parents, sums, ws}, {rows_in, ends}) || writes_into({tokens, parents, ws}, {cums}))
+    return fail(nullptr, EASYSPEC_EINVAL, "beam_select: an output or the workspace overlaps another array");
   const int rc = check_arrays(nullptr, "beam_select", {tokens_out, parents_out, scores_out, workspace}, {logits, scores, ended});
   if (rc != EASYSPEC_OK) return rc;
   launch_beam_select(logits, scores, ended, groups, beams, vocab, n_select, (double)temperature, end_token, tokens_out, parents_out, scores_out,

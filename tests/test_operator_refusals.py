@@ -171,3 +171,30 @@ def test_attn_weights_whose_arrays_touch():
     with pytest.raises(es.EasySpecError) as e:
         weigh(q=q, k=k, w_in=w_in, w_out=w_out, ws=far(0) - (ws + 15) // 16 * 16)()
     assert "overlap" not in str(e.value)
+
+
+def apart_beam(**change):
+    """Three groups of four beams, 100 words, the four best: logits 4800 bytes, scores, ends and each output 48."""
+    a = dict(logits=far(0), scores=far(1), ended=far(2), groups=3, tokens_out=far(3), parents_out=far(4), scores_out=far(5), workspace=far(6))
+    a.update(change)
+    return beam(**a)
+
+
+@pytest.mark.parametrize("change", [
+    dict(tokens_out=far(0)), dict(parents_out=far(0) + 4796), dict(scores_out=far(0) + 4), dict(workspace=far(0) + 16),      # logits
+    dict(tokens_out=far(1)), dict(parents_out=far(1) + 44), dict(workspace=far(1) - 16),                                     # scores
+    dict(tokens_out=far(2)), dict(parents_out=far(2) - 44), dict(scores_out=far(2)), dict(workspace=far(2)),                 # ends
+    dict(parents_out=far(3)), dict(scores_out=far(3) + 44), dict(scores_out=far(4)), dict(workspace=far(3)), dict(workspace=far(4)),
+    dict(workspace=far(5) - 16), dict(scores_out=far(1), tokens_out=far(1)), dict(scores_out=far(1), workspace=far(1)),
+])
+def test_beam_select_outputs_over_what_others_still_read(change):
+    refused(apart_beam(**change))
+
+
+@pytest.mark.parametrize("change", [dict(), dict(scores_out=far(1)), dict(ended=None, tokens_out=far(2), parents_out=far(2) + 48, scores_out=far(2) + 96),
+                                    dict(tokens_out=far(0) + 4800, parents_out=far(1) + 48, scores_out=far(2) - 48)])
+def test_beam_select_arrays_apart(change):
+    """What refuses these calls is that the addresses are no memory."""
+    with pytest.raises(es.EasySpecError) as e:
+        apart_beam(**change)()
+    assert "overlap" not in str(e.value)

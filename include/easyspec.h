@@ -308,9 +308,8 @@ typedef struct easyspec_kv_layout {
  *   k, v, k_out, v_out  dev  k_out == k and v_out == v (in place) or arrays apart from both
  *   parents             dev [n_seqs]
  * Other slots of k_out, v_out are left as they were.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for
- * NULL pointers, a bad layout or slot range, beams that do not divide n_seqs, arrays that overlap in part or are not 16-byte
- * aligned, or arrays that are not memory of the
- * current device. */
+ * NULL pointers, a bad layout or slot range, beams that do not divide n_seqs, caches that overlap in part or are not 16-byte
+ * aligned, parents inside k_out or v_out, or arrays that are not memory of the current device. */
 int easyspec_kv_reorder(const void *k, const void *v, const easyspec_kv_layout *layout, const int32_t *parents, int32_t beams,
                         int32_t from_slot, int32_t to_slot, void *k_out, void *v_out, void *hip_stream);
 

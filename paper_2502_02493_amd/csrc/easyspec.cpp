@@ -1028,7 +1028,10 @@ extern "C" int easyspec_kv_reorder(const void* k, const void* v, const easyspec_
   if (misaligned({k, v, k_out, v_out}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: arrays must be 16-byte aligned");
   const size_t bytes = layout_rows(layout) * layout->max_slots * slot_bytes(layout);
   rc = check_in_place("kv_reorder", k, v, bytes, k_out, v_out, bytes);
-  if (rc == EASYSPEC_OK) rc = check_arrays(nullptr, "kv_reorder", {k_out, v_out}, {k, v, parents});
+  if (rc != EASYSPEC_OK) return rc;
+  if (writes_into({{k_out, bytes}, {v_out, bytes}}, {{parents, layout->n_seqs * sizeof(int32_t)}}))
+    return fail(nullptr, EASYSPEC_EINVAL, "kv_reorder: parents lie in a cache that is written");
+  rc = check_arrays(nullptr, "kv_reorder", {k_out, v_out}, {k, v, parents});
   if (rc != EASYSPEC_OK) return rc;
   const KvLayout g = {layout->n_layers, layout->n_seqs, layout->n_kv_heads, layout->max_slots};
   launch_kv_reorder(k, v, k_out, v_out, g, slot_bytes(layout), parents, 0, 0, layout->n_seqs, beams, from_slot, to_slot, (hipStream_t)hip_stream);

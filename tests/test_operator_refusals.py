@@ -198,3 +198,17 @@ def test_beam_select_arrays_apart(change):
     with pytest.raises(es.EasySpecError) as e:
         apart_beam(**change)()
     assert "overlap" not in str(e.value)
+
+
+@pytest.mark.parametrize("change", [dict(parents=far(2)), dict(parents=far(3) + 65536 - 4), dict(parents=far(2) - 12),
+                                    dict(k_out=far(0), v_out=far(1), parents=far(0) + 64), dict(k_out=far(0), v_out=far(1), parents=far(1) + 64)])
+def test_kv_reorder_parents_in_a_cache_that_is_written(change):
+    """Caches of 64 KiB each, four parents."""
+    refused(reorder(**change))
+
+
+@pytest.mark.parametrize("change", [dict(parents=far(0) + 64), dict(parents=far(2) + 65536), dict(parents=far(3) - 16)])
+def test_kv_reorder_parents_apart(change):
+    with pytest.raises(es.EasySpecError) as e:
+        reorder(**change)()
+    assert "parents" not in str(e.value)

@@ -153,9 +153,15 @@ def easyspec_last_error(ctx=None) -> str:
     return load_library().easyspec_last_error(ctx).decode()
 
 
+class _Context(C.c_void_p):
+    """The handle that easyspec_create returns, with the length of the host arrays that hold an entry per sequence."""
+    max_batch = None
+
+
 def easyspec_create(cfg: easyspec_config, hip_stream=None):
-    h = C.c_void_p()
+    h = _Context()
     _check(load_library().easyspec_create(C.byref(cfg), _ptr(hip_stream), C.byref(h)), None)
+    h.max_batch = int(cfg.max_batch)
     return h
 
 
@@ -271,8 +277,10 @@ def easyspec_beam_select_workspace_bytes(groups: int, beams: int, vocab: int, n_
 
 
 def _host_ints(x, n):
+    """An array of n host integers, all of which the library reads (n None: a handle that does not say how many)."""
     a = np.ascontiguousarray(x, dtype=np.int32)
-    assert a.size == n
+    if n is not None and a.size != n:
+        raise EasySpecError(EASYSPEC_EINVAL, f"an array of {a.size} entries where there are {n} sequences")
     return a
 
 
@@ -312,12 +320,12 @@ def easyspec_track_attention(ctx, max_positions: int):
 
 
 def easyspec_evict(ctx, keep, recent: int):
-    k = np.ascontiguousarray(keep, dtype=np.int32)
+    k = _host_ints(keep, getattr(ctx, "max_batch", None))
     _check(load_library().easyspec_evict(ctx, _ptr(k), recent), ctx)
 
 
 def easyspec_get_evicted(ctx, max_batch: int):
-    n = np.zeros(max_batch, np.int32)
+    n = _host_ints(np.zeros(max_batch, np.int32), getattr(ctx, "max_batch", None))
     _check(load_library().easyspec_get_evicted(ctx, _ptr(n)), ctx)
     return n
 

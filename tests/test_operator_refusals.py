@@ -212,3 +212,30 @@ def test_kv_reorder_parents_apart(change):
     with pytest.raises(es.EasySpecError) as e:
         reorder(**change)()
     assert "parents" not in str(e.value)
+
+
+@pytest.mark.parametrize("n", [0, 1, 3, 5])
+def test_arrays_of_another_length_than_there_are_sequences(n):
+    """The library reads an entry per sequence: a shorter array would be read past its end."""
+    refused(weigh(n_tokens=[1] * n))
+    refused(weigh(lens=[20] * n))
+    refused(evict(lens=[20] * n))
+    refused(evict(keep=[8] * n))
+    with pytest.raises(es.EasySpecError) as e:
+        es.easyspec_attn_weights_workspace_bytes(layout(), [1] * n, [8] * 4, 4)
+    assert e.value.code == es.EASYSPEC_EINVAL
+    ctx = es.binding._Context()                  # of four sequences; no context behind it: the arrays are looked at first
+    ctx.max_batch = 4
+    for call in (lambda: es.easyspec_evict(ctx, [8] * n, 1), lambda: es.easyspec_get_evicted(ctx, n)):
+        with pytest.raises(es.EasySpecError) as e:
+            call()
+        assert e.value.code == es.EASYSPEC_EINVAL and "4 sequences" in str(e.value)
+
+
+def test_arrays_of_a_context_of_as_many_sequences():
+    ctx = es.binding._Context()
+    ctx.max_batch = 4
+    for call in (lambda: es.easyspec_evict(ctx, [8] * 4, 1), lambda: es.easyspec_get_evicted(ctx, 4)):
+        with pytest.raises(es.EasySpecError) as e:
+            call()
+        assert "ctx is NULL" in str(e.value)

@@ -119,8 +119,8 @@ int easyspec_attention_stage_walk(int32_t n_loads, int64_t *report);
  * results of timed passes may differ from the untimed ones' in their last bits.
  * profile_end synchronises the stream and returns the number of timed launches, the sum of their
  * durations in milliseconds and, where launch_ms / launch_op are not NULL (host, max_launches
- * entries each), every launch's duration and kernel class in launch order (the embedding gather
- * reports EASYSPEC_OP_ALL).  A class with two kernels per use (attention: partial + merge; head:
+ * entries each), every launch's duration and kernel class in launch order (the embedding gather and
+ * the attention weights of a context that tracks them, one or two kernels a layer, report EASYSPEC_OP_ALL).  A class with two kernels per use (attention: partial + merge; head:
  * logits + argmax) counts each kernel as a launch.  Not meant to stay on in production. */
 #define EASYSPEC_OP_QKV 0    /* stacked QKV projection + rotary + cache write */
 #define EASYSPEC_OP_ATTN 1   /* split-KV decode attention (partial + merge kernels together) */
@@ -128,7 +128,7 @@ int easyspec_attention_stage_walk(int32_t n_loads, int64_t *report);
 #define EASYSPEC_OP_GATEUP 3 /* gate/up projection + SiLU*up */
 #define EASYSPEC_OP_DOWN 4   /* down projection + residual */
 #define EASYSPEC_OP_HEAD 5   /* LM head + argmax (both kernels together) */
-#define EASYSPEC_OP_ALL 6    /* every kernel of the forward pass, the embedding gather included */
+#define EASYSPEC_OP_ALL 6    /* every kernel of the forward pass, the embedding gather and tracked attention weights included */
 int easyspec_profile_begin(easyspec_ctx *ctx, int32_t op, int32_t max_launches);
 int easyspec_profile_end(easyspec_ctx *ctx, int32_t *n_launches, float *total_ms, float *launch_ms, int32_t *launch_op);
 

@@ -546,8 +546,8 @@ static int forward(easyspec_ctx* ctx, const Cols& c, const int32_t* tokens, cons
     { ProfScope p(ctx, EASYSPEC_OP_QKV); launch_qkv(s, b, c, lo, k, st, b2, c2); }
     { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_attn(s, b, c, lo, k, cut, st); }
     if (c2) { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_attn(s, *b2, *c2, lo, k, attn_cut(s, *c2, k), st); }
-    if (weigh) weigh_layer(ctx, wa, lo);
-    if (weigh && c2) weigh_layer(ctx, wa2, lo);
+    if (weigh) { ProfScope p(ctx, EASYSPEC_OP_ALL); weigh_layer(ctx, wa, lo); }
+    if (weigh && c2) { ProfScope p(ctx, EASYSPEC_OP_ALL); weigh_layer(ctx, wa2, lo); }
     if (full_layer && k > 1) {
       // App. B ablation: the MLPs of the set also work from the set's input, each behind its own
       // layer's attention; one launch per operation for the whole set
@@ -593,7 +593,7 @@ static int wide_forward(easyspec_ctx* ctx, const Spans& sp, const int32_t* token
     const bool last = l + 1 == s.L;
     { ProfScope p(ctx, EASYSPEC_OP_QKV); launch_wide_qkv(s, b, w, sp, l, st); }
     { ProfScope p(ctx, EASYSPEC_OP_ATTN); launch_wide_attn(s, b, w, sp, l, st); }
-    if (ctx->track.weights) weigh_layer(ctx, wa, l);
+    if (ctx->track.weights) { ProfScope p(ctx, EASYSPEC_OP_ALL); weigh_layer(ctx, wa, l); }
     { ProfScope p(ctx, EASYSPEC_OP_OPROJ); launch_wide_proj(s, b, w, sp, l, false, b.g_mlp + (size_t)l * s.d, false, st); }
     { ProfScope p(ctx, EASYSPEC_OP_GATEUP); launch_wide_gateup(s, b, w, sp, l, st); }
     ProfScope p(ctx, EASYSPEC_OP_DOWN);

@@ -452,11 +452,11 @@ void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream
   auto go = [&](auto waves, auto stats, auto add, auto both) {
     const dim3 block(decltype(waves)::value * 64);
     if (one_chunk) {
-      hipLaunchKernelGGL(both, grid, block, 0, st, a);
+      ES_LAUNCH(both, grid, block, 0, st, a);
       return;
     }
-    hipLaunchKernelGGL(stats, grid, block, 0, st, a);
-    hipLaunchKernelGGL(add, grid, block, 0, st, a);
+    ES_LAUNCH(stats, grid, block, 0, st, a);
+    ES_LAUNCH(add, grid, block, 0, st, a);
   };
   typedef std::integral_constant<int, 4> Four;
   typedef std::integral_constant<int, 8> Eight;

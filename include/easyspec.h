@@ -373,7 +373,8 @@ int easyspec_kv_evict(const void *k, const void *v, const float *weights, const 
  * forwards add none) to the context's, one per layer, sequence, KV head and precise slot; slots filled before, by
  * easyspec_kv_import or by a calibration, start from zero.  Passes of such calibrations are separate launches also where a
  * small model's would be one.  max_positions: how far sequences may get, evicted slots counted (max_ctx ..
- * EASYSPEC_MAX_POSITIONS; max_ctx without this call).  Synchronous; EASYSPEC_ESTATE the second time.
+ * EASYSPEC_MAX_POSITIONS; max_ctx without this call).  Synchronous; EASYSPEC_ESTATE the second time.  A call that fails leaves the
+ * context as it was.
  * easyspec_evict: of every sequence with 0 < keep[b] < precise[b] (keep: host [max_batch]; -1 leaves a sequence alone) keep[b]
  * precise slots stay, chosen as easyspec_kv_evict does in every layer and KV head, and move together; its fuzzy slots are dropped.
  * Afterwards precise[b] = keep[b].  Later tokens take the next free slots and go on at the next positions.  In place, on the

@@ -2,7 +2,7 @@
  * easyspec_instrument.h — measurement and test hooks of the EasySpec draft library (same shared
  * library as easyspec.h).  None of them is part of the method (Alg. 2 / Sec. 3.2 / Alg. 3 of arXiv
  * 2502.02493): they time the kernels, probe the device's streaming rate, evaluate the kernels' index
- * arithmetic on the host, and poison workspaces, for the benchmark and the tests.  Conventions as in
+ * arithmetic on the host, poison workspaces, and force failures, for the benchmark and the tests.  Conventions as in
  * easyspec.h.
  */
 #ifndef EASYSPEC_INSTRUMENT_H
@@ -26,6 +26,10 @@ int easyspec_poison_workspaces(easyspec_ctx *ctx);
  * not there yet, which every pass meets; their kernels end normally.  For tests of what that does to the context.  There is such
  * a kernel for fp32 models with two query heads per KV head, EASYSPEC_EINVAL for others. */
 int easyspec_force_give_up(easyspec_ctx *ctx, int32_t on);
+
+/* The context's next device allocation but n (0: the next one; negative: none) asks for more memory than any device has and fails.
+ * For tests of what a call that allocates for the context (easyspec_track_attention) leaves behind when it cannot. */
+int easyspec_deny_allocation(easyspec_ctx *ctx, int32_t n);
 
 /* easyspec_accept whose waits end before their first look: a sequence's last workgroup reports accept_len = bonus = -1 for it unless
  * every value that it needs came with the counter that told it so, and with vocab <= 512 none has.  Its kernels end normally, and the

@@ -25,7 +25,7 @@ EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easy
            "easyspec_default_groups", "easyspec_draft_step", "easyspec_calibrate", "easyspec_greedy_accept", "easyspec_greedy_accept_host",
            "easyspec_accept", "easyspec_accept_give_up", "easyspec_accept_workspace_bytes", "easyspec_accept_static", "easyspec_accept_static_max_bytes", "easyspec_draft_tree_step", "easyspec_set_parallel_mode", "easyspec_stream_read", "easyspec_stream_read_sink_floats", "easyspec_attention_cut", "easyspec_attention_route", "easyspec_weight_walk", "easyspec_wide_walk", "easyspec_attention_stage_walk",
            "easyspec_get_lens", "easyspec_truncate", "easyspec_kv_import", "easyspec_kv_export",
-           "easyspec_get_hidden", "easyspec_poison_workspaces", "easyspec_force_give_up", "easyspec_step_bytes", "easyspec_profile_begin", "easyspec_profile_end",
+           "easyspec_get_hidden", "easyspec_poison_workspaces", "easyspec_force_give_up", "easyspec_deny_allocation", "easyspec_step_bytes", "easyspec_profile_begin", "easyspec_profile_end",
            "easyspec_beam_select", "easyspec_beam_select_workspace_bytes", "easyspec_kv_reorder",
            "easyspec_attn_weights", "easyspec_attn_weights_workspace_bytes", "easyspec_kv_evict",
            "easyspec_beam_fork", "easyspec_beam_reorder", "easyspec_track_attention", "easyspec_evict", "easyspec_get_evicted",
@@ -113,6 +113,7 @@ def load_library():
         L.easyspec_step_bytes.argtypes = [vp]
         L.easyspec_poison_workspaces.argtypes = [vp]
         L.easyspec_force_give_up.argtypes = [vp, i32]
+        L.easyspec_deny_allocation.argtypes = [vp, i32]
         L.easyspec_stream_read.argtypes = [vp, C.c_int64, vp, vp]
         L.easyspec_stream_read_sink_floats.argtypes = []
         L.easyspec_attention_cut.argtypes = [C.POINTER(easyspec_config), vp, i32, i32, vp, vp]
@@ -425,6 +426,10 @@ def easyspec_get_hidden(ctx, out, max_rows: int) -> int:
 
 def easyspec_poison_workspaces(ctx):
     _check(load_library().easyspec_poison_workspaces(ctx), ctx)
+
+
+def easyspec_deny_allocation(ctx, n: int):
+    _check(load_library().easyspec_deny_allocation(ctx, int(n)), ctx)
 
 
 def easyspec_force_give_up(ctx, on: bool):

@@ -54,6 +54,7 @@ struct easyspec_ctx {
   std::vector<int32_t> single;  // every layer alone (Alg. 1 order)
   std::vector<void*> allocs;
   std::vector<std::pair<void*, size_t>> work;  // the per-pass workspaces (easyspec_poison_workspaces)
+  int32_t deny_alloc = -1;  // allocations from here to the one that asks for too much (easyspec_deny_allocation); -1: none does
   int32_t last_rows;
   int32_t parallel_mode;  // EASYSPEC_PARALLEL_*
   // per-kernel timing (easyspec_profile_*)
@@ -102,6 +103,7 @@ static size_t packed_bytes(const Shape& s, int rows, int K, int R = 16) { return
 static int dev_alloc(easyspec_ctx* ctx, void** p, size_t bytes) {
   *p = nullptr;
   if (bytes == 0) bytes = 16;
+  if (ctx->deny_alloc >= 0 && ctx->deny_alloc-- == 0) bytes = (size_t)1 << 60;
   HIPCHK(ctx, hipMalloc(p, bytes));
   ctx->allocs.push_back(*p);
   return EASYSPEC_OK;
@@ -1198,22 +1200,37 @@ extern "C" int easyspec_track_attention(easyspec_ctx* ctx, int32_t max_positions
   if (max_positions < s.max_ctx || max_positions > EASYSPEC_MAX_POSITIONS)
     return fail(ctx, EASYSPEC_EINVAL, "track_attention: max_positions must be max_ctx (%d) .. %d", s.max_ctx, EASYSPEC_MAX_POSITIONS);
   if (ctx->track.weights) return fail(ctx, EASYSPEC_ESTATE, "track_attention: attention is tracked already");
-  const size_t n = (size_t)s.L * s.B * s.Hkv * s.max_ctx;
+  const size_t n = (size_t)s.L * s.B * s.Hkv * s.max_ctx, allocs = ctx->allocs.size(), work = ctx->work.size();
   float *weights = nullptr, *rope = nullptr;
-  ALLOC(ctx, weights, n * sizeof(float));
-  ALLOC(ctx, ctx->track.kept, n * sizeof(int32_t));
-  ctx->track.stats_bytes = weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx);
-  ALLOC(ctx, ctx->track.stats, ctx->track.stats_bytes);
-  ctx->work.push_back({ctx->track.stats, ctx->track.stats_bytes});
-  HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
-  if (max_positions > s.max_ctx) {
-    ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));
-    HIPCHK(ctx, fill_rope(ctx->cfg, (float2*)rope, max_positions));
+  easyspec_ctx::Tracked& t = ctx->track;
+  auto body = [&]() -> int {
+    ALLOC(ctx, weights, n * sizeof(float));
+    ALLOC(ctx, t.kept, n * sizeof(int32_t));
+    t.stats_bytes = weigh_workspace_limit(s.B, s.Hkv, s.Hq / s.Hkv, ctx->cfg.max_calib_tokens, s.max_ctx);
+    ALLOC_WORK(ctx, t.stats, t.stats_bytes);
+    HIPCHK(ctx, hipMemsetAsync(weights, 0, n * sizeof(float), ctx->stream));
+    if (max_positions > s.max_ctx) {
+      ALLOC(ctx, rope, (size_t)max_positions * (s.hd / 2) * sizeof(float2));
+      HIPCHK(ctx, fill_rope(ctx->cfg, (float2*)rope, max_positions));
+    }
+    HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
+    return EASYSPEC_OK;
+  };
+  const int rc = body();
+  if (rc != EASYSPEC_OK) {  // the context is what it was; a pass that follows does not report this error again
+    (void)hipStreamSynchronize(ctx->stream);
+    for (size_t i = allocs; i < ctx->allocs.size(); ++i) (void)hipFree(ctx->allocs[i]);
+    ctx->allocs.resize(allocs);
+    ctx->work.resize(work);
+    t.kept = nullptr;
+    t.stats = nullptr;
+    t.stats_bytes = 0;
+    (void)hipGetLastError();
+    return rc;
   }
-  HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
   if (rope) ctx->b.rope = ctx->b2.rope = (float2*)rope;  // the shorter table stays: a captured pass may read it
-  ctx->track.max_positions = max_positions;
-  ctx->track.weights = weights;
+  t.max_positions = max_positions;
+  t.weights = weights;
   return EASYSPEC_OK;
 }
 
@@ -1405,6 +1422,12 @@ extern "C" int easyspec_poison_workspaces(easyspec_ctx* ctx) {
   if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
   // all bits set: a NaN in float32 and in bf16, -1 as an index
   for (const auto& w : ctx->work) HIPCHK(ctx, hipMemsetAsync(w.first, 0xFF, w.second, ctx->stream));
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_deny_allocation(easyspec_ctx* ctx, int32_t n) {
+  if (!ctx) return fail(nullptr, EASYSPEC_EINVAL, "ctx is NULL");
+  ctx->deny_alloc = std::max(n, -1);
   return EASYSPEC_OK;
 }
 

@@ -380,6 +380,8 @@ int easyspec_kv_evict(const void *k, const void *v, const float *weights, const 
  * Afterwards precise[b] = keep[b].  Later tokens take the next free slots and go on at the next positions.  In place, on the
  * context's stream, not synchronised.  EASYSPEC_ESTATE if attention is not tracked.
  * easyspec_truncate refuses (EASYSPEC_ESTATE) to cut into the slots below the run of most recent ones that an eviction kept.
+ * What stays after a cut keeps its weights as they are: those that the tokens cut off gave to earlier slots are in them, and the
+ * tokens calibrated in their place add theirs.  (A calibration of tokens that are known to be accepted leaves nothing to cut off.)
  * easyspec_get_evicted: host [max_batch], the slots of each sequence evicted so far (precise + fuzzy + evicted = its position).
  * easyspec_get_attn_weights: the weights of the first n_slots precise slots of sequence b, host|dev fp32
  * [n_layers][n_kv_heads][n_slots].  Synchronous. */
@@ -393,8 +395,9 @@ int easyspec_get_attn_weights(easyspec_ctx *ctx, int32_t b, float *out, int32_t 
 int easyspec_get_lens(const easyspec_ctx *ctx, int32_t *precise, int32_t *fuzzy);
 
 /* Shorten sequence b to new_precise_len precise slots and no fuzzy ones (base-model rollback
- * after verification; 0 makes the sequence idle).  Host state only.  EASYSPEC_ESTATE if that cuts into what an eviction
- * left of the sequence's older slots (easyspec_evict). */
+ * after verification; 0 makes the sequence idle).  Host state only: tracked weights that the tokens cut off gave to the slots
+ * that stay remain in them.  EASYSPEC_ESTATE if that cuts into what an eviction left of the sequence's older slots
+ * (easyspec_evict). */
 int easyspec_truncate(easyspec_ctx *ctx, int32_t b, int32_t new_precise_len);
 
 /* Replace the cache of sequence b by n_slots precise entries.  k, v: host|dev

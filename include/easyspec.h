@@ -340,6 +340,8 @@ int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const
  *                NULL: zeros
  *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
  *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
+ * The same call gives the same bits.  How the contexts are cut goes by the longest of the call and by its most query rows, so in the
+ * last bits a sequence's weights may differ with the other sequences of the call.
  * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q and workspace may be NULL if no sequence
  * has new tokens), a bad layout, counts or lengths, weights_in and weights_out that overlap in part, weights_out or a workspace that
  * overlaps q, k or each other, a workspace that overlaps weights_in, arrays that are not 16-byte aligned (weights: 4) or not memory

@@ -389,8 +389,20 @@ __global__ __launch_bounds__(NW * 64) void weigh_short_kernel(WeighArgs a) {
 // terms, the sums of all chunks) is then done once for its share of the keys.  us a call, 32 query heads on 8 KV heads but for (*),
 // 28 on 4, with at most 256 / 512 / 1024 / 2048 workgroups: one token each at 4096 .. 32768 slots 45 / 50 / 52 / 48, 16 at 8192
 // 18 / 21 / 38 / 38, 12 each at four times 2048 16.5 / 18.2 / 33 / 33, (*) 16 at 32768 40 / 43 / 69 / 165, 6 each in fp32 at twice
-// 8192 40 / 45 / 59 / 104.  Two row tiles of bf16 are the exception: the keys that a round brings serve two waves each only, and two
-// workgroups to a CU have more of them under way: 6 each at 4096 .. 32768 54 / 49 / 58 / 72.
+// 8192 40 / 45 / 59 / 104.  Two row tiles of bf16 are the exception where their chunks are long: the keys that a round brings serve two
+// waves each only, and two workgroups to a CU have more of them under way; but twice the chunks are twice the statistics that every
+// workgroup joins, so only where a workgroup still has more than two rounds.  us a call in a graph, keys from memory, with at most
+// 256 / 512 workgroups, by the slots of a chunk that 512 leave (query heads on KV heads, tokens of each sequence, slots):
+//    64  8 on 1, 4 at 32768 16.5 / 24.1; 16 on 8, 12 at 4096 12.5 / 15.5
+//   128  32 on 8, 6 at 8192 15.4 / 16.4; 28 on 4, 4 at 16384 15.5 / 17.6; 8 on 1, 4 at 65536 19.3 / 25.0
+//   192  32 on 8, 6 at 12288 17.8 / 19.2; 28 on 4, 4 at 24576 17.8 / 20.4; 16 on 8, 12 at 12288 17.8 / 19.3
+//   256  32 on 8, 6 at 16384 21.1 / 20.3, at sixteen times 1024 21.7 / 22.2; 28 on 4, 4 at 32768 21.3 / 21.2; 8 on 1, 4 at twice 65536
+//        22.3 / 23.8; heads of 64: 32 on 8, 6 at 16384 15.6 / 14.9, 14 on 2, 3 at 65536 16.6 / 18.5
+//   320  32 on 8, 6 at 20480 26.1 / 26.1
+//   384  32 on 8, 6 at 24576 29.3 / 27.0
+//   512  32 on 8, 6 at 32768 35.3 / 33.0, 5 at sixteen times 2048 35.4 / 33.1; 28 on 4, 3 at 65536 35.2 / 34.3; heads of 64: 32 on 8,
+//        6 at 32768 23.6 / 20.1
+//  1024  32 on 8, 6 at 4096 .. 32768 61.8 / 52.2 (with at most 1024 workgroups 56.8), at 65536 58.3 / 55.5
 constexpr int kWeighCus = 256;
 static int most_rows(const WeighArgs& a) {
   int rows = 1;
@@ -402,19 +414,26 @@ static int most_rows(const WeighArgs& a) {
 // 7.1, 9.4, 13.4, sixteen sequences of six 10.9, 14.6, 15.7 and 7.4, 9.8, 14.0; but one in fp32 9.3, 9.4 and 8.7, 12.3, sixteen with
 // 28 heads on 4 14.0, 14.2 and 11.6, 17.3.
 static int weigh_short(int rows, int dtype) { return rows <= 32 && dtype == 1 ? 256 : 128; }
+constexpr int kWeighTwoRounds = 2 * 8 * 16;  // slots of two rounds of eight tiles
 static int weigh_chunk(const WeighArgs& a, int n_layers, int dtype) {
   const int rows = most_rows(a), groups = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-  const long wgs_most = groups == 2 && dtype == 1 ? 2 * kWeighCus : kWeighCus;
   int longest = 0;
   for (int i = 0; i < a.n_entries; ++i) longest = std::max(longest, a.entry[i].len);
   if (longest <= weigh_short(rows, dtype)) return (longest + 63) / 64 * 64;
-  int chunk = 64;
-  for (; chunk < kWeighSums / groups; chunk += 64) {
-    long wgs = 0;
-    for (int i = 0; i < a.n_entries; ++i) wgs += (a.entry[i].len + chunk - 1) / chunk;
-    if (wgs * a.heads * n_layers <= wgs_most) break;
+  auto cut = [&](long wgs_most) {
+    int chunk = 64;
+    for (; chunk < kWeighSums / groups; chunk += 64) {
+      long wgs = 0;
+      for (int i = 0; i < a.n_entries; ++i) wgs += (a.entry[i].len + chunk - 1) / chunk;
+      if (wgs * a.heads * n_layers <= wgs_most) break;
+    }
+    return chunk;
+  };
+  if (groups == 2 && dtype == 1) {
+    const int chunk = cut(2 * kWeighCus);
+    if (chunk > kWeighTwoRounds) return chunk;
   }
-  return chunk;
+  return cut(kWeighCus);
 }
 
 // Fills in how the entries (seq, n, len, q_first are set) are cut.

@@ -116,16 +116,16 @@ __global__ __launch_bounds__(kSliceThreads) __attribute__((amdgpu_waves_per_eu(8
   for (int i = 0; i < kSliceRegs; ++i) l[i] = l_row[min(v0 + i * kSliceThreads + tid, a.V - 1)];
 #pragma unroll
   for (int i = 0; i < kSliceRegs; ++i) l[i] = v0 + i * kSliceThreads + tid < v1 ? l[i] : -INFINITY;
-  float half_max[2] = {-INFINITY, -INFINITY};  // of the thread's two halves of the slice; a maximum passes over NaNs
+  float own = -INFINITY;  // a maximum passes over NaNs
 #pragma unroll
-  for (int i = 0; i < kSliceRegs; ++i) half_max[2 * i / kSliceRegs] = fmaxf(half_max[2 * i / kSliceRegs], l[i]);
-  const float own = fmaxf(half_max[0], half_max[1]);
-  // A bound of the n_select highest from below: of at least n_select groups of threads (of halves of them, for more than 32) the
-  // lowest maximum, which as many logits reach.  Few more do: with 16 groups of 256 logits some 50 of 4096.
-  const int lanes = a.n_select <= NW ? 64 : a.n_select <= 2 * NW ? 32 : a.n_select <= 4 * NW ? 16 : 8;
-  const float top = lanes_max(own, 64);
-  float least_max = groups_min(lanes_max(a.n_select <= 8 * NW ? own : half_max[0], lanes), lanes);
-  if (a.n_select > 8 * NW) least_max = fminf(least_max, groups_min(lanes_max(half_max[1], lanes), lanes));
+  for (int i = 0; i < kSliceRegs; ++i) own = fmaxf(own, l[i]);
+  // A bound of the n_select highest from below: of at least n_select groups of neighbouring threads the lowest maximum, which as many
+  // logits reach.  Few more do: with 16 groups of 256 logits some 50 of 4096.  A group has its share of every register's logits, so only
+  // a slice of fewer logits than threads, or masks, leave one empty; then every logit is a candidate.
+  // (For more than 32 the groups were eight threads' halves of the slice, of which the second is empty below 2048 logits: two beams of
+  // 128 256 words, 64 of them, 74.9 us a call in a graph, 32.0 with groups of four threads; slices of 4008 words 42 .. 45 both ways.)
+  const int lanes = a.n_select <= NW ? 64 : a.n_select <= 2 * NW ? 32 : a.n_select <= 4 * NW ? 16 : a.n_select <= 8 * NW ? 8 : 4;
+  const float top = lanes_max(own, 64), least_max = groups_min(lanes == 4 ? quad_max(own) : lanes_max(own, lanes), lanes);
   // Every wave's sum on top of its own maximum: no wait for the others'.  What lies 1000 powers of two below, minus infinities and
   // NaNs among it, counts as 2^-1000.
   const double ref = top == -INFINITY ? 0.0 : (double)top;

@@ -60,6 +60,10 @@ __device__ __forceinline__ V lanes_sum(V v, int n) {
 __device__ __forceinline__ float lanes_max(float v, int n) {
   return lanes_fold(v, n, [](float a, float b) { return fmaxf(a, b); });
 }
+__device__ __forceinline__ float quad_max(float v) {  // of four neighbouring lanes
+  v = fmaxf(v, dpp<0xB1>(v));
+  return fmaxf(v, dpp<0x4E>(v));
+}
 
 // Running sum over the wave's lanes, the own one included.
 __device__ __forceinline__ uint32_t lanes_running_sum(uint32_t v) {
@@ -74,9 +78,10 @@ __device__ __forceinline__ uint32_t lanes_running_sum(uint32_t v) {
   return v;
 }
 
-// The lowest of the wave's values, which are the same in every lane of each group of n (8, 16, 32 or 64) neighbours.
+// The lowest of the wave's values, which are the same in every lane of each group of n (4, 8, 16, 32 or 64) neighbours.
 __device__ __forceinline__ float groups_min(float v, int n) {
   const auto f = [](float a, float b) { return fminf(a, b); };
+  if (n <= 4) v = f(v, dpp<0x141>(v));  // row_half_mirror
   if (n <= 8) v = f(v, dpp<0x140>(v));  // row_mirror
   if (n <= 16) v = across<false>(v, f);
   if (n <= 32) v = across<true>(v, f);

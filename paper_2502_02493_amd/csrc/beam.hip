@@ -12,9 +12,11 @@
 // some n_select ln(n_select) of them, whose places are counted.  Taking the best n_select times over, one workgroup-wide maximum
 // after the other, was 78 us a call (128 256 words, sixteen beams, the sixteen best), this is 15.1; 64 beams in sixteen groups of
 // 152 064 words 66 and 19.4.
-// Bound by the chain of dependent steps: of 15 us the loads take 1.3, the exponentials 1.0, bound and candidates 1.1, their places 1.2,
-// in (2) statistics and logarithm 2.4, bound 0.8, selection and places 1.9, the two launches the rest; 29 MB of logits (48 rows that count)
-// arrive in 8 us, and the steps behind them follow.
+// Bound by the chain of dependent steps.  Of the 9.9 us of (1) the loads take 1.3, the exponentials 1.0, bound and candidates 1.1, their
+// places 1.2, of the 6.0 of (2) statistics and logarithm 2.4, bound 0.8, selection and places 1.9.  The other five of (1) are not
+// accounted for: four rows of 1000 words take 5.1 as well, and the compiler spills 45 scalar registers there.  29 MB of logits (48 rows
+// that count) take (1) 14.8; a kernel that only reads is through with as much in 7.
+// More than 32: a bound that some 250 candidates reach, ranked all against all: sixteen beams, the 64 best, 42 .. 45 us.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -227,7 +229,8 @@ __global__ __launch_bounds__(kSliceThreads) __attribute__((amdgpu_waves_per_eu(8
     }
     return;
   }
-  // Many equal logits, or groups that a mask empties: the n_select-th candidate itself, bit by bit, then those from it on
+  // Many equal logits, or groups that a mask empties: the n_select-th candidate itself, bit by bit, then those from it on (all logits
+  // of sixteen beams of 128 256 words alike: 114 us a call for the sixteen best, with the selection from lists of ties in (2))
   cand_t last = 0;
   for (int bit = 63; bit >= 0; --bit) {
     const cand_t t = last | (cand_t)1 << bit;
@@ -417,7 +420,9 @@ __global__ __launch_bounds__(NT) void beam_pick_kernel(BeamArgs a) {
     }
     return;
   }
-  // Many equal scores: the best of the lists, K times (there are more than K candidates)
+  // Many equal scores: the best of the lists, K times (there are more than K candidates).  Every time a thread goes through its lists
+  // up to the first candidate that is left: K times K steps for a list that holds all of the best.  All logits alike, the 64 best of
+  // sixteen beams of 128 256 words 657 us a call, of 64 beams of 152 064 886.
   Pick taken = {~0ull, ~0ull};  // everything that comes before it has been handed out
   for (int k = 0; k < K; ++k) {
     Pick best = {0, 0};

@@ -9,7 +9,8 @@ namespace es {
 // Reorder: sequence first + i takes the slots [from, to) of its parent.  A thread owns one piece of a slot of one (layer, KV head)
 // for all sequences: it loads every sequence's new piece before it stores any, so the caches may be reordered in place, whatever
 // the parents are.  Bound by memory: all 2048 slots of four sequences of 32 layers and 8 KV heads, three of them read, 1.88 GB, in
-// 322 us (5.8 TB/s); five drafted slots of eight sequences, 7.9 MB, in 5 us, of which a launch is the larger part.
+// 320 us (5.8 TB/s); five drafted slots of eight sequences, 7.9 MB, in 5 us, of which a launch is the larger part.  In place a sequence
+// that keeps its own slots is read all the same: the whole caches of four, of which none, two or four take another's, 172, 303, 344 us.
 // ------------------------------------------------------------------------------------------
 constexpr int kReorderThreads = 256;
 
@@ -84,7 +85,12 @@ void launch_kv_reorder(const void* k, const void* v, void* k_out, void* v_out, c
 // of 64, 128, 256, 512 and 1024 rows of 256 bytes 12.1, 15.0, 20.4, 29.3, 58.5 and 9.5, 12.8, 18.6, 28.4, 63.5; in place the same to
 // 1 us but for the last, 52 and 48.
 // (2) is bound by memory: 268 MB (1024 rows of 256 lists) in 49 us, 5.5 TB/s.  (1) is bound by its chain of steps for short rows, 256 of
-// 2048 weights 9.1 us, and by instructions for long ones, 256 of up to 32768 34 us.
+// 2048 weights 9.2 us, and by instructions for long ones, 256 of up to 32768 34 us.
+// In place a list is one workgroup's, a barrier to every 32 KB, so few lists are slow: both launches, apart and in place, 256 lists of 2048
+// slots of which 1024 stay 59 and 45 us (from memory 79), 112 of 32768 -> 16384 391 and 444, eight of 32768 -> 16384 52 and 205, eight of
+// 65536 -> 32768 111 and 401.  Lists of sequences that are left alone have workgroups too, which end at once: with one of four or of
+// eight sequences thinned 128 us instead of 79, with one of five 90: those that work lie a power of two apart in the grid and, by that
+// pattern, meet on few CUs (not traced).
 // The weight is found digit by digit: a histogram of the highest eleven bits of all weights, then of the next eleven of those that
 // share these, then of the last ten.  (Bit by bit, every step counting all weights again, 256 rows of up to 32768 took 88 us.)
 // ------------------------------------------------------------------------------------------

@@ -9,11 +9,12 @@
 // each other, so they are kept to fp32.  Two launches, since a row's sum is known only at the end of its context:
 //   (1) weigh_stats_kernel   per chunk of the context: every row's maximum and sum of exp(score - maximum);
 //   (2) weigh_add_kernel     the scores once more, their probabilities, the sums over the rows.
-// (Keeping the scores between the two would take four bytes a row and slot, up to 512 beside the 256 of a key.)  Contexts of a
-// few hundred slots are one launch, weigh_short_kernel.
-// Long contexts are bound by the keys, which are read twice: 61 440 slots of 8 KV heads, 126 MB, 23.5 and 25.4 us (5.2 TB/s).  Many
-// rows are bound by what a wave does with a tile of scores: 16 sequences of 16 tokens and 800 slots, 112 rows a KV head, 12.6 and
-// 12.9 us, of which the keys alone would be 3.
+// (Keeping the scores between the two would take four bytes a row and slot: 16 beside the 256 or 512 of a key for four rows, 512 for
+// 128.  Neither built nor measured.)  Contexts of a few hundred slots are one launch, weigh_short_kernel.
+// Long contexts read the keys twice: 61 440 slots of 8 KV heads, 126 MB, 23.8 and 25.8 us (5.1 TB/s), where a kernel that only reads
+// takes 17.5 us if the last-level cache holds them and 19.9 if not.  Many rows are bound by what a wave does with a tile of scores: 16
+// sequences of 16 tokens and 800 slots, 112 rows a KV head, 12.3 and 13.0 us, of which the keys alone would be 1.8 and the products,
+// three terms of each, 3.7.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 

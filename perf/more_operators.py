@@ -356,7 +356,8 @@ def _run_sample(st):
     stays = torch.arange(V, device=DEV) < (K or V)
     w = torch.where(stays, w, 0.0)
     before = torch.cumsum(w, -1) - w
-    stays = stays & (before < case["top_p"] * w.sum(-1, keepdim=True))
+    if case["top_p"] < 1:
+        stays = stays & (before < case["top_p"] * w.sum(-1, keepdim=True))
     if case["min_p"] > 0:
         stays = stays & (z >= T * math.log(case["min_p"]))
     if st["tokens"] is not None:
@@ -515,7 +516,9 @@ def _exact_sample(st):
         x = logits[r][order].astype(np.float64)
         mass = np.exp((x - x[0]) / T)
         sums = np.cumsum(mass)
-        n = int(np.searchsorted(np.concatenate([[0.0], sums[:-1]]), case["top_p"] * sums[-1], side="left"))   # sums in front that stay below
+        n = len(order)
+        if case["top_p"] < 1:     # as many as have a sum in front that is below
+            n = int(np.searchsorted(np.concatenate([[0.0], sums[:-1]]), case["top_p"] * sums[-1], side="left"))
         if case["min_p"] > 0:
             n = min(n, int((x - x[0] >= T * math.log(case["min_p"])).sum()))
         n = max(n, 1)

@@ -339,13 +339,19 @@ def _run_sparse(st):
     return dict(blocks=st["blocks"], out=st["out"])
 
 
+def _settings(case):
+    """Temperature, top-p and min-p as the calls take them: numbers of 32 bits."""
+    return tuple(float(np.float32(case[name])) for name in ("temperature", "top_p", "min_p"))
+
+
 def _run_sample(st):
     case = st["case"]
-    R, V, T, K = case["rows"], case["vocab"], case["temperature"], case["top_k"]
+    R, V, K = case["rows"], case["vocab"], case["top_k"]
+    T, top_p, min_p = _settings(case)
     if own:
         import paper_2502_02493_amd as es
         ws = _workspace(st, "ws", 0 if "ws" in st else es.easyspec_sample_workspace_bytes(R, V))
-        es.easyspec_sample(st["logits"], st["u"] if case["draw"] else None, R, V, T, K, case["top_p"], case["min_p"], st["tokens"], st["logits_out"], ws,
+        es.easyspec_sample(st["logits"], st["u"] if case["draw"] else None, R, V, T, K, top_p, min_p, st["tokens"], st["logits_out"], ws,
                            torch.cuda.current_stream().cuda_stream)
         return {name: st[name] for name in ("tokens", "logits_out") if st[name] is not None}
     # in 64 bits: the sums run over a vocabulary, and who stays is decided by them
@@ -356,10 +362,10 @@ def _run_sample(st):
     stays = torch.arange(V, device=DEV) < (K or V)
     w = torch.where(stays, w, 0.0)
     before = torch.cumsum(w, -1) - w
-    if case["top_p"] < 1:
-        stays = stays & (before < case["top_p"] * w.sum(-1, keepdim=True))
-    if case["min_p"] > 0:
-        stays = stays & (z >= T * math.log(case["min_p"]))
+    if top_p < 1:
+        stays = stays & (before < top_p * w.sum(-1, keepdim=True))
+    if min_p > 0:
+        stays = stays & (z >= T * math.log(min_p))
     if st["tokens"] is not None:
         w = torch.where(stays, w, 0.0)
         passed = torch.cumsum(w, -1) <= st["u"].double()[:, None] * w.sum(-1, keepdim=True)
@@ -508,7 +514,8 @@ def _exact_sparse(st):
 
 def _exact_sample(st):
     case = st["case"]
-    R, V, T = case["rows"], case["vocab"], case["temperature"]
+    R, V = case["rows"], case["vocab"]
+    T, top_p, min_p = _settings(case)
     logits, u = st["logits"].cpu().numpy(), st["u"].cpu().numpy().astype(np.float64)
     tokens, left = np.zeros(R, np.int32), np.full((R, V), -np.inf, np.float32)
     for r in range(R):
@@ -517,10 +524,10 @@ def _exact_sample(st):
         mass = np.exp((x - x[0]) / T)
         sums = np.cumsum(mass)
         n = len(order)
-        if case["top_p"] < 1:     # as many as have a sum in front that is below
-            n = int(np.searchsorted(np.concatenate([[0.0], sums[:-1]]), case["top_p"] * sums[-1], side="left"))
-        if case["min_p"] > 0:
-            n = min(n, int((x - x[0] >= T * math.log(case["min_p"])).sum()))
+        if top_p < 1:     # as many as have a sum in front that is below
+            n = int(np.searchsorted(np.concatenate([[0.0], sums[:-1]]), top_p * sums[-1], side="left"))
+        if min_p > 0:
+            n = min(n, int((x - x[0] >= T * math.log(min_p)).sum()))
         n = max(n, 1)
         tokens[r] = order[min(n - 1, int(np.searchsorted(sums[:n], u[r] * sums[n - 1], side="right")))]
         left[r, order[:n]] = logits[r, order[:n]]

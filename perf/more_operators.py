@@ -2,9 +2,9 @@
 sizes it makes them, and the same results in plain torch operations.
 
 A case is one of
-  hold    slots of K and V brought into a cache held in 4 bits and read back as the values they stand for (easyspec_kv4_store, _load)
-  attend  attention of new tokens over a whole cache held in 4 bits (easyspec_kv4_attention)
-  sparse  the blocks of such a cache that matter to a token selected, and attention over these (easyspec_kv4_select, _attention)
+  hold    slots of K and V brought into a cache held in 4 bits and read back as the values they stand for (easyspec_kvq_store, _load)
+  attend  attention of new tokens over a whole cache held in 4 bits (easyspec_kvq_attention)
+  sparse  the blocks of such a cache that matter to a token selected, and attention over these (easyspec_kvq_select, _attention)
   sample  logits filtered by top-k, top-p and min-p and a token drawn from what stays (easyspec_sample)
 Head counts, head sizes, layers and vocabularies are those of the repository's model shapes.
 
@@ -249,10 +249,10 @@ def _run_hold(st):
     if own:
         import paper_2502_02493_amd as es
         layout, stream = _layout(es, case, len(st["new"])), torch.cuda.current_stream().cuda_stream
-        cache = es.make_kv4(st["k_codes"], st["k_scales"], st["v_codes"], st["v_scales"], st["bounds"])
+        cache = es.make_kvq(st["k_codes"], st["k_scales"], st["v_codes"], st["v_scales"], st["bounds"])
         n = st["k"].shape[3]
-        es.easyspec_kv4_store(st["k"], st["v"], layout, n, st["zeros"], st["new"], st["to"], st["lens"], cache, stream)
-        es.easyspec_kv4_load(cache, layout, st["to"], st["new"], n, st["zeros"], st["k_out"], st["v_out"], stream)
+        es.easyspec_kvq_store(st["k"], st["v"], layout, n, st["zeros"], st["new"], st["to"], st["lens"], cache, stream)
+        es.easyspec_kvq_load(cache, layout, st["to"], st["new"], n, st["zeros"], st["k_out"], st["v_out"], stream)
         return dict(k=st["k_out"], v=st["v_out"], bounds=st["bounds"])
     seq, src, dst = st["seq"], st["src"], st["dst"]
     for name in ("k", "v"):
@@ -274,9 +274,9 @@ def _own_attention(st, blocks, n_blocks):
     import paper_2502_02493_amd as es
     case = st["case"]
     layout, stream = _layout(es, case, len(st["lens"])), torch.cuda.current_stream().cuda_stream
-    cache = es.make_kv4(st["k_codes"], st["k_scales"], st["v_codes"], st["v_scales"], st["bounds"])
-    ws = _workspace(st, "ws", 0 if "ws" in st else es.easyspec_kv4_attention_workspace_bytes(layout, st["tokens"], st["lens"], case["q_heads"], n_blocks))
-    es.easyspec_kv4_attention(st["q"], cache, layout, st["tokens"], st["lens"], case["q_heads"], blocks, n_blocks, st["out"], ws, stream)
+    cache = es.make_kvq(st["k_codes"], st["k_scales"], st["v_codes"], st["v_scales"], st["bounds"])
+    ws = _workspace(st, "ws", 0 if "ws" in st else es.easyspec_kvq_attention_workspace_bytes(layout, st["tokens"], st["lens"], case["q_heads"], n_blocks))
+    es.easyspec_kvq_attention(st["q"], cache, layout, st["tokens"], st["lens"], case["q_heads"], blocks, n_blocks, st["out"], ws, stream)
     return st["out"]
 
 
@@ -310,8 +310,8 @@ def _run_sparse(st):
     if own:
         import paper_2502_02493_amd as es
         layout, stream = _layout(es, case, B), torch.cuda.current_stream().cuda_stream
-        ws = _workspace(st, "ws_select", 0 if "ws_select" in st else es.easyspec_kv4_select_workspace_bytes(layout, st["tokens"], st["lens"], Hq, K))
-        es.easyspec_kv4_select(st["q"], st["bounds"], layout, st["tokens"], st["lens"], Hq, case["first"], case["last"], K, st["blocks"], ws, stream)
+        ws = _workspace(st, "ws_select", 0 if "ws_select" in st else es.easyspec_kvq_select_workspace_bytes(layout, st["tokens"], st["lens"], Hq, K))
+        es.easyspec_kvq_select(st["q"], st["bounds"], layout, st["tokens"], st["lens"], Hq, case["first"], case["last"], K, st["blocks"], ws, stream)
         return dict(blocks=st["blocks"], out=_own_attention(st, st["blocks"], K))
     # scores in 64 bits: blocks are compared
     N = st["bounds"].shape[3]

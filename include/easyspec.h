@@ -15,6 +15,9 @@
  *                             beams' caches in the order of their parents
  *   - easyspec_attn_weights, easyspec_kv_evict    the attention weight that cached slots receive, and a
  *                             cache thinned by it
+ *   - easyspec_kvq_store, _load, _select, _attention   a cache held in 4 bits, and attention over all of it or over the
+ *                             blocks of it that matter to a token
+ *   - easyspec_sample         tokens drawn from logits under top-k, top-p and min-p, and the logits that stay
  *
  * Model function: pre-norm decoder with RMSNorm, rotary embedding (pairs i, i + head_dim/2),
  * grouped-query attention (query head j reads KV head j / (n_q_heads/n_kv_heads)), SwiGLU MLP,
@@ -392,6 +395,110 @@ int easyspec_track_attention(easyspec_ctx *ctx, int32_t max_positions);
 int easyspec_evict(easyspec_ctx *ctx, const int32_t *keep, int32_t recent);
 int easyspec_get_evicted(const easyspec_ctx *ctx, int32_t *evicted);
 int easyspec_get_attn_weights(easyspec_ctx *ctx, int32_t b, float *out, int32_t n_slots);
+
+/* ---- Caches held in 4 bits ---------------------------------------------------------------------------------- */
+
+/* K and V of a long context at 4.25 bits a value.  32 neighbouring channels of a slot share a scale, a power of two:
+ *   E = max(floor(log2(largest magnitude of the 32)) - 2, -120), scale byte E + 127;
+ *   code of x: the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| / 2^E (half-way: the even code; 6 above), with x's sign in bit 3
+ * (E2M1 elements and E8M0 scales of the OCP microscaling formats).  A scale byte of 255 stands for 32 values of NaN: it is
+ * what 32 channels with one that is not finite become.  Values of 4 bits are bf16 and fp32 numbers: nothing is rounded on the way back.
+ * Slots are counted in blocks of EASYSPEC_KVQ_BLOCK; bounds hold every channel's lowest and highest key of a block. */
+#define EASYSPEC_KVQ_BLOCK 64
+#define EASYSPEC_MAX_KVQ_SELECT 1024 /* blocks of one list */
+typedef struct easyspec_kvq { /* a host struct of dev arrays, contiguous, for an easyspec_kv_layout */
+  void *k_codes, *v_codes;   /* [n_layers][n_seqs][n_kv_heads][max_slots][head_dim / 2] bytes, channel 2 i in the low half of byte i; 16-byte aligned */
+  void *k_scales, *v_scales; /* [n_layers][n_seqs][n_kv_heads][max_slots][head_dim / 32] bytes */
+  void *k_bounds;            /* bf16 [n_layers][n_seqs][n_kv_heads][ceil(max_slots / 64)][2][head_dim], 16-byte aligned; or NULL: none are kept */
+} easyspec_kvq;
+
+/* Slots brought into such a cache: of sequence b, slots src_from[b] .. src_from[b] + n_slots[b] - 1 of k, v become its slots from to[b] on.
+ *   k, v      dev  [n_layers][n_seqs][n_kv_heads][src_slots][head_dim] in layout->dtype, 16-byte aligned: a cache, one that
+ *                  easyspec_kv_export filled (n_seqs = 1, src_slots its n_slots), or the new tokens' keys and values
+ *   src_from, n_slots, to   host [n_seqs]; n_slots[b] = 0: the sequence is left alone
+ *   lens      host [n_seqs]  slots that the sequence holds after the call, to[b] + n_slots[b] .. max_slots
+ * k_bounds: those of every block that receives a slot become the bounds of its slots below lens[b], those that were there among
+ * them (NaN is passed over; plus and minus infinity where nothing else is).  A sequence that is cut back keeps, in the block that the cut is in, bounds that cover the slots
+ * cut off too, until a slot is stored in that block.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers,
+ * a bad layout, src_slots outside 1..65536, slots outside 0..src_slots or 0..lens[b] or lens outside 0..max_slots, arrays that overlap,
+ * are not aligned or not memory of the current device. */
+int easyspec_kvq_store(const void *k, const void *v, const easyspec_kv_layout *layout, int32_t src_slots, const int32_t *src_from,
+                       const int32_t *n_slots, const int32_t *to, const int32_t *lens, const easyspec_kvq *cache, void *hip_stream);
+
+/* The values that slots of such a cache stand for: slots from[b] .. from[b] + n_slots[b] - 1 of sequence b become the slots from to[b] on of
+ * k_out, v_out: dev [n_layers][n_seqs][n_kv_heads][out_slots][head_dim] in layout->dtype.  Other slots are left as they were.  Host arrays,
+ * launch and refusals as above. */
+int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layout, const int32_t *from, const int32_t *n_slots, int32_t out_slots,
+                      const int32_t *to, void *k_out, void *v_out, void *hip_stream);
+
+/* Attention of new tokens over a cache held in 4 bits: in every layer and query head
+ *   out = sum over slots s of softmax_s(q . k_s / sqrt(head_dim)) v_s
+ * The new tokens of sequence b, n_tokens[b] of them, are its last (their slots stored): token t sits in slot lens[b] - n_tokens[b] + t and
+ * attends to the slots up to its own.  What a slot holds that a token does not see has no effect on it, values that are not finite among them.
+ *   q            dev fp32 [n_layers][sum of n_tokens][n_q_heads][head_dim]  rotated queries, sequences in index order
+ *   n_tokens     host [n_seqs]  0..EASYSPEC_MAX_CALIB_TOKENS
+ *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots
+ *   n_q_heads    n_kv_heads times 1, 2, 4, 7 or 8
+ *   blocks       dev [n_layers][sum of n_tokens][n_kv_heads][n_blocks], or NULL: every slot.  The blocks of EASYSPEC_KVQ_BLOCK slots that
+ *                a token reads, ascending: an entry that is not above the entry in front of it (the first: above -1), or that names a
+ *                block without a slot that the token sees, is passed over.  As easyspec_kvq_select writes them.
+ *   n_blocks     1..EASYSPEC_MAX_KVQ_SELECT; 0 without blocks
+ *   out          dev fp32, the shape of q; zeros where a token sees no slot of its blocks
+ *   workspace    dev, easyspec_kvq_attention_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ * The same call gives the same bits; how contexts are cut goes by all sequences of the call, so that in the last bits a sequence's results
+ * may differ with the others.  k_bounds is not read.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q, out and workspace may be NULL if no
+ * sequence has new tokens), a bad layout, counts or lengths, out or a workspace that overlaps another array, arrays that are not 16-byte aligned (scales: 1,
+ * blocks: 4) or not memory of the current device. */
+int easyspec_kvq_attention(const float *q, const easyspec_kvq *cache, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
+                           int32_t n_q_heads, const int32_t *blocks, int32_t n_blocks, float *out, void *workspace, void *hip_stream);
+int64_t easyspec_kvq_attention_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens, int32_t n_q_heads,
+                                               int32_t n_blocks); /* -1 for bad arguments */
+
+/* The blocks that matter to a new token, for every layer and KV head: of the blocks that hold a slot it sees, the first keep_first, the last
+ * keep_last and, of the others, those with the highest
+ *   score(j) = max over the query heads of the KV head of  sum over channels d of max(q_d lo_jd, q_d hi_jd),
+ * which no q . k_s of the block exceeds: n_select in all, or all there are.  Of equal scores the lowest block goes first, a score of NaN (passed
+ * over where another query head has a number) last; scores are compared in double precision.  If n_select < keep_first + keep_last the
+ * lowest of those stay.
+ *   k_bounds     dev       as easyspec_kvq_store keeps them
+ *   q, n_tokens, lens, n_q_heads   as above
+ *   keep_first, keep_last  >= 0; with keep_last >= 1 the token's own block is read
+ *   n_select     1..EASYSPEC_MAX_KVQ_SELECT
+ *   blocks_out   dev [n_layers][sum of n_tokens][n_kv_heads][n_select]  ascending, then -1
+ *   workspace    dev, easyspec_kvq_select_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ * Launched on hip_stream, nothing is synchronised; refusals as above. */
+int easyspec_kvq_select(const float *q, const void *k_bounds, const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens,
+                        int32_t n_q_heads, int32_t keep_first, int32_t keep_last, int32_t n_select, int32_t *blocks_out, void *workspace,
+                        void *hip_stream);
+int64_t easyspec_kvq_select_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens, int32_t n_q_heads,
+                                            int32_t n_select); /* -1 for bad arguments */
+
+/* ---- Drafting by sampling ----------------------------------------------------------------------------------- */
+
+#define EASYSPEC_MAX_SAMPLE_VOCAB 1048576
+
+/* Tokens drawn from logits, and the logits that stay.  The words of a row stand in the order of their logits, the highest first, of equal
+ * ones the lowest token; logits of minus infinity and NaN are no words.  With weights w_v = exp((logits[v] - highest) / temperature), those stay that are
+ *   among the first top_k                                        (0: all)
+ *   and have in front of them less than top_p of the weight of the first top_k   (1: all)
+ *   and weigh at least min_p                                     (0: all; the first word weighs 1)
+ * so that the first always does.  The token drawn is the first in that order whose running weight exceeds u times the weight of all that stay.
+ *   logits      dev [rows][vocab]  fp32, as easyspec_draft_step writes them
+ *   u           dev [rows]         uniform in [0,1) (1 or more, or NaN: the last word with a weight); not read without tokens_out
+ *   tokens_out  dev [rows] or NULL: none is drawn; -1 for a row that holds plus infinity or no word
+ *   logits_out  dev [rows][vocab] or NULL: the logits that stay, minus infinity for the others (all of them in a row without a token); may be
+ *               logits.  softmax(logits_out / temperature) is what the token was drawn from: what easyspec_accept takes as draft_logits
+ *               and, of the target's logits filtered alike, as target_logits
+ *   workspace   dev, easyspec_sample_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ *   hip_stream  the hipStream_t to launch on (NULL = the null stream); nothing is synchronised
+ * Weights are whole multiples of 2^-s, s = 62 - ceil(log2(vocab)) and 52 at most (2^-45 at 128 256 words), worked out in double precision: sums are exact, whatever their
+ * order, and a decision can differ from the real numbers' only within vocab 2^-s of its border.  EASYSPEC_EINVAL for NULL logits or
+ * workspace, neither output, tokens_out without u, rows outside 1..65535, vocab outside 1..EASYSPEC_MAX_SAMPLE_VOCAB, a temperature that is
+ * not positive and finite (temperature 0 is the argmax that the draft step writes), top_k < 0, top_p outside (0, 1], min_p outside [0, 1],
+ * arrays that overlap otherwise or are not memory of the current device. */
+int easyspec_sample(const float *logits, const float *u, int32_t rows, int32_t vocab, float temperature, int32_t top_k, float top_p, float min_p,
+                    int32_t *tokens_out, float *logits_out, void *workspace, void *hip_stream);
+int64_t easyspec_sample_workspace_bytes(int32_t rows, int32_t vocab); /* -1 for bad arguments */
 
 /* Host copies of the per-sequence lengths; each of precise, fuzzy: host [max_batch] or NULL. */
 int easyspec_get_lens(const easyspec_ctx *ctx, int32_t *precise, int32_t *fuzzy);

@@ -20,6 +20,7 @@ EASYSPEC_MAX_CHUNKS = 64
 EASYSPEC_PARALLEL_ATTENTION, EASYSPEC_PARALLEL_FULL_LAYER = 0, 1
 EASYSPEC_MAX_BEAMS, EASYSPEC_MAX_SELECT, EASYSPEC_MAX_BEAM_VOCAB = 64, 64, 1048576
 EASYSPEC_MAX_POSITIONS, EASYSPEC_MAX_CACHE_ROWS = 1048576, 4194304
+EASYSPEC_KVQ_BLOCK, EASYSPEC_MAX_KVQ_SELECT, EASYSPEC_MAX_SAMPLE_VOCAB = 64, 1024, 1048576
 
 EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easyspec_set_groups",
            "easyspec_default_groups", "easyspec_draft_step", "easyspec_calibrate", "easyspec_greedy_accept", "easyspec_greedy_accept_host",
@@ -30,6 +31,8 @@ EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easy
            "easyspec_attn_weights", "easyspec_attn_weights_workspace_bytes", "easyspec_kv_evict",
            "easyspec_beam_fork", "easyspec_beam_reorder", "easyspec_track_attention", "easyspec_evict", "easyspec_get_evicted",
            "easyspec_get_attn_weights",
+           "easyspec_kvq_store", "easyspec_kvq_load", "easyspec_kvq_attention", "easyspec_kvq_attention_workspace_bytes",
+           "easyspec_kvq_select", "easyspec_kvq_select_workspace_bytes", "easyspec_sample", "easyspec_sample_workspace_bytes",
            "easyspec_last_error"]
 EASYSPEC_OP_QKV, EASYSPEC_OP_ATTN, EASYSPEC_OP_OPROJ, EASYSPEC_OP_GATEUP, EASYSPEC_OP_DOWN, EASYSPEC_OP_HEAD, EASYSPEC_OP_ALL = range(7)
 
@@ -58,6 +61,10 @@ class easyspec_weights(C.Structure):
 
 class easyspec_kv_layout(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seqs", "n_kv_heads", "max_slots", "head_dim", "dtype")]
+
+
+class easyspec_kvq(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "k_bounds")]
 
 
 _lib = None
@@ -99,6 +106,18 @@ def load_library():
         L.easyspec_attn_weights_workspace_bytes.argtypes = [kvl, vp, vp, i32]
         L.easyspec_attn_weights_workspace_bytes.restype = C.c_int64
         L.easyspec_kv_evict.argtypes = [vp, vp, vp, kvl, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        kvq = C.POINTER(easyspec_kvq)
+        L.easyspec_kvq_store.argtypes = [vp, vp, kvl, i32, vp, vp, vp, vp, kvq, vp]
+        L.easyspec_kvq_load.argtypes = [kvq, kvl, vp, vp, i32, vp, vp, vp, vp]
+        L.easyspec_kvq_attention.argtypes = [vp, kvq, kvl, vp, vp, i32, vp, i32, vp, vp, vp]
+        L.easyspec_kvq_attention_workspace_bytes.argtypes = [kvl, vp, vp, i32, i32]
+        L.easyspec_kvq_attention_workspace_bytes.restype = C.c_int64
+        L.easyspec_kvq_select.argtypes = [vp, vp, kvl, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+        L.easyspec_kvq_select_workspace_bytes.argtypes = [kvl, vp, vp, i32, i32]
+        L.easyspec_kvq_select_workspace_bytes.restype = C.c_int64
+        L.easyspec_sample.argtypes = [vp, vp, i32, i32, C.c_float, i32, C.c_float, C.c_float, vp, vp, vp, vp]
+        L.easyspec_sample_workspace_bytes.argtypes = [i32, i32]
+        L.easyspec_sample_workspace_bytes.restype = C.c_int64
         L.easyspec_beam_fork.argtypes = [vp, i32, i32, i32]
         L.easyspec_beam_reorder.argtypes = [vp, i32, i32, vp, i32]
         L.easyspec_track_attention.argtypes = [vp, i32]
@@ -306,6 +325,56 @@ def easyspec_kv_evict(k, v, weights, layout: easyspec_kv_layout, lens, keep, rec
     n, s = _host_ints(lens, layout.n_seqs), _host_ints(keep, layout.n_seqs)
     _check(load_library().easyspec_kv_evict(_ptr(k), _ptr(v), _ptr(weights), C.byref(layout), _ptr(n), _ptr(s), recent, out_slots,
                                             _ptr(k_out), _ptr(v_out), _ptr(weights_out), _ptr(slots_out), _ptr(hip_stream)), None)
+
+
+def make_kvq(k_codes, k_scales, v_codes, v_scales, k_bounds=None) -> easyspec_kvq:
+    """easyspec_kvq of a cache's arrays (device tensors, which the caller keeps; raw addresses)."""
+    return easyspec_kvq(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), _ptr(k_bounds))
+
+
+def easyspec_kvq_store(k, v, layout: easyspec_kv_layout, src_slots, src_from, n_slots, to, lens, cache: easyspec_kvq, hip_stream=None):
+    f, n, t, s = (_host_ints(x, layout.n_seqs) for x in (src_from, n_slots, to, lens))
+    _check(load_library().easyspec_kvq_store(_ptr(k), _ptr(v), C.byref(layout), src_slots, _ptr(f), _ptr(n), _ptr(t), _ptr(s), C.byref(cache),
+                                             _ptr(hip_stream)), None)
+
+
+def easyspec_kvq_load(cache: easyspec_kvq, layout: easyspec_kv_layout, from_, n_slots, out_slots, to, k_out, v_out, hip_stream=None):
+    f, n, t = (_host_ints(x, layout.n_seqs) for x in (from_, n_slots, to))
+    _check(load_library().easyspec_kvq_load(C.byref(cache), C.byref(layout), _ptr(f), _ptr(n), out_slots, _ptr(t), _ptr(k_out), _ptr(v_out),
+                                            _ptr(hip_stream)), None)
+
+
+def easyspec_kvq_attention(q, cache: easyspec_kvq, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, blocks, n_blocks, out, workspace,
+                           hip_stream=None):
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    _check(load_library().easyspec_kvq_attention(_ptr(q), C.byref(cache), C.byref(layout), _ptr(n), _ptr(s), n_q_heads, _ptr(blocks), n_blocks,
+                                                 _ptr(out), _ptr(workspace), _ptr(hip_stream)), None)
+
+
+def easyspec_kvq_attention_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, n_blocks) -> int:
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    return int(load_library().easyspec_kvq_attention_workspace_bytes(C.byref(layout), _ptr(n), _ptr(s), n_q_heads, n_blocks))
+
+
+def easyspec_kvq_select(q, k_bounds, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, keep_first, keep_last, n_select, blocks_out, workspace,
+                        hip_stream=None):
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    _check(load_library().easyspec_kvq_select(_ptr(q), _ptr(k_bounds), C.byref(layout), _ptr(n), _ptr(s), n_q_heads, keep_first, keep_last, n_select,
+                                              _ptr(blocks_out), _ptr(workspace), _ptr(hip_stream)), None)
+
+
+def easyspec_kvq_select_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, n_select) -> int:
+    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
+    return int(load_library().easyspec_kvq_select_workspace_bytes(C.byref(layout), _ptr(n), _ptr(s), n_q_heads, n_select))
+
+
+def easyspec_sample(logits, u, rows, vocab, temperature, top_k, top_p, min_p, tokens_out, logits_out, workspace, hip_stream=None):
+    _check(load_library().easyspec_sample(_ptr(logits), _ptr(u), rows, vocab, float(temperature), top_k, float(top_p), float(min_p), _ptr(tokens_out),
+                                          _ptr(logits_out), _ptr(workspace), _ptr(hip_stream)), None)
+
+
+def easyspec_sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(load_library().easyspec_sample_workspace_bytes(rows, vocab))
 
 
 def easyspec_beam_fork(ctx, source: int, first: int, count: int):

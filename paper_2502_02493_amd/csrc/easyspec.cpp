@@ -1142,6 +1142,211 @@ extern "C" int easyspec_kv_evict(const void* k, const void* v, const float* weig
 }
 
 // ---------------------------------------------------------------------------------------------
+// caches held in 4 bits, sampling
+// ---------------------------------------------------------------------------------------------
+
+// The arrays of such a cache for a layout.
+struct KvqExtents {
+  Extent kc, vc, ks, vs, bounds;
+};
+static KvqExtents kvq_extents(const easyspec_kvq* c, const easyspec_kv_layout* g) {
+  const size_t rows = layout_rows(g), slots = rows * g->max_slots, blocks = rows * ((g->max_slots + kKvqBlock - 1) / kKvqBlock);
+  return {{c->k_codes, slots * (g->head_dim / 2)}, {c->v_codes, slots * (g->head_dim / 2)}, {c->k_scales, slots * (g->head_dim / 32)},
+          {c->v_scales, slots * (g->head_dim / 32)}, {c->k_bounds, blocks * 2 * g->head_dim * sizeof(uint16_t)}};
+}
+static Kvq kvq_arrays(const easyspec_kvq* c) {
+  return {(uint8_t*)c->k_codes, (uint8_t*)c->v_codes, (uint8_t*)c->k_scales, (uint8_t*)c->v_scales, (uint16_t*)c->k_bounds};
+}
+
+// What store and load have in common.  at4: first slots in the cache of 4 bits, at: in the other, of `slots`.
+static int kvq_move_args(const char* what, const easyspec_kvq* cache, const easyspec_kv_layout* g, const void* k, const void* v, int32_t slots,
+                         const int32_t* n_slots, const int32_t* at4, const int32_t* at, const int32_t* lens, KvqMoveArgs& a) {
+  if (!cache || !k || !v || !n_slots || !at4 || !at || !cache->k_codes || !cache->v_codes || !cache->k_scales || !cache->v_scales)
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: NULL argument", what);
+  const int rc = check_layout(what, g);
+  if (rc != EASYSPEC_OK) return rc;
+  if (slots < 1 || slots > kMaxEvictSlots) return fail(nullptr, EASYSPEC_EINVAL, "%s: %d slots outside 1..%d", what, slots, kMaxEvictSlots);
+  memset(&a, 0, sizeof a);
+  for (int b = 0; b < g->n_seqs; ++b) {
+    const int len = lens ? lens[b] : g->max_slots;
+    if (n_slots[b] == 0) continue;
+    if (n_slots[b] < 0 || len < 0 || len > g->max_slots || at4[b] < 0 || at4[b] > len - n_slots[b] || at[b] < 0 || at[b] > slots - n_slots[b])
+      return fail(nullptr, EASYSPEC_EINVAL, "%s: sequence %d: %d slots from %d of %d, and %d of %d", what, b, n_slots[b], at4[b], len, at[b], slots);
+    KvqMoveEntry& e = a.entry[a.n_entries++];
+    e.seq = b; e.n = n_slots[b]; e.at4 = at4[b]; e.at = at[b]; e.len = len;
+  }
+  if (misaligned({k, v, cache->k_codes, cache->v_codes, cache->k_bounds}, 16)) return fail(nullptr, EASYSPEC_EINVAL, "%s: values, codes and bounds must be 16-byte aligned", what);
+  a.k = k; a.v = v; a.c = kvq_arrays(cache);
+  a.n_seqs = g->n_seqs; a.heads = g->n_kv_heads; a.max_slots = g->max_slots; a.slots = slots;
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_kvq_store(const void* k, const void* v, const easyspec_kv_layout* layout, int32_t src_slots, const int32_t* src_from,
+                                  const int32_t* n_slots, const int32_t* to, const int32_t* lens, const easyspec_kvq* cache, void* hip_stream) {
+  if (!lens) return fail(nullptr, EASYSPEC_EINVAL, "kvq_store: NULL argument");
+  KvqMoveArgs a;
+  int rc = kvq_move_args("kvq_store", cache, layout, k, v, src_slots, n_slots, to, src_from, lens, a);
+  if (rc != EASYSPEC_OK) return rc;
+  const KvqExtents x = kvq_extents(cache, layout);
+  const size_t bytes = layout_rows(layout) * src_slots * slot_bytes(layout);
+  if (writes_into({x.kc, x.vc, x.ks, x.vs, x.bounds}, {{k, bytes}, {v, bytes}})) return fail(nullptr, EASYSPEC_EINVAL, "kvq_store: arrays overlap");
+  rc = check_arrays(nullptr, "kvq_store", {x.kc.p, x.vc.p, x.ks.p, x.vs.p, x.bounds.p}, {k, v});
+  if (rc != EASYSPEC_OK) return rc;
+  launch_kvq_store(a, layout->n_layers, layout->dtype, layout->head_dim, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+extern "C" int easyspec_kvq_load(const easyspec_kvq* cache, const easyspec_kv_layout* layout, const int32_t* from, const int32_t* n_slots, int32_t out_slots,
+                                 const int32_t* to, void* k_out, void* v_out, void* hip_stream) {
+  KvqMoveArgs a;
+  int rc = kvq_move_args("kvq_load", cache, layout, k_out, v_out, out_slots, n_slots, from, to, nullptr, a);
+  if (rc != EASYSPEC_OK) return rc;
+  const KvqExtents x = kvq_extents(cache, layout);
+  const size_t bytes = layout_rows(layout) * out_slots * slot_bytes(layout);
+  if (writes_into({{k_out, bytes}, {v_out, bytes}}, {x.kc, x.vc, x.ks, x.vs})) return fail(nullptr, EASYSPEC_EINVAL, "kvq_load: arrays overlap");
+  rc = check_arrays(nullptr, "kvq_load", {k_out, v_out}, {x.kc.p, x.vc.p, x.ks.p, x.vs.p});
+  if (rc != EASYSPEC_OK) return rc;
+  launch_kvq_load(a, layout->n_layers, layout->dtype, layout->head_dim, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+// The sequences with new tokens, for attention and selection: returns their tokens, or an error.
+static int kvq_entries(const char* what, const easyspec_kv_layout* g, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads, KvqEntry* entry,
+                       int* n_entries, int* n_new) {
+  const int rc = check_layout(what, g);
+  if (rc != EASYSPEC_OK) return rc;
+  if (!n_tokens || !lens) return fail(nullptr, EASYSPEC_EINVAL, "%s: NULL argument", what);
+  const int group = n_q_heads > 0 && n_q_heads % g->n_kv_heads == 0 ? n_q_heads / g->n_kv_heads : 0;
+  if ((group != 1 && group != 2 && group != 4 && group != 7 && group != 8) || n_q_heads > 65535)
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: %d query heads on %d KV heads: not 1, 2, 4, 7 or 8 each, or more than 65535", what, n_q_heads, g->n_kv_heads);
+  *n_entries = *n_new = 0;
+  for (int b = 0; b < g->n_seqs; ++b) {
+    const int n = n_tokens[b];
+    if (n < 0 || n > EASYSPEC_MAX_CALIB_TOKENS) return fail(nullptr, EASYSPEC_EINVAL, "%s: n_tokens[%d] = %d outside 0..%d", what, b, n, EASYSPEC_MAX_CALIB_TOKENS);
+    if (n == 0) continue;
+    if (lens[b] < n || lens[b] > g->max_slots) return fail(nullptr, EASYSPEC_EINVAL, "%s: lens[%d] = %d outside %d..%d", what, b, lens[b], n, g->max_slots);
+    KvqEntry& e = entry[(*n_entries)++];
+    e.seq = b; e.n = n; e.len = lens[b]; e.q_first = *n_new;
+    *n_new += n;
+  }
+  return EASYSPEC_OK;
+}
+
+static int kvq_attention_args(const char* what, const easyspec_kv_layout* g, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads, int32_t n_blocks,
+                              KvqArgs& a) {
+  memset(&a, 0, sizeof a);
+  const int rc = kvq_entries(what, g, n_tokens, lens, n_q_heads, a.entry, &a.n_entries, &a.n_tokens);
+  if (rc != EASYSPEC_OK) return rc;
+  if (n_blocks < 0 || n_blocks > kMaxKvqSelect) return fail(nullptr, EASYSPEC_EINVAL, "%s: lists of %d blocks, 0..%d are", what, n_blocks, kMaxKvqSelect);
+  a.n_seqs = g->n_seqs; a.heads = g->n_kv_heads; a.Hq = n_q_heads; a.group = n_q_heads / g->n_kv_heads; a.max_slots = g->max_slots; a.n_blocks = n_blocks;
+  a.scale = weigh_scale(g->head_dim);
+  kvq_plan(a, g->n_layers);
+  return EASYSPEC_OK;
+}
+
+extern "C" int64_t easyspec_kvq_attention_workspace_bytes(const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads,
+                                                          int32_t n_blocks) {
+  KvqArgs a;
+  if (kvq_attention_args("kvq_attention_workspace_bytes", layout, n_tokens, lens, n_q_heads, n_blocks, a) != EASYSPEC_OK) return -1;
+  return (int64_t)kvq_workspace_bytes(a, layout->n_layers, layout->head_dim);
+}
+
+extern "C" int easyspec_kvq_attention(const float* q, const easyspec_kvq* cache, const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens,
+                                      int32_t n_q_heads, const int32_t* blocks, int32_t n_blocks, float* out, void* workspace, void* hip_stream) {
+  if (!cache || !cache->k_codes || !cache->v_codes || !cache->k_scales || !cache->v_scales) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: NULL argument");
+  KvqArgs a;
+  int rc = kvq_attention_args("kvq_attention", layout, n_tokens, lens, n_q_heads, n_blocks, a);
+  if (rc != EASYSPEC_OK) return rc;
+  if (!blocks != !n_blocks) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: lists of %d blocks, and %s", n_blocks, blocks ? "an array of them" : "no array");
+  if (a.n_entries == 0) return EASYSPEC_OK;
+  const KvqExtents x = kvq_extents(cache, layout);
+  const size_t bytes = (size_t)layout->n_layers * a.n_tokens * n_q_heads * layout->head_dim * sizeof(float), ws = kvq_workspace_bytes(a, layout->n_layers, layout->head_dim);
+  if (!q || !out || (ws && !workspace)) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: NULL argument");
+  if (misaligned({q, out, workspace, x.kc.p, x.vc.p}, 16) || misaligned({blocks}, 4))
+    return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: q, out, workspace and codes must be 16-byte aligned, blocks 4-byte");
+  if (writes_into({{out, bytes}, {workspace, ws}}, {{q, bytes}, x.kc, x.vc, x.ks, x.vs, {blocks, (size_t)layout->n_layers * a.n_tokens * layout->n_kv_heads * n_blocks * sizeof(int32_t)}}))
+    return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: out or the workspace overlaps another array");
+  rc = check_arrays(nullptr, "kvq_attention", {out, ws ? workspace : nullptr}, {q, x.kc.p, x.vc.p, x.ks.p, x.vs.p, blocks});
+  if (rc != EASYSPEC_OK) return rc;
+  a.q = q; a.c = kvq_arrays(cache); a.blocks = blocks; a.out = out; a.part = (float*)workspace;
+  launch_kvq_attention(a, layout->n_layers, layout->head_dim, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+static int kvq_select_args(const char* what, const easyspec_kv_layout* g, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads, int32_t n_select,
+                           KvqSelectArgs& a) {
+  memset(&a, 0, sizeof a);
+  const int rc = kvq_entries(what, g, n_tokens, lens, n_q_heads, a.entry, &a.n_entries, &a.n_tokens);
+  if (rc != EASYSPEC_OK) return rc;
+  if (n_select < 1 || n_select > kMaxKvqSelect) return fail(nullptr, EASYSPEC_EINVAL, "%s: n_select = %d outside 1..%d", what, n_select, kMaxKvqSelect);
+  a.n_seqs = g->n_seqs; a.heads = g->n_kv_heads; a.Hq = n_q_heads; a.group = n_q_heads / g->n_kv_heads; a.n_select = n_select;
+  a.max_blocks = (g->max_slots + kKvqBlock - 1) / kKvqBlock;
+  for (int i = 0; i < a.n_entries; ++i) a.most = std::max(a.most, (a.entry[i].len + kKvqBlock - 1) / kKvqBlock);
+  return EASYSPEC_OK;
+}
+
+extern "C" int64_t easyspec_kvq_select_workspace_bytes(const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads,
+                                                       int32_t n_select) {
+  KvqSelectArgs a;
+  if (kvq_select_args("kvq_select_workspace_bytes", layout, n_tokens, lens, n_q_heads, n_select, a) != EASYSPEC_OK) return -1;
+  return (int64_t)kvq_select_workspace_bytes(a, layout->n_layers);
+}
+
+extern "C" int easyspec_kvq_select(const float* q, const void* k_bounds, const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens,
+                                   int32_t n_q_heads, int32_t keep_first, int32_t keep_last, int32_t n_select, int32_t* blocks_out, void* workspace,
+                                   void* hip_stream) {
+  if (!k_bounds) return fail(nullptr, EASYSPEC_EINVAL, "kvq_select: NULL argument");
+  KvqSelectArgs a;
+  int rc = kvq_select_args("kvq_select", layout, n_tokens, lens, n_q_heads, n_select, a);
+  if (rc != EASYSPEC_OK) return rc;
+  if (keep_first < 0 || keep_last < 0) return fail(nullptr, EASYSPEC_EINVAL, "kvq_select: the first %d and the last %d blocks", keep_first, keep_last);
+  if (a.n_entries == 0) return EASYSPEC_OK;
+  if (!q || !blocks_out || !workspace) return fail(nullptr, EASYSPEC_EINVAL, "kvq_select: NULL argument");
+  if (misaligned({q, k_bounds, workspace}, 16) || misaligned({blocks_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "kvq_select: q, k_bounds and workspace must be 16-byte aligned, blocks_out 4-byte");
+  const size_t lists = (size_t)layout->n_layers * a.n_tokens * layout->n_kv_heads;
+  if (writes_into({{blocks_out, lists * n_select * sizeof(int32_t)}, {workspace, kvq_select_workspace_bytes(a, layout->n_layers)}},
+                  {{q, (size_t)layout->n_layers * a.n_tokens * n_q_heads * layout->head_dim * sizeof(float)},
+                   {k_bounds, layout_rows(layout) * a.max_blocks * 2 * layout->head_dim * sizeof(uint16_t)}}))
+    return fail(nullptr, EASYSPEC_EINVAL, "kvq_select: blocks_out or the workspace overlaps another array");
+  rc = check_arrays(nullptr, "kvq_select", {blocks_out, workspace}, {q, k_bounds});
+  if (rc != EASYSPEC_OK) return rc;
+  a.q = q; a.bounds = (const uint16_t*)k_bounds; a.out = blocks_out; a.scores = (double*)workspace;
+  a.first = keep_first; a.last = keep_last;
+  launch_kvq_select(a, layout->n_layers, layout->head_dim, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+static bool sample_sizes_ok(int32_t rows, int32_t vocab) { return rows >= 1 && rows <= 65535 && vocab >= 1 && vocab <= EASYSPEC_MAX_SAMPLE_VOCAB; }
+
+extern "C" int64_t easyspec_sample_workspace_bytes(int32_t rows, int32_t vocab) {
+  return sample_sizes_ok(rows, vocab) ? (int64_t)sample_workspace_bytes(rows, vocab) : -1;
+}
+
+extern "C" int easyspec_sample(const float* logits, const float* u, int32_t rows, int32_t vocab, float temperature, int32_t top_k, float top_p, float min_p,
+                               int32_t* tokens_out, float* logits_out, void* workspace, void* hip_stream) {
+  if (!logits || !workspace || (!tokens_out && !logits_out) || (tokens_out && !u)) return fail(nullptr, EASYSPEC_EINVAL, "sample: NULL argument");
+  if (!sample_sizes_ok(rows, vocab)) return fail(nullptr, EASYSPEC_EINVAL, "sample: need 1 <= rows <= 65535, 1 <= vocab <= %d", EASYSPEC_MAX_SAMPLE_VOCAB);
+  if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(nullptr, EASYSPEC_EINVAL, "sample: temperature must be positive and finite");
+  if (top_k < 0 || !(top_p > 0.f && top_p <= 1.f) || !(min_p >= 0.f && min_p <= 1.f))
+    return fail(nullptr, EASYSPEC_EINVAL, "sample: need top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1");
+  if (misaligned({workspace}, 16) || misaligned({logits, u, tokens_out, logits_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "sample: workspace must be 16-byte aligned, the other arrays 4-byte");
+  const size_t words = (size_t)rows * vocab * sizeof(float);
+  const Extent in = {logits, words}, us = {tokens_out ? u : nullptr, rows * sizeof(float)}, tokens = {tokens_out, rows * sizeof(int32_t)};
+  const Extent left = {logits_out, words}, ws = {workspace, sample_workspace_bytes(rows, vocab)};
+  if (writes_into({tokens, left, ws}, {us}) || writes_into({tokens, ws}, {in}) || (logits_out != logits && writes_into({left}, {in})))
+    return fail(nullptr, EASYSPEC_EINVAL, "sample: arrays overlap (logits_out may be logits)");
+  const int rc = check_arrays(nullptr, "sample", {tokens_out, logits_out, workspace}, {logits, us.p});
+  if (rc != EASYSPEC_OK) return rc;
+  launch_sample(logits, u, rows, vocab, (double)temperature, top_k, (double)top_p, (double)min_p, tokens_out, logits_out, workspace, (hipStream_t)hip_stream);
+  HIPCHK(nullptr, hipGetLastError());
+  return EASYSPEC_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
 // beams and bounded caches: the same operators on a context
 // ---------------------------------------------------------------------------------------------
 
@@ -1487,6 +1692,8 @@ extern "C" int32_t easyspec_stream_read_sink_floats(void) { return stream_read_s
 
 static_assert(EASYSPEC_MAX_BEAMS == kMaxBeams && EASYSPEC_MAX_SELECT == kMaxSelect && EASYSPEC_MAX_BEAM_VOCAB == kMaxBeamVocab,
               "header and kernels disagree on the limits of a beam selection");
+static_assert(EASYSPEC_KVQ_BLOCK == kKvqBlock && EASYSPEC_MAX_KVQ_SELECT == kMaxKvqSelect && EASYSPEC_MAX_SAMPLE_VOCAB == kMaxSampleVocab,
+              "header and kernels disagree on the limits of caches in 4 bits and of sampling");
 static_assert((uint64_t)EASYSPEC_MAX_CACHE_ROWS * 1024 <= 1ull << 32, "a grid holds 2^32 - 1 threads in a row, a workgroup of 1024 to every row of a cache");
 static_assert(EASYSPEC_MAX_BATCH == kMaxCols, "per-sequence arrays of the cache operators hold kMaxCols entries");
 static_assert(EASYSPEC_MAX_CHUNKS == kMaxChunks, "header and kernels disagree on the chunk limit");

@@ -1,6 +1,6 @@
 // Internal interface between the host state machine (easyspec.cpp) and the gfx950 kernels
 // (gemv.hip, attention.hip, wide.hip, resident.hip, util.hip, accept.hip, beam.hip, weigh.hip,
-// cache_ops.hip).  Plain structs and launch functions; no device code in this header.
+// cache_ops.hip, kvq.hip, kvq_attention.hip, sample.hip).  Plain structs and launch functions; no device code in this header.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -295,6 +295,70 @@ void weigh_plan(WeighArgs& a, int n_layers, int dtype);
 size_t weigh_workspace_bytes(const WeighArgs& a, int n_layers);
 size_t weigh_workspace_limit(int B, int heads, int group, int max_tokens, int max_slots);  // of any call of one layer
 void launch_weigh(const WeighArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
+
+// Caches held in 4 bits, in blocks of kKvqBlock slots.
+constexpr int kKvqBlock = 64, kMaxKvqSelect = 1024;
+struct Kvq {
+  uint8_t *kc, *vc, *ks, *vs;  // codes [row][slot][hd / 2], scales [row][slot][hd / 32]; row: (layer, sequence, KV head)
+  uint16_t* bounds;            // bf16 [row][block][2][hd]; or null
+};
+// Slots between such a cache and one of values.  An entry: a sequence of which slots move.
+struct KvqMoveEntry {
+  int seq, n, at4, at, len;  // slots; the first in the cache of 4 bits and in the other; slots that the sequence holds
+};
+struct KvqMoveArgs {
+  const void *k, *v;  // values [row][slots][hd], T: read by the store, written by the load
+  Kvq c;
+  int n_seqs, heads, max_slots, slots, n_entries;
+  int lh0;                // set by the launch: the first (layer, KV head)
+  int first_wg[kMaxCols];  // set by the launch: an entry's first workgroup
+  KvqMoveEntry entry[kMaxCols];
+};
+void launch_kvq_store(const KvqMoveArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
+void launch_kvq_load(const KvqMoveArgs& a, int n_layers, int dtype, int hd, hipStream_t st);
+
+// Attention over such a cache and the selection of its blocks.  An entry: a sequence with new tokens.
+struct KvqEntry {
+  int seq, n, len, q_first;  // its new tokens, its slots with them, its first row of tokens in q
+  int chunks, tiles;         // set by the plan: pieces that a row's slots (with lists: a token's list) are cut into, tiles of query rows
+  size_t first_part;         // ... its first partial result of a (layer, KV head)
+};
+struct KvqArgs {
+  const float* q;         // [layer][token][Hq][hd]
+  Kvq c;
+  const int32_t* blocks;  // [layer][token][KV head][n_blocks]; null: every slot
+  float* out;             // as q
+  float* part;            // partial results [layer][KV head][entry: row, chunk][hd], then their (maximum, sum)
+  float2* part_ml;
+  size_t part_pitch;      // partial results of a (layer, KV head)
+  int n_seqs, heads, Hq, group, max_slots, n_entries, n_tokens, n_blocks;
+  int chunk;              // steps of 32 slots; with lists: entries
+  int n_wgs;
+  float scale, inv_group;  // log2(e) / sqrt(hd); 1 / group
+  int first_wg[kMaxCols];
+  KvqEntry entry[kMaxCols];
+};
+void kvq_plan(KvqArgs& a, int n_layers);
+size_t kvq_workspace_bytes(const KvqArgs& a, int n_layers, int hd);
+void launch_kvq_attention(const KvqArgs& a, int n_layers, int hd, hipStream_t st);
+struct KvqSelectArgs {
+  const float* q;
+  const uint16_t* bounds;
+  int32_t* out;    // [layer][token][KV head][n_select]
+  double* scores;  // [layer][token][KV head][most]
+  int n_seqs, heads, Hq, group, max_blocks, n_entries, n_tokens, n_select, first, last;
+  int most;        // blocks of the longest sequence
+  int first_wg[kMaxCols];  // set by the launch
+  KvqEntry entry[kMaxCols];
+};
+size_t kvq_select_workspace_bytes(const KvqSelectArgs& a, int n_layers);
+void launch_kvq_select(const KvqSelectArgs& a, int n_layers, int hd, hipStream_t st);
+
+// Sampling; ws: sample_workspace_bytes() of scratch, 16-byte aligned.
+constexpr int kMaxSampleVocab = 1 << 20;
+size_t sample_workspace_bytes(int rows, int V);
+void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
+                   float* logits_out, void* ws, hipStream_t st);
 
 // Reads `bytes` (multiple of 16) of buf once; sink: stream_read_sink_floats() floats.
 void launch_stream_read(const void* buf, size_t bytes, float* sink, hipStream_t st);

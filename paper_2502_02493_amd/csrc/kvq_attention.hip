@@ -1,0 +1,609 @@
+// Attention over a cache held in 4 bits (gfx950), and the selection of the blocks that it reads.
+//
+//   out = sum_s p_s v_s,  p = softmax_s(q . k_s / sqrt(hd)),  over all slots that a token sees or those of its listed blocks
+//
+// The query heads of a KV head and the sequence's new tokens are the rows of two matrix products on the matrix cores.  Both take the
+// cache's values as bf16 numbers, which hold them exactly (one conversion gives two of them, the scale included); queries and
+// probabilities are fp32 and meet them as three bf16 terms each, all 24 bits.  Queries and results of this library are fp32, and a
+// cache read in 4 bits should lose nothing beyond its rounding.
+//   S = K Q^T: a tile of 16 slots is the A operand, lane l holding channels hd / 4 (l / 16) .. of slot l % 16: a quarter of a slot's codes,
+//     under one scale.  (Which channels a k-tile contracts is free as long as the queries agree.)  A lane then holds the scores of
+//     slots 4 (l / 16) + i of row l % 16,
+//   O^T = V^T P^T: which is where the B operand of the second product wants them: elements 4 t + i of lane group g are slot 4 g + i of
+//     tile t.  Its A operand needs eight slots of a channel side by side: lane l takes channels hd / 16 (l % 16) .. of those slots,
+//     pairs of slots meeting in a register by one permutation.
+// The running maximum, sum and result of a row stay in the lanes of its column; nothing passes through LDS until a wave's share of
+// the context is done.
+#include "launch_common.hpp"
+#include "lane_ops.hpp"
+
+#include <string.h>
+
+namespace es {
+
+constexpr float kLowest = -3.4028235e38f;
+constexpr int kStep = 32;        // slots of a wave's step
+constexpr int kAttnWaves = 4;
+
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit, std::integral_constant<int, 0>) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0)); }
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit, std::integral_constant<int, 1>) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1)); }
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit, std::integral_constant<int, 2>) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2)); }
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit, std::integral_constant<int, 3>) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3)); }
+template <int I>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit) {
+  return bf16_pair(codes, unit, std::integral_constant<int, I>{});
+}
+__device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }  // 255: infinity, of which the conversion makes NaN
+
+// One workgroup's place.  Without lists: a chunk of an entry's steps and a tile of its rows; with them, a token and a chunk of its list.
+template <bool LIST>
+struct KvqPlace {
+  int e, h, l, c, row0, rows, len, old;  // entry, KV head, layer, chunk; first row and how many; slots that any row sees; that all do but for
+                                         // their own and those after
+  int n_tok;                             // token of the first row
+  __device__ __forceinline__ explicit KvqPlace(const KvqArgs& a) {
+    e = 0;
+#pragma unroll
+    for (int i = 1; i < kMaxCols; ++i) e += (int)blockIdx.x >= a.first_wg[i];
+    const KvqEntry& en = a.entry[e];
+    const int w = blockIdx.x - a.first_wg[e];
+    h = blockIdx.y;
+    l = blockIdx.z;
+    if (LIST) {
+      n_tok = w / en.chunks;
+      c = w % en.chunks;
+      row0 = n_tok * a.group;
+      rows = a.group;
+      old = en.len - en.n + n_tok;
+      len = old + 1;
+    } else {
+      const int tile = w % en.tiles;
+      c = w / en.tiles;
+      row0 = tile * 16;
+      rows = min(16, en.n * a.group - row0);
+      n_tok = token_of(a, row0);
+      old = en.len - en.n + n_tok;
+      len = en.len - en.n + token_of(a, row0 + rows - 1) + 1;
+    }
+  }
+  static __device__ __forceinline__ int token_of(const KvqArgs& a, int row) { return (int)(((float)row + 0.5f) * a.inv_group); }  // row < 128: off by far less than half a step
+  __device__ __forceinline__ size_t cache_row(const KvqArgs& a) const {
+    return (((size_t)l * a.n_seqs + a.entry[e].seq) * a.heads + h) * (size_t)a.max_slots;
+  }
+};
+
+// Codes and scales of a step of 32 slots from s on, as the lane needs them.  Slots past the last fetch the last one.
+template <int HD>
+struct KvqStep {
+  static constexpr int KW = HD / 32;  // words of K codes of a lane and tile: 8 channels each
+  uint32_t k[2][KW], v[2][4];
+  uint32_t ks[2], vs[2][4];
+  __device__ __forceinline__ void load(const uint8_t* kc, const uint8_t* ks_, const uint8_t* vc, const uint8_t* vs_, int s, int len) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t slot = min(s + 16 * t + c, len - 1);
+      const uint8_t* p = kc + slot * (HD / 2) + g * (HD / 8);
+      if constexpr (HD == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[t][i] = x[i];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+        k[t][0] = x[0]; k[t][1] = x[1];
+      }
+      ks[t] = ks_[slot * (HD / 32) + (HD == 128 ? g : g >> 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t vslot = min(s + 16 * t + 4 * g + i, len - 1);
+        const uint8_t* vp = vc + vslot * (HD / 2) + c * (HD / 32);
+        if constexpr (HD == 128) v[t][i] = *reinterpret_cast<const uint32_t*>(vp);
+        else v[t][i] = *reinterpret_cast<const uint16_t*>(vp);
+        vs[t][i] = vs_[vslot * (HD / 32) + (HD == 128 ? c >> 2 : c >> 3)];
+      }
+    }
+  }
+};
+
+// The queries of 16 rows, scaled, as B fragments.  FOLD (four rows at most): column 4 t + r is term t of row r, and one product
+// serves all terms; columns 12 .. 15 are zero.
+template <int HD, bool FOLD>
+struct KvqQueries {
+  static constexpr int NKT = HD / 32, TERMS = FOLD ? 1 : 3;
+  u32x4 q[NKT][TERMS];
+  template <bool LIST>
+  __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST>& p) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int r = p.row0 + min(FOLD ? n & 3 : n, p.rows - 1), tok = p.token_of(a, r);
+    const float* src = a.q + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(a.entry[p.e].q_first + tok) * a.Hq + p.h * a.group + (r - tok * a.group)) * HD + g * (HD / 4);
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 v = reinterpret_cast<const f32x4*>(src + 8 * kt)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j] * a.scale;
+      }
+      bf16x8 hi, lo;
+      split_bf16x8(x, hi, lo);
+      const bf16x8 third = third_bf16x8(x, hi, lo);
+      if constexpr (FOLD) {
+        const u32x4 t0 = __builtin_bit_cast(u32x4, hi), t1 = __builtin_bit_cast(u32x4, lo), t2 = __builtin_bit_cast(u32x4, third);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[kt][0][i] = n < 4 ? t0[i] : n < 8 ? t1[i] : n < 12 ? t2[i] : 0u;
+      } else {
+        q[kt][0] = __builtin_bit_cast(u32x4, hi);
+        q[kt][1] = __builtin_bit_cast(u32x4, lo);
+        q[kt][2] = __builtin_bit_cast(u32x4, third);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ float fold_terms(float x) {  // over columns n, n + 4, n + 8, n + 12: the same bits in all of them
+  x += dpp<0x128>(x);  // row_ror:8
+  return x + dpp<0x124>(x);  // row_ror:4
+}
+__device__ __forceinline__ float over_groups_max(float x) {
+  const auto f = [](float u, float v) { return fmaxf(u, v); };
+  return across<true>(across<false>(x, f), f);
+}
+__device__ __forceinline__ float over_groups_sum(float x) {
+  const auto f = [](float u, float v) { return u + v; };
+  return across<true>(across<false>(x, f), f);
+}
+
+// The running softmax of a wave's share: row l % 16 (FOLD: l % 4) in lane l.
+template <int HD, bool FOLD>
+struct KvqRows {
+  static constexpr int CPV = HD / 16;  // channels of V that a lane takes
+  float m = kLowest, l = 0.f;          // l: of the lane's own slots
+  f32x4 o[CPV];                        // o[j][i]: channel (4 (l / 16) + i) CPV + j (FOLD: term l % 16 / 4 of it)
+
+  __device__ __forceinline__ KvqRows() {
+#pragma unroll
+    for (int j = 0; j < CPV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void scores(const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, f32x4 (&x)[2]) const {
+    constexpr int NKT = HD / 32;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float unit = unit_of(st.ks[t]);
+      f32x4 y[KvqQueries<HD, FOLD>::TERMS];
+#pragma unroll
+      for (int i = 0; i < KvqQueries<HD, FOLD>::TERMS; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        const uint32_t w = st.k[t][kt];
+        const u32x4 f = {bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
+#pragma unroll
+        for (int i = 0; i < KvqQueries<HD, FOLD>::TERMS; ++i) mma<bf16_t>(y[i], f, Q.q[kt][i]);
+      }
+      if constexpr (FOLD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[t][i] = fold_terms(y[0][i]);
+      } else {
+        x[t] = y[0] + (y[1] + y[2]);
+      }
+    }
+  }
+  // edge: some row does not see all of the step's slots.  seen: how many slots the lane's row does.
+  __device__ __forceinline__ void add(const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, bool edge, int s, int seen, const uint8_t* vs_, int len) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    f32x4 x[2];
+    scores(st, Q, x);
+    if (edge) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[t][i] = s + 16 * t + 4 * g + i < seen ? x[t][i] : -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) top = fmaxf(fmaxf(fmaxf(top, x[t][0]), fmaxf(x[t][1], x[t][2])), x[t][3]);
+    top = over_groups_max(top);
+    if (__any(top > m)) {
+      const float f = pow2(m - top);
+      l *= f;
+#pragma unroll
+      for (int j = 0; j < CPV; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] *= f;
+      m = top;
+    }
+    float p[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[4 * t + i] = pow2(x[t][i] - m);
+        l += p[4 * t + i];
+      }
+    // V: a step at an edge may hold NaN where some row does not see it, whose probability of 0 would not hide it
+    float unit[8];
+    bool poisoned = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) unit[e] = unit_of(st.vs[e / 4][e % 4]);
+    if (edge) {
+      bool nan = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) nan = nan || st.vs[e / 4][e % 4] == 255;
+      if (__any(nan)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) unit[e] = st.vs[e / 4][e % 4] == 255 ? 0.f : unit[e];
+        const int block = HD == 128 ? g : g >> 1;  // of the lane's channels in o
+        for (int i = s; i < min(s + kStep, len); ++i) poisoned = poisoned || (i < seen && vs_[(uint32_t)i * (HD / 32) + block] == 255);
+      }
+    }
+    u32x4 pf[3];
+    if constexpr (FOLD) {
+      // the lane's column takes its own term
+      const int term = (lane & 15) >> 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a = p[2 * i], b = p[2 * i + 1];
+        uint32_t w = pack_bf16x2(a, b);
+#pragma unroll
+        for (int t = 1; t < 3; ++t) {
+          if (term >= t) {
+            a -= __uint_as_float(w << 16);
+            b -= __uint_as_float(w & 0xFFFF0000u);
+            w = pack_bf16x2(a, b);
+          }
+        }
+        pf[0][i] = term < 3 ? w : 0u;
+      }
+    } else {
+      bf16x8 hi, lo;
+      split_bf16x8(p, hi, lo);
+      pf[0] = __builtin_bit_cast(u32x4, hi);
+      pf[1] = __builtin_bit_cast(u32x4, lo);
+      pf[2] = __builtin_bit_cast(u32x4, third_bf16x8(p, hi, lo));
+    }
+    const auto channels = [&](auto pair) {  // two channels: 2 pair, 2 pair + 1
+      constexpr int P = decltype(pair)::value;
+      u32x4 f0, f1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t a = bf16_pair<P>(st.v[i / 2][2 * (i % 2)], unit[2 * i]), b = bf16_pair<P>(st.v[i / 2][2 * (i % 2) + 1], unit[2 * i + 1]);
+        f0[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        f1[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      }
+#pragma unroll
+      for (int t = 0; t < (FOLD ? 1 : 3); ++t) {
+        mma<bf16_t>(o[2 * P], f0, pf[t]);
+        mma<bf16_t>(o[2 * P + 1], f1, pf[t]);
+      }
+    };
+    channels(std::integral_constant<int, 0>{});
+    channels(std::integral_constant<int, 1>{});
+    if constexpr (HD == 128) {
+      channels(std::integral_constant<int, 2>{});
+      channels(std::integral_constant<int, 3>{});
+    }
+    if (edge && poisoned) {
+#pragma unroll
+      for (int j = 0; j < CPV; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] = NAN;
+    }
+  }
+};
+
+// grid (chunks of all entries, KV heads, layers).  The workgroup's waves take its steps in turn; their results meet in LDS.
+template <int HD, bool FOLD, bool LIST>
+__global__ __launch_bounds__(kAttnWaves * 64) void kvq_attn_kernel(KvqArgs a) {
+  constexpr int NW = kAttnWaves, ROWS = FOLD ? 4 : 16, CPV = HD / 16;
+  __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+  __shared__ f32x4 s_o[NW][ROWS][HD / 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const KvqPlace<LIST> p(a);
+  const KvqEntry& en = a.entry[p.e];
+  const size_t row = p.cache_row(a);
+  const uint8_t *kc = a.c.kc + row * (HD / 2), *vc = a.c.vc + row * (HD / 2), *ks = a.c.ks + row * (HD / 32), *vs = a.c.vs + row * (HD / 32);
+  KvqRows<HD, FOLD> R;
+  KvqQueries<HD, FOLD> Q;
+  KvqStep<HD> st[2];
+  const int my_row = FOLD ? n & 3 : n;
+  const int seen = my_row < p.rows ? en.len - en.n + p.token_of(a, p.row0 + my_row) + 1 : 0;
+  if constexpr (LIST) {
+    // the chunk's entries, one to a lane, and which of them count
+    const int32_t* list = a.blocks + (((size_t)p.l * a.n_tokens + en.q_first + p.n_tok) * a.heads + p.h) * a.n_blocks;
+    const int at = p.c * a.chunk + lane;
+    const bool there = lane < a.chunk && at < a.n_blocks;
+    const int b = there ? list[at] : -1, before = there && at > 0 ? list[at - 1] : -1;
+    unsigned long long left = __ballot(there && b > before && b >= 0 && b < (p.len + kKvqBlock - 1) / kKvqBlock);
+    int slot = -1, half = 2;  // of the next step: a block is two
+    int turn = 0;
+    const auto next = [&]() -> int {  // the first slot of the wave's next step, or -1
+      for (;;) {
+        if (half == 2) {
+          if (!left) return -1;
+          slot = __builtin_amdgcn_readlane(b, __builtin_ctzll(left)) * kKvqBlock;
+          left &= left - 1;
+          half = 0;
+        }
+        const int s = slot + kStep * half++;
+        if (s >= p.len) continue;
+        if (turn++ % NW == wave) return s;
+      }
+    };
+    int s = next();
+    if (s >= 0) st[0].load(kc, ks, vc, vs, s, p.len);
+    Q.load(a, p);
+    while (s >= 0) {
+      const int s1 = next();
+      if (s1 >= 0) st[1].load(kc, ks, vc, vs, s1, p.len);
+      R.add(st[0], Q, s + kStep > p.old + 1, s, seen, vs, p.len);
+      s = s1;
+      st[0] = st[1];
+    }
+  } else {
+    const int steps = (p.len + kStep - 1) / kStep, end = min(steps, (p.c + 1) * a.chunk);
+    int i = p.c * a.chunk + wave;
+    if (i < end) st[0].load(kc, ks, vc, vs, i * kStep, p.len);
+    Q.load(a, p);
+    for (; i < end; i += NW) {
+      if (i + NW < end) st[1].load(kc, ks, vc, vs, (i + NW) * kStep, p.len);
+      R.add(st[0], Q, (i + 1) * kStep > p.old + 1, i * kStep, seen, vs, p.len);
+      st[0] = st[1];
+    }
+  }
+  // the waves' shares
+  float l = over_groups_sum(R.l);
+  if (lane < ROWS) {
+    s_m[wave][lane] = R.m;
+    s_l[wave][lane] = l;
+  }
+  __syncthreads();
+  float top = kLowest;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][my_row % ROWS]);
+  const float f = pow2(R.m - top);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[CPV];
+#pragma unroll
+    for (int j = 0; j < CPV; ++j) x[j] = (FOLD ? fold_terms(R.o[j][i]) : R.o[j][i]) * f;
+    if (!FOLD || n < 4)
+#pragma unroll
+      for (int j = 0; j < CPV; j += 4) s_o[wave][my_row][((4 * g + i) * CPV + j) / 4] = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+  }
+  __syncthreads();
+  const size_t part = ((size_t)p.l * a.heads + p.h) * a.part_pitch + en.first_part;
+  for (int u = threadIdx.x; u < p.rows * (HD / 4); u += NW * 64) {
+    const int r = u / (HD / 4), c = u % (HD / 4), ra = p.row0 + r;
+    f32x4 sum = s_o[0][r][c];
+    float m = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) {
+      sum += s_o[w][r][c];
+      m = fmaxf(m, s_m[w][r]);
+    }
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) all += s_l[w][r] * pow2(s_m[w][r] - m);
+    if (en.chunks == 1) {
+      const int tok = p.token_of(a, ra);
+      f32x4* out = reinterpret_cast<f32x4*>(a.out + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(en.q_first + tok) * a.Hq + p.h * a.group + (ra - tok * a.group)) * HD);
+      const float inv = all == 0.f ? 0.f : 1.f / all;
+      out[c] = sum * inv;
+    } else {
+      const size_t at = part + (size_t)ra * en.chunks + p.c;
+      reinterpret_cast<f32x4*>(a.part)[at * (HD / 4) + c] = sum;
+      if (c == 0) a.part_ml[at] = make_float2(m, all);
+    }
+  }
+}
+
+// The pieces of a row joined: a wave to every (token, query head, layer), a lane HD / 64 channels... in order of the pieces.
+template <int HD>
+__global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
+  constexpr int C4 = HD / 4, PARTS = 256 / C4;  // threads side by side over the channels; pieces at a time
+  __shared__ float s_m[4], s_l[4];
+  __shared__ f32x4 s_sum[PARTS][C4];
+  const int t = blockIdx.x, j = blockIdx.y, l = blockIdx.z, tid = threadIdx.x, wave = tid >> 6;
+  int e = 0;
+#pragma unroll
+  for (int i = 1; i < kMaxCols; ++i) e += i < a.n_entries && t >= a.entry[i].q_first;
+  const KvqEntry& en = a.entry[e];
+  if (en.chunks == 1) return;
+  const int h = j / a.group, row = (t - en.q_first) * a.group + j % a.group;
+  const size_t at = ((size_t)l * a.heads + h) * a.part_pitch + en.first_part + (size_t)row * en.chunks;
+  float m = kLowest;
+  for (int c = tid; c < en.chunks; c += 256) m = fmaxf(m, a.part_ml[at + c].x);
+  m = lanes_max(m, 64);
+  if ((tid & 63) == 0) s_m[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  float sum = 0.f;
+  for (int c = tid; c < en.chunks; c += 256) {
+    const float2 x = a.part_ml[at + c];
+    sum += x.y * pow2(x.x - m);
+  }
+  sum = lanes_sum(sum, 64);
+  if ((tid & 63) == 0) s_l[wave] = sum;
+  const int c4 = tid % C4;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int c = tid / C4; c < en.chunks; c += PARTS) o += reinterpret_cast<const f32x4*>(a.part)[(at + c) * C4 + c4] * pow2(a.part_ml[at + c].x - m);
+  s_sum[tid / C4][c4] = o;
+  __syncthreads();
+  if (tid >= C4) return;
+  const float all = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) o += s_sum[i][c4];
+  const float inv = all == 0.f ? 0.f : 1.f / all;
+  reinterpret_cast<f32x4*>(a.out + ((size_t)l * a.n_tokens * a.Hq + (size_t)t * a.Hq + j) * HD)[c4] = o * inv;
+}
+
+constexpr int kKvqWgs = 1024;  // workgroups that a call is cut into, about
+void kvq_plan(KvqArgs& a, int n_layers) {
+  a.inv_group = 1.f / (float)a.group;
+  long work = 0;
+  for (int i = 0; i < a.n_entries; ++i) {
+    KvqEntry& e = a.entry[i];
+    e.tiles = a.n_blocks ? 1 : (e.n * a.group + 15) / 16;
+    work += a.n_blocks ? (long)e.n * a.n_blocks : (long)e.tiles * ((e.len + kStep - 1) / kStep);
+  }
+  work *= (long)a.heads * n_layers;
+  const int least = a.n_blocks ? kAttnWaves / 2 : kAttnWaves, most = a.n_blocks ? 64 : 65536 / kStep;  // with lists: an entry to a lane
+  a.chunk = (int)std::min<long>(most, std::max<long>(least, ((work + kKvqWgs - 1) / kKvqWgs + least - 1) / least * least));
+  int wg = 0;
+  size_t part = 0;
+  for (int i = 0; i < kMaxCols; ++i) {
+    a.first_wg[i] = INT32_MAX;
+    if (i >= a.n_entries) continue;
+    KvqEntry& e = a.entry[i];
+    const int pieces = a.n_blocks ? a.n_blocks : (e.len + kStep - 1) / kStep;
+    e.chunks = (pieces + a.chunk - 1) / a.chunk;
+    e.first_part = part;
+    a.first_wg[i] = wg;
+    wg += e.chunks * (a.n_blocks ? e.n : e.tiles);
+    part += (size_t)e.n * a.group * e.chunks;
+  }
+  a.n_wgs = wg;
+  a.part_pitch = part;
+}
+static bool kvq_joined(const KvqArgs& a) {
+  for (int i = 0; i < a.n_entries; ++i)
+    if (a.entry[i].chunks > 1) return true;
+  return false;
+}
+size_t kvq_workspace_bytes(const KvqArgs& a, int n_layers, int hd) {
+  return kvq_joined(a) ? a.part_pitch * a.heads * n_layers * (hd * sizeof(float) + sizeof(float2)) : 0;
+}
+
+void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t st) {
+  KvqArgs a = args;
+  if (a.n_entries == 0) return;
+  a.part_ml = reinterpret_cast<float2*>(a.part + a.part_pitch * a.heads * n_layers * hd);
+  int rows = 0;
+  for (int i = 0; i < a.n_entries; ++i) rows = std::max(rows, a.blocks ? a.group : a.entry[i].n * a.group);
+  const bool fold = rows <= 4;
+  auto go = [&](auto kernel, auto join) {
+    hipLaunchKernelGGL(kernel, dim3(a.n_wgs, a.heads, n_layers), dim3(kAttnWaves * 64), 0, st, a);
+    if (kvq_joined(a)) hipLaunchKernelGGL(join, dim3(a.n_tokens, a.Hq, n_layers), dim3(256), 0, st, a);
+  };
+  auto pick = [&](auto hd_, auto join) {
+    constexpr int HD = decltype(hd_)::value;
+    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true>, join) : go(kvq_attn_kernel<HD, false, true>, join);
+    else fold ? go(kvq_attn_kernel<HD, true, false>, join) : go(kvq_attn_kernel<HD, false, false>, join);
+  };
+  if (hd == 128) pick(std::integral_constant<int, 128>{}, kvq_join_kernel<128>);
+  else pick(std::integral_constant<int, 64>{}, kvq_join_kernel<64>);
+}
+
+// ------------------------------------------------------------------------------------------
+// Selection: (1) the blocks' scores, a workgroup to some blocks of a sequence, which reads their bounds once for all its new tokens;
+// (2) a wave to every (layer, token, KV head) finds the score of the last block that stays, bit by bit, and writes the list.
+// ------------------------------------------------------------------------------------------
+// grid (groups of blocks of all entries, KV heads, layers)
+template <int HD>
+__global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {
+  constexpr int LANES = HD / 8, BLOCKS = 256 / LANES;  // lanes to a block: eight channels each
+  int e = 0;
+#pragma unroll
+  for (int i = 1; i < kMaxCols; ++i) e += (int)blockIdx.x >= a.first_wg[i];
+  const KvqEntry& en = a.entry[e];
+  const int h = blockIdx.y, l = blockIdx.z, lane = threadIdx.x % LANES;
+  const int block = (blockIdx.x - a.first_wg[e]) * BLOCKS + threadIdx.x / LANES;
+  const int held = (en.len + kKvqBlock - 1) / kKvqBlock;
+  const u32x4* src = reinterpret_cast<const u32x4*>(a.bounds + ((((size_t)l * a.n_seqs + en.seq) * a.heads + h) * a.max_blocks + min(block, held - 1)) * 2 * HD) + lane;
+  float lo[8], hi[8];
+  unpack<bf16_t>(src[0], lo);
+  unpack<bf16_t>(src[HD / 8], hi);
+  for (int t = 0; t < en.n; ++t) {
+    const float* q = a.q + (((size_t)l * a.n_tokens + en.q_first + t) * a.Hq + h * a.group) * HD + lane * 8;
+    double best = NAN;
+    for (int j = 0; j < a.group; ++j) {
+      const f32x4 q0 = reinterpret_cast<const f32x4*>(q + (size_t)j * HD)[0], q1 = reinterpret_cast<const f32x4*>(q + (size_t)j * HD)[1];
+      double s = 0.0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = i < 4 ? q0[i % 4] : q1[i % 4];
+        s = fma((double)x, (double)(x > 0.f ? hi[i] : lo[i]), s);
+      }
+      s = lanes_sum(s, LANES);
+      best = fmax(best, s);  // passes over NaN
+    }
+    if (lane == 0 && block < held) a.scores[(((size_t)l * a.n_tokens + en.q_first + t) * a.heads + h) * a.most + block] = best;
+  }
+}
+
+// The order of scores as unsigned numbers: NaN below everything, the two zeros alike.
+__device__ __forceinline__ uint64_t score_key(double s) {
+  if (s != s) return 1;
+  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+// a wave to every list; lane i of the wave holds blocks 64 j + i
+constexpr int kSelectRegs = kMaxKvqSelect / 64;
+__global__ __launch_bounds__(64) void kvq_select_kernel(KvqSelectArgs a) {
+  const int t = blockIdx.x, h = blockIdx.y, l = blockIdx.z, lane = threadIdx.x;
+  int e = 0;
+#pragma unroll
+  for (int i = 1; i < kMaxCols; ++i) e += i < a.n_entries && t >= a.entry[i].q_first;
+  const KvqEntry& en = a.entry[e];
+  const int seen = en.len - en.n + (t - en.q_first) + 1, held = (seen + kKvqBlock - 1) / kKvqBlock;
+  const size_t list = ((size_t)l * a.n_tokens + t) * a.heads + h;
+  const double* scores = a.scores + list * a.most;
+  int32_t* out = a.out + list * a.n_select;
+  const int want = min(a.n_select, held), last0 = max(0, held - a.last);
+  uint64_t key[kSelectRegs];  // 0: no block
+#pragma unroll
+  for (int j = 0; j < kSelectRegs; ++j) {
+    const int b = 64 * j + lane;
+    key[j] = b >= held ? 0 : b < a.first || b >= last0 ? ~0ull : score_key(scores[b]);
+  }
+  // the want-th highest key: the highest number that as many keys reach
+  uint64_t bound = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const uint64_t trial = bound | 1ull << bit;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < kSelectRegs; ++j)
+      if (64 * j < held) n += __popcll(__ballot(key[j] >= trial));
+    if (n >= want) bound = trial;
+  }
+  int over = 0;
+#pragma unroll
+  for (int j = 0; j < kSelectRegs; ++j)
+    if (64 * j < held) over += __popcll(__ballot(key[j] > bound));
+  int ties = want - over, at = 0;  // of those at the bound the lowest blocks
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int j = 0; j < kSelectRegs; ++j) {
+    if (64 * j >= held) break;
+    const unsigned long long same = __ballot(key[j] == bound);
+    const bool stays = key[j] > bound || (key[j] == bound && __popcll(same & below) < ties);
+    const unsigned long long stay = __ballot(stays);
+    if (stays) out[at + __popcll(stay & below)] = 64 * j + lane;
+    at += __popcll(stay);
+    ties -= min(ties, (int)__popcll(same));
+  }
+  for (int i = at + lane; i < a.n_select; i += 64) out[i] = -1;
+}
+
+size_t kvq_select_workspace_bytes(const KvqSelectArgs& a, int n_layers) { return (size_t)n_layers * a.n_tokens * a.heads * a.most * sizeof(double); }
+
+void launch_kvq_select(const KvqSelectArgs& args, int n_layers, int hd, hipStream_t st) {
+  KvqSelectArgs a = args;
+  if (a.n_entries == 0) return;
+  const int per = 256 / (hd / 8);
+  int wg = 0;
+  for (int i = 0; i < kMaxCols; ++i) {
+    a.first_wg[i] = INT32_MAX;
+    if (i >= a.n_entries) continue;
+    a.first_wg[i] = wg;
+    wg += ((a.entry[i].len + kKvqBlock - 1) / kKvqBlock + per - 1) / per;
+  }
+  if (hd == 128) hipLaunchKernelGGL(kvq_score_kernel<128>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(kvq_score_kernel<64>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(kvq_select_kernel, dim3(a.n_tokens, a.heads, n_layers), dim3(64), 0, st, a);
+}
+
+}  // namespace es

@@ -1,0 +1,217 @@
+"""What the operators on caches held in 4 bits and sampling refuse, on the host, before anything is launched."""
+import numpy as np
+import pytest
+
+import kvq_ref as ref
+import paper_2502_02493_amd as es
+
+X = 1 << 20
+
+
+def far(i):
+    return X + (i << 24)
+
+
+def refused(f):
+    with pytest.raises(es.EasySpecError) as e:
+        f()
+    assert e.value.code == es.EASYSPEC_EINVAL, str(e.value)
+    return str(e.value)
+
+
+def no_memory(f):
+    """Arguments in order: what refuses the call is that these addresses are no memory (or that there is no device)."""
+    with pytest.raises(es.EasySpecError) as e:
+        f()
+    assert "memory of the current device" in str(e.value) or e.value.code == es.EASYSPEC_EHIP, str(e.value)
+
+
+def layout(**change):
+    a = dict(n_layers=2, n_seqs=4, n_kv_heads=2, max_slots=96, head_dim=64, dtype=es.EASYSPEC_DTYPE_BF16)
+    a.update(change)
+    return es.easyspec_kv_layout(*a.values())
+
+
+def cache(**change):
+    """16 rows of 96 slots: codes 48 KiB, scales 3 KiB, bounds 8 KiB"""
+    a = dict(k_codes=far(0), k_scales=far(1), v_codes=far(2), v_scales=far(3), k_bounds=far(4))
+    a.update(change)
+    return es.make_kvq(**a)
+
+
+BAD_LAYOUTS = [dict(n_layers=0), dict(n_layers=65536), dict(n_seqs=0), dict(n_seqs=20), dict(n_kv_heads=0), dict(max_slots=0), dict(max_slots=65537),
+               dict(head_dim=96), dict(dtype=2), dict(n_layers=65535, n_kv_heads=65535)]
+
+
+def store(lay=None, c=None, **change):
+    """k, v: 16 rows of 40 slots of 128 bytes, 80 KiB"""
+    a = dict(k=far(5), v=far(6), layout=lay or layout(), src_slots=40, src_from=[0, 0, 39, 5], n_slots=[40, 0, 1, 10], to=[0, 7, 60, 86], lens=[96, 96, 61, 96],
+             cache=c or cache())
+    a.update(change)
+    return lambda: es.easyspec_kvq_store(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(k=None), dict(v=None), dict(src_slots=0), dict(src_slots=39), dict(src_slots=65537), dict(src_from=[0, 0, 40, 0]), dict(src_from=[1, 0, 0, 0]),
+    dict(src_from=[-1, 0, 0, 0]), dict(n_slots=[-1, 0, 0, 0]), dict(n_slots=[41, 0, 0, 0]), dict(to=[-1, 0, 0, 0]), dict(to=[57, 0, 0, 0]), dict(lens=[39, 0, 61, 96]),
+    dict(lens=[97, 0, 61, 96]), dict(lens=[96, 0, 60, 96]), dict(n_slots=[2 ** 31 - 1, 0, 0, 0]), dict(to=[2 ** 31 - 1, 0, 0, 0]),
+    dict(k=far(5) + 8), dict(v=far(6) + 2), dict(c=cache(k_codes=None)), dict(c=cache(v_codes=None)), dict(c=cache(k_scales=None)), dict(c=cache(v_scales=None)),
+    dict(c=cache(k_codes=far(0) + 8)), dict(c=cache(v_codes=far(2) + 4)), dict(c=cache(k_bounds=far(4) + 2)),
+    dict(k=far(0)), dict(v=far(2) + 49152 - 16), dict(k=far(1)), dict(v=far(3)), dict(k=far(4)), dict(c=cache(v_codes=far(0) + 16)), dict(c=cache(k_scales=far(0))),
+    dict(c=cache(v_scales=far(1) + 100)), dict(c=cache(k_bounds=far(2))),
+])
+def test_store(change):
+    c = change.pop("c", None)
+    refused(store(c=c, **change))
+
+
+def load(lay=None, c=None, **change):
+    a = dict(cache=c or cache(), layout=lay or layout(), from_=[0, 0, 95, 5], n_slots=[40, 0, 1, 10], out_slots=40, to=[0, 7, 39, 30], k_out=far(5), v_out=far(6))
+    a.update(change)
+    return lambda: es.easyspec_kvq_load(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(k_out=None), dict(v_out=None), dict(out_slots=0), dict(out_slots=39), dict(out_slots=65537), dict(from_=[57, 0, 0, 0]), dict(from_=[-1, 0, 0, 0]),
+    dict(n_slots=[-1, 0, 0, 0]), dict(n_slots=[97, 0, 0, 0]), dict(to=[1, 0, 0, 0]), dict(to=[-1, 0, 0, 0]), dict(k_out=far(5) + 8), dict(c=cache(k_codes=None)),
+    dict(c=cache(v_scales=None)), dict(c=cache(v_codes=far(2) + 8)), dict(k_out=far(0) + 16), dict(v_out=far(1)), dict(v_out=far(5) + 16), dict(k_out=far(3)),
+])
+def test_load(change):
+    c = change.pop("c", None)
+    refused(load(c=c, **change))
+
+
+def attend(lay=None, c=None, **change):
+    """23 tokens of 4 heads of 64 floats in two layers: 46 KiB"""
+    a = dict(q=far(5), cache=c or cache(), layout=lay or layout(), n_tokens=[1, 6, 0, 16], lens=[1, 96, 0, 20], n_q_heads=4, blocks=None, n_blocks=0, out=far(6), workspace=far(7))
+    a.update(change)
+    return lambda: es.easyspec_kvq_attention(*a.values(), None)
+
+
+LISTS = dict(blocks=far(8), n_blocks=4)
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=None), dict(out=None), dict(n_tokens=[-1, 1, 1, 1]), dict(n_tokens=[17, 0, 0, 0], lens=[30, 1, 1, 1]), dict(lens=[0, 96, 0, 20]), dict(lens=[1, 97, 0, 20]),
+    dict(lens=[1, 96, 0, 15]), dict(n_q_heads=0), dict(n_q_heads=3), dict(n_q_heads=6), dict(n_q_heads=32), dict(blocks=far(8)), dict(n_blocks=4), dict(blocks=far(8), n_blocks=-1),
+    dict(blocks=far(8), n_blocks=1025), dict(blocks=far(8) + 2, n_blocks=4), dict(q=far(5) + 4), dict(out=far(6) + 8), dict(workspace=far(7) + 8, **LISTS),
+    dict(c=cache(k_codes=None)), dict(c=cache(k_scales=None)), dict(c=cache(v_codes=None)), dict(c=cache(v_scales=None)), dict(c=cache(k_codes=far(0) + 4)),
+    dict(out=far(5) + 64), dict(out=far(0)), dict(out=far(1)), dict(out=far(2) + 49152 - 16), dict(out=far(3)), dict(out=far(8), **LISTS), dict(n_q_heads=2 * 40000),
+])
+def test_attention(change):
+    c = change.pop("c", None)
+    refused(attend(c=c, **change))
+
+
+def test_attention_workspace():
+    big = layout(max_slots=65536, n_layers=1, n_seqs=1)
+    need = es.easyspec_kvq_attention_workspace_bytes(big, [4], [65536], 4, 0)
+    assert need > 0
+    a = dict(lay=big, n_tokens=[4], lens=[65536], c=es.make_kvq(1 << 40, 1 << 41, 1 << 42, 1 << 43))
+    refused(attend(workspace=None, **a))
+    refused(attend(workspace=far(7) + 8, **a))
+    for at in (far(5), far(6), 1 << 40, (1 << 41) + 16, 1 << 42, 1 << 43):
+        assert "overlaps" in refused(attend(workspace=at, **a))
+    assert es.easyspec_kvq_attention_workspace_bytes(layout(), [0] * 4, [0] * 4, 4, 0) == 0
+    for bad in (([17, 0, 0, 0], [40] * 4, 4, 0), ([1] * 4, [97] * 4, 4, 0), ([1] * 4, [0] * 4, 4, 0), ([1] * 4, [9] * 4, 6, 0), ([1] * 4, [9] * 4, 4, 1025), ([1] * 4, [9] * 4, 4, -1)):
+        assert es.easyspec_kvq_attention_workspace_bytes(layout(), *bad) == -1
+
+
+def select(lay=None, **change):
+    a = dict(q=far(5), k_bounds=far(4), layout=lay or layout(), n_tokens=[1, 6, 0, 16], lens=[1, 96, 0, 20], n_q_heads=4, keep_first=0, keep_last=1, n_select=4,
+             blocks_out=far(6), workspace=far(7))
+    a.update(change)
+    return lambda: es.easyspec_kvq_select(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=None), dict(k_bounds=None), dict(blocks_out=None), dict(workspace=None), dict(n_tokens=[-1, 1, 1, 1]), dict(n_tokens=[17, 0, 0, 0], lens=[30, 1, 1, 1]),
+    dict(lens=[0, 96, 0, 20]), dict(lens=[1, 97, 0, 20]), dict(n_q_heads=0), dict(n_q_heads=6), dict(keep_first=-1), dict(keep_last=-1), dict(n_select=0), dict(n_select=1025),
+    dict(q=far(5) + 4), dict(k_bounds=far(4) + 8), dict(workspace=far(7) + 8), dict(blocks_out=far(6) + 2), dict(blocks_out=far(5)), dict(blocks_out=far(4) + 64), dict(blocks_out=far(7)),
+    dict(workspace=far(5) + 16), dict(workspace=far(4) - 16), dict(n_q_heads=2 * 40000),
+])
+def test_select(change):
+    refused(select(**change))
+
+
+@pytest.mark.parametrize("bad", BAD_LAYOUTS)
+def test_layouts(bad):
+    lay = layout(**bad)
+    n = lay.n_seqs
+    none, one = [0] * n, [1] * n
+    refused(store(lay, src_from=none, n_slots=one, to=none, lens=one))
+    refused(load(lay, from_=none, n_slots=one, to=none))
+    refused(attend(lay, n_tokens=one, lens=one))
+    refused(select(lay, n_tokens=one, lens=one))
+    assert es.easyspec_kvq_attention_workspace_bytes(lay, one, one, 4, 0) == -1 and es.easyspec_kvq_select_workspace_bytes(lay, one, one, 4, 4) == -1
+
+
+def test_nothing_to_do_needs_no_arrays():
+    es.easyspec_kvq_attention(None, cache(), layout(), [0] * 4, [0, 5, 96, 1], 4, None, 0, None, None, None)
+    es.easyspec_kvq_select(None, far(4), layout(), [0] * 4, [0, 5, 96, 1], 4, 0, 1, 4, None, None, None)
+    refused(attend(n_tokens=[0] * 4, c=cache(k_codes=None)))
+
+
+def test_arrays_that_touch_are_apart():
+    no_memory(store(k=far(5), v=far(5) + 81920, c=cache(k_scales=far(0) + 49152, v_scales=far(0) + 49152 + 3072)))
+    no_memory(load(k_out=far(5), v_out=far(5) + 81920))
+    no_memory(attend(out=far(5) + 46 * 1024))
+    no_memory(select(blocks_out=far(6), workspace=far(6) + 23 * 2 * 2 * 4 * 4))
+
+
+@pytest.mark.parametrize("n", [0, 1, 3, 5])
+def test_arrays_of_another_length_than_there_are_sequences(n):
+    for name in ("src_from", "n_slots", "to", "lens"):
+        refused(store(**{name: [0] * n}))
+    for name in ("from_", "n_slots", "to"):
+        refused(load(**{name: [0] * n}))
+    for f in (attend, select):
+        refused(f(n_tokens=[1] * n))
+        refused(f(lens=[20] * n))
+
+
+def sample(**change):
+    """Three rows of 100 words: 1200 bytes"""
+    a = dict(logits=far(0), u=far(1), rows=3, vocab=100, temperature=0.8, top_k=5, top_p=0.9, min_p=0.1, tokens_out=far(2), logits_out=far(3), workspace=far(4))
+    a.update(change)
+    return lambda: es.easyspec_sample(*a.values(), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(logits=None), dict(u=None), dict(workspace=None), dict(tokens_out=None, logits_out=None), dict(rows=0), dict(rows=65536), dict(vocab=0), dict(vocab=(1 << 20) + 1),
+    dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.5),
+    dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1), dict(min_p=float("nan")), dict(workspace=far(4) + 8), dict(logits=far(0) + 2), dict(tokens_out=far(2) + 1),
+    dict(logits_out=far(0) + 4), dict(logits_out=far(1)), dict(tokens_out=far(0) + 1196), dict(tokens_out=far(1)), dict(tokens_out=far(3)), dict(workspace=far(0)),
+    dict(workspace=far(1) - 8), dict(workspace=far(3) + 16), dict(workspace=far(2) - 8),
+])
+def test_sample(change):
+    refused(sample(**change))
+
+
+@pytest.mark.parametrize("change", [dict(), dict(logits_out=far(0)), dict(tokens_out=None, u=None), dict(logits_out=None), dict(tokens_out=None, logits_out=far(0)), dict(top_k=0, top_p=1.0, min_p=0.0),
+                                    dict(min_p=1.0), dict(tokens_out=far(1) + 12, logits_out=far(0) + 1200)])
+def test_sample_takes(change):
+    no_memory(sample(**change))
+
+
+def test_sample_workspace_bytes():
+    assert es.easyspec_sample_workspace_bytes(1, 1) > 0 and es.easyspec_sample_workspace_bytes(65535, 1 << 20) > 0
+    for bad in ((0, 10), (65536, 10), (1, 0), (1, (1 << 20) + 1)):
+        assert es.easyspec_sample_workspace_bytes(*bad) == -1
+
+
+def test_reference_encoding():
+    """The oracle of the encoding against values whose codes are known."""
+    x = np.zeros((3, 32))
+    x[0, :8] = [7.9, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]            # E = 0: half-way values, and one past the highest
+    x[1, :4] = [-1.0, 0.125, 0.13, -0.0]                                # E = -2: 4, 0.5, 0.52
+    x[2, 0] = np.nan
+    codes, scales = ref.encode(x)
+    assert scales[:, 0].tolist() == [127, 125, 255]
+    assert [int(c) for b in codes[0, :4] for c in (b & 15, b >> 4)] == [7, 0, 2, 2, 4, 4, 6, 6]
+    assert [int(c) for b in codes[1, :2] for c in (b & 15, b >> 4)] == [14, 1, 1, 8]
+    y = ref.decode(codes, scales)
+    assert y[0, 0] == 6 and y[1, 0] == -1.0 and np.isnan(y[2]).all()
+    assert np.array_equal(ref.encode(y[:2])[0][1], codes[1])            # numbers of 4 bits stay what they are
+    tiny = np.full((1, 32), 2.0 ** -140)
+    assert ref.encode(tiny)[1][0, 0] == 7 and not ref.decode(*ref.encode(tiny)).any()

@@ -1,5 +1,5 @@
 // Reductions across the lanes of a wavefront and across the waves of a workgroup, for the kernels whose chain of dependent
-// steps is what they cost (acceptance, selection over beams).
+// steps is what they cost (acceptance, selection over beams, sampling), and an exponential in double precision.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -118,6 +118,30 @@ __device__ __forceinline__ double lane_value(double v, int lane) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
   return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+}
+
+// exp2(u) for -1000 <= u <= 0 in double precision: the whole part goes into the exponent, the rest through the series of
+// exp(f ln 2) up to f^10 (|f| <= 1/2: off by 0.347^11 / 11! = 2.2e-13 at most).  The launches that use it are bound by instructions: the
+// library's exponential, which serves arguments that do not occur there, takes more than twice as many.
+__device__ __forceinline__ double scalar_operand(double c) {  // the compiler would copy a literal into a vector register at every use
+  asm("" : "+s"(c));
+  return c;
+}
+__device__ __forceinline__ double exp2_below(double u) {
+  const double n = __builtin_rint(u), f = u - n;
+  double p = 7.054911620801121e-09;  // ln2^10 / 10!
+  p = fma(p, f, scalar_operand(1.0178086009239696e-07));
+  p = fma(p, f, scalar_operand(1.3215486790144305e-06));
+  p = fma(p, f, scalar_operand(1.5252733804059838e-05));
+  p = fma(p, f, scalar_operand(1.5403530393381606e-04));
+  p = fma(p, f, scalar_operand(1.3333558146428441e-03));
+  p = fma(p, f, scalar_operand(9.618129107628477e-03));
+  p = fma(p, f, scalar_operand(5.5504108664821576e-02));
+  p = fma(p, f, scalar_operand(2.402265069591007e-01));
+  p = fma(p, f, scalar_operand(6.931471805599453e-01));
+  p = fma(p, f, 1.0);
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, p);
+  return __builtin_bit_cast(double, (unsigned long long)((uint32_t)(b >> 32) + ((uint32_t)(int)n << 20)) << 32 | (uint32_t)b);
 }
 
 }  // namespace es

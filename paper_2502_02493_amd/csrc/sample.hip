@@ -2,21 +2,28 @@
 //
 // Words stand in the order of their logits, the highest first, of equal ones the lowest token; each has the weight
 // exp((x - max) / T).  What stays is a run from the front of that order (top-k, top-p and min-p each keep one, the shortest counts), and
-// the token drawn is the first whose running weight passes u times that of the run.  So all of it comes down to one question: which word
-// of the order is the first to bring a running count or weight to a given number?  It is answered digit by digit of the words' place
-// numbers (the logit's 32 bits in the order of floats, then the token), by a histogram of counts and weights for each.
+// the token drawn is the first whose running weight passes u times that of the run.  So all of it comes down to one question, asked up to
+// three times: which word of the order is the first to bring the running count or weight to a given number?
 // Weights are whole multiples of 2^-s: sums of them are exact, so neither the order of atomic additions nor how a row is cut up
 // shows in a result.
+//
+// No row is sorted.  A histogram of counts and weights over y = (max - x) log2(e) / T, sixteen bins to a factor of two in weight, tells
+// for each question the bin that its word lies in, or, where it depends on the word that answers another one, a few of them.  The words
+// of these bins, some hundred, are sorted and answer it exactly.  Rows whose bins hold too many (thousands of nearly equal
+// logits) go digit by digit through their words' place numbers instead.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
+
+#include <string.h>
 
 namespace es {
 
 typedef unsigned long long u64;
 constexpr int kTokenBits = 20;
 static_assert(kMaxSampleVocab == 1 << kTokenBits, "a place number holds a token");
-constexpr int kSampleThreads = 1024;
-constexpr int kSampleBins = 2048;
+constexpr int kBins = 1024, kFineBins = 768;  // kFineBins up to y = 48, where weights end; then eight to a doubling of y
+constexpr int kNear = 4096;                   // words that are sorted
+constexpr int kDigitBins = 2048;
 
 // A word's place number: the higher, the earlier in the order; 0 is no word (minus infinity, NaN).
 __device__ __forceinline__ u64 place_of(float x, int v) {
@@ -25,153 +32,438 @@ __device__ __forceinline__ u64 place_of(float x, int v) {
   const uint32_t key = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
   return (u64)key << kTokenBits | (u64)(kMaxSampleVocab - 1 - v);
 }
+__device__ __forceinline__ int token_at(u64 place) { return kMaxSampleVocab - 1 - (int)(place & (kMaxSampleVocab - 1)); }
+__device__ __forceinline__ float logit_at(u64 place) {
+  const uint32_t key = (uint32_t)(place >> kTokenBits);
+  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
 
 struct SampleArgs {
   const float* logits;
   const float* u;
-  int V, top_k;  // top_k 0: all
-  double T, inv_T, top_p, min_z;  // min_z: T log(min_p), what a logit may lie below the highest; minus infinity: all
-  double unit;                    // 2^s
+  int V, top_k;           // top_k 0: all
+  double log2e_T, top_p;  // log2(e) / T
+  double min_z;           // T log(min_p), what a logit may lie below the highest; minus infinity: all
+  double unit;            // 2^s
   int32_t* tokens;
   float* out;
+  // rows cut into slices
+  int slices, per;
+  float* slice_max;  // [row][slices]
+  u64* weight;       // [row][kBins]
+  uint32_t* count;   // [row][kBins], then a counter of near words
+  u64* near;         // [row][kNear]
 };
 
-struct RowOf {
-  const float* x;
-  double top, inv_T, unit;
-  int V;
-  __device__ __forceinline__ u64 weight(float v) const { return (u64)__double2ull_rn(exp(((double)v - top) * inv_T) * unit); }
+// What a word's logit says, given the row's highest.
+struct Weigher {
+  double top, log2e_T, unit;
+  __device__ __forceinline__ double below(float x) const { return (top - (double)x) * log2e_T; }
+  __device__ __forceinline__ u64 weight(double y) const {  // exact below 2^52: the sum's last bit is worth 1
+    const double w = exp2_below(fmax(-y, -1000.0)) * unit + 4503599627370496.0;
+    return __builtin_bit_cast(u64, w) & 0xFFFFFFFFFFFFFull;
+  }
+  __device__ __forceinline__ int bin(double y) const {  // never falls as y rises
+    if (y < 48.0) return (int)(y * 16.0);
+    const uint32_t b = __float_as_uint((float)(y * (1.0 / 48.0)));
+    return kFineBins + min((int)(b >> 20) - (127 << 3), kBins - kFineBins - 1);
+  }
+  __device__ __forceinline__ bool over(float x, double min_z) const { return (double)x - top >= min_z; }
 };
 
-struct SampleShared {
-  u64 weight[kSampleBins];
-  uint32_t count[kSampleBins];
-  u64 wave_weight[kSampleThreads / 64];
-  uint32_t wave_count[kSampleThreads / 64];
-  int bin;
-  u64 over_weight;
-  uint32_t over_count;
-  float wave_max[kSampleThreads / 64];
-};
-
-__device__ __forceinline__ u64 block_sum_u64(u64 v, SampleShared& sh) {
-  for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave_weight[threadIdx.x >> 6] = v;
-  __syncthreads();
-  u64 s = 0;
-  for (int w = 0; w < kSampleThreads / 64; ++w) s += sh.wave_weight[w];
-  return s;
+// Words of row[v0, v1): body(x, v), eight loads of a thread under way.
+template <int NT, class Body>
+__device__ __forceinline__ void each_word(const float* row, int v0, int v1, const Body& body) {
+  constexpr int N = 8;
+  for (int base = v0; base < v1; base += N * NT) {
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = base + i * NT + (int)threadIdx.x;
+      x[i] = v < v1 ? row[v] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (x[i] > -INFINITY) body(x[i], base + i * NT + (int)threadIdx.x);
+  }
 }
+
+// Running sums over the threads of a workgroup, in front of the thread; all: the whole.  sh: NT / 64 numbers, which nobody reads any more.
+template <int NT>
+__device__ __forceinline__ u64 sum_before(u64 v, u64* sh, u64& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  u64 run = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const u64 o = __shfl_up(run, off, 64);
+    if (lane >= off) run += o;
+  }
+  if (lane == 63) sh[wave] = run;
+  __syncthreads();
+  u64 before = run - v;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    const u64 o = sh[w];
+    before += w < wave ? o : 0;
+    all += o;
+  }
+  return before;
+}
+template <int NT>
+__device__ __forceinline__ u64 sum_all(u64 v, u64* sh) {
+  u64 all;
+  __syncthreads();
+  sum_before<NT>(v, sh, all);
+  return all;
+}
+
+// A row's bins in LDS: counts and weights in front of each.
+template <int NT>
+struct Bins {
+  u64 weight[kBins + 1], near_weight[kBins];  // in front of the bin; of those words that are near
+  uint32_t count[kBins + 1], near_count[kBins];
+  u64 scan[4][NT / 64];
+  int found[2];
+};
+struct Near {  // bins whose words are sorted: four ranges, and where the cutoff is sought
+  int lo[4], hi[4];
+  bool k_on, p_on, m_on;
+  __device__ __forceinline__ bool has(int bin) const {
+    bool in = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) in = in || (bin >= lo[i] && bin <= hi[i]);
+    return in;
+  }
+};
+__device__ __forceinline__ u64 top_p_target(double top_p, u64 all) { return max((u64)1, min(all, (u64)ceil(top_p * (double)all))); }
+__device__ __forceinline__ u64 draw_target(double u, u64 all) { return u < 1.0 ? max((u64)1, min(all, (u64)(fmax(u, 0.0) * (double)all) + 1)) : max((u64)1, all); }
+
+// counts and weights of the bins -> those in front of each (in place)
+template <int NT>
+__device__ __forceinline__ void scan_bins(Bins<NT>& b) {
+  constexpr int N = kBins / NT;
+  const int tid = threadIdx.x;
+  u64 w[N], sw = 0;
+  uint32_t c[N];
+  u64 sc = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sw += w[i] = b.weight[tid * N + i];
+    sc += c[i] = b.count[tid * N + i];
+  }
+  u64 all_w, all_c;
+  u64 before_w = sum_before<NT>(sw, b.scan[0], all_w), before_c = sum_before<NT>(sc, b.scan[1], all_c);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    b.weight[tid * N + i] = before_w;
+    b.count[tid * N + i] = (uint32_t)before_c;
+    before_w += w[i];
+    before_c += c[i];
+  }
+  if (tid == 0) b.weight[kBins] = all_w, b.count[kBins] = (uint32_t)all_c;
+  __syncthreads();
+}
+
+// The bins that hold the words at which the running weight (count) reaches two targets, 1 or more and no more than there is.
+template <int NT, class A>
+__device__ __forceinline__ void bins_that_reach(Bins<NT>& b, const A* run, u64 t0, u64 t1, int& b0, int& b1) {
+  for (int i = threadIdx.x; i < kBins; i += NT) {
+    const u64 before = run[i], after = run[i + 1];
+    if (before < t0 && t0 <= after) b.found[0] = i;
+    if (before < t1 && t1 <= after) b.found[1] = i;
+  }
+  __syncthreads();
+  b0 = b.found[0];
+  b1 = b.found[1];
+  __syncthreads();
+}
+
+// Which bins matter.  b: sums in front of the bins.  The weight of the first top_k words, and of all that stay, is known here up to the
+// words of one bin: whatever depends on it gets the bins between what either end asks for.
+template <int NT>
+__device__ __forceinline__ Near near_bins(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b) {
+  Near n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) n.lo[i] = 1, n.hi[i] = 0;
+  const u64 all = b.weight[kBins];
+  u64 z0 = all, z1 = all;
+  int cut0 = kBins, cut1 = kBins;
+  n.k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count[kBins];
+  n.p_on = a.top_p < 1.0;
+  n.m_on = a.min_z > -INFINITY;
+  if (n.k_on) {
+    bins_that_reach(b, b.count, (u64)a.top_k, (u64)a.top_k, cut0, cut1);
+    n.lo[0] = n.hi[0] = cut0;
+    z0 = b.weight[cut0];
+    z1 = b.weight[cut0 + 1];
+  }
+  if (n.p_on) {
+    bins_that_reach(b, b.weight, top_p_target(a.top_p, z0), top_p_target(a.top_p, z1), n.lo[1], n.hi[1]);
+    cut0 = min(cut0, n.lo[1]);
+    cut1 = min(cut1, n.hi[1]);
+  }
+  if (n.m_on) {
+    n.lo[2] = n.hi[2] = w.bin(-a.min_z * w.log2e_T);
+    cut0 = min(cut0, n.lo[2]);
+    cut1 = min(cut1, n.hi[2]);
+  }
+  if (a.tokens) {
+    const u64 t0 = cut0 < kBins ? b.weight[cut0] : all, t1 = cut1 < kBins ? b.weight[cut1 + 1] : all;
+    bins_that_reach(b, b.weight, draw_target(u, t0), draw_target(u, t1), n.lo[3], n.hi[3]);
+  }
+  return n;
+}
+
+// The words that stay: those up to a place, and over the highest logit plus min_z.
+struct Cut {
+  u64 from;
+  int token;
+};
+
+// n words of the near bins, sorted here, answer all questions.  b: sums in front of the bins.
+template <int NT>
+__device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b, const Near& near, u64* words, int n) {
+  const int tid = threadIdx.x;
+  int size = 2;
+  while (size < n) size *= 2;
+  for (int i = n + tid; i < size; i += NT) words[i] = 0;
+  {  // what of the sums in front of a bin is of near words
+    constexpr int N = kBins / NT;
+    u64 sw = 0, sc = 0, nw[N], nc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = tid * N + i;
+      const bool in = near.has(at);
+      sw += nw[i] = in ? b.weight[at + 1] - b.weight[at] : 0;
+      sc += nc[i] = in ? b.count[at + 1] - b.count[at] : 0;
+    }
+    u64 all;
+    u64 before_w = sum_before<NT>(sw, b.scan[2], all), before_c = sum_before<NT>(sc, b.scan[3], all);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      b.near_weight[tid * N + i] = before_w;
+      b.near_count[tid * N + i] = (uint32_t)before_c;
+      before_w += nw[i];
+      before_c += nc[i];
+    }
+  }
+  __syncthreads();
+  for (int k = 2; k <= size; k *= 2)
+    for (int j = k / 2; j > 0; j /= 2) {
+      for (int i = tid; i < size / 2; i += NT) {
+        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+        const u64 x = words[lo], y = words[hi];
+        if ((x < y) == ((lo & k) == 0)) words[lo] = y, words[hi] = x;
+      }
+      __syncthreads();
+    }
+  // running weights, a thread's words side by side
+  const int per = (size + NT - 1) / NT, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  u64 own = 0, all;
+  for (int i = i0; i < i1; ++i) own += w.weight(w.below(logit_at(words[i])));
+  const u64 before = sum_before<NT>(own, b.scan[0], all);
+  const auto first_of_mine = [&](auto reaches) {  // reaches(count, weight, place) with the words up to this one
+    u64 run = before;
+    for (int i = i0; i < i1; ++i) {
+      const double y = w.below(logit_at(words[i]));
+      const int bin = w.bin(y);
+      run += w.weight(y);
+      if (reaches((u64)(i + 1) + b.count[bin] - b.near_count[bin], run + b.weight[bin] - b.near_weight[bin], words[i])) return;
+    }
+  };
+  __shared__ u64 s_place, s_weight;
+  // where the running count (weight) first reaches a number, inside a thread's words: the word in front of it has not
+  const auto find = [&](bool by_count, u64 target, u64& place, u64& weight) {
+    __syncthreads();
+    first_of_mine([&](u64 c, u64 wt, u64 p) {
+      const u64 self = w.weight(w.below(logit_at(p)));
+      const u64 now = by_count ? c : wt, front = by_count ? c - 1 : wt - self;
+      if (front < target && target <= now) s_place = p, s_weight = wt;
+      return now >= target;
+    });
+    __syncthreads();
+    place = s_place;
+    weight = s_weight;
+  };
+  Cut cut = {1, -1};
+  u64 stay = b.weight[kBins], place, weight;
+  if (near.k_on) {
+    find(true, (u64)a.top_k, place, weight);
+    cut.from = place;
+    stay = weight;
+  }
+  if (near.p_on) {
+    find(false, top_p_target(a.top_p, stay), place, weight);
+    cut.from = max(cut.from, place);
+    stay = weight;
+  }
+  if (a.tokens) {
+    if (near.m_on) {
+      // the weight of the words over the border: of the bins in front of the border's, and of its own words that are
+      u64 in_bin = 0;
+      for (int i = i0; i < i1; ++i) {
+        const float x = logit_at(words[i]);
+        const double y = w.below(x);
+        if (w.bin(y) == near.lo[2] && w.over(x, a.min_z)) in_bin += w.weight(y);
+      }
+      stay = min(stay, b.weight[near.lo[2]] + sum_all<NT>(in_bin, b.scan[1]));
+    }
+    find(false, draw_target(u, stay), place, weight);
+    cut.token = token_at(place);
+  }
+  return cut;
+}
+
+// ------------------------------------------------------------------------------------------
+// Digit by digit: for rows whose bins hold more words than are sorted.
+// ------------------------------------------------------------------------------------------
+struct Digits {
+  u64 weight[kDigitBins];
+  uint32_t count[kDigitBins];
+};
 
 // The place of the first word at which the count (or weight) of the words so far reaches `target`, 1 or more, which all words from `limit`
 // on together do.
-template <bool BY_WEIGHT>
-__device__ u64 first_to_reach(const RowOf& r, u64 target, u64 limit, SampleShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+template <int NT, bool BY_WEIGHT>
+__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 target, u64 limit, Digits& d, u64 (&scan)[NT / 64], u64& s_bin) {
+  const int tid = threadIdx.x;
+  constexpr int N = kDigitBins / NT;
   u64 prefix = 0;
   int shift = 32 + kTokenBits;
   for (int digit = 0; digit < 5; ++digit) {
     const int bits = digit < 2 ? 11 : 10, above = shift;
     shift -= bits;
-    for (int i = tid; i < kSampleBins; i += kSampleThreads) sh.weight[i] = 0, sh.count[i] = 0;
+    for (int i = tid; i < kDigitBins; i += NT) d.weight[i] = 0, d.count[i] = 0;
     __syncthreads();
-    for (int v = tid; v < r.V; v += kSampleThreads) {
-      const float x = r.x[v];
+    each_word<NT>(row, 0, V, [&](float x, int v) {
       const u64 p = place_of(x, v);
-      if (p == 0 || p < limit || p >> above != prefix) continue;
-      const int bin = (int)(p >> shift) & ((1 << bits) - 1);
-      atomicAdd(&sh.count[bin], 1u);
-      if (BY_WEIGHT) {
-        const u64 w = r.weight(x);
-        if (w) atomicAdd(&sh.weight[bin], w);
+      if (p < limit || p >> above != prefix) return;
+      const int bin = kDigitBins - 1 - ((int)(p >> shift) & ((1 << bits) - 1));  // the highest first
+      if (BY_WEIGHT) atomicAdd(&d.weight[bin], w.weight(w.below(x)));
+      else atomicAdd(&d.count[bin], 1u);
+    });
+    __syncthreads();
+    u64 n[N], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += n[i] = BY_WEIGHT ? d.weight[tid * N + i] : d.count[tid * N + i];
+    u64 before = sum_before<NT>(sum, scan, all);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (before < target && target <= before + n[i]) {
+        s_bin = kDigitBins - 1 - (tid * N + i);
+        d.weight[0] = before;  // read as a bin already
       }
+      before += n[i];
     }
     __syncthreads();
-    // running sums from the highest bin down, two bins a thread
-    const int b1 = kSampleBins - 1 - 2 * tid, b0 = b1 - 1;
-    const u64 n1 = BY_WEIGHT ? sh.weight[b1] : sh.count[b1], n0 = BY_WEIGHT ? sh.weight[b0] : sh.count[b0];
-    u64 run = n1 + n0;
-    for (int off = 1; off < 64; off <<= 1) {
-      const u64 o = __shfl_up(run, off, 64);
-      if (lane >= off) run += o;
-    }
-    if (lane == 63) sh.wave_weight[wave] = run;
+    prefix = prefix << bits | s_bin;
+    target -= d.weight[0];
     __syncthreads();
-    u64 before = run - (n1 + n0);
-    for (int w = 0; w < wave; ++w) before += sh.wave_weight[w];
-    if (before < target && target <= before + n1) sh.bin = b1, sh.over_weight = before;
-    else if (before + n1 < target && target <= before + n1 + n0) sh.bin = b0, sh.over_weight = before + n1;
-    __syncthreads();
-    prefix = prefix << bits | (u64)sh.bin;
-    target -= sh.over_weight;
   }
   return prefix;
 }
 
-__global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a) {
-  __shared__ SampleShared sh;
-  const int tid = threadIdx.x;
-  const float* row = a.logits + (size_t)blockIdx.x * a.V;
-  float top = -INFINITY;
-  for (int v = tid; v < a.V; v += kSampleThreads) {
-    const float x = row[v];
-    if (x > top) top = x;
+template <int NT>
+__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const float* row, Digits& d, u64 (&scan)[NT / 64]) {
+  __shared__ u64 s_bin;
+  const auto sum_from = [&](u64 limit, auto of) {
+    u64 s = 0;
+    each_word<NT>(row, 0, a.V, [&](float x, int v) {
+      if (place_of(x, v) >= limit) s += of(x);
+    });
+    return sum_all<NT>(s, scan);
+  };
+  const auto weight = [&](float x) { return w.weight(w.below(x)); };
+  Cut cut = {1, -1};
+  if (a.top_k > 0 && sum_from(1, [](float) { return (u64)1; }) > (u64)a.top_k) cut.from = first_to_reach<NT, false>(row, a.V, w, a.top_k, 1, d, scan, s_bin);
+  if (a.top_p < 1.0) cut.from = first_to_reach<NT, true>(row, a.V, w, top_p_target(a.top_p, sum_from(cut.from, weight)), cut.from, d, scan, s_bin);
+  if (a.tokens) {
+    const u64 stay = sum_from(cut.from, [&](float x) { return w.over(x, a.min_z) ? weight(x) : 0; });
+    cut.token = token_at(first_to_reach<NT, true>(row, a.V, w, draw_target(u, stay), cut.from, d, scan, s_bin));
   }
-  top = block_max<kSampleThreads / 64>(top, sh.wave_max);
-  const bool none = !(top > -INFINITY && top < INFINITY);
-  float* out = a.out ? a.out + (size_t)blockIdx.x * a.V : nullptr;
-  if (none) {
-    if (a.tokens && tid == 0) a.tokens[blockIdx.x] = -1;
+  return cut;
+}
+
+// ------------------------------------------------------------------------------------------
+// A row to a workgroup.
+// ------------------------------------------------------------------------------------------
+template <int NT>
+union SampleSpace {
+  struct {
+    Bins<NT> bins;
+    u64 words[kNear];
+  };
+  Digits digits;
+};
+
+template <int NT>
+__device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w, const Cut& cut, const float* row, float* out, int v0, int v1) {
+  constexpr int N = 8;
+  for (int base = v0; base < v1; base += N * NT) {
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = base + i * NT + (int)threadIdx.x;
+      x[i] = v < v1 ? row[v] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = base + i * NT + (int)threadIdx.x;
+      const u64 p = place_of(x[i], v);
+      if (v < v1) out[v] = p >= cut.from && w.over(x[i], a.min_z) ? x[i] : -INFINITY;
+    }
+  }
+}
+
+template <int NT>
+__global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
+  __shared__ SampleSpace<NT> sp;
+  __shared__ float s_max[NT / 64];
+  __shared__ int s_near;
+  __shared__ u64 s_scan[NT / 64];
+  const int tid = threadIdx.x;
+  const size_t r = blockIdx.x;
+  const float* row = a.logits + r * a.V;
+  float* out = a.out ? a.out + r * a.V : nullptr;
+  for (int i = tid; i < kBins; i += NT) sp.bins.weight[i] = 0, sp.bins.count[i] = 0;
+  if (tid == 0) s_near = 0;
+  float top = -INFINITY;
+  each_word<NT>(row, 0, a.V, [&](float x, int) { top = fmaxf(top, x); });
+  top = block_max<NT / 64>(top, s_max);
+  if (!(top > -INFINITY && top < INFINITY)) {
+    if (a.tokens && tid == 0) a.tokens[r] = -1;
     if (out)
-      for (int v = tid; v < a.V; v += kSampleThreads) out[v] = -INFINITY;
+      for (int v = tid; v < a.V; v += NT) out[v] = -INFINITY;
     return;
   }
-  const RowOf r = {row, (double)top, a.inv_T, a.unit, a.V};
-  u64 from = 1;  // the last place that stays
-  if (a.top_k > 0) {
-    u64 words = 0;
-    for (int v = tid; v < a.V; v += kSampleThreads) words += row[v] > -INFINITY;
-    if (block_sum_u64(words, sh) > (u64)a.top_k) from = first_to_reach<false>(r, a.top_k, from, sh);
-  }
-  const auto weight_from = [&](u64 limit) {
-    u64 w = 0;
-    for (int v = tid; v < a.V; v += kSampleThreads) {
-      const u64 p = place_of(row[v], v);
-      if (p && p >= limit) w += r.weight(row[v]);
-    }
-    return block_sum_u64(w, sh);
-  };
-  if (a.top_p < 1.0) {
-    const u64 all = weight_from(from);
-    from = first_to_reach<true>(r, min(all, max((u64)1, (u64)ceil(a.top_p * (double)all))), from, sh);
-  }
-  if (a.min_z > -INFINITY) {
-    u64 least = ~0ull;
-    for (int v = tid; v < a.V; v += kSampleThreads) {
-      const float x = row[v];
-      if ((double)x - r.top >= a.min_z) least = min(least, place_of(x, v));
-    }
-    for (int off = 32; off; off >>= 1) least = min(least, __shfl_xor(least, off, 64));
+  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  const double u = a.tokens ? (double)a.u[r] : 0.0;
+  each_word<NT>(row, 0, a.V, [&](float x, int) {
+    const double y = w.below(x);
+    const int b = w.bin(y);
+    atomicAdd(&sp.bins.count[b], 1u);
+    atomicAdd(&sp.bins.weight[b], w.weight(y));
+  });
+  __syncthreads();
+  scan_bins(sp.bins);
+  const Near near = near_bins(a, w, u, sp.bins);
+  each_word<NT>(row, 0, a.V, [&](float x, int v) {
+    if (!near.has(w.bin(w.below(x)))) return;
+    const int at = atomicAdd(&s_near, 1);
+    if (at < kNear) sp.words[at] = place_of(x, v);
+  });
+  __syncthreads();
+  const int n = s_near;
+  Cut cut;
+  if (n <= kNear) {
+    cut = resolve(a, w, u, sp.bins, near, sp.words, n);
+  } else {
     __syncthreads();
-    if ((tid & 63) == 0) sh.wave_weight[tid >> 6] = least;
-    __syncthreads();
-    for (int w = 0; w < kSampleThreads / 64; ++w) least = min(least, sh.wave_weight[w]);
-    from = max(from, least);
+    cut = resolve_by_digits<NT>(a, w, u, row, sp.digits, s_scan);
   }
-  if (a.tokens) {
-    const u64 all = weight_from(from);
-    const double u = (double)a.u[blockIdx.x];
-    const u64 target = u < 1.0 ? min(all, (u64)(max(u, 0.0) * (double)all) + 1) : all;
-    const u64 at = first_to_reach<true>(r, target, from, sh);
-    if (tid == 0) a.tokens[blockIdx.x] = kMaxSampleVocab - 1 - (int)(at & (kMaxSampleVocab - 1));
-  }
-  if (out)
-    for (int v = tid; v < a.V; v += kSampleThreads) {
-      const float x = row[v];
-      const u64 p = place_of(x, v);
-      out[v] = p && p >= from ? x : -INFINITY;
-    }
+  if (a.tokens && tid == 0) a.tokens[r] = cut.token;
+  if (out) write_row<NT>(a, w, cut, row, out, 0, a.V);
 }
 
 size_t sample_workspace_bytes(int rows, int V) { return 16; }
@@ -179,13 +471,16 @@ size_t sample_workspace_bytes(int rows, int V) { return 16; }
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
                    float* logits_out, void* ws, hipStream_t st) {
   SampleArgs a;
-  a.logits = logits; a.u = u; a.V = V; a.top_k = top_k; a.T = T; a.inv_T = 1.0 / T; a.top_p = top_p;
+  memset(&a, 0, sizeof a);
+  a.logits = logits; a.u = u; a.V = V; a.top_k = top_k; a.top_p = top_p;
+  a.log2e_T = 1.4426950408889634 / T;
   a.min_z = min_p > 0.0 ? T * log(min_p) : -INFINITY;
   int bits = 0;
   while ((1 << bits) < V) ++bits;
-  a.unit = ldexp(1.0, std::min(52, 62 - bits));
+  a.unit = ldexp(1.0, std::min(51, 62 - bits));
   a.tokens = tokens_out; a.out = logits_out;
-  hipLaunchKernelGGL(sample_row_kernel, dim3(rows), dim3(kSampleThreads), 0, st, a);
+  if (V <= 2048) hipLaunchKernelGGL(sample_row_kernel<256>, dim3(rows), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
 }
 
 }  // namespace es

@@ -24,6 +24,7 @@ static_assert(kMaxSampleVocab == 1 << kTokenBits, "a place number holds a token"
 constexpr int kBins = 1024, kFineBins = 768;  // kFineBins up to y = 48, where weights end; then eight to a doubling of y
 constexpr int kNear = 4096;                   // words that are sorted
 constexpr int kDigitBins = 2048;
+constexpr int kShortRow = 2048;  // words of a row that one small workgroup takes
 
 // A word's place number: the higher, the earlier in the order; 0 is no word (minus infinity, NaN).
 __device__ __forceinline__ u64 place_of(float x, int v) {
@@ -51,7 +52,7 @@ struct SampleArgs {
   int slices, per;
   float* slice_max;  // [row][slices]
   u64* weight;       // [row][kBins]
-  uint32_t* count;   // [row][kBins], then a counter of near words
+  uint32_t* count;   // [row][kBins + 1], the last one counting near words
   u64* near;         // [row][kNear]
 };
 
@@ -466,7 +467,133 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   if (out) write_row<NT>(a, w, cut, row, out, 0, a.V);
 }
 
-size_t sample_workspace_bytes(int rows, int V) { return 16; }
+// ------------------------------------------------------------------------------------------
+// A row to several workgroups, in four launches: (1) the slices' highest logits; (2) their bins, added up; (3) the words of the near
+// bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
+// ------------------------------------------------------------------------------------------
+constexpr int kSliceNT = 512, kMaxSlices = 64;
+
+__device__ __forceinline__ float top_of(const SampleArgs& a, float* s_top) {
+  if (threadIdx.x < 64) {
+    const float* m = a.slice_max + (size_t)blockIdx.y * kMaxSlices;
+    const float top = lanes_max((int)threadIdx.x < a.slices ? m[threadIdx.x] : -INFINITY, 64);
+    if (threadIdx.x == 0) *s_top = top;
+  }
+  __syncthreads();
+  return *s_top;
+}
+__device__ __forceinline__ bool no_word(float top) { return !(top > -INFINITY && top < INFINITY); }
+
+// grid (slices, rows), all of them
+__global__ __launch_bounds__(kSliceNT) void sample_max_kernel(SampleArgs a) {
+  __shared__ float s_max[kSliceNT / 64];
+  const size_t r = blockIdx.y;
+  const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  for (int i = blockIdx.x * kSliceNT + threadIdx.x; i <= kBins; i += a.slices * kSliceNT) {
+    if (i < kBins) a.weight[r * kBins + i] = 0;
+    a.count[r * (kBins + 1) + i] = 0;
+  }
+  float top = -INFINITY;
+  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int) { top = fmaxf(top, x); });
+  top = block_max<kSliceNT / 64>(top, s_max);
+  if (threadIdx.x == 0) a.slice_max[r * kMaxSlices + blockIdx.x] = top;
+}
+
+__global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
+  __shared__ u64 s_weight[kBins];
+  __shared__ uint32_t s_count[kBins];
+  __shared__ float s_top;
+  const int tid = threadIdx.x;
+  const size_t r = blockIdx.y;
+  const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  for (int i = tid; i < kBins; i += kSliceNT) s_weight[i] = 0, s_count[i] = 0;
+  const float top = top_of(a, &s_top);
+  if (no_word(top)) return;
+  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int) {
+    const double y = w.below(x);
+    const int b = w.bin(y);
+    atomicAdd(&s_count[b], 1u);
+    atomicAdd(&s_weight[b], w.weight(y));
+  });
+  __syncthreads();
+  for (int i = tid; i < kBins; i += kSliceNT)
+    if (s_count[i]) {
+      atomicAdd(&a.count[r * (kBins + 1) + i], s_count[i]);
+      if (s_weight[i]) atomicAdd(&a.weight[r * kBins + i], s_weight[i]);
+    }
+}
+
+template <int NT>
+__device__ __forceinline__ void load_bins(const SampleArgs& a, size_t r, Bins<NT>& b) {
+  for (int i = threadIdx.x; i < kBins; i += NT) {
+    b.weight[i] = a.weight[r * kBins + i];
+    b.count[i] = a.count[r * (kBins + 1) + i];
+  }
+  __syncthreads();
+  scan_bins(b);
+}
+
+__global__ __launch_bounds__(kSliceNT) void sample_near_kernel(SampleArgs a) {
+  __shared__ Bins<kSliceNT> bins;
+  __shared__ float s_top;
+  const size_t r = blockIdx.y;
+  const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  const float top = top_of(a, &s_top);
+  if (no_word(top)) return;
+  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  load_bins(a, r, bins);
+  const Near near = near_bins(a, w, a.tokens ? (double)a.u[r] : 0.0, bins);
+  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int v) {
+    if (!near.has(w.bin(w.below(x)))) return;
+    const uint32_t at = atomicAdd(&a.count[r * (kBins + 1) + kBins], 1u);
+    if (at < kNear) a.near[r * kNear + at] = place_of(x, v);
+  });
+}
+
+// grid (slices or 1, rows)
+__global__ __launch_bounds__(kSliceNT) void sample_finish_kernel(SampleArgs a) {
+  __shared__ SampleSpace<kSliceNT> sp;
+  __shared__ float s_top;
+  __shared__ u64 s_scan[kSliceNT / 64];
+  const int tid = threadIdx.x;
+  const size_t r = blockIdx.y;
+  const float* row = a.logits + r * a.V;
+  float* out = a.out ? a.out + r * a.V : nullptr;
+  int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  const float top = top_of(a, &s_top);
+  if (no_word(top)) {
+    if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = -1;
+    if (out)
+      for (int v = v0 + tid; v < v1; v += kSliceNT) out[v] = -INFINITY;
+    return;
+  }
+  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  const double u = a.tokens ? (double)a.u[r] : 0.0;
+  const uint32_t n = a.count[r * (kBins + 1) + kBins];
+  Cut cut;
+  if (n <= kNear) {
+    load_bins(a, r, sp.bins);
+    const Near near = near_bins(a, w, u, sp.bins);
+    for (int i = tid; i < (int)n; i += kSliceNT) sp.words[i] = a.near[r * kNear + i];
+    cut = resolve(a, w, u, sp.bins, near, sp.words, (int)n);
+  } else {
+    // one workgroup reads the whole row, which may be where the results go
+    if (blockIdx.x > 0) return;
+    v0 = 0;
+    v1 = a.V;
+    cut = resolve_by_digits<kSliceNT>(a, w, u, row, sp.digits, s_scan);
+  }
+  if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = cut.token;
+  if (out) write_row<kSliceNT>(a, w, cut, row, out, v0, v1);
+}
+
+static int sample_slices(int rows, int V) {
+  if (V <= kShortRow) return 1;
+  return std::max(1, std::min({kMaxSlices, (V + 2047) / 2048, 512 / rows}));
+}
+static size_t sample_row_bytes() { return kMaxSlices * sizeof(float) + kBins * sizeof(u64) + (kBins + 4) * sizeof(uint32_t) + kNear * sizeof(u64); }
+size_t sample_workspace_bytes(int rows, int V) { return sample_slices(rows, V) > 1 ? rows * sample_row_bytes() : 16; }
 
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
                    float* logits_out, void* ws, hipStream_t st) {
@@ -479,8 +606,22 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   while ((1 << bits) < V) ++bits;
   a.unit = ldexp(1.0, std::min(51, 62 - bits));
   a.tokens = tokens_out; a.out = logits_out;
-  if (V <= 2048) hipLaunchKernelGGL(sample_row_kernel<256>, dim3(rows), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
+  a.slices = sample_slices(rows, V);
+  if (a.slices == 1) {
+    if (V <= kShortRow) hipLaunchKernelGGL(sample_row_kernel<256>, dim3(rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
+    return;
+  }
+  a.per = (V + a.slices - 1) / a.slices;
+  a.weight = (u64*)ws;
+  a.near = a.weight + (size_t)rows * kBins;
+  a.count = (uint32_t*)(a.near + (size_t)rows * kNear);
+  a.slice_max = (float*)(a.count + (size_t)rows * (kBins + 1));
+  const dim3 grid(a.slices, rows), block(kSliceNT);
+  hipLaunchKernelGGL(sample_max_kernel, grid, block, 0, st, a);
+  hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
+  hipLaunchKernelGGL(sample_near_kernel, grid, block, 0, st, a);
+  hipLaunchKernelGGL(sample_finish_kernel, dim3(a.out ? a.slices : 1, rows), block, 0, st, a);
 }
 
 }  // namespace es

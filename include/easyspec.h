@@ -492,7 +492,7 @@ int64_t easyspec_kvq_select_workspace_bytes(const easyspec_kv_layout *layout, co
  *   workspace   dev, easyspec_sample_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
  *   hip_stream  the hipStream_t to launch on (NULL = the null stream); nothing is synchronised
  * Weights are worked out in double precision (to 2.2e-13) and kept as whole multiples of 2^-s, s = 62 - ceil(log2(vocab)) and 51 at most (45 at
- * 128 256 words): sums of them are exact, so results do not depend on their order, and a decision can differ from that of the real numbers only
+ * 128 256 words), below 2^-48 as 0: sums of them are exact, so results do not depend on their order, and a decision can differ from that of the real numbers only
  * within about vocab 2^-s of its border.  EASYSPEC_EINVAL for NULL logits or
  * workspace, neither output, tokens_out without u, rows outside 1..65535, vocab outside 1..EASYSPEC_MAX_SAMPLE_VOCAB, a temperature that is
  * not positive and finite (temperature 0 is the argmax that the draft step writes), top_k < 0, top_p outside (0, 1], min_p outside [0, 1],

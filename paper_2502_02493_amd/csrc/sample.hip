@@ -7,7 +7,7 @@
 // Weights are whole multiples of 2^-s: sums of them are exact, so neither the order of atomic additions nor how a row is cut up
 // shows in a result.
 //
-// No row is sorted.  A histogram of counts and weights over y = (max - x) log2(e) / T, sixteen bins to a factor of two in weight, tells
+// No row is sorted.  A histogram of counts and weights over y = (max - x) log2(e) / T tells
 // for each question the bin that its word lies in, or, where it depends on the word that answers another one, a few of them.  The words
 // of these bins, some hundred, are sorted and answer it exactly.  Rows whose bins hold too many (thousands of nearly equal
 // logits) go digit by digit through their words' place numbers instead.
@@ -21,10 +21,11 @@ namespace es {
 typedef unsigned long long u64;
 constexpr int kTokenBits = 20;
 static_assert(kMaxSampleVocab == 1 << kTokenBits, "a place number holds a token");
-constexpr int kBins = 1024, kFineBins = 768;  // kFineBins up to y = 48, where weights end; then eight to a doubling of y
-constexpr int kNear = 4096;                   // words that are sorted
+constexpr int kBins = 1024, kFineBins = 896;  // evenly over y up to 48, where weights end, or to the lowest logit's; then four to a doubling
+constexpr int kNear = 4096;                    // words that are sorted
 constexpr int kDigitBins = 2048;
-constexpr int kShortRow = 2048;  // words of a row that one small workgroup takes
+constexpr int kShortRow = 2048;  // words of a row that are sorted, all of them
+constexpr double kFar = 48.0;
 
 // A word's place number: the higher, the earlier in the order; 0 is no word (minus infinity, NaN).
 __device__ __forceinline__ u64 place_of(float x, int v) {
@@ -50,24 +51,34 @@ struct SampleArgs {
   float* out;
   // rows cut into slices
   int slices, per;
-  float* slice_max;  // [row][slices]
-  u64* weight;       // [row][kBins]
-  uint32_t* count;   // [row][kBins + 1], the last one counting near words
-  u64* near;         // [row][kNear]
+  float2* slice_ends;  // [row][slices]  highest and lowest logit
+  u64* weight;         // [row][kBins]
+  uint32_t* count;     // [row][kBins + 1], the last one counting near words
+  u64* near;           // [row][kNear]
+  struct NearBins* bins;  // [row]
 };
 
-// What a word's logit says, given the row's highest.
+// What a word's logit says, given the row's highest and lowest.
 struct Weigher {
-  double top, log2e_T, unit;
+  double top, log2e_T, unit, far, per_y;  // fine bins reach to y = far, per_y of them to 1
+  __device__ __forceinline__ Weigher(const SampleArgs& a, float highest, float lowest)
+      : top((double)highest), log2e_T(a.log2e_T), unit(a.unit) {
+    far = fmin(kFar, fmax(below(lowest), 1e-6));
+    per_y = (double)kFineBins / far;
+  }
   __device__ __forceinline__ double below(float x) const { return (top - (double)x) * log2e_T; }
-  __device__ __forceinline__ u64 weight(double y) const {  // exact below 2^52: the sum's last bit is worth 1
-    const double w = exp2_below(fmax(-y, -1000.0)) * unit + 4503599627370496.0;
-    return __builtin_bit_cast(u64, w) & 0xFFFFFFFFFFFFFull;
+  __device__ __forceinline__ u64 weight(double y) const {
+    const double w = exp2_below(-fmin(y, kFar)) * unit + 4503599627370496.0;  // 2^52: the sum's last bit is worth 1
+    return y < kFar ? __builtin_bit_cast(u64, w) & 0xFFFFFFFFFFFFFull : 0;
   }
   __device__ __forceinline__ int bin(double y) const {  // never falls as y rises
-    if (y < 48.0) return (int)(y * 16.0);
-    const uint32_t b = __float_as_uint((float)(y * (1.0 / 48.0)));
-    return kFineBins + min((int)(b >> 20) - (127 << 3), kBins - kFineBins - 1);
+    if (y < far) return min((int)(y * per_y), kFineBins - 1);
+    const uint32_t b = __float_as_uint((float)(y * (1.0 / far)));
+    return kFineBins + min(max((int)(b >> 21) - (127 << 2), 0), kBins - kFineBins - 1);
+  }
+  __device__ __forceinline__ float bin_start(int b) const {  // y, to 1e-6
+    if (b <= kFineBins) return (float)((double)b / per_y);
+    return b >= kBins ? INFINITY : (float)far * __uint_as_float((uint32_t)(b - kFineBins + (127 << 2)) << 21);
   }
   __device__ __forceinline__ bool over(float x, double min_z) const { return (double)x - top >= min_z; }
 };
@@ -89,90 +100,117 @@ __device__ __forceinline__ void each_word(const float* row, int v0, int v1, cons
   }
 }
 
-// Running sums over the threads of a workgroup, in front of the thread; all: the whole.  sh: NT / 64 numbers, which nobody reads any more.
+// Running sum over the wave's lanes, the own one included.
+__device__ __forceinline__ u64 running_sum(u64 v) {
+  const auto moved = [](u64 x, auto ctrl, auto rows) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    return (u64)hi << 32 | lo;
+  };
+  typedef std::integral_constant<int, 0xF> All;
+  v += moved(v, std::integral_constant<int, 0x111>{}, All{});  // row_shr by 1, 2, 4, 8: zeros come in
+  v += moved(v, std::integral_constant<int, 0x112>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x114>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x118>{}, All{});
+  v += moved(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});  // row_bcast15
+  v += moved(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});  // row_bcast31
+  return v;
+}
+// Running sums of two numbers over the threads of a workgroup, in front of the thread; all: the whole sums.  sh: NT / 64 pairs, which nobody
+// reads any more.
+struct Sums {
+  u64 weight, count;
+};
 template <int NT>
-__device__ __forceinline__ u64 sum_before(u64 v, u64* sh, u64& all) {
+__device__ __forceinline__ Sums sums_before(Sums v, Sums* sh, Sums& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u64 run = v;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const u64 o = __shfl_up(run, off, 64);
-    if (lane >= off) run += o;
-  }
+  const Sums run = {running_sum(v.weight), running_sum(v.count)};
   if (lane == 63) sh[wave] = run;
   __syncthreads();
-  u64 before = run - v;
-  all = 0;
+  Sums before = {run.weight - v.weight, run.count - v.count};
+  all = Sums{0, 0};
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) {
-    const u64 o = sh[w];
-    before += w < wave ? o : 0;
-    all += o;
+    const Sums o = sh[w];
+    before.weight += w < wave ? o.weight : 0;
+    before.count += w < wave ? o.count : 0;
+    all.weight += o.weight;
+    all.count += o.count;
   }
   return before;
 }
 template <int NT>
-__device__ __forceinline__ u64 sum_all(u64 v, u64* sh) {
-  u64 all;
+__device__ __forceinline__ u64 sum_all(u64 v, Sums* sh) {
+  Sums all;
   __syncthreads();
-  sum_before<NT>(v, sh, all);
-  return all;
+  sums_before<NT>(Sums{v, 0}, sh, all);
+  return all.weight;
 }
 
-// A row's bins in LDS: counts and weights in front of each.
+// A row's bins in LDS: first their counts and weights, then those in front of each.
 template <int NT>
 struct Bins {
-  u64 weight[kBins + 1], near_weight[kBins];  // in front of the bin; of those words that are near
-  uint32_t count[kBins + 1], near_count[kBins];
-  u64 scan[4][NT / 64];
+  u64 weight[kBins + 1];
+  uint32_t count[kBins + 1];
+  Sums scan[NT / 64];
   int found[2];
 };
-struct Near {  // bins whose words are sorted: four ranges, and where the cutoff is sought
-  int lo[4], hi[4];
-  bool k_on, p_on, m_on;
+
+// The bins that matter, as up to four runs in ascending order, apart from each other: what is in front of a word is what its list has in
+// front of it and what lies between the runs.
+struct NearBins {
+  int lo[4], hi[4], n_count, k_on, p_on, m_on, m_bin, pad;
+  u64 weight[4], count[4];  // not on the list, in front of the run
+  u64 all, m_front;         // the row's weight; what is in front of the border's bin of min_p
+  float y0[4], y1[4];       // the runs in y, a little wider
   __device__ __forceinline__ bool has(int bin) const {
     bool in = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) in = in || (bin >= lo[i] && bin <= hi[i]);
     return in;
   }
+  __device__ __forceinline__ bool may_have(float y) const {
+    bool in = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) in = in || (y >= y0[i] && y <= y1[i]);
+    return in;
+  }
 };
 __device__ __forceinline__ u64 top_p_target(double top_p, u64 all) { return max((u64)1, min(all, (u64)ceil(top_p * (double)all))); }
 __device__ __forceinline__ u64 draw_target(double u, u64 all) { return u < 1.0 ? max((u64)1, min(all, (u64)(fmax(u, 0.0) * (double)all) + 1)) : max((u64)1, all); }
 
-// counts and weights of the bins -> those in front of each (in place)
+// counts and weights of the thread's bins, from tid * kBins / NT on -> those in front of every bin
 template <int NT>
-__device__ __forceinline__ void scan_bins(Bins<NT>& b) {
+__device__ __forceinline__ void scan_bins(Bins<NT>& b, u64 (&w)[kBins / NT], uint32_t (&c)[kBins / NT]) {
   constexpr int N = kBins / NT;
   const int tid = threadIdx.x;
-  u64 w[N], sw = 0;
-  uint32_t c[N];
-  u64 sc = 0;
+  Sums own = {0, 0}, all;
+#pragma unroll
+  for (int i = 0; i < N; ++i) own.weight += w[i], own.count += c[i];
+  Sums before = sums_before<NT>(own, b.scan, all);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    sw += w[i] = b.weight[tid * N + i];
-    sc += c[i] = b.count[tid * N + i];
+    b.weight[tid * N + i] = before.weight;
+    b.count[tid * N + i] = (uint32_t)before.count;
+    before.weight += w[i];
+    before.count += c[i];
   }
-  u64 all_w, all_c;
-  u64 before_w = sum_before<NT>(sw, b.scan[0], all_w), before_c = sum_before<NT>(sc, b.scan[1], all_c);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    b.weight[tid * N + i] = before_w;
-    b.count[tid * N + i] = (uint32_t)before_c;
-    before_w += w[i];
-    before_c += c[i];
-  }
-  if (tid == 0) b.weight[kBins] = all_w, b.count[kBins] = (uint32_t)all_c;
+  if (tid == 0) b.weight[kBins] = all.weight, b.count[kBins] = (uint32_t)all.count;
   __syncthreads();
 }
 
 // The bins that hold the words at which the running weight (count) reaches two targets, 1 or more and no more than there is.
 template <int NT, class A>
 __device__ __forceinline__ void bins_that_reach(Bins<NT>& b, const A* run, u64 t0, u64 t1, int& b0, int& b1) {
-  for (int i = threadIdx.x; i < kBins; i += NT) {
-    const u64 before = run[i], after = run[i + 1];
+  constexpr int N = kBins / NT;
+  u64 before = run[threadIdx.x * N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = threadIdx.x * N + j;
+    const u64 after = run[i + 1];
     if (before < t0 && t0 <= after) b.found[0] = i;
     if (before < t1 && t1 <= after) b.found[1] = i;
+    before = after;
   }
   __syncthreads();
   b0 = b.found[0];
@@ -180,140 +218,244 @@ __device__ __forceinline__ void bins_that_reach(Bins<NT>& b, const A* run, u64 t
   __syncthreads();
 }
 
+// Four runs of bins in ascending order, those that meet made one (the later of them empty), and what lies in front of each.
+template <int NT>
+__device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, int (&lo)[4], int (&hi)[4], NearBins& n) {
+  const auto order = [&](int i, int j) {
+    if (lo[j] < lo[i]) {
+      const int l = lo[i], h = hi[i];
+      lo[i] = lo[j]; hi[i] = hi[j];
+      lo[j] = l; hi[j] = h;
+    }
+  };
+  order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
+  int end = -1;  // of the runs so far
+  u64 listed_w = 0, listed_c = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n.lo[i] = max(lo[i], end + 1);
+    n.hi[i] = lo[i] < kBins ? hi[i] : -1;
+    const bool any = n.lo[i] <= n.hi[i];
+    n.y0[i] = INFINITY;
+    n.y1[i] = -INFINITY;
+    n.weight[i] = n.count[i] = 0;
+    if (any) {
+      const u64 w0 = b.weight[n.lo[i]], c0 = b.count[n.lo[i]];
+      n.weight[i] = w0 - listed_w;
+      n.count[i] = c0 - listed_c;
+      listed_w += b.weight[n.hi[i] + 1] - w0;
+      listed_c += b.count[n.hi[i] + 1] - c0;
+      end = n.hi[i];
+      n.y0[i] = w.bin_start(n.lo[i]) * (1.f - 1e-5f) - 1e-30f;
+      n.y1[i] = w.bin_start(n.hi[i] + 1) * (1.f + 1e-5f);
+    }
+  }
+  n.n_count = (int)listed_c;
+}
+
 // Which bins matter.  b: sums in front of the bins.  The weight of the first top_k words, and of all that stay, is known here up to the
 // words of one bin: whatever depends on it gets the bins between what either end asks for.
 template <int NT>
-__device__ __forceinline__ Near near_bins(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b) {
-  Near n;
+__device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b, NearBins& n) {
+  int lo[4], hi[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) n.lo[i] = 1, n.hi[i] = 0;
+  for (int i = 0; i < 4; ++i) lo[i] = kBins, hi[i] = -1;
   const u64 all = b.weight[kBins];
   u64 z0 = all, z1 = all;
   int cut0 = kBins, cut1 = kBins;
-  n.k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count[kBins];
-  n.p_on = a.top_p < 1.0;
-  n.m_on = a.min_z > -INFINITY;
-  if (n.k_on) {
+  const bool k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count[kBins], p_on = a.top_p < 1.0, m_on = a.min_z > -INFINITY;
+  if (k_on) {
     bins_that_reach(b, b.count, (u64)a.top_k, (u64)a.top_k, cut0, cut1);
-    n.lo[0] = n.hi[0] = cut0;
+    lo[0] = hi[0] = cut0;
     z0 = b.weight[cut0];
     z1 = b.weight[cut0 + 1];
   }
-  if (n.p_on) {
-    bins_that_reach(b, b.weight, top_p_target(a.top_p, z0), top_p_target(a.top_p, z1), n.lo[1], n.hi[1]);
-    cut0 = min(cut0, n.lo[1]);
-    cut1 = min(cut1, n.hi[1]);
+  if (p_on) {
+    bins_that_reach(b, b.weight, top_p_target(a.top_p, z0), top_p_target(a.top_p, z1), lo[1], hi[1]);
+    cut0 = min(cut0, lo[1]);
+    cut1 = min(cut1, hi[1]);
   }
-  if (n.m_on) {
-    n.lo[2] = n.hi[2] = w.bin(-a.min_z * w.log2e_T);
-    cut0 = min(cut0, n.lo[2]);
-    cut1 = min(cut1, n.hi[2]);
+  if (m_on) {
+    lo[2] = hi[2] = w.bin(-a.min_z * w.log2e_T);
+    cut0 = min(cut0, lo[2]);
+    cut1 = min(cut1, hi[2]);
   }
   if (a.tokens) {
     const u64 t0 = cut0 < kBins ? b.weight[cut0] : all, t1 = cut1 < kBins ? b.weight[cut1 + 1] : all;
-    bins_that_reach(b, b.weight, draw_target(u, t0), draw_target(u, t1), n.lo[3], n.hi[3]);
+    bins_that_reach(b, b.weight, draw_target(u, t0), draw_target(u, t1), lo[3], hi[3]);
   }
-  return n;
+  if (threadIdx.x < 64) {  // one wave: the same in all its lanes
+    n.k_on = k_on; n.p_on = p_on; n.m_on = m_on;
+    n.m_bin = m_on ? lo[2] : -1;
+    n.all = all;
+    n.m_front = m_on ? b.weight[lo[2]] : 0;
+    order_runs(w, b, lo, hi, n);
+  }
+  __syncthreads();
 }
-
 // The words that stay: those up to a place, and over the highest logit plus min_z.
 struct Cut {
   u64 from;
   int token;
 };
 
-// n words of the near bins, sorted here, answer all questions.  b: sums in front of the bins.
-template <int NT>
-__device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b, const Near& near, u64* words, int n) {
-  const int tid = threadIdx.x;
-  int size = 2;
-  while (size < n) size *= 2;
-  for (int i = n + tid; i < size; i += NT) words[i] = 0;
-  {  // what of the sums in front of a bin is of near words
-    constexpr int N = kBins / NT;
-    u64 sw = 0, sc = 0, nw[N], nc[N];
+// A workgroup's words in descending order, word E tid + e in the thread's e; size, a power of two from 2 E on, counts the places
+// that may hold one.  Exchanges inside a thread, inside a wave by operand swizzles, between waves through LDS.  SIZE: known to
+// the compiler, so that no step has to look up which exchange it is (which costs as much again), or 0.
+__device__ __forceinline__ u64 exchanged(u64 own, u64 other, bool larger) { return (own > other) == larger ? own : other; }
+template <int NT, int E, int SIZE>
+__device__ __forceinline__ void sort_words(u64 (&x)[E], int any_size, u64* lds) {
+  const int tid = threadIdx.x, size = SIZE ? SIZE : any_size;
+  const bool works = (tid & ~63) * E < size;  // a wave without places only keeps the others company
+  constexpr int kUnroll = SIZE ? 16 : 1;
+#pragma unroll kUnroll
+  for (int k = 2; k <= size; k *= 2) {
+#pragma unroll kUnroll
+    for (int j = k / 2; j > 0; j /= 2) {
+      const int m = j / E;
+      const bool larger = ((tid & m) == 0) == (((tid * E) & k) == 0);  // from E on: what the thread keeps of its pairs
+      if (j >= 64 * E) {
+        __syncthreads();
+        if (works)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = tid * N + i;
-      const bool in = near.has(at);
-      sw += nw[i] = in ? b.weight[at + 1] - b.weight[at] : 0;
-      sc += nc[i] = in ? b.count[at + 1] - b.count[at] : 0;
-    }
-    u64 all;
-    u64 before_w = sum_before<NT>(sw, b.scan[2], all), before_c = sum_before<NT>(sc, b.scan[3], all);
+          for (int e = 0; e < E; ++e) lds[e * NT + tid] = x[e];
+        __syncthreads();
+        if (works)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      b.near_weight[tid * N + i] = before_w;
-      b.near_count[tid * N + i] = (uint32_t)before_c;
-      before_w += nw[i];
-      before_c += nc[i];
+          for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], lds[e * NT + (tid ^ m)], larger);
+      } else if (works && j < E) {
+#pragma unroll
+        for (int step = 1; step < E; step *= 2) {
+          if (step != j) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            if (e & step) continue;
+            const bool swap = (x[e] < x[e + step]) == (((tid * E + e) & k) == 0);
+            const u64 a = x[e];
+            x[e] = swap ? x[e + step] : a;
+            x[e + step] = swap ? a : x[e + step];
+          }
+        }
+      } else if (works) {
+        const auto by = [&](auto other) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], other((uint64_t)x[e]), larger);
+        };
+        const auto swapped = [](uint64_t v, auto half) {  // the value of lane l ^ 32 (l ^ 16): the other of the two that the swap leaves
+          const uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
+          constexpr bool H = decltype(half)::value;
+          const auto l = H ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+          const auto h = H ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+          const bool upper = threadIdx.x & (H ? 32 : 16);
+          return (uint64_t)(uint32_t)(upper ? h[0] : h[1]) << 32 | (uint32_t)(upper ? l[0] : l[1]);
+        };
+        if (m == 1) by([](uint64_t v) { return dpp<0xB1>(v); });
+        else if (m == 2) by([](uint64_t v) { return dpp<0x4E>(v); });
+        else if (m == 4) by([](uint64_t v) { return dpp<0x1B>(dpp<0x141>(v)); });  // 7, then 3
+        else if (m == 8) by([](uint64_t v) { return dpp<0x128>(v); });
+        else if (m == 16) by([&](uint64_t v) { return swapped(v, std::false_type{}); });
+        else by([&](uint64_t v) { return swapped(v, std::true_type{}); });
+      }
     }
   }
-  __syncthreads();
-  for (int k = 2; k <= size; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
-      for (int i = tid; i < size / 2; i += NT) {
-        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-        const u64 x = words[lo], y = words[hi];
-        if ((x < y) == ((lo & k) == 0)) words[lo] = y, words[hi] = x;
-      }
-      __syncthreads();
-    }
-  // running weights, a thread's words side by side
-  const int per = (size + NT - 1) / NT, i0 = min(n, tid * per), i1 = min(n, i0 + per);
-  u64 own = 0, all;
-  for (int i = i0; i < i1; ++i) own += w.weight(w.below(logit_at(words[i])));
-  const u64 before = sum_before<NT>(own, b.scan[0], all);
-  const auto first_of_mine = [&](auto reaches) {  // reaches(count, weight, place) with the words up to this one
-    u64 run = before;
-    for (int i = i0; i < i1; ++i) {
-      const double y = w.below(logit_at(words[i]));
+}
+
+struct Answer {
+  u64 place, weight;
+};
+template <int NT>
+struct ResolveSpace {
+  Sums scan[NT / 64];
+  Answer answer[3];
+};
+
+// Sorted words, E of them in a thread (0: none), answer all questions: those of the near bins, or (ALL) every one of a row.
+template <int NT, int E, bool ALL>
+__device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64 (&x)[E], ResolveSpace<NT>& sp) {
+  const int tid = threadIdx.x;
+  // weights and counts up to and with every word
+  u64 own[E], weight[E], count[E];
+  Sums sum = {0, 0}, all;
+  u64 in_bin = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float v = logit_at(x[e]);
+    const double y = w.below(v);
+    const bool word = x[e] != 0;
+    own[e] = word ? w.weight(y) : 0;
+    sum.weight += own[e];
+    weight[e] = sum.weight;
+    count[e] = tid * E + e + 1;
+    bool in_m_bin = true;
+    if constexpr (!ALL) {
       const int bin = w.bin(y);
-      run += w.weight(y);
-      if (reaches((u64)(i + 1) + b.count[bin] - b.near_count[bin], run + b.weight[bin] - b.near_weight[bin], words[i])) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool here = word && bin >= near.lo[i] && bin <= near.hi[i];
+        weight[e] += here ? near.weight[i] : 0;
+        count[e] += here ? near.count[i] : 0;
+      }
+      in_m_bin = bin == near.m_bin;
     }
-  };
-  __shared__ u64 s_place, s_weight;
-  // where the running count (weight) first reaches a number, inside a thread's words: the word in front of it has not
-  const auto find = [&](bool by_count, u64 target, u64& place, u64& weight) {
+    if (word && in_m_bin && w.over(v, a.min_z)) in_bin += own[e];
+  }
+  sum.count = in_bin;
+  const Sums before = sums_before<NT>(sum, sp.scan, all);
+  in_bin = all.count;
+#pragma unroll
+  for (int e = 0; e < E; ++e) weight[e] += before.weight;
+  const auto find = [&](int question, bool by_count, u64 target) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const u64 now = by_count ? count[e] : weight[e], front = now - (by_count ? 1 : own[e]);
+      if (x[e] && front < target && target <= now) sp.answer[question] = Answer{x[e], weight[e]};
+    }
     __syncthreads();
-    first_of_mine([&](u64 c, u64 wt, u64 p) {
-      const u64 self = w.weight(w.below(logit_at(p)));
-      const u64 now = by_count ? c : wt, front = by_count ? c - 1 : wt - self;
-      if (front < target && target <= now) s_place = p, s_weight = wt;
-      return now >= target;
-    });
-    __syncthreads();
-    place = s_place;
-    weight = s_weight;
+    return sp.answer[question];
   };
   Cut cut = {1, -1};
-  u64 stay = b.weight[kBins], place, weight;
+  u64 stay = ALL ? all.weight : near.all;
   if (near.k_on) {
-    find(true, (u64)a.top_k, place, weight);
-    cut.from = place;
-    stay = weight;
+    const Answer k = find(0, true, (u64)a.top_k);
+    cut.from = k.place;
+    stay = k.weight;
   }
   if (near.p_on) {
-    find(false, top_p_target(a.top_p, stay), place, weight);
-    cut.from = max(cut.from, place);
-    stay = weight;
+    const Answer p = find(1, false, top_p_target(a.top_p, stay));
+    cut.from = max(cut.from, p.place);
+    stay = p.weight;
   }
   if (a.tokens) {
-    if (near.m_on) {
-      // the weight of the words over the border: of the bins in front of the border's, and of its own words that are
-      u64 in_bin = 0;
-      for (int i = i0; i < i1; ++i) {
-        const float x = logit_at(words[i]);
-        const double y = w.below(x);
-        if (w.bin(y) == near.lo[2] && w.over(x, a.min_z)) in_bin += w.weight(y);
-      }
-      stay = min(stay, b.weight[near.lo[2]] + sum_all<NT>(in_bin, b.scan[1]));
-    }
-    find(false, draw_target(u, stay), place, weight);
-    cut.token = token_at(place);
+    // over the border of min_p: the bins in front of the border's, and its own words that are
+    if (near.m_on) stay = min(stay, (ALL ? 0 : near.m_front) + in_bin);
+    cut.token = token_at(find(2, false, draw_target(u, stay)).place);
   }
   return cut;
+}
+template <int NT, int E>
+__device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, u64* lds, ResolveSpace<NT>& sp) {
+  u64 x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = threadIdx.x * E + e;
+    x[e] = i < n ? words[i] : 0;
+  }
+  if constexpr (E == 2) {
+    if (n <= 128) sort_words<NT, E, 128>(x, 0, lds);
+    else if (n <= 256) sort_words<NT, E, 256>(x, 0, lds);
+    else if (n <= 512) sort_words<NT, E, 512>(x, 0, lds);
+    else sort_words<NT, E, 1024>(x, 0, lds);
+  } else {
+    int size = 2048;
+    while (size < n) size *= 2;
+    sort_words<NT, E, 0>(x, size, lds);
+  }
+  return resolve<NT, E, false>(a, w, u, near, x, sp);
+}
+template <int NT>
+__device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, u64* lds, ResolveSpace<NT>& sp) {
+  if (n <= 1024) return resolve_list<NT, 2>(a, w, u, near, words, n, lds, sp);
+  return resolve_list<NT, kNear / NT>(a, w, u, near, words, n, lds, sp);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -327,7 +469,7 @@ struct Digits {
 // The place of the first word at which the count (or weight) of the words so far reaches `target`, 1 or more, which all words from `limit`
 // on together do.
 template <int NT, bool BY_WEIGHT>
-__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 target, u64 limit, Digits& d, u64 (&scan)[NT / 64], u64& s_bin) {
+__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 target, u64 limit, Digits& d, Sums* scan, u64& s_bin) {
   const int tid = threadIdx.x;
   constexpr int N = kDigitBins / NT;
   u64 prefix = 0;
@@ -345,10 +487,11 @@ __device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 tar
       else atomicAdd(&d.count[bin], 1u);
     });
     __syncthreads();
-    u64 n[N], sum = 0, all;
+    u64 n[N], sum = 0;
+    Sums all;
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += n[i] = BY_WEIGHT ? d.weight[tid * N + i] : d.count[tid * N + i];
-    u64 before = sum_before<NT>(sum, scan, all);
+    u64 before = sums_before<NT>(Sums{sum, 0}, scan, all).weight;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (before < target && target <= before + n[i]) {
@@ -366,7 +509,7 @@ __device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 tar
 }
 
 template <int NT>
-__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const float* row, Digits& d, u64 (&scan)[NT / 64]) {
+__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const float* row, Digits& d, Sums* scan) {
   __shared__ u64 s_bin;
   const auto sum_from = [&](u64 limit, auto of) {
     u64 s = 0;
@@ -397,6 +540,40 @@ union SampleSpace {
   };
   Digits digits;
 };
+__device__ __forceinline__ bool no_word(float top) { return !(top > -INFINITY && top < INFINITY); }
+
+// Highest and lowest logit of the words of a workgroup's part of a row.
+template <int NT>
+__device__ __forceinline__ float2 ends_of(const float* row, int v0, int v1, float* sh) {
+  float hi = -INFINITY, lo = INFINITY;
+  each_word<NT>(row, v0, v1, [&](float x, int) {
+    hi = fmaxf(hi, x);
+    lo = fminf(lo, x);
+  });
+  hi = block_max<NT / 64>(hi, sh);
+  lo = -block_max<NT / 64>(-lo, sh + NT / 64);
+  return make_float2(hi, lo);
+}
+template <int NT>
+__device__ __forceinline__ void add_to_bins(const Weigher& w, const float* row, int v0, int v1, u64* weight, uint32_t* count) {
+  each_word<NT>(row, v0, v1, [&](float x, int) {
+    const double y = w.below(x);
+    const int b = w.bin(y);
+    atomicAdd(&count[b], 1u);
+    if (y < kFar) atomicAdd(&weight[b], w.weight(y));
+  });
+}
+// The near words of a part of a row, listed in LDS in any order; *n counts them, those past kNear too.
+template <int NT>
+__device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, int v0, int v1, u64* words, int* n) {
+  const float half = 0.5f * (float)w.top, per = 2.f * (float)w.log2e_T;  // the difference of two logits may overflow, of their halves not
+  const bool rough = w.log2e_T > 1e-30 && w.log2e_T < 1e30;
+  each_word<NT>(row, v0, v1, [&](float x, int v) {
+    if ((rough && !near.may_have((half - 0.5f * x) * per)) || !near.has(w.bin(w.below(x)))) return;
+    const int at = atomicAdd(n, 1);
+    if (at < kNear) words[at] = place_of(x, v);
+  });
+}
 
 template <int NT>
 __device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w, const Cut& cut, const float* row, float* out, int v0, int v1) {
@@ -420,102 +597,139 @@ __device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w,
 template <int NT>
 __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   __shared__ SampleSpace<NT> sp;
-  __shared__ float s_max[NT / 64];
+  __shared__ ResolveSpace<NT> rs;
+  __shared__ float s_ends[2 * NT / 64];
+  __shared__ NearBins near;
   __shared__ int s_near;
-  __shared__ u64 s_scan[NT / 64];
   const int tid = threadIdx.x;
   const size_t r = blockIdx.x;
   const float* row = a.logits + r * a.V;
   float* out = a.out ? a.out + r * a.V : nullptr;
   for (int i = tid; i < kBins; i += NT) sp.bins.weight[i] = 0, sp.bins.count[i] = 0;
   if (tid == 0) s_near = 0;
-  float top = -INFINITY;
-  each_word<NT>(row, 0, a.V, [&](float x, int) { top = fmaxf(top, x); });
-  top = block_max<NT / 64>(top, s_max);
-  if (!(top > -INFINITY && top < INFINITY)) {
+  const float2 ends = ends_of<NT>(row, 0, a.V, s_ends);
+  if (no_word(ends.x)) {
     if (a.tokens && tid == 0) a.tokens[r] = -1;
     if (out)
       for (int v = tid; v < a.V; v += NT) out[v] = -INFINITY;
     return;
   }
-  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  const Weigher w(a, ends.x, ends.y);
   const double u = a.tokens ? (double)a.u[r] : 0.0;
-  each_word<NT>(row, 0, a.V, [&](float x, int) {
-    const double y = w.below(x);
-    const int b = w.bin(y);
-    atomicAdd(&sp.bins.count[b], 1u);
-    atomicAdd(&sp.bins.weight[b], w.weight(y));
-  });
+  add_to_bins<NT>(w, row, 0, a.V, sp.bins.weight, sp.bins.count);
   __syncthreads();
-  scan_bins(sp.bins);
-  const Near near = near_bins(a, w, u, sp.bins);
-  each_word<NT>(row, 0, a.V, [&](float x, int v) {
-    if (!near.has(w.bin(w.below(x)))) return;
-    const int at = atomicAdd(&s_near, 1);
-    if (at < kNear) sp.words[at] = place_of(x, v);
-  });
-  __syncthreads();
-  const int n = s_near;
+  constexpr int N = kBins / NT;
+  u64 bw[N];
+  uint32_t bc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) bw[i] = sp.bins.weight[tid * N + i], bc[i] = sp.bins.count[tid * N + i];
+  scan_bins(sp.bins, bw, bc);
+  near_bins(a, w, u, sp.bins, near);
   Cut cut;
-  if (n <= kNear) {
-    cut = resolve(a, w, u, sp.bins, near, sp.words, n);
+  if (near.n_count <= kNear) {
+    list_near<NT>(w, near, row, 0, a.V, sp.words, &s_near);
+    __syncthreads();
+    cut = resolve_any<NT>(a, w, u, near, sp.words, near.n_count, sp.words, rs);
   } else {
     __syncthreads();
-    cut = resolve_by_digits<NT>(a, w, u, row, sp.digits, s_scan);
+    cut = resolve_by_digits<NT>(a, w, u, row, sp.digits, rs.scan);
   }
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
   if (out) write_row<NT>(a, w, cut, row, out, 0, a.V);
 }
 
-// ------------------------------------------------------------------------------------------
-// A row to several workgroups, in four launches: (1) the slices' highest logits; (2) their bins, added up; (3) the words of the near
-// bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
-// ------------------------------------------------------------------------------------------
-constexpr int kSliceNT = 512, kMaxSlices = 64;
+// A short row: all of its words are sorted.
+template <int E>
+__global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
+  constexpr int NT = 256;
+  __shared__ u64 s_words[NT * E];
+  __shared__ ResolveSpace<NT> rs;
+  __shared__ float s_ends[2 * NT / 64];
+  const int tid = threadIdx.x;
+  const size_t r = blockIdx.x;
+  const float* row = a.logits + r * a.V;
+  float* out = a.out ? a.out + r * a.V : nullptr;
+  const double u = a.tokens ? (double)a.u[r] : 0.0;
+  float v[E];  // which words a thread brings is all the same to the sort: those that lie side by side in memory
+  u64 x[E];
+  float hi = -INFINITY;
+  int words = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = e * NT + tid;
+    v[e] = i < a.V ? row[i] : -INFINITY;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    x[e] = place_of(v[e], e * NT + tid);
+    words += x[e] != 0;
+    hi = fmaxf(hi, v[e]);
+  }
+  const float top = block_max<NT / 64>(hi, s_ends);
+  if (no_word(top)) {
+    if (a.tokens && tid == 0) a.tokens[r] = -1;
+    if (out)
+      for (int i = tid; i < a.V; i += NT) out[i] = -INFINITY;
+    return;
+  }
+  const Weigher w(a, top, top);
+  NearBins near;
+  near.k_on = a.top_k > 0 && (u64)a.top_k < sum_all<NT>((u64)words, rs.scan);
+  near.p_on = a.top_p < 1.0;
+  near.m_on = a.min_z > -INFINITY;
+  sort_words<NT, E, NT * E>(x, 0, s_words);
+  __syncthreads();
+  const Cut cut = resolve<NT, E, true>(a, w, u, near, x, rs);
+  if (a.tokens && tid == 0) a.tokens[r] = cut.token;
+  if (out)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = e * NT + tid;
+      if (i < a.V) out[i] = place_of(v[e], i) >= cut.from && w.over(v[e], a.min_z) ? v[e] : -INFINITY;
+    }
+}
 
-__device__ __forceinline__ float top_of(const SampleArgs& a, float* s_top) {
+// ------------------------------------------------------------------------------------------
+// A row to several workgroups, in four launches: (1) the slices' highest and lowest logits; (2) their bins, added up; (3) the words of the
+// near bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
+// ------------------------------------------------------------------------------------------
+constexpr int kSliceNT = 1024, kMaxSlices = 64;
+
+__device__ __forceinline__ float2 row_ends(const SampleArgs& a, float2* s_ends) {
   if (threadIdx.x < 64) {
-    const float* m = a.slice_max + (size_t)blockIdx.y * kMaxSlices;
-    const float top = lanes_max((int)threadIdx.x < a.slices ? m[threadIdx.x] : -INFINITY, 64);
-    if (threadIdx.x == 0) *s_top = top;
+    const float2 e = (int)threadIdx.x < a.slices ? a.slice_ends[(size_t)blockIdx.y * kMaxSlices + threadIdx.x] : make_float2(-INFINITY, INFINITY);
+    const float hi = lanes_max(e.x, 64), lo = -lanes_max(-e.y, 64);
+    if (threadIdx.x == 0) *s_ends = make_float2(hi, lo);
   }
   __syncthreads();
-  return *s_top;
+  return *s_ends;
 }
-__device__ __forceinline__ bool no_word(float top) { return !(top > -INFINITY && top < INFINITY); }
 
 // grid (slices, rows), all of them
-__global__ __launch_bounds__(kSliceNT) void sample_max_kernel(SampleArgs a) {
-  __shared__ float s_max[kSliceNT / 64];
+__global__ __launch_bounds__(kSliceNT) void sample_ends_kernel(SampleArgs a) {
+  __shared__ float s_ends[2 * kSliceNT / 64];
   const size_t r = blockIdx.y;
   const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
   for (int i = blockIdx.x * kSliceNT + threadIdx.x; i <= kBins; i += a.slices * kSliceNT) {
     if (i < kBins) a.weight[r * kBins + i] = 0;
     a.count[r * (kBins + 1) + i] = 0;
   }
-  float top = -INFINITY;
-  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int) { top = fmaxf(top, x); });
-  top = block_max<kSliceNT / 64>(top, s_max);
-  if (threadIdx.x == 0) a.slice_max[r * kMaxSlices + blockIdx.x] = top;
+  const float2 ends = ends_of<kSliceNT>(a.logits + r * a.V, v0, v1, s_ends);
+  if (threadIdx.x == 0) a.slice_ends[r * kMaxSlices + blockIdx.x] = ends;
 }
 
 __global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
   __shared__ u64 s_weight[kBins];
   __shared__ uint32_t s_count[kBins];
-  __shared__ float s_top;
+  __shared__ float2 s_ends;
   const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
   const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
   for (int i = tid; i < kBins; i += kSliceNT) s_weight[i] = 0, s_count[i] = 0;
-  const float top = top_of(a, &s_top);
-  if (no_word(top)) return;
-  const Weigher w = {(double)top, a.log2e_T, a.unit};
-  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int) {
-    const double y = w.below(x);
-    const int b = w.bin(y);
-    atomicAdd(&s_count[b], 1u);
-    atomicAdd(&s_weight[b], w.weight(y));
-  });
+  const float2 ends = row_ends(a, &s_ends);
+  if (no_word(ends.x)) return;
+  const Weigher w(a, ends.x, ends.y);
+  add_to_bins<kSliceNT>(w, a.logits + r * a.V, v0, v1, s_weight, s_count);
   __syncthreads();
   for (int i = tid; i < kBins; i += kSliceNT)
     if (s_count[i]) {
@@ -524,65 +738,70 @@ __global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
     }
 }
 
-template <int NT>
-__device__ __forceinline__ void load_bins(const SampleArgs& a, size_t r, Bins<NT>& b) {
-  for (int i = threadIdx.x; i < kBins; i += NT) {
-    b.weight[i] = a.weight[r * kBins + i];
-    b.count[i] = a.count[r * (kBins + 1) + i];
-  }
-  __syncthreads();
-  scan_bins(b);
-}
-
 __global__ __launch_bounds__(kSliceNT) void sample_near_kernel(SampleArgs a) {
   __shared__ Bins<kSliceNT> bins;
-  __shared__ float s_top;
+  __shared__ u64 s_words[kNear];
+  __shared__ float2 s_ends;
+  __shared__ NearBins near;
+  __shared__ int s_n, s_at;
+  constexpr int N = kBins / kSliceNT;
+  const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
   const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
-  const float top = top_of(a, &s_top);
-  if (no_word(top)) return;
-  const Weigher w = {(double)top, a.log2e_T, a.unit};
-  load_bins(a, r, bins);
-  const Near near = near_bins(a, w, a.tokens ? (double)a.u[r] : 0.0, bins);
-  each_word<kSliceNT>(a.logits + r * a.V, v0, v1, [&](float x, int v) {
-    if (!near.has(w.bin(w.below(x)))) return;
-    const uint32_t at = atomicAdd(&a.count[r * (kBins + 1) + kBins], 1u);
-    if (at < kNear) a.near[r * kNear + at] = place_of(x, v);
-  });
+  u64 bw[N];
+  uint32_t bc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) bw[i] = a.weight[r * kBins + tid * N + i], bc[i] = a.count[r * (kBins + 1) + tid * N + i];
+  const double u = a.tokens ? (double)a.u[r] : 0.0;
+  if (tid == 0) s_n = 0;
+  const float2 ends = row_ends(a, &s_ends);
+  if (no_word(ends.x)) return;
+  const Weigher w(a, ends.x, ends.y);
+  scan_bins(bins, bw, bc);
+  near_bins(a, w, u, bins, near);
+  if (blockIdx.x == 0 && tid == 0) a.bins[r] = near;
+  if (near.n_count > kNear) return;
+  list_near<kSliceNT>(w, near, a.logits + r * a.V, v0, v1, s_words, &s_n);
+  __syncthreads();
+  const int n = s_n;
+  if (n == 0) return;
+  if (tid == 0) s_at = (int)atomicAdd(&a.count[r * (kBins + 1) + kBins], (uint32_t)n);
+  __syncthreads();
+  for (int i = tid; i < n; i += kSliceNT) a.near[r * kNear + s_at + i] = s_words[i];
 }
 
 // grid (slices or 1, rows)
 __global__ __launch_bounds__(kSliceNT) void sample_finish_kernel(SampleArgs a) {
-  __shared__ SampleSpace<kSliceNT> sp;
-  __shared__ float s_top;
-  __shared__ u64 s_scan[kSliceNT / 64];
+  __shared__ union {
+    u64 words[kNear];
+    Digits digits;
+  } sp;
+  __shared__ ResolveSpace<kSliceNT> rs;
+  __shared__ float2 s_ends;
   const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
   const float* row = a.logits + r * a.V;
   float* out = a.out ? a.out + r * a.V : nullptr;
   int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
-  const float top = top_of(a, &s_top);
-  if (no_word(top)) {
+  const float2 ends = row_ends(a, &s_ends);
+  if (no_word(ends.x)) {
     if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = -1;
     if (out)
       for (int v = v0 + tid; v < v1; v += kSliceNT) out[v] = -INFINITY;
     return;
   }
-  const Weigher w = {(double)top, a.log2e_T, a.unit};
+  const Weigher w(a, ends.x, ends.y);
   const double u = a.tokens ? (double)a.u[r] : 0.0;
-  const uint32_t n = a.count[r * (kBins + 1) + kBins];
+  const NearBins near = a.bins[r];
   Cut cut;
-  if (n <= kNear) {
-    load_bins(a, r, sp.bins);
-    const Near near = near_bins(a, w, u, sp.bins);
-    for (int i = tid; i < (int)n; i += kSliceNT) sp.words[i] = a.near[r * kNear + i];
-    cut = resolve(a, w, u, sp.bins, near, sp.words, (int)n);
+  if (near.n_count <= kNear) {
+    cut = resolve_any<kSliceNT>(a, w, u, near, a.near + r * kNear, near.n_count, sp.words, rs);
   } else {
     // one workgroup reads the whole row, which may be where the results go
     if (blockIdx.x > 0) return;
     v0 = 0;
     v1 = a.V;
-    cut = resolve_by_digits<kSliceNT>(a, w, u, row, sp.digits, s_scan);
+    cut = resolve_by_digits<kSliceNT>(a, w, u, row, sp.digits, rs.scan);
   }
   if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = cut.token;
   if (out) write_row<kSliceNT>(a, w, cut, row, out, v0, v1);
@@ -590,9 +809,9 @@ __global__ __launch_bounds__(kSliceNT) void sample_finish_kernel(SampleArgs a) {
 
 static int sample_slices(int rows, int V) {
   if (V <= kShortRow) return 1;
-  return std::max(1, std::min({kMaxSlices, (V + 2047) / 2048, 512 / rows}));
+  return std::max(1, std::min({kMaxSlices, (V + 4095) / 4096, 512 / rows}));
 }
-static size_t sample_row_bytes() { return kMaxSlices * sizeof(float) + kBins * sizeof(u64) + (kBins + 4) * sizeof(uint32_t) + kNear * sizeof(u64); }
+static size_t sample_row_bytes() { return kMaxSlices * sizeof(float2) + kBins * sizeof(u64) + (kBins + 1) * sizeof(uint32_t) + kNear * sizeof(u64) + sizeof(NearBins); }
 size_t sample_workspace_bytes(int rows, int V) { return sample_slices(rows, V) > 1 ? rows * sample_row_bytes() : 16; }
 
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
@@ -608,17 +827,20 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   a.tokens = tokens_out; a.out = logits_out;
   a.slices = sample_slices(rows, V);
   if (a.slices == 1) {
-    if (V <= kShortRow) hipLaunchKernelGGL(sample_row_kernel<256>, dim3(rows), dim3(256), 0, st, a);
+    if (V <= 512) hipLaunchKernelGGL(sample_short_kernel<2>, dim3(rows), dim3(256), 0, st, a);
+    else if (V <= 1024) hipLaunchKernelGGL(sample_short_kernel<4>, dim3(rows), dim3(256), 0, st, a);
+    else if (V <= kShortRow) hipLaunchKernelGGL(sample_short_kernel<8>, dim3(rows), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
     return;
   }
   a.per = (V + a.slices - 1) / a.slices;
   a.weight = (u64*)ws;
   a.near = a.weight + (size_t)rows * kBins;
-  a.count = (uint32_t*)(a.near + (size_t)rows * kNear);
-  a.slice_max = (float*)(a.count + (size_t)rows * (kBins + 1));
+  a.bins = (NearBins*)(a.near + (size_t)rows * kNear);
+  a.slice_ends = (float2*)(a.bins + rows);
+  a.count = (uint32_t*)(a.slice_ends + (size_t)rows * kMaxSlices);
   const dim3 grid(a.slices, rows), block(kSliceNT);
-  hipLaunchKernelGGL(sample_max_kernel, grid, block, 0, st, a);
+  hipLaunchKernelGGL(sample_ends_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_near_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_finish_kernel, dim3(a.out ? a.slices : 1, rows), block, 0, st, a);

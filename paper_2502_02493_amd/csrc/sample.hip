@@ -49,8 +49,8 @@ struct SampleArgs {
   double unit;            // 2^s
   int32_t* tokens;
   float* out;
-  // rows cut into slices
-  int slices, per;
+  // rows cut into slices, and into more of them where a workgroup has little to do
+  int slices, per, cuts, per_cut, parts, per_part;
   float2* slice_ends;  // [row][slices]  highest and lowest logit
   u64* weight;         // [row][kBins]
   uint32_t* count;     // [row][kBins + 1], the last one counting near words
@@ -76,11 +76,26 @@ struct Weigher {
     const uint32_t b = __float_as_uint((float)(y * (1.0 / far)));
     return kFineBins + min(max((int)(b >> 21) - (127 << 2), 0), kBins - kFineBins - 1);
   }
-  __device__ __forceinline__ float bin_start(int b) const {  // y, to 1e-6
-    if (b <= kFineBins) return (float)((double)b / per_y);
-    return b >= kBins ? INFINITY : (float)far * __uint_as_float((uint32_t)(b - kFineBins + (127 << 2)) << 21);
+  // A logit that all words of bin b are below (times < 1) or above (times > 1): y at the bin's start, rounded outwards.
+  __device__ __forceinline__ float logit_at_bin(int b, double times) const {
+    if (b >= kBins) return times > 1.0 ? -INFINITY : INFINITY;
+    const double y = b <= kFineBins ? (double)b / per_y : far * (double)__uint_as_float((uint32_t)(b - kFineBins + (127 << 2)) << 21);
+    const double x = top - y * times / log2e_T, room = 1e-6 * (fabs(top) + fabs(x)) + 1e-37;
+    return (float)(times > 1.0 ? x - room : x + room);
   }
   __device__ __forceinline__ bool over(float x, double min_z) const { return (double)x - top >= min_z; }
+  __device__ __forceinline__ float least_over(double min_z) const {  // the lowest number that is
+    if (min_z == -INFINITY) return -INFINITY;
+    const float x = (float)(top + min_z);  // or its neighbour
+    if (!over(x, min_z)) return next(x, true);
+    const float below = next(x, false);
+    return over(below, min_z) ? below : x;
+  }
+  static __device__ __forceinline__ float next(float x, bool up) {
+    if (x == 0.f) return __uint_as_float(up ? 1u : 0x80000001u);
+    const uint32_t u = __float_as_uint(x);
+    return __uint_as_float((x > 0.f) == up ? u + 1 : u - 1);
+  }
 };
 
 // Words of row[v0, v1): body(x, v), eight loads of a thread under way.
@@ -162,17 +177,11 @@ struct NearBins {
   int lo[4], hi[4], n_count, k_on, p_on, m_on, m_bin, pad;
   u64 weight[4], count[4];  // not on the list, in front of the run
   u64 all, m_front;         // the row's weight; what is in front of the border's bin of min_p
-  float y0[4], y1[4];       // the runs in y, a little wider
+  float x0, x1;             // logits outside are in none of the runs
   __device__ __forceinline__ bool has(int bin) const {
     bool in = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) in = in || (bin >= lo[i] && bin <= hi[i]);
-    return in;
-  }
-  __device__ __forceinline__ bool may_have(float y) const {
-    bool in = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) in = in || (y >= y0[i] && y <= y1[i]);
     return in;
   }
 };
@@ -229,15 +238,13 @@ __device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, 
     }
   };
   order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
-  int end = -1;  // of the runs so far
+  int end = -1, first = kBins;  // of the runs so far
   u64 listed_w = 0, listed_c = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     n.lo[i] = max(lo[i], end + 1);
     n.hi[i] = lo[i] < kBins ? hi[i] : -1;
     const bool any = n.lo[i] <= n.hi[i];
-    n.y0[i] = INFINITY;
-    n.y1[i] = -INFINITY;
     n.weight[i] = n.count[i] = 0;
     if (any) {
       const u64 w0 = b.weight[n.lo[i]], c0 = b.count[n.lo[i]];
@@ -246,11 +253,12 @@ __device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, 
       listed_w += b.weight[n.hi[i] + 1] - w0;
       listed_c += b.count[n.hi[i] + 1] - c0;
       end = n.hi[i];
-      n.y0[i] = w.bin_start(n.lo[i]) * (1.f - 1e-5f) - 1e-30f;
-      n.y1[i] = w.bin_start(n.hi[i] + 1) * (1.f + 1e-5f);
+      first = min(first, n.lo[i]);
     }
   }
   n.n_count = (int)listed_c;
+  n.x0 = w.logit_at_bin(end + 1, 1.0 + 1e-5);
+  n.x1 = w.logit_at_bin(first, 1.0 - 1e-5);
 }
 
 // Which bins matter.  b: sums in front of the bins.  The weight of the first top_k words, and of all that stay, is known here up to the
@@ -440,22 +448,27 @@ __device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& 
     const int i = threadIdx.x * E + e;
     x[e] = i < n ? words[i] : 0;
   }
-  if constexpr (E == 2) {
-    if (n <= 128) sort_words<NT, E, 128>(x, 0, lds);
-    else if (n <= 256) sort_words<NT, E, 256>(x, 0, lds);
-    else if (n <= 512) sort_words<NT, E, 512>(x, 0, lds);
-    else sort_words<NT, E, 1024>(x, 0, lds);
-  } else {
-    int size = 2048;
-    while (size < n) size *= 2;
-    sort_words<NT, E, 0>(x, size, lds);
-  }
+  if (n <= 128) sort_words<NT, E, 128>(x, 0, lds);
+  else if (n <= 256) sort_words<NT, E, 256>(x, 0, lds);
+  else if (n <= 512) sort_words<NT, E, 512>(x, 0, lds);
+  else if constexpr (NT * E >= 1024) sort_words<NT, E, 1024>(x, 0, lds);
   return resolve<NT, E, false>(a, w, u, near, x, sp);
 }
 template <int NT>
 __device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, u64* lds, ResolveSpace<NT>& sp) {
-  if (n <= 1024) return resolve_list<NT, 2>(a, w, u, near, words, n, lds, sp);
-  return resolve_list<NT, kNear / NT>(a, w, u, near, words, n, lds, sp);
+  if (n <= (NT >= 512 ? 1024 : 512)) return resolve_list<NT, 2>(a, w, u, near, words, n, lds, sp);
+  // more than that: not unrolled
+  constexpr int E = kNear / NT;
+  u64 x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = threadIdx.x * E + e;
+    x[e] = i < n ? words[i] : 0;
+  }
+  int size = 2 * E;
+  while (size < n) size *= 2;
+  sort_words<NT, E, 0>(x, size, lds);
+  return resolve<NT, E, false>(a, w, u, near, x, sp);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -563,21 +576,46 @@ __device__ __forceinline__ void add_to_bins(const Weigher& w, const float* row, 
     if (y < kFar) atomicAdd(&weight[b], w.weight(y));
   });
 }
-// The near words of a part of a row, listed in LDS in any order; *n counts them, those past kNear too.
+// The near words of a part of a row, listed in any order: a wave asks for places once for every eight words of its lanes.
 template <int NT>
-__device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, int v0, int v1, u64* words, int* n) {
-  const float half = 0.5f * (float)w.top, per = 2.f * (float)w.log2e_T;  // the difference of two logits may overflow, of their halves not
-  const bool rough = w.log2e_T > 1e-30 && w.log2e_T < 1e30;
-  each_word<NT>(row, v0, v1, [&](float x, int v) {
-    if ((rough && !near.may_have((half - 0.5f * x) * per)) || !near.has(w.bin(w.below(x)))) return;
-    const int at = atomicAdd(n, 1);
-    if (at < kNear) words[at] = place_of(x, v);
-  });
+__device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, int v0, int v1, u64* words, uint32_t* n) {
+  constexpr int kAhead = 8;
+  const float x0 = near.x0, x1 = near.x1;
+  const int lane = threadIdx.x & 63;
+  for (int base = v0; base < v1; base += kAhead * NT) {
+    float x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int v = base + i * NT + (int)threadIdx.x;
+      x[i] = v < v1 ? row[v] : -INFINITY;
+    }
+    unsigned long long in[kAhead];
+    int found = 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      bool is = x[i] > -INFINITY && x[i] >= x0 && x[i] <= x1;
+      if (is) is = near.has(w.bin(w.below(x[i])));
+      in[i] = __ballot(is);
+      found += __popcll(in[i]);
+    }
+    if (found == 0) continue;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(n, (uint32_t)found);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (in[i] >> lane & 1) words[at + __popcll(in[i] & ((1ull << lane) - 1))] = place_of(x[i], base + i * NT + (int)threadIdx.x);
+      at += __popcll(in[i]);
+    }
+  }
 }
 
 template <int NT>
 __device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w, const Cut& cut, const float* row, float* out, int v0, int v1) {
   constexpr int N = 8;
+  // what stays, as numbers: logits over one, and of those equal to it the first tokens
+  const float last = cut.from > 1 ? logit_at(cut.from) : -INFINITY, least = w.least_over(a.min_z);
+  const int token = cut.from > 1 ? token_at(cut.from) : -1;
   for (int base = v0; base < v1; base += N * NT) {
     float x[N];
 #pragma unroll
@@ -588,8 +626,8 @@ __device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w,
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int v = base + i * NT + (int)threadIdx.x;
-      const u64 p = place_of(x[i], v);
-      if (v < v1) out[v] = p >= cut.from && w.over(x[i], a.min_z) ? x[i] : -INFINITY;
+      const bool stays = (x[i] > last || (x[i] == last && v <= token)) && x[i] >= least;
+      if (v < v1) out[v] = stays ? x[i] : -INFINITY;
     }
   }
 }
@@ -600,7 +638,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   __shared__ ResolveSpace<NT> rs;
   __shared__ float s_ends[2 * NT / 64];
   __shared__ NearBins near;
-  __shared__ int s_near;
+  __shared__ uint32_t s_near;
   const int tid = threadIdx.x;
   const size_t r = blockIdx.x;
   const float* row = a.logits + r * a.V;
@@ -694,6 +732,8 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
 // near bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
 // ------------------------------------------------------------------------------------------
 constexpr int kSliceNT = 1024, kMaxSlices = 64;
+constexpr int kCutNT = 256, kMaxCuts = 64, kCutWgs = 2048;
+constexpr int kPartNT = 512, kMaxParts = 64, kPartWgs = 512;
 
 __device__ __forceinline__ float2 row_ends(const SampleArgs& a, float2* s_ends) {
   if (threadIdx.x < 64) {
@@ -738,56 +778,47 @@ __global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
     }
 }
 
-__global__ __launch_bounds__(kSliceNT) void sample_near_kernel(SampleArgs a) {
-  __shared__ Bins<kSliceNT> bins;
-  __shared__ u64 s_words[kNear];
-  __shared__ float2 s_ends;
+// grid (cuts, rows)
+__global__ __launch_bounds__(kCutNT) void sample_near_kernel(SampleArgs a) {
+  __shared__ Bins<kCutNT> bins;
   __shared__ NearBins near;
-  __shared__ int s_n, s_at;
-  constexpr int N = kBins / kSliceNT;
+  __shared__ float2 s_ends;
+  constexpr int N = kBins / kCutNT;
   const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
-  const int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  const int v0 = min(a.V, (int)blockIdx.x * a.per_cut), v1 = min(a.V, v0 + a.per_cut);
   u64 bw[N];
   uint32_t bc[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) bw[i] = a.weight[r * kBins + tid * N + i], bc[i] = a.count[r * (kBins + 1) + tid * N + i];
   const double u = a.tokens ? (double)a.u[r] : 0.0;
-  if (tid == 0) s_n = 0;
   const float2 ends = row_ends(a, &s_ends);
   if (no_word(ends.x)) return;
   const Weigher w(a, ends.x, ends.y);
   scan_bins(bins, bw, bc);
   near_bins(a, w, u, bins, near);
   if (blockIdx.x == 0 && tid == 0) a.bins[r] = near;
-  if (near.n_count > kNear) return;
-  list_near<kSliceNT>(w, near, a.logits + r * a.V, v0, v1, s_words, &s_n);
-  __syncthreads();
-  const int n = s_n;
-  if (n == 0) return;
-  if (tid == 0) s_at = (int)atomicAdd(&a.count[r * (kBins + 1) + kBins], (uint32_t)n);
-  __syncthreads();
-  for (int i = tid; i < n; i += kSliceNT) a.near[r * kNear + s_at + i] = s_words[i];
+  if (near.n_count <= kNear) list_near<kCutNT>(w, near, a.logits + r * a.V, v0, v1, a.near + r * kNear, &a.count[r * (kBins + 1) + kBins]);
 }
 
-// grid (slices or 1, rows)
-__global__ __launch_bounds__(kSliceNT) void sample_finish_kernel(SampleArgs a) {
+// grid (parts or 1, rows)
+__global__ __launch_bounds__(kPartNT) void sample_finish_kernel(SampleArgs a) {
   __shared__ union {
     u64 words[kNear];
     Digits digits;
   } sp;
-  __shared__ ResolveSpace<kSliceNT> rs;
+  __shared__ ResolveSpace<kPartNT> rs;
   __shared__ float2 s_ends;
   const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
   const float* row = a.logits + r * a.V;
   float* out = a.out ? a.out + r * a.V : nullptr;
-  int v0 = min(a.V, (int)blockIdx.x * a.per), v1 = min(a.V, v0 + a.per);
+  int v0 = min(a.V, (int)blockIdx.x * a.per_part), v1 = min(a.V, v0 + a.per_part);
   const float2 ends = row_ends(a, &s_ends);
   if (no_word(ends.x)) {
     if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = -1;
     if (out)
-      for (int v = v0 + tid; v < v1; v += kSliceNT) out[v] = -INFINITY;
+      for (int v = v0 + tid; v < v1; v += kPartNT) out[v] = -INFINITY;
     return;
   }
   const Weigher w(a, ends.x, ends.y);
@@ -795,16 +826,16 @@ __global__ __launch_bounds__(kSliceNT) void sample_finish_kernel(SampleArgs a) {
   const NearBins near = a.bins[r];
   Cut cut;
   if (near.n_count <= kNear) {
-    cut = resolve_any<kSliceNT>(a, w, u, near, a.near + r * kNear, near.n_count, sp.words, rs);
+    cut = resolve_any<kPartNT>(a, w, u, near, a.near + r * kNear, near.n_count, sp.words, rs);
   } else {
     // one workgroup reads the whole row, which may be where the results go
     if (blockIdx.x > 0) return;
     v0 = 0;
     v1 = a.V;
-    cut = resolve_by_digits<kSliceNT>(a, w, u, row, sp.digits, rs.scan);
+    cut = resolve_by_digits<kPartNT>(a, w, u, row, sp.digits, rs.scan);
   }
   if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = cut.token;
-  if (out) write_row<kSliceNT>(a, w, cut, row, out, v0, v1);
+  if (out) write_row<kPartNT>(a, w, cut, row, out, v0, v1);
 }
 
 static int sample_slices(int rows, int V) {
@@ -834,6 +865,10 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
     return;
   }
   a.per = (V + a.slices - 1) / a.slices;
+  a.cuts = std::max(1, std::min({kMaxCuts, (V + 2047) / 2048, kCutWgs / rows}));
+  a.per_cut = (V + a.cuts - 1) / a.cuts;
+  a.parts = std::max(1, std::min({kMaxParts, (V + 2047) / 2048, kPartWgs / rows}));
+  a.per_part = (V + a.parts - 1) / a.parts;
   a.weight = (u64*)ws;
   a.near = a.weight + (size_t)rows * kBins;
   a.bins = (NearBins*)(a.near + (size_t)rows * kNear);
@@ -842,8 +877,8 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   const dim3 grid(a.slices, rows), block(kSliceNT);
   hipLaunchKernelGGL(sample_ends_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
-  hipLaunchKernelGGL(sample_near_kernel, grid, block, 0, st, a);
-  hipLaunchKernelGGL(sample_finish_kernel, dim3(a.out ? a.slices : 1, rows), block, 0, st, a);
+  hipLaunchKernelGGL(sample_near_kernel, dim3(a.cuts, rows), dim3(kCutNT), 0, st, a);
+  hipLaunchKernelGGL(sample_finish_kernel, dim3(a.out ? a.parts : 1, rows), dim3(kPartNT), 0, st, a);
 }
 
 }  // namespace es

@@ -36,8 +36,8 @@ __device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit) {
 }
 __device__ __forceinline__ float unit_of(uint32_t scale) { return __uint_as_float(scale << 23); }  // 255: infinity, of which the conversion makes NaN
 
-// One workgroup's place.  Without lists: a chunk of an entry's steps and a tile of its rows; with them, a token and a chunk of its list.
-template <bool LIST>
+// One workgroup's place.  Without lists: a chunk of an entry's steps and RT tiles of its rows; with them, a token and a chunk of its list.
+template <bool LIST, int RT>
 struct KvqPlace {
   int e, h, l, c, row0, rows, len, old;  // entry, KV head, layer, chunk; first row and how many; slots that any row sees; that all do but for
                                          // their own and those after
@@ -60,8 +60,8 @@ struct KvqPlace {
     } else {
       const int tile = w % en.tiles;
       c = w / en.tiles;
-      row0 = tile * 16;
-      rows = min(16, en.n * a.group - row0);
+      row0 = tile * 16 * RT;
+      rows = min(16 * RT, en.n * a.group - row0);
       n_tok = token_of(a, row0);
       old = en.len - en.n + n_tok;
       len = en.len - en.n + token_of(a, row0 + rows - 1) + 1;
@@ -73,72 +73,126 @@ struct KvqPlace {
   }
 };
 
-// Codes and scales of a step of 32 slots from s on, as the lane needs them.  Slots past the last fetch the last one.
+// The (layer, sequence, KV head)'s arrays.
+struct KvqRow {
+  const uint8_t *kc, *vc, *ks, *vs;
+};
+
+// Codes and scales of a step of 32 slots from s on, as the lane needs them.
 template <int HD>
 struct KvqStep {
-  static constexpr int KW = HD / 32;  // words of K codes of a lane and tile: 8 channels each
+  static constexpr int KW = HD / 32;  // words of K codes of a lane and tile: 8 channels each; scales of a slot
   uint32_t k[2][KW], v[2][4];
-  uint32_t ks[2], vs[2][4];
-  __device__ __forceinline__ void load(const uint8_t* kc, const uint8_t* ks_, const uint8_t* vc, const uint8_t* vs_, int s, int len) {
+  uint32_t ks[2], vs[2][KW];  // vs: the scales of the lane's four slots of a tile side by side
+  template <class T>
+  static __device__ __forceinline__ T fetch(const uint8_t* base, uint32_t offset) {  // scales may lie anywhere
+    T x;
+    __builtin_memcpy(&x, base + offset, sizeof(T));
+    return x;
+  }
+  __device__ __forceinline__ void load(const KvqRow& row, int s, int len) {
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    typedef uint32_t kword __attribute__((ext_vector_type(KW)));
+    if (s + kStep <= len) {
+      const uint8_t *kc = row.kc + (size_t)s * (HD / 2), *vc = row.vc + (size_t)s * (HD / 2), *ksb = row.ks + (size_t)s * KW, *vsb = row.vs + (size_t)s * KW;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t slot = min(s + 16 * t + c, len - 1);
-      const uint8_t* p = kc + slot * (HD / 2) + g * (HD / 8);
-      if constexpr (HD == 128) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+      for (int t = 0; t < 2; ++t) {
+        const kword x = *reinterpret_cast<const kword*>(kc + (uint32_t)(c * (HD / 2) + g * (HD / 8)) + t * 16 * (HD / 2));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) k[t][i] = x[i];
-      } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-        k[t][0] = x[0]; k[t][1] = x[1];
+        for (int i = 0; i < KW; ++i) k[t][i] = x[i];
+        ks[t] = (ksb + (uint32_t)(c * KW + (HD == 128 ? g : g >> 1)))[t * 16 * KW];
+        const uint8_t* vp = vc + (uint32_t)(4 * g * (HD / 2) + c * (HD / 32)) + t * 16 * (HD / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (HD == 128) v[t][i] = *reinterpret_cast<const uint32_t*>(vp + i * (HD / 2));
+          else v[t][i] = *reinterpret_cast<const uint16_t*>(vp + i * (HD / 2));
+        }
+        const kword z = fetch<kword>(vsb, (uint32_t)(4 * g * KW) + t * 16 * KW);
+#pragma unroll
+        for (int i = 0; i < KW; ++i) vs[t][i] = z[i];
       }
-      ks[t] = ks_[slot * (HD / 32) + (HD == 128 ? g : g >> 1)];
+    } else {  // slots past the last fetch the last one
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t vslot = min(s + 16 * t + 4 * g + i, len - 1);
-        const uint8_t* vp = vc + vslot * (HD / 2) + c * (HD / 32);
-        if constexpr (HD == 128) v[t][i] = *reinterpret_cast<const uint32_t*>(vp);
-        else v[t][i] = *reinterpret_cast<const uint16_t*>(vp);
-        vs[t][i] = vs_[vslot * (HD / 32) + (HD == 128 ? c >> 2 : c >> 3)];
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t slot = min(s + 16 * t + c, len - 1);
+        const kword x = *reinterpret_cast<const kword*>(row.kc + slot * (HD / 2) + g * (HD / 8));
+#pragma unroll
+        for (int i = 0; i < KW; ++i) k[t][i] = x[i];
+        ks[t] = row.ks[slot * KW + (HD == 128 ? g : g >> 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t vslot = min(s + 16 * t + 4 * g + i, len - 1);
+          const uint8_t* vp = row.vc + vslot * (HD / 2) + c * (HD / 32);
+          if constexpr (HD == 128) {
+            v[t][i] = *reinterpret_cast<const uint32_t*>(vp);
+            vs[t][i] = fetch<uint32_t>(row.vs, vslot * KW);
+          } else {
+            v[t][i] = *reinterpret_cast<const uint16_t*>(vp);
+            const uint32_t both = fetch<uint16_t>(row.vs, vslot * KW);
+            vs[t][i / 2] = i % 2 ? vs[t][i / 2] | both << 16 : both;
+          }
+        }
       }
     }
   }
+  // The scale of the lane's channels of V in slot i of tile t.
+  __device__ __forceinline__ uint32_t v_scale(int t, int i) const {
+    const int c = threadIdx.x & 15;
+    if constexpr (HD == 128) return __builtin_amdgcn_ubfe(vs[t][i], 8 * (c >> 2), 8);
+    else return __builtin_amdgcn_ubfe(vs[t][i / 2], 16 * (i % 2) + 8 * (c >> 3), 8);
+  }
 };
 
-// The queries of 16 rows, scaled, as B fragments.  FOLD (four rows at most): column 4 t + r is term t of row r, and one product
-// serves all terms; columns 12 .. 15 are zero.
+// A row's query, scaled, from element 8 kt of the lane's quarter on: its three bf16 terms.
+template <int HD, bool LIST, int RT>
+__device__ __forceinline__ void query_terms(const KvqArgs& a, const KvqPlace<LIST, RT>& p, int row, int kt, u32x4 (&out)[3]) {
+  const int g = (threadIdx.x & 63) >> 4, r = p.row0 + row, tok = p.token_of(a, r);
+  const float* src = a.q + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(a.entry[p.e].q_first + tok) * a.Hq + p.h * a.group + (r - tok * a.group)) * HD + g * (HD / 4);
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x4 v = reinterpret_cast<const f32x4*>(src + 8 * kt)[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j] * a.scale;
+  }
+  bf16x8 hi, lo;
+  split_bf16x8(x, hi, lo);
+  out[0] = __builtin_bit_cast(u32x4, hi);
+  out[1] = __builtin_bit_cast(u32x4, lo);
+  out[2] = __builtin_bit_cast(u32x4, third_bf16x8(x, hi, lo));
+}
+
+// The queries of RT tiles of 16 rows as B fragments, in LDS, which all waves of the workgroup read; rows past the last are the last one's.  FOLD (four
+// rows at most): in registers; column 4 t + r is term t of row r, and one product serves all terms; columns 12 .. 15 are zero.
 template <int HD, bool FOLD>
 struct KvqQueries {
   static constexpr int NKT = HD / 32, TERMS = FOLD ? 1 : 3;
-  u32x4 q[NKT][TERMS];
-  template <bool LIST>
-  __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST>& p) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int r = p.row0 + min(FOLD ? n & 3 : n, p.rows - 1), tok = p.token_of(a, r);
-    const float* src = a.q + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(a.entry[p.e].q_first + tok) * a.Hq + p.h * a.group + (r - tok * a.group)) * HD + g * (HD / 4);
+  u32x4 q[FOLD ? NKT : 1];
+  const u32x4* lds;
+  template <bool LIST, int RT>
+  __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST, RT>& p, u32x4* stage) {
+    const int lane = threadIdx.x & 63, n = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u32x4 f[3];
+    if constexpr (FOLD) {
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      float x[8];
+      for (int kt = 0; kt < NKT; ++kt) {
+        query_terms<HD>(a, p, min(n & 3, p.rows - 1), kt, f);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f32x4 v = reinterpret_cast<const f32x4*>(src + 8 * kt)[i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j] * a.scale;
+        for (int i = 0; i < 4; ++i) q[kt][i] = n < 4 ? f[0][i] : n < 8 ? f[1][i] : n < 12 ? f[2][i] : 0u;
       }
-      bf16x8 hi, lo;
-      split_bf16x8(x, hi, lo);
-      const bf16x8 third = third_bf16x8(x, hi, lo);
-      if constexpr (FOLD) {
-        const u32x4 t0 = __builtin_bit_cast(u32x4, hi), t1 = __builtin_bit_cast(u32x4, lo), t2 = __builtin_bit_cast(u32x4, third);
+    } else {
+      lds = stage + lane;
+      for (int i = wave; i < RT * NKT; i += kAttnWaves) {
+        query_terms<HD>(a, p, min(i / NKT * 16 + n, p.rows - 1), i % NKT, f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[kt][0][i] = n < 4 ? t0[i] : n < 8 ? t1[i] : n < 12 ? t2[i] : 0u;
-      } else {
-        q[kt][0] = __builtin_bit_cast(u32x4, hi);
-        q[kt][1] = __builtin_bit_cast(u32x4, lo);
-        q[kt][2] = __builtin_bit_cast(u32x4, third);
+        for (int t = 0; t < 3; ++t) stage[(i * 3 + t) * 64 + lane] = f[t];
       }
+      __syncthreads();
     }
+  }
+  __device__ __forceinline__ u32x4 get(int tile, int kt, int term) const {
+    if constexpr (FOLD) return q[kt];
+    else return lds[((tile * NKT + kt) * 3 + term) * 64];
   }
 };
 
@@ -155,7 +209,7 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return across<true>(across<false>(x, f), f);
 }
 
-// The running softmax of a wave's share: row l % 16 (FOLD: l % 4) in lane l.
+// The running softmax of a wave's share of a row tile: row l % 16 (FOLD: l % 4) in lane l.
 template <int HD, bool FOLD>
 struct KvqRows {
   static constexpr int CPV = HD / 16;  // channels of V that a lane takes
@@ -166,34 +220,9 @@ struct KvqRows {
 #pragma unroll
     for (int j = 0; j < CPV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  __device__ __forceinline__ void scores(const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, f32x4 (&x)[2]) const {
-    constexpr int NKT = HD / 32;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float unit = unit_of(st.ks[t]);
-      f32x4 y[KvqQueries<HD, FOLD>::TERMS];
-#pragma unroll
-      for (int i = 0; i < KvqQueries<HD, FOLD>::TERMS; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const uint32_t w = st.k[t][kt];
-        const u32x4 f = {bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
-#pragma unroll
-        for (int i = 0; i < KvqQueries<HD, FOLD>::TERMS; ++i) mma<bf16_t>(y[i], f, Q.q[kt][i]);
-      }
-      if constexpr (FOLD) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[t][i] = fold_terms(y[0][i]);
-      } else {
-        x[t] = y[0] + (y[1] + y[2]);
-      }
-    }
-  }
-  // edge: some row does not see all of the step's slots.  seen: how many slots the lane's row does.
-  __device__ __forceinline__ void add(const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, bool edge, int s, int seen, const uint8_t* vs_, int len) {
+  // Scores -> weights, as the fragments of the second product.  edge: some row does not see all of the step's slots; seen: how many the lane's does.
+  __device__ __forceinline__ void weigh(f32x4 (&x)[2], bool edge, int s, int seen, u32x4 (&pf)[FOLD ? 1 : 3]) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
-    f32x4 x[2];
-    scores(st, Q, x);
     if (edge) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -221,23 +250,6 @@ struct KvqRows {
         p[4 * t + i] = pow2(x[t][i] - m);
         l += p[4 * t + i];
       }
-    // V: a step at an edge may hold NaN where some row does not see it, whose probability of 0 would not hide it
-    float unit[8];
-    bool poisoned = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) unit[e] = unit_of(st.vs[e / 4][e % 4]);
-    if (edge) {
-      bool nan = false;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) nan = nan || st.vs[e / 4][e % 4] == 255;
-      if (__any(nan)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) unit[e] = st.vs[e / 4][e % 4] == 255 ? 0.f : unit[e];
-        const int block = HD == 128 ? g : g >> 1;  // of the lane's channels in o
-        for (int i = s; i < min(s + kStep, len); ++i) poisoned = poisoned || (i < seen && vs_[(uint32_t)i * (HD / 32) + block] == 255);
-      }
-    }
-    u32x4 pf[3];
     if constexpr (FOLD) {
       // the lane's column takes its own term
       const int term = (lane & 15) >> 2;
@@ -247,11 +259,10 @@ struct KvqRows {
         uint32_t w = pack_bf16x2(a, b);
 #pragma unroll
         for (int t = 1; t < 3; ++t) {
-          if (term >= t) {
-            a -= __uint_as_float(w << 16);
-            b -= __uint_as_float(w & 0xFFFF0000u);
-            w = pack_bf16x2(a, b);
-          }
+          const bool next = term >= t;
+          a -= next ? __uint_as_float(w << 16) : 0.f;
+          b -= next ? __uint_as_float(w & 0xFFFF0000u) : 0.f;
+          w = pack_bf16x2(a, b);
         }
         pf[0][i] = term < 3 ? w : 0u;
       }
@@ -262,53 +273,127 @@ struct KvqRows {
       pf[1] = __builtin_bit_cast(u32x4, lo);
       pf[2] = __builtin_bit_cast(u32x4, third_bf16x8(p, hi, lo));
     }
-    const auto channels = [&](auto pair) {  // two channels: 2 pair, 2 pair + 1
-      constexpr int P = decltype(pair)::value;
-      u32x4 f0, f1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t a = bf16_pair<P>(st.v[i / 2][2 * (i % 2)], unit[2 * i]), b = bf16_pair<P>(st.v[i / 2][2 * (i % 2) + 1], unit[2 * i + 1]);
-        f0[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-        f1[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-      }
-#pragma unroll
-      for (int t = 0; t < (FOLD ? 1 : 3); ++t) {
-        mma<bf16_t>(o[2 * P], f0, pf[t]);
-        mma<bf16_t>(o[2 * P + 1], f1, pf[t]);
-      }
-    };
-    channels(std::integral_constant<int, 0>{});
-    channels(std::integral_constant<int, 1>{});
-    if constexpr (HD == 128) {
-      channels(std::integral_constant<int, 2>{});
-      channels(std::integral_constant<int, 3>{});
-    }
-    if (edge && poisoned) {
-#pragma unroll
-      for (int j = 0; j < CPV; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] = NAN;
-    }
   }
 };
 
-// grid (chunks of all entries, KV heads, layers).  The workgroup's waves take its steps in turn; their results meet in LDS.
-template <int HD, bool FOLD, bool LIST>
-__global__ __launch_bounds__(kAttnWaves * 64) void kvq_attn_kernel(KvqArgs a) {
-  constexpr int NW = kAttnWaves, ROWS = FOLD ? 4 : 16, CPV = HD / 16;
+// A step added to a wave's RT row tiles.
+template <int HD, bool FOLD, int RT>
+__device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, bool edge, int s,
+                                         const int (&seen)[RT], const uint8_t* vs, int len) {
+  constexpr int NKT = HD / 32, CPV = HD / 16, TERMS = KvqQueries<HD, FOLD>::TERMS;
+  const int g = (threadIdx.x & 63) >> 4;
+  f32x4 x[RT][2];
+  if (!FOLD) asm volatile("" ::: "memory");  // queries are read from LDS at every step: in registers they would leave no room for the results
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float unit = unit_of(st.ks[t]);
+    u32x4 f[NKT];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const uint32_t w = st.k[t][kt];
+      f[kt] = u32x4{bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      f32x4 y[TERMS];
+#pragma unroll
+      for (int i = 0; i < TERMS; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) mma<bf16_t>(y[i], f[kt], Q.get(r, kt, i));
+      if constexpr (FOLD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[r][t][i] = fold_terms(y[0][i]);
+      } else {
+        x[r][t] = y[0] + (y[1] + y[2]);
+      }
+    }
+  }
+  // V.  A step at an edge may hold NaN where some row does not see it, whose weight of 0 would not hide it
+  float unit[8];
+  bool poisoned[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) poisoned[r] = false;
+  uint32_t scale[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) scale[e] = st.v_scale(e / 4, e % 4);
+  if (edge) {
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) nan = nan || scale[e] == 255;
+    if (__any(nan)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) scale[e] = scale[e] == 255 ? 0 : scale[e];
+      const int block = HD == 128 ? g : g >> 1;  // of the lane's channels in o
+      for (int i = s; i < min(s + kStep, len); ++i) {
+        const bool here = vs[(uint32_t)i * (HD / 32) + block] == 255;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) poisoned[r] = poisoned[r] || (here && i < seen[r]);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) unit[e] = unit_of(scale[e]);
+  u32x4 f[CPV];  // eight slots of a channel
+  const auto channels = [&](auto pair) {
+    constexpr int P = decltype(pair)::value;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = bf16_pair<P>(st.v[i / 2][2 * (i % 2)], unit[2 * i]), b = bf16_pair<P>(st.v[i / 2][2 * (i % 2) + 1], unit[2 * i + 1]);
+      f[2 * P][i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+      f[2 * P + 1][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    }
+  };
+  channels(std::integral_constant<int, 0>{});
+  channels(std::integral_constant<int, 1>{});
+  if constexpr (HD == 128) {
+    channels(std::integral_constant<int, 2>{});
+    channels(std::integral_constant<int, 3>{});
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    u32x4 pf[TERMS];
+    R[r].weigh(x[r], edge, s, seen[r], pf);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int j = 0; j < CPV; ++j) mma<bf16_t>(R[r].o[j], f[j], pf[t]);
+    if (edge && poisoned[r]) {
+#pragma unroll
+      for (int j = 0; j < CPV; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) R[r].o[j][i] = NAN;
+    }
+  }
+}
+
+// grid (chunks and groups of row tiles of all entries, KV heads, layers).  The workgroup's waves take its steps in turn; their results meet in LDS.
+// (Two waves to a SIMD at least: otherwise the compiler keeps results in the other half of the registers and moves them to and fro.)
+template <int HD, bool FOLD, bool LIST, int RT>
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void kvq_attn_kernel(KvqArgs a) {
+  constexpr int NW = kAttnWaves, ROWS = FOLD ? 4 : 16, CPV = HD / 16, NKT = HD / 32;
   __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
-  __shared__ f32x4 s_o[NW][ROWS][HD / 4];
+  __shared__ union Space {
+    f32x4 o[NW][ROWS][HD / 4];
+    u32x4 q[FOLD ? 1 : RT * NKT * 3 * 64];
+    __device__ Space() {}
+  } space;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
-  const KvqPlace<LIST> p(a);
+  const KvqPlace<LIST, RT> p(a);
   const KvqEntry& en = a.entry[p.e];
-  const size_t row = p.cache_row(a);
-  const uint8_t *kc = a.c.kc + row * (HD / 2), *vc = a.c.vc + row * (HD / 2), *ks = a.c.ks + row * (HD / 32), *vs = a.c.vs + row * (HD / 32);
-  KvqRows<HD, FOLD> R;
+  const size_t at_row = p.cache_row(a);
+  const KvqRow row = {a.c.kc + at_row * (HD / 2), a.c.vc + at_row * (HD / 2), a.c.ks + at_row * (HD / 32), a.c.vs + at_row * (HD / 32)};
+  KvqRows<HD, FOLD> R[RT];
   KvqQueries<HD, FOLD> Q;
   KvqStep<HD> st[2];
-  const int my_row = FOLD ? n & 3 : n;
-  const int seen = my_row < p.rows ? en.len - en.n + p.token_of(a, p.row0 + my_row) + 1 : 0;
+  int seen[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int my_row = FOLD ? n & 3 : 16 * r + n;
+    seen[r] = my_row < p.rows ? en.len - en.n + p.token_of(a, p.row0 + my_row) + 1 : 0;
+  }
   if constexpr (LIST) {
     // the chunk's entries, one to a lane, and which of them count
     const int32_t* list = a.blocks + (((size_t)p.l * a.n_tokens + en.q_first + p.n_tok) * a.heads + p.h) * a.n_blocks;
@@ -332,69 +417,76 @@ __global__ __launch_bounds__(kAttnWaves * 64) void kvq_attn_kernel(KvqArgs a) {
       }
     };
     int s = next();
-    if (s >= 0) st[0].load(kc, ks, vc, vs, s, p.len);
-    Q.load(a, p);
+    if (s >= 0) st[0].load(row, s, p.len);
+    Q.load(a, p, space.q);
     while (s >= 0) {
       const int s1 = next();
-      if (s1 >= 0) st[1].load(kc, ks, vc, vs, s1, p.len);
-      R.add(st[0], Q, s + kStep > p.old + 1, s, seen, vs, p.len);
+      if (s1 >= 0) st[1].load(row, s1, p.len);
+      add_step(R, st[0], Q, s + kStep > p.old + 1, s, seen, row.vs, p.len);
       s = s1;
       st[0] = st[1];
     }
   } else {
     const int steps = (p.len + kStep - 1) / kStep, end = min(steps, (p.c + 1) * a.chunk);
     int i = p.c * a.chunk + wave;
-    if (i < end) st[0].load(kc, ks, vc, vs, i * kStep, p.len);
-    Q.load(a, p);
+    if (i < end) st[0].load(row, i * kStep, p.len);
+    Q.load(a, p, space.q);
     for (; i < end; i += NW) {
-      if (i + NW < end) st[1].load(kc, ks, vc, vs, (i + NW) * kStep, p.len);
-      R.add(st[0], Q, (i + 1) * kStep > p.old + 1, i * kStep, seen, vs, p.len);
+      if (i + NW < end) st[1].load(row, (i + NW) * kStep, p.len);
+      add_step(R, st[0], Q, (i + 1) * kStep > p.old + 1, i * kStep, seen, row.vs, p.len);
       st[0] = st[1];
     }
   }
   // the waves' shares
-  float l = over_groups_sum(R.l);
-  if (lane < ROWS) {
-    s_m[wave][lane] = R.m;
-    s_l[wave][lane] = l;
-  }
-  __syncthreads();
-  float top = kLowest;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][my_row % ROWS]);
-  const float f = pow2(R.m - top);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[CPV];
-#pragma unroll
-    for (int j = 0; j < CPV; ++j) x[j] = (FOLD ? fold_terms(R.o[j][i]) : R.o[j][i]) * f;
-    if (!FOLD || n < 4)
-#pragma unroll
-      for (int j = 0; j < CPV; j += 4) s_o[wave][my_row][((4 * g + i) * CPV + j) / 4] = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
-  }
-  __syncthreads();
   const size_t part = ((size_t)p.l * a.heads + p.h) * a.part_pitch + en.first_part;
-  for (int u = threadIdx.x; u < p.rows * (HD / 4); u += NW * 64) {
-    const int r = u / (HD / 4), c = u % (HD / 4), ra = p.row0 + r;
-    f32x4 sum = s_o[0][r][c];
-    float m = s_m[0][r];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) {
-      sum += s_o[w][r][c];
-      m = fmaxf(m, s_m[w][r]);
+  for (int r = 0; r < RT; ++r) {
+    if (r > 0 && 16 * r >= p.rows) break;
+    const float l = over_groups_sum(R[r].l);
+    if (!FOLD || r > 0) __syncthreads();  // queries and the last tile's shares have been read
+    if (lane < ROWS) {
+      s_m[wave][lane] = R[r].m;
+      s_l[wave][lane] = l;
     }
-    float all = 0.f;
+    __syncthreads();
+    const int my_row = n % ROWS;
+    float top = kLowest;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) all += s_l[w][r] * pow2(s_m[w][r] - m);
-    if (en.chunks == 1) {
-      const int tok = p.token_of(a, ra);
-      f32x4* out = reinterpret_cast<f32x4*>(a.out + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(en.q_first + tok) * a.Hq + p.h * a.group + (ra - tok * a.group)) * HD);
-      const float inv = all == 0.f ? 0.f : 1.f / all;
-      out[c] = sum * inv;
-    } else {
-      const size_t at = part + (size_t)ra * en.chunks + p.c;
-      reinterpret_cast<f32x4*>(a.part)[at * (HD / 4) + c] = sum;
-      if (c == 0) a.part_ml[at] = make_float2(m, all);
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][my_row]);
+    const float f = pow2(R[r].m - top);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[CPV];
+#pragma unroll
+      for (int j = 0; j < CPV; ++j) x[j] = (FOLD ? fold_terms(R[r].o[j][i]) : R[r].o[j][i]) * f;
+      if (!FOLD || n < 4)
+#pragma unroll
+        for (int j = 0; j < CPV; j += 4) space.o[wave][my_row][((4 * g + i) * CPV + j) / 4] = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+    }
+    __syncthreads();
+    const int rows = min(ROWS, p.rows - 16 * r);
+    for (int u = threadIdx.x; u < rows * (HD / 4); u += NW * 64) {
+      const int k = u / (HD / 4), c = u % (HD / 4), ra = p.row0 + 16 * r + k;
+      f32x4 sum = space.o[0][k][c];
+      float m = s_m[0][k];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) {
+        sum += space.o[w][k][c];
+        m = fmaxf(m, s_m[w][k]);
+      }
+      float all = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) all += s_l[w][k] * pow2(s_m[w][k] - m);
+      if (en.chunks == 1) {
+        const int tok = p.token_of(a, ra);
+        f32x4* out = reinterpret_cast<f32x4*>(a.out + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(en.q_first + tok) * a.Hq + p.h * a.group + (ra - tok * a.group)) * HD);
+        const float inv = all == 0.f ? 0.f : 1.f / all;
+        out[c] = sum * inv;
+      } else {
+        const size_t at = part + (size_t)ra * en.chunks + p.c;
+        reinterpret_cast<f32x4*>(a.part)[at * (HD / 4) + c] = sum;
+        if (c == 0) a.part_ml[at] = make_float2(m, all);
+      }
     }
   }
 }
@@ -439,18 +531,26 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   reinterpret_cast<f32x4*>(a.out + ((size_t)l * a.n_tokens * a.Hq + (size_t)t * a.Hq + j) * HD)[c4] = o * inv;
 }
 
+// How a call is cut.  Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
+static int kvq_row_tiles(const KvqArgs& a) {
+  int rows = 0;
+  for (int i = 0; i < a.n_entries; ++i) rows = std::max(rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
+  return rows <= 16 ? 1 : 2;
+}
 constexpr int kKvqWgs = 1024;  // workgroups that a call is cut into, about
 void kvq_plan(KvqArgs& a, int n_layers) {
   a.inv_group = 1.f / (float)a.group;
+  const int rt = kvq_row_tiles(a);
   long work = 0;
   for (int i = 0; i < a.n_entries; ++i) {
     KvqEntry& e = a.entry[i];
-    e.tiles = a.n_blocks ? 1 : (e.n * a.group + 15) / 16;
+    e.tiles = a.n_blocks ? 1 : (e.n * a.group + 16 * rt - 1) / (16 * rt);
     work += a.n_blocks ? (long)e.n * a.n_blocks : (long)e.tiles * ((e.len + kStep - 1) / kStep);
   }
   work *= (long)a.heads * n_layers;
   const int least = a.n_blocks ? kAttnWaves / 2 : kAttnWaves, most = a.n_blocks ? 64 : 65536 / kStep;  // with lists: an entry to a lane
-  a.chunk = (int)std::min<long>(most, std::max<long>(least, ((work + kKvqWgs - 1) / kKvqWgs + least - 1) / least * least));
+  static const int wgs = env_int("KVQ_WGS", kKvqWgs);
+  a.chunk = (int)std::min<long>(most, std::max<long>(least, ((work + wgs - 1) / wgs + least - 1) / least * least));
   int wg = 0;
   size_t part = 0;
   for (int i = 0; i < kMaxCols; ++i) {
@@ -489,8 +589,9 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
   };
   auto pick = [&](auto hd_, auto join) {
     constexpr int HD = decltype(hd_)::value;
-    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true>, join) : go(kvq_attn_kernel<HD, false, true>, join);
-    else fold ? go(kvq_attn_kernel<HD, true, false>, join) : go(kvq_attn_kernel<HD, false, false>, join);
+    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true, 1>, join) : go(kvq_attn_kernel<HD, false, true, 1>, join);
+    else if (fold) go(kvq_attn_kernel<HD, true, false, 1>, join);
+    else rows <= 16 ? go(kvq_attn_kernel<HD, false, false, 1>, join) : go(kvq_attn_kernel<HD, false, false, 2>, join);
   };
   if (hd == 128) pick(std::integral_constant<int, 128>{}, kvq_join_kernel<128>);
   else pick(std::integral_constant<int, 64>{}, kvq_join_kernel<64>);
@@ -498,7 +599,7 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
 
 // ------------------------------------------------------------------------------------------
 // Selection: (1) the blocks' scores, a workgroup to some blocks of a sequence, which reads their bounds once for all its new tokens;
-// (2) a wave to every (layer, token, KV head) finds the score of the last block that stays, bit by bit, and writes the list.
+// (2) a wave to every (layer, token, KV head) finds a score that as many blocks reach as shall stay, bit by bit, and writes the list.
 // ------------------------------------------------------------------------------------------
 // grid (groups of blocks of all entries, KV heads, layers)
 template <int HD>
@@ -552,22 +653,37 @@ __global__ __launch_bounds__(64) void kvq_select_kernel(KvqSelectArgs a) {
   const size_t list = ((size_t)l * a.n_tokens + t) * a.heads + h;
   const double* scores = a.scores + list * a.most;
   int32_t* out = a.out + list * a.n_select;
-  const int want = min(a.n_select, held), last0 = max(0, held - a.last);
+  const int last0 = max(0, held - a.last);
+  const auto forced = [&](int b) { return b < a.first || b >= last0; };
   uint64_t key[kSelectRegs];  // 0: no block
+  int n_forced = 0;
+  uint64_t most = 0, least = ~0ull;  // of the others'
 #pragma unroll
   for (int j = 0; j < kSelectRegs; ++j) {
     const int b = 64 * j + lane;
-    key[j] = b >= held ? 0 : b < a.first || b >= last0 ? ~0ull : score_key(scores[b]);
+    key[j] = 0;
+    if (64 * j >= held) continue;
+    if (b < held) key[j] = forced(b) ? ~0ull : score_key(scores[b]);
+    n_forced += __popcll(__ballot(key[j] == ~0ull));
+    if (key[j] != 0 && key[j] != ~0ull) most = max(most, key[j]), least = min(least, key[j]);
   }
-  // the want-th highest key: the highest number that as many keys reach
-  uint64_t bound = 0;
-  for (int bit = 63; bit >= 0; --bit) {
-    const uint64_t trial = bound | 1ull << bit;
-    int n = 0;
+  most = lanes_fold(most, 64, [](uint64_t x, uint64_t y) { return max(x, y); });
+  least = lanes_fold(least, 64, [](uint64_t x, uint64_t y) { return min(x, y); });
+  // a number that exactly `want` keys reach, or the want-th highest key: bit by bit from the highest that the keys differ in
+  const int want = min(a.n_select, held);
+  uint64_t bound = n_forced >= want ? ~0ull : 1;
+  if (n_forced < want && want < held) {
+    const int top = most == least ? -1 : 63 - __builtin_clzll(most ^ least);
+    bound = most & (top < 0 ? ~0ull : ~((2ull << top) - 1));
+    for (int bit = top; bit >= 0; --bit) {
+      const uint64_t trial = bound | 1ull << bit;
+      int n = 0;
 #pragma unroll
-    for (int j = 0; j < kSelectRegs; ++j)
-      if (64 * j < held) n += __popcll(__ballot(key[j] >= trial));
-    if (n >= want) bound = trial;
+      for (int j = 0; j < kSelectRegs; ++j)
+        if (64 * j < held) n += __popcll(__ballot(key[j] >= trial));
+      if (n >= want) bound = trial;
+      if (n == want) break;
+    }
   }
   int over = 0;
 #pragma unroll

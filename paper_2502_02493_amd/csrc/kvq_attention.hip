@@ -190,9 +190,9 @@ struct KvqQueries {
       __syncthreads();
     }
   }
-  __device__ __forceinline__ u32x4 get(int tile, int kt, int term) const {
+  __device__ __forceinline__ u32x4 get(int tile, int kt, int term, int zero) const {
     if constexpr (FOLD) return q[kt];
-    else return lds[((tile * NKT + kt) * 3 + term) * 64];
+    else return (lds + zero)[((tile * NKT + kt) * 3 + term) * 64];
   }
 };
 
@@ -209,18 +209,23 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return across<true>(across<false>(x, f), f);
 }
 
-// The running softmax of a wave's share of a row tile: row l % 16 (FOLD: l % 4) in lane l.
+// The running softmax of a wave's share of a row tile: row l % 16 (FOLD: l % 4) in lane l.  Weights are taken relative to a reference m, a score that
+// was the highest once: it moves only when one lies more than kHeadroom above it, since every move multiplies the results, and 2^kHeadroom times too
+// large a weight is as exact.
+constexpr float kHeadroom = 8.f;
 template <int HD, bool FOLD>
 struct KvqRows {
   static constexpr int CPV = HD / 16;  // channels of V that a lane takes
-  float m = kLowest, l = 0.f;          // l: of the lane's own slots
+  float m = kLowest, shift = 0.f;      // shift: -m, 0 while there is none; where the first product's accumulator starts
+  float l = 0.f;                       // sum of the lane's own slots' weights
   f32x4 o[CPV];                        // o[j][i]: channel (4 (l / 16) + i) CPV + j (FOLD: term l % 16 / 4 of it)
 
   __device__ __forceinline__ KvqRows() {
 #pragma unroll
     for (int j = 0; j < CPV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // Scores -> weights, as the fragments of the second product.  edge: some row does not see all of the step's slots; seen: how many the lane's does.
+  // Scores, shifted, -> weights, as the fragments of the second product.  edge: some row does not see all of the step's slots; seen: how many the
+  // lane's does.
   __device__ __forceinline__ void weigh(f32x4 (&x)[2], bool edge, int s, int seen, u32x4 (&pf)[FOLD ? 1 : 3]) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
     if (edge) {
@@ -229,49 +234,46 @@ struct KvqRows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[t][i] = s + 16 * t + 4 * g + i < seen ? x[t][i] : -INFINITY;
     }
-    float top = m;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) top = fmaxf(fmaxf(fmaxf(top, x[t][0]), fmaxf(x[t][1], x[t][2])), x[t][3]);
-    top = over_groups_max(top);
-    if (__any(top > m)) {
-      const float f = pow2(m - top);
+    float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+    if (__any(top > kHeadroom || m == kLowest)) {
+      top = fmaxf(m, over_groups_max(top - shift));
+      const float f = pow2(m - top), back = top == kLowest ? 0.f : -top - shift;
       l *= f;
 #pragma unroll
       for (int j = 0; j < CPV; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[j][i] *= f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[t][i] += back;
       m = top;
+      shift += back;
     }
     float p[8];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[4 * t + i] = pow2(x[t][i] - m);
+        p[4 * t + i] = pow2(x[t][i]);
         l += p[4 * t + i];
       }
-    if constexpr (FOLD) {
-      // the lane's column takes its own term
-      const int term = (lane & 15) >> 2;
+    // in three terms (FOLD: the lane's column takes its own)
+    const int term = (lane & 15) >> 2;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float a = p[2 * i], b = p[2 * i + 1];
-        uint32_t w = pack_bf16x2(a, b);
+    for (int i = 0; i < 4; ++i) {
+      float a = p[2 * i], b = p[2 * i + 1];
+      uint32_t w = pack_bf16x2(a, b);
+      if (!FOLD) pf[0][i] = w;
 #pragma unroll
-        for (int t = 1; t < 3; ++t) {
-          const bool next = term >= t;
-          a -= next ? __uint_as_float(w << 16) : 0.f;
-          b -= next ? __uint_as_float(w & 0xFFFF0000u) : 0.f;
-          w = pack_bf16x2(a, b);
-        }
-        pf[0][i] = term < 3 ? w : 0u;
+      for (int t = 1; t < 3; ++t) {
+        const bool next = !FOLD || term >= t;
+        a -= next ? __uint_as_float(w << 16) : 0.f;
+        b -= next ? __uint_as_float(w & 0xFFFF0000u) : 0.f;
+        w = pack_bf16x2(a, b);
+        if (!FOLD) pf[t % (FOLD ? 1 : 3)][i] = w;
       }
-    } else {
-      bf16x8 hi, lo;
-      split_bf16x8(p, hi, lo);
-      pf[0] = __builtin_bit_cast(u32x4, hi);
-      pf[1] = __builtin_bit_cast(u32x4, lo);
-      pf[2] = __builtin_bit_cast(u32x4, third_bf16x8(p, hi, lo));
+      if (FOLD) pf[0][i] = term < 3 ? w : 0u;
     }
   }
 };
@@ -283,32 +285,41 @@ __device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], const KvqSt
   constexpr int NKT = HD / 32, CPV = HD / 16, TERMS = KvqQueries<HD, FOLD>::TERMS;
   const int g = (threadIdx.x & 63) >> 4;
   f32x4 x[RT][2];
-  if (!FOLD) asm volatile("" ::: "memory");  // queries are read from LDS at every step: in registers they would leave no room for the results
+  // queries are read from LDS at every step, which the compiler has to be kept from doing once: in registers they would leave no room for the results
+  int again = 0;
+  if (!FOLD) asm volatile("" : "+v"(again));
+u32x4 k[2][NKT];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const float unit = unit_of(st.ks[t]);
-    u32x4 f[NKT];
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt) {
       const uint32_t w = st.k[t][kt];
-      f[kt] = u32x4{bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
+      k[t][kt] = u32x4{bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      f32x4 y[TERMS];
-#pragma unroll
-      for (int i = 0; i < TERMS; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) mma<bf16_t>(y[i], f[kt], Q.get(r, kt, i));
-      if constexpr (FOLD) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[r][t][i] = fold_terms(y[0][i]);
-      } else {
-        x[r][t] = y[0] + (y[1] + y[2]);
-      }
+      // FOLD: the shift in the columns of one term, whose sum they become
+      const float start = !FOLD || (threadIdx.x & 12) == 0 ? R[r].shift : 0.f;
+      x[r][t] = f32x4{start, start, start, start};
     }
+  }
+  // the smallest term first; products on one accumulator 2 RT apart
+#pragma unroll
+  for (int i = TERMS - 1; i >= 0; --i)
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const u32x4 q = Q.get(r, kt, i, again);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) mma<bf16_t>(x[r][t], k[t][kt], q);
+      }
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[0][t][i] = fold_terms(x[0][t][i]);
   }
   // V.  A step at an edge may hold NaN where some row does not see it, whose weight of 0 would not hide it
   float unit[8];

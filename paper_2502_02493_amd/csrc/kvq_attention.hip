@@ -23,7 +23,6 @@ namespace es {
 
 constexpr float kLowest = -3.4028235e38f;
 constexpr int kStep = 32;        // slots of a wave's step
-constexpr int kAttnWaves = 4;
 
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, float unit, std::integral_constant<int, 0>) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0)); }
@@ -78,60 +77,60 @@ struct KvqRow {
   const uint8_t *kc, *vc, *ks, *vs;
 };
 
-// Codes and scales of a step of 32 slots from s on, as the lane needs them.
+// Codes and scales of a step of 32 slots from s on, as the lane needs them.  Slots past the last fetch the last one.
 template <int HD>
 struct KvqStep {
   static constexpr int KW = HD / 32;  // words of K codes of a lane and tile: 8 channels each; scales of a slot
-  uint32_t k[2][KW], v[2][4];
-  uint32_t ks[2], vs[2][KW];  // vs: the scales of the lane's four slots of a tile side by side
+  typedef uint32_t kword __attribute__((ext_vector_type(KW)));
+  kword k[2], vs[2];  // vs: the scales of the lane's four slots of a tile side by side
+  uint32_t ks[2], v[2][4];
   template <class T>
-  static __device__ __forceinline__ T fetch(const uint8_t* base, uint32_t offset) {  // scales may lie anywhere
+  static __device__ __forceinline__ T fetch(const uint8_t* p) {  // scales may lie anywhere
     T x;
-    __builtin_memcpy(&x, base + offset, sizeof(T));
+    __builtin_memcpy(&x, p, sizeof(T));
     return x;
   }
-  __device__ __forceinline__ void load(const KvqRow& row, int s, int len) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-    typedef uint32_t kword __attribute__((ext_vector_type(KW)));
+  __device__ __forceinline__ void load_k(const KvqRow& row, int s, int len) {
+    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, own = g * (HD / 8), own_scale = HD == 128 ? g : g >> 1;
     if (s + kStep <= len) {
-      const uint8_t *kc = row.kc + (size_t)s * (HD / 2), *vc = row.vc + (size_t)s * (HD / 2), *ksb = row.ks + (size_t)s * KW, *vsb = row.vs + (size_t)s * KW;
+      const uint8_t *kc = row.kc + (size_t)s * (HD / 2), *sc = row.ks + (size_t)s * KW;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const kword x = *reinterpret_cast<const kword*>(kc + (uint32_t)(c * (HD / 2) + g * (HD / 8)) + t * 16 * (HD / 2));
-#pragma unroll
-        for (int i = 0; i < KW; ++i) k[t][i] = x[i];
-        ks[t] = (ksb + (uint32_t)(c * KW + (HD == 128 ? g : g >> 1)))[t * 16 * KW];
-        const uint8_t* vp = vc + (uint32_t)(4 * g * (HD / 2) + c * (HD / 32)) + t * 16 * (HD / 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (HD == 128) v[t][i] = *reinterpret_cast<const uint32_t*>(vp + i * (HD / 2));
-          else v[t][i] = *reinterpret_cast<const uint16_t*>(vp + i * (HD / 2));
-        }
-        const kword z = fetch<kword>(vsb, (uint32_t)(4 * g * KW) + t * 16 * KW);
-#pragma unroll
-        for (int i = 0; i < KW; ++i) vs[t][i] = z[i];
+        k[t] = *reinterpret_cast<const kword*>(kc + (c * (HD / 2) + own) + t * 16 * (HD / 2));
+        ks[t] = (sc + (c * KW + own_scale))[t * 16 * KW];
       }
-    } else {  // slots past the last fetch the last one
+    } else {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint32_t slot = min(s + 16 * t + c, len - 1);
-        const kword x = *reinterpret_cast<const kword*>(row.kc + slot * (HD / 2) + g * (HD / 8));
+        const uint32_t slot = min((uint32_t)s + 16 * t + c, (uint32_t)len - 1);
+        k[t] = *reinterpret_cast<const kword*>(row.kc + (slot * (HD / 2) + own));
+        ks[t] = row.ks[slot * KW + own_scale];
+      }
+    }
+  }
+  __device__ __forceinline__ void load_v(const KvqRow& row, int s, int len) {
+    typedef typename std::conditional<HD == 128, uint32_t, uint16_t>::type part;  // a lane's channels; a slot's scales
+    const uint32_t lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    if (s + kStep <= len) {
+      const uint8_t *vc = row.vc + (size_t)s * (HD / 2), *sc = row.vs + (size_t)s * KW;
 #pragma unroll
-        for (int i = 0; i < KW; ++i) k[t][i] = x[i];
-        ks[t] = row.ks[slot * KW + (HD == 128 ? g : g >> 1)];
+      for (int t = 0; t < 2; ++t) {
+        const uint8_t* vp = vc + (4 * g * (HD / 2) + c * sizeof(part)) + t * 16 * (HD / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[t][i] = *reinterpret_cast<const part*>(vp + i * (HD / 2));
+        vs[t] = fetch<kword>(sc + 4 * g * KW + t * 16 * KW);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        part sc[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t vslot = min(s + 16 * t + 4 * g + i, len - 1);
-          const uint8_t* vp = row.vc + vslot * (HD / 2) + c * (HD / 32);
-          if constexpr (HD == 128) {
-            v[t][i] = *reinterpret_cast<const uint32_t*>(vp);
-            vs[t][i] = fetch<uint32_t>(row.vs, vslot * KW);
-          } else {
-            v[t][i] = *reinterpret_cast<const uint16_t*>(vp);
-            const uint32_t both = fetch<uint16_t>(row.vs, vslot * KW);
-            vs[t][i / 2] = i % 2 ? vs[t][i / 2] | both << 16 : both;
-          }
+          const uint32_t slot = min((uint32_t)s + 16 * t + 4 * g + i, (uint32_t)len - 1);
+          v[t][i] = *reinterpret_cast<const part*>(row.vc + (slot * (HD / 2) + c * (uint32_t)sizeof(part)));
+          sc[i] = fetch<part>(row.vs + slot * KW);
         }
+        vs[t] = __builtin_bit_cast(kword, sc);
       }
     }
   }
@@ -169,7 +168,7 @@ struct KvqQueries {
   static constexpr int NKT = HD / 32, TERMS = FOLD ? 1 : 3;
   u32x4 q[FOLD ? NKT : 1];
   const u32x4* lds;
-  template <bool LIST, int RT>
+  template <int NW, bool LIST, int RT>
   __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST, RT>& p, u32x4* stage) {
     const int lane = threadIdx.x & 63, n = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     u32x4 f[3];
@@ -182,7 +181,7 @@ struct KvqQueries {
       }
     } else {
       lds = stage + lane;
-      for (int i = wave; i < RT * NKT; i += kAttnWaves) {
+      for (int i = wave; i < RT * NKT; i += NW) {
         query_terms<HD>(a, p, min(i / NKT * 16 + n, p.rows - 1), i % NKT, f);
 #pragma unroll
         for (int t = 0; t < 3; ++t) stage[(i * 3 + t) * 64 + lane] = f[t];
@@ -278,10 +277,10 @@ struct KvqRows {
   }
 };
 
-// A step added to a wave's RT row tiles.
+// A step added to a wave's RT row tiles.  The next one's codes (next < 0: there is none) are requested as soon as this one's have been made bf16.
 template <int HD, bool FOLD, int RT>
-__device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], const KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, bool edge, int s,
-                                         const int (&seen)[RT], const uint8_t* vs, int len) {
+__device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, const KvqRow& row, bool edge, int s,
+                                         int next, const int (&seen)[RT], int len) {
   constexpr int NKT = HD / 32, CPV = HD / 16, TERMS = KvqQueries<HD, FOLD>::TERMS;
   const int g = (threadIdx.x & 63) >> 4;
   f32x4 x[RT][2];
@@ -304,6 +303,7 @@ u32x4 k[2][NKT];
       x[r][t] = f32x4{start, start, start, start};
     }
   }
+  if (next >= 0) st.load_k(row, next, len);
   // the smallest term first; products on one accumulator 2 RT apart
 #pragma unroll
   for (int i = TERMS - 1; i >= 0; --i)
@@ -338,7 +338,7 @@ u32x4 k[2][NKT];
       for (int e = 0; e < 8; ++e) scale[e] = scale[e] == 255 ? 0 : scale[e];
       const int block = HD == 128 ? g : g >> 1;  // of the lane's channels in o
       for (int i = s; i < min(s + kStep, len); ++i) {
-        const bool here = vs[(uint32_t)i * (HD / 32) + block] == 255;
+        const bool here = row.vs[(uint32_t)i * (HD / 32) + block] == 255;
 #pragma unroll
         for (int r = 0; r < RT; ++r) poisoned[r] = poisoned[r] || (here && i < seen[r]);
       }
@@ -362,6 +362,7 @@ u32x4 k[2][NKT];
     channels(std::integral_constant<int, 2>{});
     channels(std::integral_constant<int, 3>{});
   }
+  if (next >= 0) st.load_v(row, next, len);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     u32x4 pf[TERMS];
@@ -381,9 +382,9 @@ u32x4 k[2][NKT];
 
 // grid (chunks and groups of row tiles of all entries, KV heads, layers).  The workgroup's waves take its steps in turn; their results meet in LDS.
 // (Two waves to a SIMD at least: otherwise the compiler keeps results in the other half of the registers and moves them to and fro.)
-template <int HD, bool FOLD, bool LIST, int RT>
-__global__ __launch_bounds__(kAttnWaves * 64, 2) void kvq_attn_kernel(KvqArgs a) {
-  constexpr int NW = kAttnWaves, ROWS = FOLD ? 4 : 16, CPV = HD / 16, NKT = HD / 32;
+template <int HD, bool FOLD, bool LIST, int RT, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
+  constexpr int ROWS = FOLD ? 4 : 16, CPV = HD / 16, NKT = HD / 32;
   __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
   __shared__ union Space {
     f32x4 o[NW][ROWS][HD / 4];
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void kvq_attn_kernel(KvqArgs a)
   const KvqRow row = {a.c.kc + at_row * (HD / 2), a.c.vc + at_row * (HD / 2), a.c.ks + at_row * (HD / 32), a.c.vs + at_row * (HD / 32)};
   KvqRows<HD, FOLD> R[RT];
   KvqQueries<HD, FOLD> Q;
-  KvqStep<HD> st[2];
+  KvqStep<HD> st;
   int seen[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -428,25 +429,25 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void kvq_attn_kernel(KvqArgs a)
       }
     };
     int s = next();
-    if (s >= 0) st[0].load(row, s, p.len);
-    Q.load(a, p, space.q);
+    if (s >= 0) {
+      st.load_k(row, s, p.len);
+      st.load_v(row, s, p.len);
+    }
+    Q.template load<NW>(a, p, space.q);
     while (s >= 0) {
-      const int s1 = next();
-      if (s1 >= 0) st[1].load(row, s1, p.len);
-      add_step(R, st[0], Q, s + kStep > p.old + 1, s, seen, row.vs, p.len);
-      s = s1;
-      st[0] = st[1];
+      const int after = next();
+      add_step(R, st, Q, row, s + kStep > p.old + 1, s, after, seen, p.len);
+      s = after;
     }
   } else {
     const int steps = (p.len + kStep - 1) / kStep, end = min(steps, (p.c + 1) * a.chunk);
     int i = p.c * a.chunk + wave;
-    if (i < end) st[0].load(row, i * kStep, p.len);
-    Q.load(a, p, space.q);
-    for (; i < end; i += NW) {
-      if (i + NW < end) st[1].load(row, (i + NW) * kStep, p.len);
-      add_step(R, st[0], Q, (i + 1) * kStep > p.old + 1, i * kStep, seen, row.vs, p.len);
-      st[0] = st[1];
+    if (i < end) {
+      st.load_k(row, i * kStep, p.len);
+      st.load_v(row, i * kStep, p.len);
     }
+    Q.template load<NW>(a, p, space.q);
+    for (; i < end; i += NW) add_step(R, st, Q, row, (i + 1) * kStep > p.old + 1, i * kStep, i + NW < end ? (i + NW) * kStep : -1, seen, p.len);
   }
   // the waves' shares
   const size_t part = ((size_t)p.l * a.heads + p.h) * a.part_pitch + en.first_part;
@@ -543,33 +544,40 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
 }
 
 // How a call is cut.  Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
-static int kvq_row_tiles(const KvqArgs& a) {
-  int rows = 0;
-  for (int i = 0; i < a.n_entries; ++i) rows = std::max(rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
-  return rows <= 16 ? 1 : 2;
+struct KvqCut {
+  int rows, tiles, waves, wgs;  // rows of a workgroup's sequence or token; row tiles to a wave; waves of a workgroup; workgroups, at most
+};
+static KvqCut kvq_cut(const KvqArgs& a) {
+  KvqCut c;
+  c.rows = 0;
+  for (int i = 0; i < a.n_entries; ++i) c.rows = std::max(c.rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
+  c.tiles = c.rows <= 16 ? 1 : 2;
+  c.waves = c.tiles == 2 ? 8 : 4;
+  static const int w8 = env_int("KVQ_W8", 256), w4 = env_int("KVQ_WGS", 768);
+  c.wgs = c.tiles == 2 ? w8 : w4;
+  return c;
 }
-constexpr int kKvqWgs = 1024;  // workgroups that a call is cut into, about
 void kvq_plan(KvqArgs& a, int n_layers) {
   a.inv_group = 1.f / (float)a.group;
-  const int rt = kvq_row_tiles(a);
-  long work = 0;
-  for (int i = 0; i < a.n_entries; ++i) {
-    KvqEntry& e = a.entry[i];
-    e.tiles = a.n_blocks ? 1 : (e.n * a.group + 16 * rt - 1) / (16 * rt);
-    work += a.n_blocks ? (long)e.n * a.n_blocks : (long)e.tiles * ((e.len + kStep - 1) / kStep);
+  const KvqCut cut = kvq_cut(a);
+  const auto pieces = [&](const KvqEntry& e) { return a.n_blocks ? a.n_blocks : (e.len + kStep - 1) / kStep; };
+  for (int i = 0; i < a.n_entries; ++i) a.entry[i].tiles = a.n_blocks ? 1 : (a.entry[i].n * a.group + 16 * cut.tiles - 1) / (16 * cut.tiles);
+  const auto count = [&](int chunk) {
+    long wgs = 0;
+    for (int i = 0; i < a.n_entries; ++i) wgs += (long)((pieces(a.entry[i]) + chunk - 1) / chunk) * (a.n_blocks ? a.entry[i].n : a.entry[i].tiles);
+    return wgs * a.heads * n_layers;
+  };
+  // a step at least for every wave (a block of a list is two); with lists an entry to a lane at most
+  const int least = a.n_blocks ? cut.waves / 2 : cut.waves, most = a.n_blocks ? 64 : 65536 / kStep;
+  for (a.chunk = least; a.chunk < most && count(a.chunk) > cut.wgs; a.chunk += least) {
   }
-  work *= (long)a.heads * n_layers;
-  const int least = a.n_blocks ? kAttnWaves / 2 : kAttnWaves, most = a.n_blocks ? 64 : 65536 / kStep;  // with lists: an entry to a lane
-  static const int wgs = env_int("KVQ_WGS", kKvqWgs);
-  a.chunk = (int)std::min<long>(most, std::max<long>(least, ((work + wgs - 1) / wgs + least - 1) / least * least));
   int wg = 0;
   size_t part = 0;
   for (int i = 0; i < kMaxCols; ++i) {
     a.first_wg[i] = INT32_MAX;
     if (i >= a.n_entries) continue;
     KvqEntry& e = a.entry[i];
-    const int pieces = a.n_blocks ? a.n_blocks : (e.len + kStep - 1) / kStep;
-    e.chunks = (pieces + a.chunk - 1) / a.chunk;
+    e.chunks = (pieces(e) + a.chunk - 1) / a.chunk;
     e.first_part = part;
     a.first_wg[i] = wg;
     wg += e.chunks * (a.n_blocks ? e.n : e.tiles);
@@ -591,18 +599,17 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
   KvqArgs a = args;
   if (a.n_entries == 0) return;
   a.part_ml = reinterpret_cast<float2*>(a.part + a.part_pitch * a.heads * n_layers * hd);
-  int rows = 0;
-  for (int i = 0; i < a.n_entries; ++i) rows = std::max(rows, a.blocks ? a.group : a.entry[i].n * a.group);
-  const bool fold = rows <= 4;
+  const KvqCut cut = kvq_cut(a);
+  const bool fold = cut.rows <= 4;
   auto go = [&](auto kernel, auto join) {
-    hipLaunchKernelGGL(kernel, dim3(a.n_wgs, a.heads, n_layers), dim3(kAttnWaves * 64), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3(a.n_wgs, a.heads, n_layers), dim3(cut.waves * 64), 0, st, a);
     if (kvq_joined(a)) hipLaunchKernelGGL(join, dim3(a.n_tokens, a.Hq, n_layers), dim3(256), 0, st, a);
   };
   auto pick = [&](auto hd_, auto join) {
     constexpr int HD = decltype(hd_)::value;
-    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true, 1>, join) : go(kvq_attn_kernel<HD, false, true, 1>, join);
-    else if (fold) go(kvq_attn_kernel<HD, true, false, 1>, join);
-    else rows <= 16 ? go(kvq_attn_kernel<HD, false, false, 1>, join) : go(kvq_attn_kernel<HD, false, false, 2>, join);
+    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true, 1, 4>, join) : go(kvq_attn_kernel<HD, false, true, 1, 4>, join);
+    else if (fold) go(kvq_attn_kernel<HD, true, false, 1, 4>, join);
+    else cut.tiles == 1 ? go(kvq_attn_kernel<HD, false, false, 1, 4>, join) : go(kvq_attn_kernel<HD, false, false, 2, 8>, join);
   };
   if (hd == 128) pick(std::integral_constant<int, 128>{}, kvq_join_kernel<128>);
   else pick(std::integral_constant<int, 64>{}, kvq_join_kernel<64>);

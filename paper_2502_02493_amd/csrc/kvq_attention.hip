@@ -387,7 +387,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
   constexpr int ROWS = FOLD ? 4 : 16, CPV = HD / 16, NKT = HD / 32;
   __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
   __shared__ union Space {
-    f32x4 o[NW][ROWS][HD / 4];
+    f32x4 o[NW][ROWS][HD / 4 + 1];  // a row's results four banks behind the last's: sixteen lanes store the same channels of sixteen rows
     u32x4 q[FOLD ? 1 : RT * NKT * 3 * 64];
     __device__ Space() {}
   } space;

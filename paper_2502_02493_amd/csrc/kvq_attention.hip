@@ -617,7 +617,7 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
 
 // ------------------------------------------------------------------------------------------
 // Selection: (1) the blocks' scores, a workgroup to some blocks of a sequence, which reads their bounds once for all its new tokens;
-// (2) a wave to every (layer, token, KV head) finds a score that as many blocks reach as shall stay, bit by bit, and writes the list.
+// (2) a workgroup to every (layer, token, KV head) finds a score that as many blocks reach as shall stay, bit by bit, and writes the list.
 // ------------------------------------------------------------------------------------------
 // grid (groups of blocks of all entries, KV heads, layers)
 template <int HD>
@@ -654,15 +654,49 @@ __global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {
 
 // The order of scores as unsigned numbers: NaN below everything, the two zeros alike.
 __device__ __forceinline__ uint64_t score_key(double s) {
-  if (s != s) return 1;
+  if (s != s) return 1ull << 32;
   const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-// a wave to every list; lane i of the wave holds blocks 64 j + i
-constexpr int kSelectRegs = kMaxKvqSelect / 64;
-__global__ __launch_bounds__(64) void kvq_select_kernel(KvqSelectArgs a) {
-  const int t = blockIdx.x, h = blockIdx.y, l = blockIdx.z, lane = threadIdx.x;
+// A workgroup to every list; thread i holds blocks kSelectThreads j + i.  (A wave with all blocks in its registers: 10 us for 512 of them, much of
+// which its instructions took to arrive, three thousand, each executed a few times.)
+constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / 64, kSelectRegs = kMaxKvqSelect / kSelectThreads;
+struct SelectShared {
+  int count[2][kSelectWaves];
+  uint32_t any[kSelectWaves], all[kSelectWaves];
+};
+// How many of the workgroup's `yes` are set; turn: 0 and 1 in turn, so that a call's numbers are read before the next but one writes there.
+__device__ __forceinline__ int count_all(const bool (&yes)[kSelectRegs], SelectShared& sh, int& turn) {
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < kSelectRegs; ++j) n += __popcll(__ballot(yes[j]));
+  if ((threadIdx.x & 63) == 0) sh.count[turn][threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kSelectWaves; ++w) n += sh.count[turn][w];
+  turn ^= 1;
+  return n;
+}
+// A bound that `want` of the numbers reach, or, where equal ones prevent that, the want-th highest.  Bit by bit from `bit` down, the bits above being
+// those of `bound`, until as many reach it as are wanted.  A 0 counts for nothing.
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[kSelectRegs], int want, uint32_t bound, int bit, SelectShared& sh, int& turn) {
+  for (; bit >= 0; --bit) {
+    const uint32_t trial = bound | 1u << bit;
+    bool reaches[kSelectRegs];
+#pragma unroll
+    for (int j = 0; j < kSelectRegs; ++j) reaches[j] = key[j] >= trial;
+    const int n = count_all(reaches, sh, turn);
+    if (n >= want) bound = trial;
+    if (n == want) break;
+  }
+  return bound;
+}
+
+__global__ __launch_bounds__(kSelectThreads) void kvq_select_kernel(KvqSelectArgs a) {
+  __shared__ SelectShared sh;
+  const int t = blockIdx.x, h = blockIdx.y, l = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int e = 0;
 #pragma unroll
   for (int i = 1; i < kMaxCols; ++i) e += i < a.n_entries && t >= a.entry[i].q_first;
@@ -671,55 +705,83 @@ __global__ __launch_bounds__(64) void kvq_select_kernel(KvqSelectArgs a) {
   const size_t list = ((size_t)l * a.n_tokens + t) * a.heads + h;
   const double* scores = a.scores + list * a.most;
   int32_t* out = a.out + list * a.n_select;
-  const int last0 = max(0, held - a.last);
-  const auto forced = [&](int b) { return b < a.first || b >= last0; };
-  uint64_t key[kSelectRegs];  // 0: no block
-  int n_forced = 0;
-  uint64_t most = 0, least = ~0ull;  // of the others'
+  const int want = min(a.n_select, held), last0 = max(0, held - a.last), n_forced = min(held, a.first) + held - max(last0, min(held, a.first));
+  // the halves of the keys; 0, 0: no block.  A key's upper half is never 0; 0, ~0: a block that stays anyway
+  uint32_t hi[kSelectRegs], lo[kSelectRegs], any = 0, all = ~0u;
 #pragma unroll
   for (int j = 0; j < kSelectRegs; ++j) {
-    const int b = 64 * j + lane;
-    key[j] = 0;
-    if (64 * j >= held) continue;
-    if (b < held) key[j] = forced(b) ? ~0ull : score_key(scores[b]);
-    n_forced += __popcll(__ballot(key[j] == ~0ull));
-    if (key[j] != 0 && key[j] != ~0ull) most = max(most, key[j]), least = min(least, key[j]);
+    const int b = kSelectThreads * j + tid;
+    const bool there = b < held, forced = there && (b < a.first || b >= last0);
+    uint64_t key = 0;
+    if (there) key = score_key(scores[b]);
+    hi[j] = forced ? 0 : (uint32_t)(key >> 32);
+    lo[j] = forced ? ~0u : (uint32_t)key;
+    any |= hi[j];
+    all &= hi[j] ? hi[j] : ~0u;
   }
-  most = lanes_fold(most, 64, [](uint64_t x, uint64_t y) { return max(x, y); });
-  least = lanes_fold(least, 64, [](uint64_t x, uint64_t y) { return min(x, y); });
-  // a number that exactly `want` keys reach, or the want-th highest key: bit by bit from the highest that the keys differ in
-  const int want = min(a.n_select, held);
-  uint64_t bound = n_forced >= want ? ~0ull : 1;
-  if (n_forced < want && want < held) {
-    const int top = most == least ? -1 : 63 - __builtin_clzll(most ^ least);
-    bound = most & (top < 0 ? ~0ull : ~((2ull << top) - 1));
-    for (int bit = top; bit >= 0; --bit) {
-      const uint64_t trial = bound | 1ull << bit;
-      int n = 0;
+  // those that stay: over (bound_hi, bound_lo), and of those at it the lowest blocks; the forced ones first of all
+  const bool only_forced = n_forced >= want;
+  uint32_t bound_hi = ~0u, bound_lo = ~0u;
+  int turn = 0;
+  if (!only_forced) {
+    const int more = want - n_forced;
+    any = wave_or(any);
+    all = ~wave_or(~all);
+    if (lane == 0) sh.any[wave] = any, sh.all[wave] = all;
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kSelectRegs; ++j)
-        if (64 * j < held) n += __popcll(__ballot(key[j] >= trial));
-      if (n >= want) bound = trial;
-      if (n == want) break;
+    for (int w = 0; w < kSelectWaves; ++w) any |= sh.any[w], all &= sh.all[w];
+    const int top = 31 - __builtin_clz((any ^ all) | 1u);  // the highest bit that they differ in
+    bound_hi = bound_of(hi, more, all >> top >> 1 << top << 1, top, sh, turn);
+    bool yes[kSelectRegs];
+#pragma unroll
+    for (int j = 0; j < kSelectRegs; ++j) yes[j] = hi[j] >= bound_hi;
+    bound_lo = 0;
+    if (count_all(yes, sh, turn) > more) {  // scores alike in the upper half
+      uint32_t same[kSelectRegs];
+#pragma unroll
+      for (int j = 0; j < kSelectRegs; ++j) {
+        yes[j] = hi[j] > bound_hi;
+        same[j] = hi[j] == bound_hi ? lo[j] : 0;
+      }
+      const int over = count_all(yes, sh, turn);
+      bound_lo = bound_of(same, more - over, 0, 31, sh, turn);
     }
   }
-  int over = 0;
-#pragma unroll
-  for (int j = 0; j < kSelectRegs; ++j)
-    if (64 * j < held) over += __popcll(__ballot(key[j] > bound));
-  int ties = want - over, at = 0;  // of those at the bound the lowest blocks
-  const unsigned long long below = (1ull << lane) - 1;
+  int group[kSelectRegs];  // 2: stays, 1: stays as one of the lowest, 0: does not
+  bool yes[kSelectRegs];
 #pragma unroll
   for (int j = 0; j < kSelectRegs; ++j) {
-    if (64 * j >= held) break;
-    const unsigned long long same = __ballot(key[j] == bound);
-    const bool stays = key[j] > bound || (key[j] == bound && __popcll(same & below) < ties);
-    const unsigned long long stay = __ballot(stays);
-    if (stays) out[at + __popcll(stay & below)] = 64 * j + lane;
-    at += __popcll(stay);
-    ties -= min(ties, (int)__popcll(same));
+    const bool forced = hi[j] == 0 && lo[j] != 0;
+    group[j] = only_forced ? forced : forced || hi[j] > bound_hi || (hi[j] == bound_hi && lo[j] > bound_lo) ? 2 : hi[j] == bound_hi && lo[j] == bound_lo;
+    yes[j] = group[j] == 2;
   }
-  for (int i = at + lane; i < a.n_select; i += 64) out[i] = -1;
+  int ties = want - count_all(yes, sh, turn), at = 0;
+  const unsigned long long below = (1ull << lane) - 1;
+  // in the order of the blocks: runs of kSelectThreads, in them the waves.  tied and stay: of the waves in front, then of all
+#pragma unroll
+  for (int j = 0; j < kSelectRegs; ++j) {
+    if (kSelectThreads * j < held) {
+      const unsigned long long tied = __ballot(group[j] == 1), sure = __ballot(group[j] == 2);
+      __syncthreads();
+      if (lane == 0) sh.count[0][wave] = __popcll(tied), sh.count[1][wave] = __popcll(sure);
+      __syncthreads();
+      int tied_before = 0, tied_all = 0, sure_before = 0, sure_all = 0;
+#pragma unroll
+      for (int w = 0; w < kSelectWaves; ++w) {
+        tied_before += w < wave ? sh.count[0][w] : 0;
+        sure_before += w < wave ? sh.count[1][w] : 0;
+        tied_all += sh.count[0][w];
+        sure_all += sh.count[1][w];
+      }
+      const int tied_in_front = tied_before + __popcll(tied & below);
+      if (group[j] == 2 || (group[j] == 1 && tied_in_front < ties))
+        out[at + sure_before + __popcll(sure & below) + min(tied_in_front, ties)] = kSelectThreads * j + tid;
+      at += sure_all + min(tied_all, ties);
+      ties -= min(tied_all, ties);
+    }
+  }
+  for (int i = at + tid; i < a.n_select; i += kSelectThreads) out[i] = -1;
 }
 
 size_t kvq_select_workspace_bytes(const KvqSelectArgs& a, int n_layers) { return (size_t)n_layers * a.n_tokens * a.heads * a.most * sizeof(double); }
@@ -737,7 +799,7 @@ void launch_kvq_select(const KvqSelectArgs& args, int n_layers, int hd, hipStrea
   }
   if (hd == 128) hipLaunchKernelGGL(kvq_score_kernel<128>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
   else hipLaunchKernelGGL(kvq_score_kernel<64>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
-  hipLaunchKernelGGL(kvq_select_kernel, dim3(a.n_tokens, a.heads, n_layers), dim3(64), 0, st, a);
+  hipLaunchKernelGGL(kvq_select_kernel, dim3(a.n_tokens, a.heads, n_layers), dim3(kSelectThreads), 0, st, a);
 }
 
 }  // namespace es

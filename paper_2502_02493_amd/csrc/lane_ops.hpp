@@ -78,6 +78,12 @@ __device__ __forceinline__ uint32_t lanes_running_sum(uint32_t v) {
   return v;
 }
 
+// The bits that are set in any of the wave's lanes.
+__device__ __forceinline__ uint32_t wave_or(uint32_t v) {
+  const auto f = [](float a, float b) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) | __builtin_bit_cast(uint32_t, b)); };
+  return __builtin_bit_cast(uint32_t, lanes_fold(__builtin_bit_cast(float, v), 64, f));
+}
+
 // The lowest of the wave's values, which are the same in every lane of each group of n (4, 8, 16, 32 or 64) neighbours.
 __device__ __forceinline__ float groups_min(float v, int n) {
   const auto f = [](float a, float b) { return fminf(a, b); };

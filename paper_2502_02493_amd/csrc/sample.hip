@@ -174,7 +174,7 @@ struct Bins {
 // The bins that matter, as up to four runs in ascending order, apart from each other: what is in front of a word is what its list has in
 // front of it and what lies between the runs.
 struct NearBins {
-  int lo[4], hi[4], n_count, k_on, p_on, m_on, m_bin, pad;
+  int lo[4], hi[4], k_on, p_on, m_on, m_bin;
   u64 weight[4], count[4];  // not on the list, in front of the run
   u64 all, m_front;         // the row's weight; what is in front of the border's bin of min_p
   float x0, x1;             // logits outside are in none of the runs
@@ -256,7 +256,6 @@ __device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, 
       first = min(first, n.lo[i]);
     }
   }
-  n.n_count = (int)listed_c;
   n.x0 = w.logit_at_bin(end + 1, 1.0 + 1e-5);
   n.x1 = w.logit_at_bin(first, 1.0 - 1e-5);
 }
@@ -567,16 +566,22 @@ __device__ __forceinline__ float2 ends_of(const float* row, int v0, int v1, floa
   lo = -block_max<NT / 64>(-lo, sh + NT / 64);
   return make_float2(hi, lo);
 }
+// counts: only top_k asks for them.
 template <int NT>
-__device__ __forceinline__ void add_to_bins(const Weigher& w, const float* row, int v0, int v1, u64* weight, uint32_t* count) {
-  each_word<NT>(row, v0, v1, [&](float x, int) {
-    const double y = w.below(x);
-    const int b = w.bin(y);
-    atomicAdd(&count[b], 1u);
-    if (y < kFar) atomicAdd(&weight[b], w.weight(y));
-  });
+__device__ __forceinline__ void add_to_bins(const Weigher& w, const float* row, int v0, int v1, u64* weight, uint32_t* count, bool counts) {
+  const auto all = [&](auto with_counts) {
+    each_word<NT>(row, v0, v1, [&](float x, int) {
+      const double y = w.below(x);
+      const int b = w.bin(y);
+      if (decltype(with_counts)::value) atomicAdd(&count[b], 1u);
+      if (y < kFar) atomicAdd(&weight[b], w.weight(y));
+    });
+  };
+  if (counts) all(std::true_type{});
+  else all(std::false_type{});
 }
-// The near words of a part of a row, listed in any order: a wave asks for places once for every eight words of its lanes.
+// The near words of a part of a row, listed in any order: a wave asks for places once for every eight words of its lanes.  *n counts
+// them all, those past kNear, which are not listed, too.
 template <int NT>
 __device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, int v0, int v1, u64* words, uint32_t* n) {
   constexpr int kAhead = 8;
@@ -604,7 +609,8 @@ __device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near
     at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (in[i] >> lane & 1) words[at + __popcll(in[i] & ((1ull << lane) - 1))] = place_of(x[i], base + i * NT + (int)threadIdx.x);
+      const uint32_t mine = at + __popcll(in[i] & ((1ull << lane) - 1));
+      if ((in[i] >> lane & 1) && mine < kNear) words[mine] = place_of(x[i], base + i * NT + (int)threadIdx.x);
       at += __popcll(in[i]);
     }
   }
@@ -654,7 +660,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   }
   const Weigher w(a, ends.x, ends.y);
   const double u = a.tokens ? (double)a.u[r] : 0.0;
-  add_to_bins<NT>(w, row, 0, a.V, sp.bins.weight, sp.bins.count);
+  add_to_bins<NT>(w, row, 0, a.V, sp.bins.weight, sp.bins.count, a.top_k > 0);
   __syncthreads();
   constexpr int N = kBins / NT;
   u64 bw[N];
@@ -664,12 +670,12 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   scan_bins(sp.bins, bw, bc);
   near_bins(a, w, u, sp.bins, near);
   Cut cut;
-  if (near.n_count <= kNear) {
-    list_near<NT>(w, near, row, 0, a.V, sp.words, &s_near);
-    __syncthreads();
-    cut = resolve_any<NT>(a, w, u, near, sp.words, near.n_count, sp.words, rs);
+  list_near<NT>(w, near, row, 0, a.V, sp.words, &s_near);
+  __syncthreads();
+  const int n = (int)s_near;
+  if (n <= kNear) {
+    cut = resolve_any<NT>(a, w, u, near, sp.words, n, sp.words, rs);
   } else {
-    __syncthreads();
     cut = resolve_by_digits<NT>(a, w, u, row, sp.digits, rs.scan);
   }
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
@@ -769,13 +775,12 @@ __global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
   const float2 ends = row_ends(a, &s_ends);
   if (no_word(ends.x)) return;
   const Weigher w(a, ends.x, ends.y);
-  add_to_bins<kSliceNT>(w, a.logits + r * a.V, v0, v1, s_weight, s_count);
+  add_to_bins<kSliceNT>(w, a.logits + r * a.V, v0, v1, s_weight, s_count, a.top_k > 0);
   __syncthreads();
-  for (int i = tid; i < kBins; i += kSliceNT)
-    if (s_count[i]) {
-      atomicAdd(&a.count[r * (kBins + 1) + i], s_count[i]);
-      if (s_weight[i]) atomicAdd(&a.weight[r * kBins + i], s_weight[i]);
-    }
+  for (int i = tid; i < kBins; i += kSliceNT) {
+    if (s_count[i]) atomicAdd(&a.count[r * (kBins + 1) + i], s_count[i]);
+    if (s_weight[i]) atomicAdd(&a.weight[r * kBins + i], s_weight[i]);
+  }
 }
 
 // grid (cuts, rows)
@@ -798,7 +803,7 @@ __global__ __launch_bounds__(kCutNT) void sample_near_kernel(SampleArgs a) {
   scan_bins(bins, bw, bc);
   near_bins(a, w, u, bins, near);
   if (blockIdx.x == 0 && tid == 0) a.bins[r] = near;
-  if (near.n_count <= kNear) list_near<kCutNT>(w, near, a.logits + r * a.V, v0, v1, a.near + r * kNear, &a.count[r * (kBins + 1) + kBins]);
+  list_near<kCutNT>(w, near, a.logits + r * a.V, v0, v1, a.near + r * kNear, &a.count[r * (kBins + 1) + kBins]);
 }
 
 // grid (parts or 1, rows)
@@ -825,8 +830,9 @@ __global__ __launch_bounds__(kPartNT) void sample_finish_kernel(SampleArgs a) {
   const double u = a.tokens ? (double)a.u[r] : 0.0;
   const NearBins near = a.bins[r];
   Cut cut;
-  if (near.n_count <= kNear) {
-    cut = resolve_any<kPartNT>(a, w, u, near, a.near + r * kNear, near.n_count, sp.words, rs);
+  const uint32_t n = a.count[r * (kBins + 1) + kBins];
+  if (n <= kNear) {
+    cut = resolve_any<kPartNT>(a, w, u, near, a.near + r * kNear, (int)n, sp.words, rs);
   } else {
     // one workgroup reads the whole row, which may be where the results go
     if (blockIdx.x > 0) return;

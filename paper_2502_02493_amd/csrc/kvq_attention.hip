@@ -619,8 +619,8 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
 // Selection: (1) the blocks' scores, a workgroup to some blocks of a sequence, which reads their bounds once for all its new tokens;
 // (2) a workgroup to every (layer, token, KV head) finds a score that as many blocks reach as shall stay, bit by bit, and writes the list.
 // ------------------------------------------------------------------------------------------
-// grid (groups of blocks of all entries, KV heads, layers)
-template <int HD>
+// grid (groups of blocks of all entries, KV heads, layers).  G: query heads of a KV head, or one more: their queries are requested together.
+template <int HD, int G>
 __global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {
   constexpr int LANES = HD / 8, BLOCKS = 256 / LANES;  // lanes to a block: eight channels each
   int e = 0;
@@ -631,22 +631,27 @@ __global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {
   const int block = (blockIdx.x - a.first_wg[e]) * BLOCKS + threadIdx.x / LANES;
   const int held = (en.len + kKvqBlock - 1) / kKvqBlock;
   const u32x4* src = reinterpret_cast<const u32x4*>(a.bounds + ((((size_t)l * a.n_seqs + en.seq) * a.heads + h) * a.max_blocks + min(block, held - 1)) * 2 * HD) + lane;
-  float lo[8], hi[8];
-  unpack<bf16_t>(src[0], lo);
-  unpack<bf16_t>(src[HD / 8], hi);
+  const u32x4 lo_bits = src[0], hi_bits = src[HD / 8];
   for (int t = 0; t < en.n; ++t) {
-    const float* q = a.q + (((size_t)l * a.n_tokens + en.q_first + t) * a.Hq + h * a.group) * HD + lane * 8;
+    const f32x4* q = reinterpret_cast<const f32x4*>(a.q + (((size_t)l * a.n_tokens + en.q_first + t) * a.Hq + h * a.group) * HD + lane * 8);
+    f32x4 x[G][2];
+#pragma unroll
+    for (int j = 0; j < G; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) x[j][i] = q[min(j, a.group - 1) * (HD / 4) + i];
+    float lo[8], hi[8];
+    unpack<bf16_t>(lo_bits, lo);
+    unpack<bf16_t>(hi_bits, hi);
     double best = NAN;
-    for (int j = 0; j < a.group; ++j) {
-      const f32x4 q0 = reinterpret_cast<const f32x4*>(q + (size_t)j * HD)[0], q1 = reinterpret_cast<const f32x4*>(q + (size_t)j * HD)[1];
+#pragma unroll
+    for (int j = 0; j < G; ++j) {
       double s = 0.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = i < 4 ? q0[i % 4] : q1[i % 4];
-        s = fma((double)x, (double)(x > 0.f ? hi[i] : lo[i]), s);
+        const float v = x[j][i / 4][i % 4];
+        s = fma((double)v, (double)(v > 0.f ? hi[i] : lo[i]), s);
       }
-      s = lanes_sum(s, LANES);
-      best = fmax(best, s);  // passes over NaN
+      best = fmax(best, lanes_sum(s, LANES));  // passes over NaN; a head twice is the head
     }
     if (lane == 0 && block < held) a.scores[(((size_t)l * a.n_tokens + en.q_first + t) * a.heads + h) * a.most + block] = best;
   }
@@ -663,33 +668,44 @@ __device__ __forceinline__ uint64_t score_key(double s) {
 // which its instructions took to arrive, three thousand, each executed a few times.)
 constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / 64, kSelectRegs = kMaxKvqSelect / kSelectThreads;
 struct SelectShared {
-  int count[2][kSelectWaves];
+  int count[2][3][kSelectWaves];
   uint32_t any[kSelectWaves], all[kSelectWaves];
 };
-// How many of the workgroup's `yes` are set; turn: 0 and 1 in turn, so that a call's numbers are read before the next but one writes there.
-__device__ __forceinline__ int count_all(const bool (&yes)[kSelectRegs], SelectShared& sh, int& turn) {
-  int n = 0;
+// How many of the workgroup's keys reach each of three numbers; turn: 0 and 1 in turn, so that a call's counts are read before the next but one writes there.
+struct Three {
+  int n[3];
+};
+__device__ __forceinline__ Three count_from(const uint32_t (&key)[kSelectRegs], uint32_t a, uint32_t b, uint32_t c, SelectShared& sh, int& turn) {
+  Three r = {{0, 0, 0}};
 #pragma unroll
-  for (int j = 0; j < kSelectRegs; ++j) n += __popcll(__ballot(yes[j]));
-  if ((threadIdx.x & 63) == 0) sh.count[turn][threadIdx.x >> 6] = n;
+  for (int j = 0; j < kSelectRegs; ++j) {
+    r.n[0] += __popcll(__ballot(key[j] >= a));
+    r.n[1] += __popcll(__ballot(key[j] >= b));
+    r.n[2] += __popcll(__ballot(key[j] >= c));
+  }
+  if ((threadIdx.x & 63) < 3) {
+    const int i = threadIdx.x & 63;
+    sh.count[turn][i][threadIdx.x >> 6] = i == 0 ? r.n[0] : i == 1 ? r.n[1] : r.n[2];
+  }
   __syncthreads();
-  n = 0;
 #pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) n += sh.count[turn][w];
+  for (int i = 0; i < 3; ++i) {
+    r.n[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) r.n[i] += sh.count[turn][i][w];
+  }
   turn ^= 1;
-  return n;
+  return r;
 }
-// A bound that `want` of the numbers reach, or, where equal ones prevent that, the want-th highest.  Bit by bit from `bit` down, the bits above being
-// those of `bound`, until as many reach it as are wanted.  A 0 counts for nothing.
+// A bound that `want` of the numbers reach, or, where equal ones prevent that, the want-th highest.  Two bits at a time from `bit` (odd) down, the bits
+// above being those of `bound`, until as many reach it as are wanted.  A 0 counts for nothing.
 __device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[kSelectRegs], int want, uint32_t bound, int bit, SelectShared& sh, int& turn) {
-  for (; bit >= 0; --bit) {
-    const uint32_t trial = bound | 1u << bit;
-    bool reaches[kSelectRegs];
-#pragma unroll
-    for (int j = 0; j < kSelectRegs; ++j) reaches[j] = key[j] >= trial;
-    const int n = count_all(reaches, sh, turn);
-    if (n >= want) bound = trial;
-    if (n == want) break;
+  for (bit -= 1; bit >= 0; bit -= 2) {
+    const uint32_t step = 1u << bit;
+    const Three r = count_from(key, bound + step, bound + 2 * step, bound + 3 * step, sh, turn);
+    const int digit = r.n[2] >= want ? 3 : r.n[1] >= want ? 2 : r.n[0] >= want ? 1 : 0;
+    bound += digit * step;
+    if (r.n[2] == want || r.n[1] == want || r.n[0] == want) break;  // the highest number that as many reach is one that exactly they reach
   }
   return bound;
 }
@@ -731,32 +747,26 @@ __global__ __launch_bounds__(kSelectThreads) void kvq_select_kernel(KvqSelectArg
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kSelectWaves; ++w) any |= sh.any[w], all &= sh.all[w];
-    const int top = 31 - __builtin_clz((any ^ all) | 1u);  // the highest bit that they differ in
+    const int top = (31 - __builtin_clz((any ^ all) | 1u)) | 1;  // the highest bit that they differ in, or the one above
     bound_hi = bound_of(hi, more, all >> top >> 1 << top << 1, top, sh, turn);
-    bool yes[kSelectRegs];
-#pragma unroll
-    for (int j = 0; j < kSelectRegs; ++j) yes[j] = hi[j] >= bound_hi;
+    const Three r = count_from(hi, bound_hi, bound_hi + 1, ~0u, sh, turn);  // no upper half is all ones
     bound_lo = 0;
-    if (count_all(yes, sh, turn) > more) {  // scores alike in the upper half
+    if (r.n[0] > more) {  // scores alike in the upper half
       uint32_t same[kSelectRegs];
 #pragma unroll
-      for (int j = 0; j < kSelectRegs; ++j) {
-        yes[j] = hi[j] > bound_hi;
-        same[j] = hi[j] == bound_hi ? lo[j] : 0;
-      }
-      const int over = count_all(yes, sh, turn);
-      bound_lo = bound_of(same, more - over, 0, 31, sh, turn);
+      for (int j = 0; j < kSelectRegs; ++j) same[j] = hi[j] == bound_hi ? lo[j] : 0;
+      bound_lo = bound_of(same, more - r.n[1], 0, 31, sh, turn);
     }
   }
   int group[kSelectRegs];  // 2: stays, 1: stays as one of the lowest, 0: does not
-  bool yes[kSelectRegs];
+  uint32_t grade[kSelectRegs];
 #pragma unroll
   for (int j = 0; j < kSelectRegs; ++j) {
     const bool forced = hi[j] == 0 && lo[j] != 0;
     group[j] = only_forced ? forced : forced || hi[j] > bound_hi || (hi[j] == bound_hi && lo[j] > bound_lo) ? 2 : hi[j] == bound_hi && lo[j] == bound_lo;
-    yes[j] = group[j] == 2;
+    grade[j] = (uint32_t)group[j];
   }
-  int ties = want - count_all(yes, sh, turn), at = 0;
+  int ties = want - count_from(grade, 2, 3, 3, sh, turn).n[0], at = 0;
   const unsigned long long below = (1ull << lane) - 1;
   // in the order of the blocks: runs of kSelectThreads, in them the waves.  tied and stay: of the waves in front, then of all
 #pragma unroll
@@ -764,15 +774,15 @@ __global__ __launch_bounds__(kSelectThreads) void kvq_select_kernel(KvqSelectArg
     if (kSelectThreads * j < held) {
       const unsigned long long tied = __ballot(group[j] == 1), sure = __ballot(group[j] == 2);
       __syncthreads();
-      if (lane == 0) sh.count[0][wave] = __popcll(tied), sh.count[1][wave] = __popcll(sure);
+      if (lane == 0) sh.count[0][0][wave] = __popcll(tied), sh.count[0][1][wave] = __popcll(sure);
       __syncthreads();
       int tied_before = 0, tied_all = 0, sure_before = 0, sure_all = 0;
 #pragma unroll
       for (int w = 0; w < kSelectWaves; ++w) {
-        tied_before += w < wave ? sh.count[0][w] : 0;
-        sure_before += w < wave ? sh.count[1][w] : 0;
-        tied_all += sh.count[0][w];
-        sure_all += sh.count[1][w];
+        tied_before += w < wave ? sh.count[0][0][w] : 0;
+        sure_before += w < wave ? sh.count[0][1][w] : 0;
+        tied_all += sh.count[0][0][w];
+        sure_all += sh.count[0][1][w];
       }
       const int tied_in_front = tied_before + __popcll(tied & below);
       if (group[j] == 2 || (group[j] == 1 && tied_in_front < ties))
@@ -797,8 +807,15 @@ void launch_kvq_select(const KvqSelectArgs& args, int n_layers, int hd, hipStrea
     a.first_wg[i] = wg;
     wg += ((a.entry[i].len + kKvqBlock - 1) / kKvqBlock + per - 1) / per;
   }
-  if (hd == 128) hipLaunchKernelGGL(kvq_score_kernel<128>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(kvq_score_kernel<64>, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a);
+  auto score = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wg, a.heads, n_layers), dim3(256), 0, st, a); };
+  auto pick = [&](auto hd_) {
+    constexpr int HD = decltype(hd_)::value;
+    if (a.group > 4) score(kvq_score_kernel<HD, 8>);
+    else if (a.group > 2) score(kvq_score_kernel<HD, 4>);
+    else score(kvq_score_kernel<HD, 2>);
+  };
+  if (hd == 128) pick(std::integral_constant<int, 128>{});
+  else pick(std::integral_constant<int, 64>{});
   hipLaunchKernelGGL(kvq_select_kernel, dim3(a.n_tokens, a.heads, n_layers), dim3(kSelectThreads), 0, st, a);
 }
 

@@ -543,34 +543,49 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   reinterpret_cast<f32x4*>(a.out + ((size_t)l * a.n_tokens * a.Hq + (size_t)t * a.Hq + j) * HD)[c4] = o * inv;
 }
 
-// How a call is cut.  Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
+// How a call is cut: into no more workgroups than CUs.  What one does before its first step and after its last (queries, results of its waves joined,
+// 5 us) costs as much as three to five steps of a wave, and a second round of workgroups adds it again.  us a call in a graph, with at most 256 / 512
+// workgroups: one token at 32768 and 65536 slots of 8 KV heads 16.9 / 22.3 and 22.4 / 27.7, sixteen at 8192 35.1 / 42.0, six at 16384 17.9 / 24.2,
+// sixteen of 16 tokens at 512 .. 1067 on 4 heads 20.7 / 46.
+//   Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
+//   Waves: eight, but four where a wave of eight would have a step or less.  four / eight: one token at 65536 slots 23.5 / 22.4, sixteen at
+//   8192 41.6 / 35.1, with seven heads to a KV head 25.9 / 23.4; at 16384 (2048 steps) 11.8 / 11.9.
+constexpr int kKvqCus = 256, kKvqFewSteps = 2048;
 struct KvqCut {
-  int rows, tiles, waves, wgs;  // rows of a workgroup's sequence or token; row tiles to a wave; waves of a workgroup; workgroups, at most
+  int rows, tiles, waves;  // rows of a sequence's (a token's) queries on a KV head; row tiles to a wave; waves of a workgroup
 };
-static KvqCut kvq_cut(const KvqArgs& a) {
-  KvqCut c;
-  c.rows = 0;
-  for (int i = 0; i < a.n_entries; ++i) c.rows = std::max(c.rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
-  c.tiles = c.rows <= 16 ? 1 : 2;
-  c.waves = c.tiles == 2 ? 8 : 4;
-  static const int w8 = env_int("KVQ_W8", 256), w4 = env_int("KVQ_WGS", 768);
-  c.wgs = c.tiles == 2 ? w8 : w4;
+static KvqCut kvq_cut(const KvqArgs& a, int n_layers) {
+  KvqCut c = {0, 1, 4};
+  long steps = 0;
+  for (int i = 0; i < a.n_entries; ++i) {
+    c.rows = std::max(c.rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
+    steps += a.n_blocks ? 2l * a.entry[i].n * a.n_blocks : (a.entry[i].len + kStep - 1) / kStep;
+  }
+  if (c.rows > 16) c.tiles = 2;
+  if (c.tiles == 2 || steps * a.heads * n_layers > kKvqFewSteps) c.waves = 8;
   return c;
 }
 void kvq_plan(KvqArgs& a, int n_layers) {
   a.inv_group = 1.f / (float)a.group;
-  const KvqCut cut = kvq_cut(a);
+  const KvqCut cut = kvq_cut(a, n_layers);
   const auto pieces = [&](const KvqEntry& e) { return a.n_blocks ? a.n_blocks : (e.len + kStep - 1) / kStep; };
   for (int i = 0; i < a.n_entries; ++i) a.entry[i].tiles = a.n_blocks ? 1 : (a.entry[i].n * a.group + 16 * cut.tiles - 1) / (16 * cut.tiles);
-  const auto count = [&](int chunk) {
+  const auto count = [&](int chunk) {  // workgroups; of chunks of one, their work
     long wgs = 0;
     for (int i = 0; i < a.n_entries; ++i) wgs += (long)((pieces(a.entry[i]) + chunk - 1) / chunk) * (a.n_blocks ? a.entry[i].n : a.entry[i].tiles);
     return wgs * a.heads * n_layers;
   };
-  // a step at least for every wave (a block of a list is two); with lists an entry to a lane at most
-  const int least = a.n_blocks ? cut.waves / 2 : cut.waves, most = a.n_blocks ? 64 : 65536 / kStep;
-  for (a.chunk = least; a.chunk < most && count(a.chunk) > cut.wgs; a.chunk += least) {
+  // a step at least for every wave (a block of a list is two); with lists an entry to a lane at most; no more than twice what a CU has to do on
+  // average, so that one long context beside many short ones is not one workgroup's
+  const int least = a.n_blocks ? cut.waves / 2 : cut.waves;
+  const long most = std::min<long>(a.n_blocks ? 64 : 65536 / kStep, std::max<long>(least, (2 * count(1) / kKvqCus + least - 1) / least * least));
+  int lo = 1, hi = (int)(most / least);  // the shortest chunk, in these units, that leaves no more workgroups than CUs, or the longest
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (count(mid * least) <= kKvqCus) hi = mid;
+    else lo = mid + 1;
   }
+  a.chunk = lo * least;
   int wg = 0;
   size_t part = 0;
   for (int i = 0; i < kMaxCols; ++i) {
@@ -599,7 +614,7 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
   KvqArgs a = args;
   if (a.n_entries == 0) return;
   a.part_ml = reinterpret_cast<float2*>(a.part + a.part_pitch * a.heads * n_layers * hd);
-  const KvqCut cut = kvq_cut(a);
+  const KvqCut cut = kvq_cut(a, n_layers);
   const bool fold = cut.rows <= 4;
   auto go = [&](auto kernel, auto join) {
     hipLaunchKernelGGL(kernel, dim3(a.n_wgs, a.heads, n_layers), dim3(cut.waves * 64), 0, st, a);
@@ -607,9 +622,13 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
   };
   auto pick = [&](auto hd_, auto join) {
     constexpr int HD = decltype(hd_)::value;
-    if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true, 1, 4>, join) : go(kvq_attn_kernel<HD, false, true, 1, 4>, join);
-    else if (fold) go(kvq_attn_kernel<HD, true, false, 1, 4>, join);
-    else cut.tiles == 1 ? go(kvq_attn_kernel<HD, false, false, 1, 4>, join) : go(kvq_attn_kernel<HD, false, false, 2, 8>, join);
+    const auto by_waves = [&](auto waves) {
+      constexpr int NW = decltype(waves)::value;
+      if (a.blocks) fold ? go(kvq_attn_kernel<HD, true, true, 1, NW>, join) : go(kvq_attn_kernel<HD, false, true, 1, NW>, join);
+      else fold ? go(kvq_attn_kernel<HD, true, false, 1, NW>, join) : go(kvq_attn_kernel<HD, false, false, 1, NW>, join);
+    };
+    if (cut.tiles == 2) go(kvq_attn_kernel<HD, false, false, 2, 8>, join);
+    else cut.waves == 8 ? by_waves(std::integral_constant<int, 8>{}) : by_waves(std::integral_constant<int, 4>{});
   };
   if (hd == 128) pick(std::integral_constant<int, 128>{}, kvq_join_kernel<128>);
   else pick(std::integral_constant<int, 64>{}, kvq_join_kernel<64>);

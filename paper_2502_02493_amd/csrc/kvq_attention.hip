@@ -550,17 +550,24 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
 //   Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
 //   Waves: eight, but four where a wave of eight would have a step or less.  four / eight: one token at 65536 slots 23.5 / 22.4, sixteen at
 //   8192 41.6 / 35.1, with seven heads to a KV head 25.9 / 23.4; at 16384 (2048 steps) 11.8 / 11.9.
-constexpr int kKvqCus = 256, kKvqFewSteps = 2048;
+//   Contexts of two steps a wave are not cut: no second launch.  cut / whole, 32 query heads on 8 KV heads: one token at 256, 512, 768 slots 8.5 / 7.2,
+//   8.5 / 8.5, 8.7 / 9.7, six at 512 and 1024 11.9 / 11.2, 11.9 / 16.
+constexpr int kKvqCus = 256, kKvqFewSteps = 2048, kKvqWhole = 16;
 struct KvqCut {
   int rows, tiles, waves;  // rows of a sequence's (a token's) queries on a KV head; row tiles to a wave; waves of a workgroup
+  bool whole;              // no context is cut
 };
 static KvqCut kvq_cut(const KvqArgs& a, int n_layers) {
-  KvqCut c = {0, 1, 4};
+  KvqCut c = {0, 1, 4, false};
   long steps = 0;
   for (int i = 0; i < a.n_entries; ++i) {
     c.rows = std::max(c.rows, a.n_blocks ? a.group : a.entry[i].n * a.group);
     steps += a.n_blocks ? 2l * a.entry[i].n * a.n_blocks : (a.entry[i].len + kStep - 1) / kStep;
   }
+  int longest = 0;
+  for (int i = 0; i < a.n_entries; ++i) longest = std::max(longest, a.n_blocks ? 2 * a.n_blocks : (a.entry[i].len + kStep - 1) / kStep);
+  c.whole = longest <= kKvqWhole;
+  if (c.whole && longest > 4) c.waves = 8;
   if (c.rows > 16) c.tiles = 2;
   if (c.tiles == 2 || steps * a.heads * n_layers > kKvqFewSteps) c.waves = 8;
   return c;
@@ -586,6 +593,7 @@ void kvq_plan(KvqArgs& a, int n_layers) {
     else lo = mid + 1;
   }
   a.chunk = lo * least;
+  if (cut.whole) a.chunk = a.n_blocks ? a.n_blocks : 65536 / kStep;
   int wg = 0;
   size_t part = 0;
   for (int i = 0; i < kMaxCols; ++i) {

@@ -24,7 +24,8 @@ static_assert(kMaxSampleVocab == 1 << kTokenBits, "a place number holds a token"
 constexpr int kBins = 1024, kFineBins = 896;  // evenly over y up to 48, where weights end, or to the lowest logit's; then four to a doubling
 constexpr int kNear = 4096;                    // words that are sorted
 constexpr int kDigitBins = 2048;
-constexpr int kShortRow = 2048;  // words of a row that are sorted, all of them
+constexpr int kShortRow = 2048;   // words of a row that are sorted, all of them
+constexpr int kRowWords = 12288;  // words of a row that stays with one workgroup
 constexpr double kFar = 48.0;
 
 // A word's place number: the higher, the earlier in the order; 0 is no word (minus infinity, NaN).
@@ -737,7 +738,7 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
 // A row to several workgroups, in four launches: (1) the slices' highest and lowest logits; (2) their bins, added up; (3) the words of the
 // near bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
 // ------------------------------------------------------------------------------------------
-constexpr int kSliceNT = 1024, kMaxSlices = 64;
+constexpr int kSliceNT = 1024, kMaxSlices = 64, kSliceWgs = 512;
 constexpr int kCutNT = 256, kMaxCuts = 64, kCutWgs = 2048;
 constexpr int kPartNT = 512, kMaxParts = 64, kPartWgs = 512;
 
@@ -844,9 +845,14 @@ __global__ __launch_bounds__(kPartNT) void sample_finish_kernel(SampleArgs a) {
   if (out) write_row<kPartNT>(a, w, cut, row, out, v0, v1);
 }
 
+// One launch or four.  A row kept to one workgroup costs one launch, and a time that grows with the row alone; slices pay from some
+// 12 thousand words on (us in a graph, one launch : four): 1 row of 6000 16.6 : 20.0, of 12 000 23.0 : 21.1 and of 24 000
+// 32.6 : 21.4; 96 rows of 8000 18.8 : 26.8, of 12 000 24.3 : 29.9, of 24 000 34.8 : 34.9, of 50 000 64 : 48, of 152 064 172 : 93; and
+// beside each stand the 8 us that three more launches take from the host.  Past 512 rows the rows alone fill the chip twice: 300 rows
+// of 152 064 365 : 290, 600 rows 565 : 507, 1200 rows 947 : 938 (with top_k 776 : 847).
 static int sample_slices(int rows, int V) {
-  if (V <= kShortRow) return 1;
-  return std::max(1, std::min({kMaxSlices, (V + 4095) / 4096, 512 / rows}));
+  if (V <= kRowWords || rows > kSliceWgs) return 1;
+  return std::max(2, std::min({kMaxSlices, (V + 4095) / 4096, kSliceWgs / rows}));
 }
 static size_t sample_row_bytes() { return kMaxSlices * sizeof(float2) + kBins * sizeof(u64) + (kBins + 1) * sizeof(uint32_t) + kNear * sizeof(u64) + sizeof(NearBins); }
 size_t sample_workspace_bytes(int rows, int V) { return sample_slices(rows, V) > 1 ? rows * sample_row_bytes() : 16; }

@@ -163,6 +163,14 @@ def test_many_rows(es):
     check(es, logits, u, 0.8, 0, 0.9, 0.0)
 
 
+@pytest.mark.parametrize("R,V", [(2, 2048), (2, 2049), (3, 12288), (3, 12289), (300, 13001), (512, 12300), (513, 12300)])
+def test_where_the_ways_of_cutting_rows_change(es, R, V):
+    logits, u = normal(R + V, R, V)
+    logits[-1] = np.round(logits[-1] * 2) / 2              # thousands of equal ones
+    check(es, logits, u, 0.9, 0, 0.85, 0.0)
+    check(es, logits, u, 0.8, 60, 0.95, 0.01)
+
+
 def test_streams_and_graphs(es):
     """Captured calls with their own workspaces, replayed between eager ones: bits do not change."""
     import torch

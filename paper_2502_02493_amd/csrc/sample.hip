@@ -51,7 +51,7 @@ struct SampleArgs {
   int32_t* tokens;
   float* out;
   // rows cut into slices, and into more of them where a workgroup has little to do
-  int slices, per, cuts, per_cut, parts, per_part;
+  int slices, per, cuts, per_cut;
   float2* slice_ends;  // [row][slices]  highest and lowest logit
   u64* weight;         // [row][kBins]
   uint32_t* count;     // [row][kBins + 1], the last one counting near words
@@ -85,18 +85,6 @@ struct Weigher {
     return (float)(times > 1.0 ? x - room : x + room);
   }
   __device__ __forceinline__ bool over(float x, double min_z) const { return (double)x - top >= min_z; }
-  __device__ __forceinline__ float least_over(double min_z) const {  // the lowest number that is
-    if (min_z == -INFINITY) return -INFINITY;
-    const float x = (float)(top + min_z);  // or its neighbour
-    if (!over(x, min_z)) return next(x, true);
-    const float below = next(x, false);
-    return over(below, min_z) ? below : x;
-  }
-  static __device__ __forceinline__ float next(float x, bool up) {
-    if (x == 0.f) return __uint_as_float(up ? 1u : 0x80000001u);
-    const uint32_t u = __float_as_uint(x);
-    return __uint_as_float((x > 0.f) == up ? u + 1 : u - 1);
-  }
 };
 
 // Words of row[v0, v1): body(x, v), eight loads of a thread under way.
@@ -175,15 +163,25 @@ struct Bins {
 // The bins that matter, as up to four runs in ascending order, apart from each other: what is in front of a word is what its list has in
 // front of it and what lies between the runs.
 struct NearBins {
-  int lo[4], hi[4], k_on, p_on, m_on, m_bin;
+  int lo[4], hi[4], k_on, p_on, m_on, k_bin, p_bin, m_bin, draw_bin;  // ..._bin: the first that may hold the answer
+  int keep;                                                            // words of bins before it stay; of the others only such as are in the runs may
   u64 weight[4], count[4];  // not on the list, in front of the run
   u64 all, m_front;         // the row's weight; what is in front of the border's bin of min_p
   float x0, x1;             // logits outside are in none of the runs
+  float stays;              // logits over it stay
   __device__ __forceinline__ bool has(int bin) const {
     bool in = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) in = in || (bin >= lo[i] && bin <= hi[i]);
     return in;
+  }
+  __device__ __forceinline__ bool lists(const Weigher& w, float x) const { return x >= x0 && x <= x1 && has(w.bin(w.below(x))); }
+  // What is not on the list in front of a word of a listed bin.
+  __device__ __forceinline__ u64 unlisted(const u64 (&of)[4], int bin) const {
+    u64 n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += bin >= lo[i] && bin <= hi[i] ? of[i] : 0;
+    return n;
   }
 };
 __device__ __forceinline__ u64 top_p_target(double top_p, u64 all) { return max((u64)1, min(all, (u64)ceil(top_p * (double)all))); }
@@ -294,7 +292,12 @@ __device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w,
   }
   if (threadIdx.x < 64) {  // one wave: the same in all its lanes
     n.k_on = k_on; n.p_on = p_on; n.m_on = m_on;
+    n.k_bin = lo[0];
+    n.p_bin = lo[1];
     n.m_bin = m_on ? lo[2] : -1;
+    n.draw_bin = lo[3];
+    n.keep = cut0;
+    n.stays = cut0 < kBins ? w.logit_at_bin(cut0, 1.0 - 1e-5) : -INFINITY;
     n.all = all;
     n.m_front = m_on ? b.weight[lo[2]] : 0;
     order_runs(w, b, lo, hi, n);
@@ -377,9 +380,10 @@ struct ResolveSpace {
   Answer answer[3];
 };
 
-// Sorted words, E of them in a thread (0: none), answer all questions: those of the near bins, or (ALL) every one of a row.
+// Sorted words, E of them in a thread (0: none), answer all questions: those of the near bins, or (ALL) every one of a row.  Near words
+// stand in out (if any) already: those that go are put out.
 template <int NT, int E, bool ALL>
-__device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64 (&x)[E], ResolveSpace<NT>& sp) {
+__device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64 (&x)[E], float* out, ResolveSpace<NT>& sp) {
   const int tid = threadIdx.x;
   // weights and counts up to and with every word
   u64 own[E], weight[E], count[E];
@@ -397,11 +401,9 @@ __device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, do
     bool in_m_bin = true;
     if constexpr (!ALL) {
       const int bin = w.bin(y);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool here = word && bin >= near.lo[i] && bin <= near.hi[i];
-        weight[e] += here ? near.weight[i] : 0;
-        count[e] += here ? near.count[i] : 0;
+      if (word) {
+        weight[e] += near.unlisted(near.weight, bin);
+        count[e] += near.unlisted(near.count, bin);
       }
       in_m_bin = bin == near.m_bin;
     }
@@ -438,10 +440,15 @@ __device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, do
     if (near.m_on) stay = min(stay, (ALL ? 0 : near.m_front) + in_bin);
     cut.token = token_at(find(2, false, draw_target(u, stay)).place);
   }
+  if constexpr (!ALL)
+    if (out)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (x[e] && !(x[e] >= cut.from && w.over(logit_at(x[e]), a.min_z))) out[token_at(x[e])] = -INFINITY;
   return cut;
 }
 template <int NT, int E>
-__device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, u64* lds, ResolveSpace<NT>& sp) {
+__device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds, ResolveSpace<NT>& sp) {
   u64 x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -452,11 +459,11 @@ __device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& 
   else if (n <= 256) sort_words<NT, E, 256>(x, 0, lds);
   else if (n <= 512) sort_words<NT, E, 512>(x, 0, lds);
   else if constexpr (NT * E >= 1024) sort_words<NT, E, 1024>(x, 0, lds);
-  return resolve<NT, E, false>(a, w, u, near, x, sp);
+  return resolve<NT, E, false>(a, w, u, near, x, out, sp);
 }
 template <int NT>
-__device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, u64* lds, ResolveSpace<NT>& sp) {
-  if (n <= (NT >= 512 ? 1024 : 512)) return resolve_list<NT, 2>(a, w, u, near, words, n, lds, sp);
+__device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds, ResolveSpace<NT>& sp) {
+  if (n <= (NT >= 512 ? 1024 : 512)) return resolve_list<NT, 2>(a, w, u, near, words, n, out, lds, sp);
   // more than that: not unrolled
   constexpr int E = kNear / NT;
   u64 x[E];
@@ -468,7 +475,7 @@ __device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w
   int size = 2 * E;
   while (size < n) size *= 2;
   sort_words<NT, E, 0>(x, size, lds);
-  return resolve<NT, E, false>(a, w, u, near, x, sp);
+  return resolve<NT, E, false>(a, w, u, near, x, out, sp);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -479,10 +486,9 @@ struct Digits {
   uint32_t count[kDigitBins];
 };
 
-// The place of the first word at which the count (or weight) of the words so far reaches `target`, 1 or more, which all words from `limit`
-// on together do.
+// The place of the first near word at which the count (or weight) of the near words so far reaches `target`, 1 or more and no more than all do.
 template <int NT, bool BY_WEIGHT>
-__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 target, u64 limit, Digits& d, Sums* scan, u64& s_bin) {
+__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, const NearBins& near, u64 target, Digits& d, Sums* scan, u64& s_bin) {
   const int tid = threadIdx.x;
   constexpr int N = kDigitBins / NT;
   u64 prefix = 0;
@@ -494,7 +500,7 @@ __device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 tar
     __syncthreads();
     each_word<NT>(row, 0, V, [&](float x, int v) {
       const u64 p = place_of(x, v);
-      if (p < limit || p >> above != prefix) return;
+      if (p >> above != prefix || !near.lists(w, x)) return;
       const int bin = kDigitBins - 1 - ((int)(p >> shift) & ((1 << bits) - 1));  // the highest first
       if (BY_WEIGHT) atomicAdd(&d.weight[bin], w.weight(w.below(x)));
       else atomicAdd(&d.count[bin], 1u);
@@ -521,24 +527,37 @@ __device__ u64 first_to_reach(const float* row, int V, const Weigher& w, u64 tar
   return prefix;
 }
 
+// row: where the near words stand, which is out if there is one (what is neither near nor stays is gone from it).
 template <int NT>
-__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const float* row, Digits& d, Sums* scan) {
+__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const float* row, float* out, Digits& d, Sums* scan) {
   __shared__ u64 s_bin;
-  const auto sum_from = [&](u64 limit, auto of) {
+  const auto weight_from = [&](u64 place, auto which) {
     u64 s = 0;
     each_word<NT>(row, 0, a.V, [&](float x, int v) {
-      if (place_of(x, v) >= limit) s += of(x);
+      if (place_of(x, v) >= place && near.lists(w, x) && which(x)) s += w.weight(w.below(x));
     });
     return sum_all<NT>(s, scan);
   };
-  const auto weight = [&](float x) { return w.weight(w.below(x)); };
+  const auto any = [](float) { return true; };
   Cut cut = {1, -1};
-  if (a.top_k > 0 && sum_from(1, [](float) { return (u64)1; }) > (u64)a.top_k) cut.from = first_to_reach<NT, false>(row, a.V, w, a.top_k, 1, d, scan, s_bin);
-  if (a.top_p < 1.0) cut.from = first_to_reach<NT, true>(row, a.V, w, top_p_target(a.top_p, sum_from(cut.from, weight)), cut.from, d, scan, s_bin);
-  if (a.tokens) {
-    const u64 stay = sum_from(cut.from, [&](float x) { return w.over(x, a.min_z) ? weight(x) : 0; });
-    cut.token = token_at(first_to_reach<NT, true>(row, a.V, w, draw_target(u, stay), cut.from, d, scan, s_bin));
+  u64 stay = near.all;
+  if (near.k_on) {
+    cut.from = first_to_reach<NT, false>(row, a.V, w, near, (u64)a.top_k - near.unlisted(near.count, near.k_bin), d, scan, s_bin);
+    stay = near.unlisted(near.weight, near.k_bin) + weight_from(cut.from, any);
   }
+  if (near.p_on) {
+    const u64 p = first_to_reach<NT, true>(row, a.V, w, near, top_p_target(a.top_p, stay) - near.unlisted(near.weight, near.p_bin), d, scan, s_bin);
+    cut.from = max(cut.from, p);
+    stay = near.unlisted(near.weight, near.p_bin) + weight_from(p, any);
+  }
+  if (a.tokens) {
+    if (near.m_on) stay = min(stay, near.m_front + weight_from(1, [&](float x) { return w.bin(w.below(x)) == near.m_bin && w.over(x, a.min_z); }));
+    cut.token = token_at(first_to_reach<NT, true>(row, a.V, w, near, draw_target(u, stay) - near.unlisted(near.weight, near.draw_bin), d, scan, s_bin));
+  }
+  if (out)
+    each_word<NT>(row, 0, a.V, [&](float x, int v) {
+      if (near.lists(w, x) && !(place_of(x, v) >= cut.from && w.over(x, a.min_z))) out[v] = -INFINITY;
+    });
   return cut;
 }
 
@@ -582,11 +601,11 @@ __device__ __forceinline__ void add_to_bins(const Weigher& w, const float* row, 
   else all(std::false_type{});
 }
 // The near words of a part of a row, listed in any order: a wave asks for places once for every eight words of its lanes.  *n counts
-// them all, those past kNear, which are not listed, too.
+// them all, those past kNear, which are not listed, too.  out (if any): the words that stay, and near ones.
 template <int NT>
-__device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, int v0, int v1, u64* words, uint32_t* n) {
+__device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near, const float* row, float* out, int v0, int v1, u64* words, uint32_t* n) {
   constexpr int kAhead = 8;
-  const float x0 = near.x0, x1 = near.x1;
+  const float x0 = near.x0, x1 = near.x1, stays = near.stays;
   const int lane = threadIdx.x & 63;
   for (int base = v0; base < v1; base += kAhead * NT) {
     float x[kAhead];
@@ -599,8 +618,14 @@ __device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near
     int found = 0;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      bool is = x[i] > -INFINITY && x[i] >= x0 && x[i] <= x1;
-      if (is) is = near.has(w.bin(w.below(x[i])));
+      bool is = x[i] > -INFINITY && x[i] >= x0 && x[i] <= x1, keep = x[i] > stays;
+      if (is) {
+        const int bin = w.bin(w.below(x[i]));
+        is = near.has(bin);
+        keep = keep || is || bin < near.keep;
+      }
+      const int v = base + i * NT + (int)threadIdx.x;
+      if (out && v < v1) out[v] = keep ? x[i] : -INFINITY;
       in[i] = __ballot(is);
       found += __popcll(in[i]);
     }
@@ -613,28 +638,6 @@ __device__ __forceinline__ void list_near(const Weigher& w, const NearBins& near
       const uint32_t mine = at + __popcll(in[i] & ((1ull << lane) - 1));
       if ((in[i] >> lane & 1) && mine < kNear) words[mine] = place_of(x[i], base + i * NT + (int)threadIdx.x);
       at += __popcll(in[i]);
-    }
-  }
-}
-
-template <int NT>
-__device__ __forceinline__ void write_row(const SampleArgs& a, const Weigher& w, const Cut& cut, const float* row, float* out, int v0, int v1) {
-  constexpr int N = 8;
-  // what stays, as numbers: logits over one, and of those equal to it the first tokens
-  const float last = cut.from > 1 ? logit_at(cut.from) : -INFINITY, least = w.least_over(a.min_z);
-  const int token = cut.from > 1 ? token_at(cut.from) : -1;
-  for (int base = v0; base < v1; base += N * NT) {
-    float x[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int v = base + i * NT + (int)threadIdx.x;
-      x[i] = v < v1 ? row[v] : -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int v = base + i * NT + (int)threadIdx.x;
-      const bool stays = (x[i] > last || (x[i] == last && v <= token)) && x[i] >= least;
-      if (v < v1) out[v] = stays ? x[i] : -INFINITY;
     }
   }
 }
@@ -671,16 +674,12 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   scan_bins(sp.bins, bw, bc);
   near_bins(a, w, u, sp.bins, near);
   Cut cut;
-  list_near<NT>(w, near, row, 0, a.V, sp.words, &s_near);
+  list_near<NT>(w, near, row, out, 0, a.V, sp.words, &s_near);
   __syncthreads();
   const int n = (int)s_near;
-  if (n <= kNear) {
-    cut = resolve_any<NT>(a, w, u, near, sp.words, n, sp.words, rs);
-  } else {
-    cut = resolve_by_digits<NT>(a, w, u, row, sp.digits, rs.scan);
-  }
+  if (n <= kNear) cut = resolve_any<NT>(a, w, u, near, sp.words, n, out, sp.words, rs);
+  else cut = resolve_by_digits<NT>(a, w, u, near, out ? out : row, out, sp.digits, rs.scan);
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
-  if (out) write_row<NT>(a, w, cut, row, out, 0, a.V);
 }
 
 // A short row: all of its words are sorted.
@@ -724,7 +723,7 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
   near.m_on = a.min_z > -INFINITY;
   sort_words<NT, E, NT * E>(x, 0, s_words);
   __syncthreads();
-  const Cut cut = resolve<NT, E, true>(a, w, u, near, x, rs);
+  const Cut cut = resolve<NT, E, true>(a, w, u, near, x, nullptr, rs);
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
   if (out)
 #pragma unroll
@@ -736,11 +735,11 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // A row to several workgroups, in four launches: (1) the slices' highest and lowest logits; (2) their bins, added up; (3) the words of the
-// near bins, in one list; (4) which sorts it, every slice's workgroup for itself where kept logits are written.
+// near bins, in one list, and what stays without them; (4) one workgroup sorts the list, draws, and puts out the near words that go.
 // ------------------------------------------------------------------------------------------
 constexpr int kSliceNT = 1024, kMaxSlices = 64, kSliceWgs = 512;
 constexpr int kCutNT = 256, kMaxCuts = 64, kCutWgs = 2048;
-constexpr int kPartNT = 512, kMaxParts = 64, kPartWgs = 512;
+constexpr int kFinishNT = 512;
 
 __device__ __forceinline__ float2 row_ends(const SampleArgs& a, float2* s_ends) {
   if (threadIdx.x < 64) {
@@ -798,51 +797,44 @@ __global__ __launch_bounds__(kCutNT) void sample_near_kernel(SampleArgs a) {
 #pragma unroll
   for (int i = 0; i < N; ++i) bw[i] = a.weight[r * kBins + tid * N + i], bc[i] = a.count[r * (kBins + 1) + tid * N + i];
   const double u = a.tokens ? (double)a.u[r] : 0.0;
+  float* out = a.out ? a.out + r * a.V : nullptr;
   const float2 ends = row_ends(a, &s_ends);
-  if (no_word(ends.x)) return;
+  if (no_word(ends.x)) {
+    if (out)
+      for (int v = v0 + tid; v < v1; v += kCutNT) out[v] = -INFINITY;
+    return;
+  }
   const Weigher w(a, ends.x, ends.y);
   scan_bins(bins, bw, bc);
   near_bins(a, w, u, bins, near);
   if (blockIdx.x == 0 && tid == 0) a.bins[r] = near;
-  list_near<kCutNT>(w, near, a.logits + r * a.V, v0, v1, a.near + r * kNear, &a.count[r * (kBins + 1) + kBins]);
+  list_near<kCutNT>(w, near, a.logits + r * a.V, out, v0, v1, a.near + r * kNear, &a.count[r * (kBins + 1) + kBins]);
 }
 
-// grid (parts or 1, rows)
-__global__ __launch_bounds__(kPartNT) void sample_finish_kernel(SampleArgs a) {
+// grid (1, rows)
+__global__ __launch_bounds__(kFinishNT) void sample_finish_kernel(SampleArgs a) {
   __shared__ union {
     u64 words[kNear];
     Digits digits;
   } sp;
-  __shared__ ResolveSpace<kPartNT> rs;
+  __shared__ ResolveSpace<kFinishNT> rs;
   __shared__ float2 s_ends;
-  const int tid = threadIdx.x;
   const size_t r = blockIdx.y;
   const float* row = a.logits + r * a.V;
   float* out = a.out ? a.out + r * a.V : nullptr;
-  int v0 = min(a.V, (int)blockIdx.x * a.per_part), v1 = min(a.V, v0 + a.per_part);
   const float2 ends = row_ends(a, &s_ends);
   if (no_word(ends.x)) {
-    if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = -1;
-    if (out)
-      for (int v = v0 + tid; v < v1; v += kPartNT) out[v] = -INFINITY;
+    if (a.tokens && threadIdx.x == 0) a.tokens[r] = -1;
     return;
   }
   const Weigher w(a, ends.x, ends.y);
   const double u = a.tokens ? (double)a.u[r] : 0.0;
   const NearBins near = a.bins[r];
-  Cut cut;
   const uint32_t n = a.count[r * (kBins + 1) + kBins];
-  if (n <= kNear) {
-    cut = resolve_any<kPartNT>(a, w, u, near, a.near + r * kNear, (int)n, sp.words, rs);
-  } else {
-    // one workgroup reads the whole row, which may be where the results go
-    if (blockIdx.x > 0) return;
-    v0 = 0;
-    v1 = a.V;
-    cut = resolve_by_digits<kPartNT>(a, w, u, row, sp.digits, rs.scan);
-  }
-  if (a.tokens && blockIdx.x == 0 && tid == 0) a.tokens[r] = cut.token;
-  if (out) write_row<kPartNT>(a, w, cut, row, out, v0, v1);
+  Cut cut;
+  if (n <= kNear) cut = resolve_any<kFinishNT>(a, w, u, near, a.near + r * kNear, (int)n, out, sp.words, rs);
+  else cut = resolve_by_digits<kFinishNT>(a, w, u, near, out ? out : row, out, sp.digits, rs.scan);
+  if (a.tokens && threadIdx.x == 0) a.tokens[r] = cut.token;
 }
 
 // One launch or four.  A row kept to one workgroup costs one launch, and a time that grows with the row alone; slices pay from some
@@ -879,8 +871,6 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   a.per = (V + a.slices - 1) / a.slices;
   a.cuts = std::max(1, std::min({kMaxCuts, (V + 2047) / 2048, kCutWgs / rows}));
   a.per_cut = (V + a.cuts - 1) / a.cuts;
-  a.parts = std::max(1, std::min({kMaxParts, (V + 2047) / 2048, kPartWgs / rows}));
-  a.per_part = (V + a.parts - 1) / a.parts;
   a.weight = (u64*)ws;
   a.near = a.weight + (size_t)rows * kBins;
   a.bins = (NearBins*)(a.near + (size_t)rows * kNear);
@@ -890,7 +880,7 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   hipLaunchKernelGGL(sample_ends_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
   hipLaunchKernelGGL(sample_near_kernel, dim3(a.cuts, rows), dim3(kCutNT), 0, st, a);
-  hipLaunchKernelGGL(sample_finish_kernel, dim3(a.out ? a.parts : 1, rows), dim3(kPartNT), 0, st, a);
+  hipLaunchKernelGGL(sample_finish_kernel, dim3(1, rows), dim3(kFinishNT), 0, st, a);
 }
 
 }  // namespace es

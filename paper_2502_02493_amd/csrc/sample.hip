@@ -310,31 +310,34 @@ struct Cut {
   int token;
 };
 
-// A workgroup's words in descending order, word E tid + e in the thread's e; size, a power of two from 2 E on, counts the places
-// that may hold one.  Exchanges inside a thread, inside a wave by operand swizzles, between waves through LDS.  SIZE: known to
-// the compiler, so that no step has to look up which exchange it is (which costs as much again), or 0.
+// A workgroup's words in descending order, word E tid + e in the thread's e: by buckets that follow the order, or, where one of them
+// would hold too many (equal logits, one far away from the others), by exchanges.
+constexpr int kBuckets = 2048, kMaxBucket = 32;
+template <int NT>
+struct SortSpace {
+  uint32_t start[kBuckets + 1];
+  uint32_t waves[NT / 64], too_many;
+};
+
+// Exchanges inside a thread, inside a wave, and between waves through LDS.
 __device__ __forceinline__ u64 exchanged(u64 own, u64 other, bool larger) { return (own > other) == larger ? own : other; }
-template <int NT, int E, int SIZE>
-__device__ __forceinline__ void sort_words(u64 (&x)[E], int any_size, u64* lds) {
-  const int tid = threadIdx.x, size = SIZE ? SIZE : any_size;
-  const bool works = (tid & ~63) * E < size;  // a wave without places only keeps the others company
-  constexpr int kUnroll = SIZE ? 16 : 1;
-#pragma unroll kUnroll
-  for (int k = 2; k <= size; k *= 2) {
-#pragma unroll kUnroll
+template <int NT, int E>
+__device__ __forceinline__ void sort_by_exchanges(u64 (&x)[E], u64* lds) {
+  const int tid = threadIdx.x;
+#pragma unroll 1
+  for (int k = 2; k <= NT * E; k *= 2) {
+#pragma unroll 1
     for (int j = k / 2; j > 0; j /= 2) {
       const int m = j / E;
       const bool larger = ((tid & m) == 0) == (((tid * E) & k) == 0);  // from E on: what the thread keeps of its pairs
       if (j >= 64 * E) {
         __syncthreads();
-        if (works)
 #pragma unroll
-          for (int e = 0; e < E; ++e) lds[e * NT + tid] = x[e];
+        for (int e = 0; e < E; ++e) lds[e * NT + tid] = x[e];
         __syncthreads();
-        if (works)
 #pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], lds[e * NT + (tid ^ m)], larger);
-      } else if (works && j < E) {
+        for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], lds[e * NT + (tid ^ m)], larger);
+      } else if (j < E) {
 #pragma unroll
         for (int step = 1; step < E; step *= 2) {
           if (step != j) continue;
@@ -347,28 +350,72 @@ __device__ __forceinline__ void sort_words(u64 (&x)[E], int any_size, u64* lds) 
             x[e + step] = swap ? a : x[e + step];
           }
         }
-      } else if (works) {
-        const auto by = [&](auto other) {
+      } else {
 #pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], other((uint64_t)x[e]), larger);
-        };
-        const auto swapped = [](uint64_t v, auto half) {  // the value of lane l ^ 32 (l ^ 16): the other of the two that the swap leaves
-          const uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
-          constexpr bool H = decltype(half)::value;
-          const auto l = H ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
-          const auto h = H ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
-          const bool upper = threadIdx.x & (H ? 32 : 16);
-          return (uint64_t)(uint32_t)(upper ? h[0] : h[1]) << 32 | (uint32_t)(upper ? l[0] : l[1]);
-        };
-        if (m == 1) by([](uint64_t v) { return dpp<0xB1>(v); });
-        else if (m == 2) by([](uint64_t v) { return dpp<0x4E>(v); });
-        else if (m == 4) by([](uint64_t v) { return dpp<0x1B>(dpp<0x141>(v)); });  // 7, then 3
-        else if (m == 8) by([](uint64_t v) { return dpp<0x128>(v); });
-        else if (m == 16) by([&](uint64_t v) { return swapped(v, std::false_type{}); });
-        else by([&](uint64_t v) { return swapped(v, std::true_type{}); });
+        for (int e = 0; e < E; ++e) x[e] = exchanged(x[e], __shfl_xor(x[e], m), larger);
       }
     }
   }
+}
+
+// x: n words altogether (0: none), each in bucket[e] (-1: none), which do not fall along the order; lds: NT * E words, nobody reads or
+// writes any.  One pass counts the buckets, their starts are summed up, the words go there, and each looks for its place among the few of its own.
+template <int NT, int E>
+__device__ __forceinline__ void sort_words(u64 (&x)[E], const int (&bucket)[E], int n, u64* lds, SortSpace<NT>& sp) {
+  constexpr int N = kBuckets / NT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) sp.start[i * NT + tid] = 0;
+  if (tid == 0) sp.too_many = 0;
+  __syncthreads();
+  uint32_t at[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) at[e] = bucket[e] >= 0 ? atomicAdd(&sp.start[bucket[e]], 1u) : 0;
+  __syncthreads();
+  uint32_t own[N], sum = 0;
+  bool many = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    own[i] = sp.start[tid * N + i];
+    sum += own[i];
+    many = many || own[i] > kMaxBucket;
+  }
+  const uint32_t run = (uint32_t)running_sum(sum);
+  if (lane == 63) sp.waves[wave] = run;
+  if (__ballot(many) && lane == 0) sp.too_many = 1;
+  __syncthreads();
+  if (sp.too_many) {
+    sort_by_exchanges<NT, E>(x, lds);
+    return;
+  }
+  uint32_t before = run - sum;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) before += w < wave ? sp.waves[w] : 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sp.start[tid * N + i] = before;
+    before += own[i];
+  }
+  if (tid == NT - 1) sp.start[kBuckets] = before;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (bucket[e] >= 0) lds[sp.start[bucket[e]] + at[e]] = x[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (bucket[e] < 0) continue;
+    const uint32_t first = sp.start[bucket[e]], end = sp.start[bucket[e] + 1];
+    at[e] = first;
+    for (uint32_t i = first; i < end; ++i) at[e] += lds[i] > x[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (bucket[e] >= 0) lds[at[e]] = x[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = tid * E + e < n ? lds[tid * E + e] : 0;
 }
 
 struct Answer {
@@ -448,34 +495,38 @@ __device__ __forceinline__ Cut resolve(const SampleArgs& a, const Weigher& w, do
   return cut;
 }
 template <int NT, int E>
-__device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds, ResolveSpace<NT>& sp) {
+__device__ __forceinline__ Cut resolve_list(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds,
+                                            ResolveSpace<NT>& sp, SortSpace<NT>& sort) {
   u64 x[E];
+  int bucket[E];
+  int bins = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bins += max(0, near.hi[i] - near.lo[i] + 1);
+  const int parts = kBuckets / max(1, bins);  // buckets of a near bin
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int i = threadIdx.x * E + e;
+    const int i = e * NT + threadIdx.x;
     x[e] = i < n ? words[i] : 0;
   }
-  if (n <= 128) sort_words<NT, E, 128>(x, 0, lds);
-  else if (n <= 256) sort_words<NT, E, 256>(x, 0, lds);
-  else if (n <= 512) sort_words<NT, E, 512>(x, 0, lds);
-  else if constexpr (NT * E >= 1024) sort_words<NT, E, 1024>(x, 0, lds);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const double y = w.below(logit_at(x[e]));
+    const int bin = w.bin(y);
+    int index = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) index += min(bin, near.hi[i] + 1) > near.lo[i] ? min(bin, near.hi[i] + 1) - near.lo[i] : 0;
+    const int part = bin < kFineBins ? min((int)((y * w.per_y - (double)bin) * (double)parts), parts - 1) : 0;
+    bucket[e] = x[e] ? index * parts + part : -1;
+  }
+  __syncthreads();  // words may stand where they are sorted
+  sort_words<NT, E>(x, bucket, n, lds, sort);
   return resolve<NT, E, false>(a, w, u, near, x, out, sp);
 }
 template <int NT>
-__device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds, ResolveSpace<NT>& sp) {
-  if (n <= (NT >= 512 ? 1024 : 512)) return resolve_list<NT, 2>(a, w, u, near, words, n, out, lds, sp);
-  // more than that: not unrolled
-  constexpr int E = kNear / NT;
-  u64 x[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int i = threadIdx.x * E + e;
-    x[e] = i < n ? words[i] : 0;
-  }
-  int size = 2 * E;
-  while (size < n) size *= 2;
-  sort_words<NT, E, 0>(x, size, lds);
-  return resolve<NT, E, false>(a, w, u, near, x, out, sp);
+__device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const u64* words, int n, float* out, u64* lds,
+                                           ResolveSpace<NT>& sp, SortSpace<NT>& sort) {
+  if (n <= 2 * NT) return resolve_list<NT, 2>(a, w, u, near, words, n, out, lds, sp, sort);
+  return resolve_list<NT, kNear / NT>(a, w, u, near, words, n, out, lds, sp, sort);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -488,7 +539,7 @@ struct Digits {
 
 // The place of the first near word at which the count (or weight) of the near words so far reaches `target`, 1 or more and no more than all do.
 template <int NT, bool BY_WEIGHT>
-__device__ u64 first_to_reach(const float* row, int V, const Weigher& w, const NearBins& near, u64 target, Digits& d, Sums* scan, u64& s_bin) {
+__device__ __forceinline__ u64 first_to_reach(const float* row, int V, const Weigher& w, const NearBins& near, u64 target, Digits& d, Sums* scan, u64& s_bin) {
   const int tid = threadIdx.x;
   constexpr int N = kDigitBins / NT;
   u64 prefix = 0;
@@ -529,7 +580,7 @@ __device__ u64 first_to_reach(const float* row, int V, const Weigher& w, const N
 
 // row: where the near words stand, which is out if there is one (what is neither near nor stays is gone from it).
 template <int NT>
-__device__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const float* row, float* out, Digits& d, Sums* scan) {
+__device__ __forceinline__ Cut resolve_by_digits(const SampleArgs& a, const Weigher& w, double u, const NearBins& near, const float* row, float* out, Digits& d, Sums* scan) {
   __shared__ u64 s_bin;
   const auto weight_from = [&](u64 place, auto which) {
     u64 s = 0;
@@ -646,6 +697,7 @@ template <int NT>
 __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   __shared__ SampleSpace<NT> sp;
   __shared__ ResolveSpace<NT> rs;
+  __shared__ SortSpace<NT> sort;
   __shared__ float s_ends[2 * NT / 64];
   __shared__ NearBins near;
   __shared__ uint32_t s_near;
@@ -677,7 +729,7 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   list_near<NT>(w, near, row, out, 0, a.V, sp.words, &s_near);
   __syncthreads();
   const int n = (int)s_near;
-  if (n <= kNear) cut = resolve_any<NT>(a, w, u, near, sp.words, n, out, sp.words, rs);
+  if (n <= kNear) cut = resolve_any<NT>(a, w, u, near, sp.words, n, out, sp.words, rs, sort);
   else cut = resolve_by_digits<NT>(a, w, u, near, out ? out : row, out, sp.digits, rs.scan);
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
 }
@@ -688,6 +740,7 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
   constexpr int NT = 256;
   __shared__ u64 s_words[NT * E];
   __shared__ ResolveSpace<NT> rs;
+  __shared__ SortSpace<NT> sort;
   __shared__ float s_ends[2 * NT / 64];
   const int tid = threadIdx.x;
   const size_t r = blockIdx.x;
@@ -696,7 +749,7 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
   const double u = a.tokens ? (double)a.u[r] : 0.0;
   float v[E];  // which words a thread brings is all the same to the sort: those that lie side by side in memory
   u64 x[E];
-  float hi = -INFINITY;
+  float hi = -INFINITY, lo = INFINITY;
   int words = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -708,20 +761,26 @@ __global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
     x[e] = place_of(v[e], e * NT + tid);
     words += x[e] != 0;
     hi = fmaxf(hi, v[e]);
+    if (x[e]) lo = fminf(lo, v[e]);
   }
-  const float top = block_max<NT / 64>(hi, s_ends);
+  const float top = block_max<NT / 64>(hi, s_ends), low = -block_max<NT / 64>(-lo, s_ends + NT / 64);
   if (no_word(top)) {
     if (a.tokens && tid == 0) a.tokens[r] = -1;
     if (out)
       for (int i = tid; i < a.V; i += NT) out[i] = -INFINITY;
     return;
   }
-  const Weigher w(a, top, top);
+  const Weigher w(a, top, low);
+  const int n = (int)sum_all<NT>((u64)words, rs.scan);
   NearBins near;
-  near.k_on = a.top_k > 0 && (u64)a.top_k < sum_all<NT>((u64)words, rs.scan);
+  near.k_on = a.top_k > 0 && a.top_k < n;
   near.p_on = a.top_p < 1.0;
   near.m_on = a.min_z > -INFINITY;
-  sort_words<NT, E, NT * E>(x, 0, s_words);
+  const double per_y = (double)(kBuckets - 1) / fmax(w.below(low), 1e-6);
+  int bucket[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) bucket[e] = x[e] ? min((int)(w.below(v[e]) * per_y), kBuckets - 1) : -1;
+  sort_words<NT, E>(x, bucket, n, s_words, sort);
   __syncthreads();
   const Cut cut = resolve<NT, E, true>(a, w, u, near, x, nullptr, rs);
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
@@ -818,6 +877,7 @@ __global__ __launch_bounds__(kFinishNT) void sample_finish_kernel(SampleArgs a) 
     Digits digits;
   } sp;
   __shared__ ResolveSpace<kFinishNT> rs;
+  __shared__ SortSpace<kFinishNT> sort;
   __shared__ float2 s_ends;
   const size_t r = blockIdx.y;
   const float* row = a.logits + r * a.V;
@@ -832,7 +892,7 @@ __global__ __launch_bounds__(kFinishNT) void sample_finish_kernel(SampleArgs a) 
   const NearBins near = a.bins[r];
   const uint32_t n = a.count[r * (kBins + 1) + kBins];
   Cut cut;
-  if (n <= kNear) cut = resolve_any<kFinishNT>(a, w, u, near, a.near + r * kNear, (int)n, out, sp.words, rs);
+  if (n <= kNear) cut = resolve_any<kFinishNT>(a, w, u, near, a.near + r * kNear, (int)n, out, sp.words, rs, sort);
   else cut = resolve_by_digits<kFinishNT>(a, w, u, near, out ? out : row, out, sp.digits, rs.scan);
   if (a.tokens && threadIdx.x == 0) a.tokens[r] = cut.token;
 }

@@ -24,7 +24,7 @@ static_assert(kMaxSampleVocab == 1 << kTokenBits, "a place number holds a token"
 constexpr int kBins = 1024, kFineBins = 896;  // evenly over y up to 48, where weights end, or to the lowest logit's; then four to a doubling
 constexpr int kNear = 4096;                    // words that are sorted
 constexpr int kDigitBins = 2048;
-constexpr int kShortRow = 2048;   // words of a row that are sorted, all of them
+constexpr int kShortRow = 4096;   // words of a row that are sorted, all of them
 constexpr int kRowWords = 12288;  // words of a row that stays with one workgroup
 constexpr double kFar = 48.0;
 
@@ -734,10 +734,12 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleArgs a) {
   if (a.tokens && tid == 0) a.tokens[r] = cut.token;
 }
 
-// A short row: all of its words are sorted.
-template <int E>
-__global__ __launch_bounds__(256) void sample_short_kernel(SampleArgs a) {
-  constexpr int NT = 256;
+// A short row: all of its words are sorted.  As wide as pays (us in a graph, 1 row : 600 rows, threads x words): 250 words 256 x 1
+// 4.6 : 6.6, 256 x 2 5.0 : 7.1; 500 words 256 x 2 5.5 : 7.8, 512 x 1 5.4 : 8.9; 1000 words 512 x 2 6.5 : 10.8, 256 x 4 7.2 : 10.4,
+// 1024 x 1 7.8 : 21.3; 2000 words 512 x 4 8.9 : 18.6, 256 x 8 11.5 : 16.5, 1024 x 2 9.2 : 25.8; 4000 words 1024 x 4 12.8 : 39.0,
+// 512 x 8 14.9 : 33.5, the way of longer rows 16.5 : 48.9; 8000 words 1024 x 8 27.8 : 88.8, the way of longer rows 18.7 : 57.3.
+template <int NT, int E>
+__global__ __launch_bounds__(NT) void sample_short_kernel(SampleArgs a) {
   __shared__ u64 s_words[NT * E];
   __shared__ ResolveSpace<NT> rs;
   __shared__ SortSpace<NT> sort;
@@ -922,9 +924,18 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   a.tokens = tokens_out; a.out = logits_out;
   a.slices = sample_slices(rows, V);
   if (a.slices == 1) {
-    if (V <= 512) hipLaunchKernelGGL(sample_short_kernel<2>, dim3(rows), dim3(256), 0, st, a);
-    else if (V <= 1024) hipLaunchKernelGGL(sample_short_kernel<4>, dim3(rows), dim3(256), 0, st, a);
-    else if (V <= kShortRow) hipLaunchKernelGGL(sample_short_kernel<8>, dim3(rows), dim3(256), 0, st, a);
+    const auto short_row = [&](auto nt, auto e) {
+      constexpr int NT = decltype(nt)::value, E = decltype(e)::value;
+      hipLaunchKernelGGL((sample_short_kernel<NT, E>), dim3(rows), dim3(NT), 0, st, a);
+    };
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 2> Two;
+    typedef std::integral_constant<int, 4> Four;
+    if (V <= 256) short_row(std::integral_constant<int, 256>{}, One{});
+    else if (V <= 512) short_row(std::integral_constant<int, 256>{}, Two{});
+    else if (V <= 1024) short_row(std::integral_constant<int, 512>{}, Two{});
+    else if (V <= 2048) short_row(std::integral_constant<int, 512>{}, Four{});
+    else if (V <= kShortRow) short_row(std::integral_constant<int, 1024>{}, Four{});
     else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
     return;
   }

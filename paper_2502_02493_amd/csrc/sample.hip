@@ -25,7 +25,7 @@ constexpr int kBins = 1024, kFineBins = 896;  // evenly over y up to 48, where w
 constexpr int kNear = 4096;                    // words that are sorted
 constexpr int kDigitBins = 2048;
 constexpr int kShortRow = 4096;   // words of a row that are sorted, all of them
-constexpr int kRowWords = 12288;  // words of a row that stays with one workgroup
+constexpr int kRowWords = 8192;   // words of a row that stays with one workgroup
 constexpr double kFar = 48.0;
 
 // A word's place number: the higher, the earlier in the order; 0 is no word (minus infinity, NaN).
@@ -50,7 +50,7 @@ struct SampleArgs {
   double unit;            // 2^s
   int32_t* tokens;
   float* out;
-  // rows cut into slices, and into more of them where a workgroup has little to do
+  // a row's slices, and its cuts: more of them, where a workgroup has less to do
   int slices, per, cuts, per_cut;
   float2* slice_ends;  // [row][slices]  highest and lowest logit
   u64* weight;         // [row][kBins]
@@ -798,7 +798,7 @@ __global__ __launch_bounds__(NT) void sample_short_kernel(SampleArgs a) {
 // A row to several workgroups, in four launches: (1) the slices' highest and lowest logits; (2) their bins, added up; (3) the words of the
 // near bins, in one list, and what stays without them; (4) one workgroup sorts the list, draws, and puts out the near words that go.
 // ------------------------------------------------------------------------------------------
-constexpr int kSliceNT = 1024, kMaxSlices = 64, kSliceWgs = 512;
+constexpr int kSliceNT = 1024, kMaxSlices = 64, kSliceWgs = 512, kMaxSlicedRows = 1024;
 constexpr int kCutNT = 256, kMaxCuts = 64, kCutWgs = 2048;
 constexpr int kFinishNT = 512;
 
@@ -899,17 +899,13 @@ __global__ __launch_bounds__(kFinishNT) void sample_finish_kernel(SampleArgs a) 
   if (a.tokens && threadIdx.x == 0) a.tokens[r] = cut.token;
 }
 
-// One launch or four.  A row kept to one workgroup costs one launch, and a time that grows with the row alone; slices pay from some
-// 12 thousand words on (us in a graph, one launch : four): 1 row of 6000 16.6 : 20.0, of 12 000 23.0 : 21.1 and of 24 000
-// 32.6 : 21.4; 96 rows of 8000 18.8 : 26.8, of 12 000 24.3 : 29.9, of 24 000 34.8 : 34.9, of 50 000 64 : 48, of 152 064 172 : 93; and
-// beside each stand the 8 us that three more launches take from the host.  Past 512 rows the rows alone fill the chip twice: 300 rows
-// of 152 064 365 : 290, 600 rows 565 : 507, 1200 rows 947 : 938 (with top_k 776 : 847).
-static int sample_slices(int rows, int V) {
-  if (V <= kRowWords || rows > kSliceWgs) return 1;
-  return std::max(2, std::min({kMaxSlices, (V + 4095) / 4096, kSliceWgs / rows}));
-}
+// One launch or four.  A row kept to one workgroup costs one launch, and a time that grows with the row; cut up it pays from some
+// 8 thousand words on (us in a graph, one launch : four): 1 row of 6000 17.7 : 19.6, of 12 000 23.5 : 20.1 and of 152 064 142 : 24;
+// 96 rows of 6000 18.5 : 23.7, of 12 000 24.7 : 28.4, of 24 000 34.7 : 32.0, of 152 064 156 : 77; 600 rows of 12 000 71 : 60, of
+// 152 064 502 : 403.  Rows that fill the chip by themselves gain little: 1200 of 152 064 849 : 792, with top_k 676 : 715.
+static bool whole_rows(int rows, int V) { return V <= kRowWords || rows > kMaxSlicedRows; }
 static size_t sample_row_bytes() { return kMaxSlices * sizeof(float2) + kBins * sizeof(u64) + (kBins + 1) * sizeof(uint32_t) + kNear * sizeof(u64) + sizeof(NearBins); }
-size_t sample_workspace_bytes(int rows, int V) { return sample_slices(rows, V) > 1 ? rows * sample_row_bytes() : 16; }
+size_t sample_workspace_bytes(int rows, int V) { return whole_rows(rows, V) ? 16 : rows * sample_row_bytes(); }
 
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
                    float* logits_out, void* ws, hipStream_t st) {
@@ -922,8 +918,7 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
   while ((1 << bits) < V) ++bits;
   a.unit = ldexp(1.0, std::min(51, 62 - bits));
   a.tokens = tokens_out; a.out = logits_out;
-  a.slices = sample_slices(rows, V);
-  if (a.slices == 1) {
+  if (whole_rows(rows, V)) {
     const auto short_row = [&](auto nt, auto e) {
       constexpr int NT = decltype(nt)::value, E = decltype(e)::value;
       hipLaunchKernelGGL((sample_short_kernel<NT, E>), dim3(rows), dim3(NT), 0, st, a);
@@ -939,6 +934,7 @@ void launch_sample(const float* logits, const float* u, int rows, int V, double 
     else hipLaunchKernelGGL(sample_row_kernel<1024>, dim3(rows), dim3(1024), 0, st, a);
     return;
   }
+  a.slices = std::max(1, std::min({kMaxSlices, (V + 4095) / 4096, kSliceWgs / rows}));
   a.per = (V + a.slices - 1) / a.slices;
   a.cuts = std::max(1, std::min({kMaxCuts, (V + 2047) / 2048, kCutWgs / rows}));
   a.per_cut = (V + a.cuts - 1) / a.cuts;

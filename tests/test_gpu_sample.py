@@ -102,6 +102,23 @@ def test_equal_logits(es, V):
     check(es, np.where(g.random((4, V)) < 0.5, np.float32(0.0), np.float32(-0.0)), u, 1.0, V // 3, 1.0, 0.0)      # the two zeros are one number
 
 
+@pytest.mark.parametrize("V", [700, 6000, 90000])
+def test_nearly_equal_logits_in_place(es, V):
+    """More words near a border than are sorted, or in one bucket, where the logits are overwritten: every filter, alone and with the others."""
+    g = np.random.default_rng(V)
+    logits = np.empty((4, V), np.float32)
+    logits[0] = 2.0 + g.integers(0, 3, V) * np.float32(2.0 ** -22)
+    logits[1] = g.integers(0, 6, V) / 4
+    logits[2] = np.where(g.random(V) < 0.7, np.float32(-1.0), np.float32(3.0))
+    logits[3] = g.normal(0, 1e-6, V)
+    logits[3, 5] = -1e30                                   # so that all others lie in the first bin
+    u = np.array([0.3, 0.99, 0.02, 0.6], np.float32)
+    for k, p, m in ((V // 3, 1.0, 0.0), (0, 0.6, 0.0), (0, 1.0, 0.4), (V // 2, 0.7, 0.0), (V // 2, 0.9, 0.3), (0, 0.95, 0.8), (0, 1.0, 0.0)):
+        check(es, logits, u, 0.9, k, p, m, in_place=True)
+        check(es, logits, u, 0.9, k, p, m, filtered=False)
+    check(es, logits, None, 0.9, V // 2, 0.7, 0.3, in_place=True)
+
+
 def test_words_that_are_none(es):
     V = 9000
     logits, u = normal(8, 8, V)
@@ -163,7 +180,7 @@ def test_many_rows(es):
     check(es, logits, u, 0.8, 0, 0.9, 0.0)
 
 
-@pytest.mark.parametrize("R,V", [(2, 2048), (2, 2049), (3, 12288), (3, 12289), (300, 13001), (512, 12300), (513, 12300)])
+@pytest.mark.parametrize("R,V", [(2, 256), (2, 257), (2, 513), (3, 1025), (2, 2049), (2, 4096), (2, 4097), (3, 8192), (3, 8193), (300, 9001), (1024, 8200), (1025, 8200)])
 def test_where_the_ways_of_cutting_rows_change(es, R, V):
     logits, u = normal(R + V, R, V)
     logits[-1] = np.round(logits[-1] * 2) / 2              # thousands of equal ones

@@ -332,40 +332,45 @@ def make_kvq(k_codes, k_scales, v_codes, v_scales, k_bounds=None) -> easyspec_kv
     return easyspec_kvq(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), _ptr(k_bounds))
 
 
+def _int_bytes(x, n):
+    """_host_ints for arrays that are only read during the call: bytes, which ctypes passes on as they are (an array's address takes 0.7 us to ask for)."""
+    return _host_ints(x, n).tobytes()
+
+
 def easyspec_kvq_store(k, v, layout: easyspec_kv_layout, src_slots, src_from, n_slots, to, lens, cache: easyspec_kvq, hip_stream=None):
-    f, n, t, s = (_host_ints(x, layout.n_seqs) for x in (src_from, n_slots, to, lens))
-    _check(load_library().easyspec_kvq_store(_ptr(k), _ptr(v), C.byref(layout), src_slots, _ptr(f), _ptr(n), _ptr(t), _ptr(s), C.byref(cache),
+    f, n, t, s = (_int_bytes(x, layout.n_seqs) for x in (src_from, n_slots, to, lens))
+    _check(load_library().easyspec_kvq_store(_ptr(k), _ptr(v), C.byref(layout), src_slots, f, n, t, s, C.byref(cache),
                                              _ptr(hip_stream)), None)
 
 
 def easyspec_kvq_load(cache: easyspec_kvq, layout: easyspec_kv_layout, from_, n_slots, out_slots, to, k_out, v_out, hip_stream=None):
-    f, n, t = (_host_ints(x, layout.n_seqs) for x in (from_, n_slots, to))
-    _check(load_library().easyspec_kvq_load(C.byref(cache), C.byref(layout), _ptr(f), _ptr(n), out_slots, _ptr(t), _ptr(k_out), _ptr(v_out),
+    f, n, t = (_int_bytes(x, layout.n_seqs) for x in (from_, n_slots, to))
+    _check(load_library().easyspec_kvq_load(C.byref(cache), C.byref(layout), f, n, out_slots, t, _ptr(k_out), _ptr(v_out),
                                             _ptr(hip_stream)), None)
 
 
 def easyspec_kvq_attention(q, cache: easyspec_kvq, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, blocks, n_blocks, out, workspace,
                            hip_stream=None):
-    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
-    _check(load_library().easyspec_kvq_attention(_ptr(q), C.byref(cache), C.byref(layout), _ptr(n), _ptr(s), n_q_heads, _ptr(blocks), n_blocks,
+    n, s = _int_bytes(n_tokens, layout.n_seqs), _int_bytes(lens, layout.n_seqs)
+    _check(load_library().easyspec_kvq_attention(_ptr(q), C.byref(cache), C.byref(layout), n, s, n_q_heads, _ptr(blocks), n_blocks,
                                                  _ptr(out), _ptr(workspace), _ptr(hip_stream)), None)
 
 
 def easyspec_kvq_attention_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, n_blocks) -> int:
-    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
-    return int(load_library().easyspec_kvq_attention_workspace_bytes(C.byref(layout), _ptr(n), _ptr(s), n_q_heads, n_blocks))
+    n, s = _int_bytes(n_tokens, layout.n_seqs), _int_bytes(lens, layout.n_seqs)
+    return int(load_library().easyspec_kvq_attention_workspace_bytes(C.byref(layout), n, s, n_q_heads, n_blocks))
 
 
 def easyspec_kvq_select(q, k_bounds, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, keep_first, keep_last, n_select, blocks_out, workspace,
                         hip_stream=None):
-    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
-    _check(load_library().easyspec_kvq_select(_ptr(q), _ptr(k_bounds), C.byref(layout), _ptr(n), _ptr(s), n_q_heads, keep_first, keep_last, n_select,
+    n, s = _int_bytes(n_tokens, layout.n_seqs), _int_bytes(lens, layout.n_seqs)
+    _check(load_library().easyspec_kvq_select(_ptr(q), _ptr(k_bounds), C.byref(layout), n, s, n_q_heads, keep_first, keep_last, n_select,
                                               _ptr(blocks_out), _ptr(workspace), _ptr(hip_stream)), None)
 
 
 def easyspec_kvq_select_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, n_select) -> int:
-    n, s = _host_ints(n_tokens, layout.n_seqs), _host_ints(lens, layout.n_seqs)
-    return int(load_library().easyspec_kvq_select_workspace_bytes(C.byref(layout), _ptr(n), _ptr(s), n_q_heads, n_select))
+    n, s = _int_bytes(n_tokens, layout.n_seqs), _int_bytes(lens, layout.n_seqs)
+    return int(load_library().easyspec_kvq_select_workspace_bytes(C.byref(layout), n, s, n_q_heads, n_select))
 
 
 def easyspec_sample(logits, u, rows, vocab, temperature, top_k, top_p, min_p, tokens_out, logits_out, workspace, hip_stream=None):

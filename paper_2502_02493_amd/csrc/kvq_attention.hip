@@ -2,18 +2,23 @@
 //
 //   out = sum_s p_s v_s,  p = softmax_s(q . k_s / sqrt(hd)),  over all slots that a token sees or those of its listed blocks
 //
-// The query heads of a KV head and the sequence's new tokens are the rows of two matrix products on the matrix cores.  Both take the
-// cache's values as bf16 numbers, which hold them exactly (one conversion gives two of them, the scale included); queries and
-// probabilities are fp32 and meet them as three bf16 terms each, all 24 bits.  Queries and results of this library are fp32, and a
-// cache read in 4 bits should lose nothing beyond its rounding.
-//   S = K Q^T: a tile of 16 slots is the A operand, lane l holding channels hd / 4 (l / 16) .. of slot l % 16: a quarter of a slot's codes,
-//     under one scale.  (Which channels a k-tile contracts is free as long as the queries agree.)  A lane then holds the scores of
-//     slots 4 (l / 16) + i of row l % 16,
+// The query heads of a KV head and the sequence's new tokens are the rows of two products on the matrix cores.  Queries and results of this
+// library are fp32, and a cache read in 4 bits should lose nothing beyond its rounding: both products take the cache's values as they are and
+// the fp32 operand as a sum of short terms that hold all 24 bits.
+//   S = K Q^T: on the product of scaled 4-bit and 6-bit numbers, which takes K's codes and scale bytes unchanged and a slot's 128 channels at once.  A tile
+//     of 16 slots is the A operand, lane l holding channels hd / 4 (l / 16) .. of slot l % 16: a quarter of a slot's codes, under one scale; a
+//     query is five terms of 6 bits (16 x 16 x 128 products in the 16 cycles of 16 x 16 x 32 bf16 ones).  A lane then holds the scores of slots
+//     4 (l / 16) + i of row l % 16,
 //   O^T = V^T P^T: which is where the B operand of the second product wants them: elements 4 t + i of lane group g are slot 4 g + i of
-//     tile t.  Its A operand needs eight slots of a channel side by side: lane l takes channels hd / 16 (l % 16) .. of those slots,
-//     pairs of slots meeting in a register by one permutation.
+//     tile t.  Here the sum runs over slots, each with a scale of its own, so that V is made bf16 (exactly; one conversion gives two numbers, the
+//     scale included) and the weights are three bf16 terms.  The A operand needs eight slots of a channel side by side: lane l takes channels
+//     hd / 16 (l % 16) .. of those slots, pairs of slots meeting in a register by one permutation.
 // The running maximum, sum and result of a row stay in the lanes of its column; nothing passes through LDS until a wave's share of
 // the context is done.
+// Bound: a single token by the chain of one step a wave (2048 slots of 8 KV heads 6.5 us and 4 of the join; 0.3 us of bytes), long contexts with many
+// rows by the instructions of a step on two waves a SIMD: 48 products of 16 cycles, 20 of the other kind and some 230 vector instructions for 32 slots of 32 rows.
+// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 31 us in a graph (35 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
+// heads, 112 rows each, 18.8 (20.4); a large bf16 product's rate would allow 13 and 6.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -82,13 +87,17 @@ template <int HD>
 struct KvqStep {
   static constexpr int KW = HD / 32;  // words of K codes of a lane and tile: 8 channels each; scales of a slot
   typedef uint32_t kword __attribute__((ext_vector_type(KW)));
-  kword k[2], vs[2];  // vs: the scales of the lane's four slots of a tile side by side
-  uint32_t ks[2], v[2][4];
+  uint32_t k[2][KW], ks[2], v[2][4];
+  kword vs[2];  // the scales of the lane's four slots of a tile side by side
   template <class T>
   static __device__ __forceinline__ T fetch(const uint8_t* p) {  // scales may lie anywhere
     T x;
     __builtin_memcpy(&x, p, sizeof(T));
     return x;
+  }
+  __device__ __forceinline__ void set_k(int t, kword w) {
+#pragma unroll
+    for (int i = 0; i < KW; ++i) k[t][i] = w[i];
   }
   __device__ __forceinline__ void load_k(const KvqRow& row, int s, int len) {
     const uint32_t lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, own = g * (HD / 8), own_scale = HD == 128 ? g : g >> 1;
@@ -96,14 +105,14 @@ struct KvqStep {
       const uint8_t *kc = row.kc + (size_t)s * (HD / 2), *sc = row.ks + (size_t)s * KW;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        k[t] = *reinterpret_cast<const kword*>(kc + (c * (HD / 2) + own) + t * 16 * (HD / 2));
+        set_k(t, *reinterpret_cast<const kword*>(kc + (c * (HD / 2) + own) + t * 16 * (HD / 2)));
         ks[t] = (sc + (c * KW + own_scale))[t * 16 * KW];
       }
     } else {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const uint32_t slot = min((uint32_t)s + 16 * t + c, (uint32_t)len - 1);
-        k[t] = *reinterpret_cast<const kword*>(row.kc + (slot * (HD / 2) + own));
+        set_k(t, *reinterpret_cast<const kword*>(row.kc + (slot * (HD / 2) + own)));
         ks[t] = row.ks[slot * KW + own_scale];
       }
     }
@@ -142,56 +151,114 @@ struct KvqStep {
   }
 };
 
-// A row's query, scaled, from element 8 kt of the lane's quarter on: its three bf16 terms.
+// A row's query in the lane's quarter of the channels, scaled, as kTerms times 32 E2M3 numbers (head_dim 64: sixteen, and zeros), the scale of a
+// term 2^-5 of that of the one before.  The first one's makes the largest magnitude of the 32 2 .. 4, where a place is worth a quarter: what a
+// term leaves is an eighth at most, and 4 to the next one; what the last leaves, 2^-24 of the largest magnitude.  units: the scales' bytes (255,
+// NaN, where a channel is not finite).
+constexpr int kTerms = 5;
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x6 __attribute__((ext_vector_type(6)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <int HD, bool LIST, int RT>
-__device__ __forceinline__ void query_terms(const KvqArgs& a, const KvqPlace<LIST, RT>& p, int row, int kt, u32x4 (&out)[3]) {
+__device__ __forceinline__ void query_terms(const KvqArgs& a, const KvqPlace<LIST, RT>& p, int row, u32x6 (&code)[kTerms], uint32_t (&unit)[kTerms]) {
   const int g = (threadIdx.x & 63) >> 4, r = p.row0 + row, tok = p.token_of(a, r);
-  const float* src = a.q + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(a.entry[p.e].q_first + tok) * a.Hq + p.h * a.group + (r - tok * a.group)) * HD + g * (HD / 4);
-  float x[8];
+  const f32x4* src = reinterpret_cast<const f32x4*>(a.q + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(a.entry[p.e].q_first + tok) * a.Hq + p.h * a.group + (r - tok * a.group)) * HD + g * (HD / 4));
+  f32x16 even = {}, odd = {};  // as the conversion takes them
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x4 v = reinterpret_cast<const f32x4*>(src + 8 * kt)[i];
+  for (int i = 0; i < HD / 16; ++i) {
+    const f32x4 v = src[i];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j] * a.scale;
-  }
-  bf16x8 hi, lo;
-  split_bf16x8(x, hi, lo);
-  out[0] = __builtin_bit_cast(u32x4, hi);
-  out[1] = __builtin_bit_cast(u32x4, lo);
-  out[2] = __builtin_bit_cast(u32x4, third_bf16x8(x, hi, lo));
-}
-
-// The queries of RT tiles of 16 rows as B fragments, in LDS, which all waves of the workgroup read; rows past the last are the last one's.  FOLD (four
-// rows at most): in registers; column 4 t + r is term t of row r, and one product serves all terms; columns 12 .. 15 are zero.
-template <int HD, bool FOLD>
-struct KvqQueries {
-  static constexpr int NKT = HD / 32, TERMS = FOLD ? 1 : 3;
-  u32x4 q[FOLD ? NKT : 1];
-  const u32x4* lds;
-  template <int NW, bool LIST, int RT>
-  __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST, RT>& p, u32x4* stage) {
-    const int lane = threadIdx.x & 63, n = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    u32x4 f[3];
-    if constexpr (FOLD) {
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        query_terms<HD>(a, p, min(n & 3, p.rows - 1), kt, f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[kt][i] = n < 4 ? f[0][i] : n < 8 ? f[1][i] : n < 12 ? f[2][i] : 0u;
-      }
-    } else {
-      lds = stage + lane;
-      for (int i = wave; i < RT * NKT; i += NW) {
-        query_terms<HD>(a, p, min(i / NKT * 16 + n, p.rows - 1), i % NKT, f);
-#pragma unroll
-        for (int t = 0; t < 3; ++t) stage[(i * 3 + t) * 64 + lane] = f[t];
-      }
-      __syncthreads();
+    for (int j = 0; j < 4; ++j) {
+      const float x = v[j] * a.scale;
+      top = max(top, __float_as_uint(x) & 0x7FFFFFFFu);
+      if (j % 2) odd[2 * i + j / 2] = x;
+      else even[2 * i + j / 2] = x;
     }
   }
-  __device__ __forceinline__ u32x4 get(int tile, int kt, int term, int zero) const {
-    if constexpr (FOLD) return q[kt];
-    else return (lds + zero)[((tile * NKT + kt) * 3 + term) * 64];
+  const uint32_t first = max(top >> 23, 22u) - 1;  // the largest magnitude becomes 2 .. 4; the last scale is a normal number
+#pragma unroll
+  for (int t = 0; t < kTerms; ++t) {
+    const float u = __uint_as_float((first - 5 * t) << 23);
+    code[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, u);
+    unit[t] = top >= 0x7F800000u ? 255u : first - 5 * t;
+    if (t + 1 == kTerms) break;
+    const auto taken = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(code[t], u);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      even[i] -= taken[2 * i];
+      odd[i] -= taken[2 * i + 1];
+    }
+  }
+}
+
+// The queries of RT tiles of 16 rows as B operands: split by one wave, held by all; rows past the last are the last one's.  FOLD (four rows at most):
+// column 4 t + r of the first operand is term t of row r, column r of the second the last term, its other columns are zero.
+template <int HD, bool FOLD, int RT>
+struct KvqQueries {
+  static constexpr int N = FOLD ? 2 : kTerms;
+  u32x6 q[RT][N];
+  uint32_t unit[RT][2];  // four to a word (FOLD: one)
+  struct Stage {
+    u32x6 q[RT][FOLD ? 1 : kTerms][FOLD ? 1 : 64];
+    uint32_t unit[RT][2][FOLD ? 1 : 64];
+  };
+  template <int NW, bool LIST>
+  __device__ __forceinline__ void load(const KvqArgs& a, const KvqPlace<LIST, RT>& p, Stage& stage) {
+    const int lane = threadIdx.x & 63, n = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u32x6 c[kTerms];
+    uint32_t u[kTerms];
+    if constexpr (FOLD) {
+      query_terms<HD>(a, p, min(n & 3, p.rows - 1), c, u);
+      const int t = n >> 2;
+      q[0][0] = t == 0 ? c[0] : t == 1 ? c[1] : t == 2 ? c[2] : c[3];
+      unit[0][0] = t == 0 ? u[0] : t == 1 ? u[1] : t == 2 ? u[2] : u[3];
+      q[0][1] = t == 0 ? c[4] : u32x6{};
+      unit[0][1] = u[4];
+    } else {
+      if (wave < RT) {
+        query_terms<HD>(a, p, min(wave * 16 + n, p.rows - 1), c, u);
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) stage.q[wave][t][lane] = c[t];
+        stage.unit[wave][0][lane] = u[0] | u[1] << 8 | u[2] << 16 | u[3] << 24;
+        stage.unit[wave][1][lane] = u[4];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) q[r][t] = stage.q[r][t][lane];
+        unit[r][0] = stage.unit[r][0][lane];
+        unit[r][1] = stage.unit[r][1][lane];
+      }
+    }
+  }
+  // += K Q^T of 16 slots: a lane's 32 codes of a slot, and their scale
+  template <int I, int U, int BYTE>
+  __device__ __forceinline__ void add(f32x4& x, int r, i32x8 k, uint32_t k_unit) const {
+    const i32x6 b = __builtin_bit_cast(i32x6, q[r][I]);
+    const i32x8 wide = __builtin_shufflevector(b, b, 0, 1, 2, 3, 4, 5, -1, -1);
+    x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, wide, x, 4, 2, 0, (int)k_unit, BYTE, (int)unit[r][U]);
+  }
+  __device__ __forceinline__ void scores(f32x4 (&x)[RT][2], const i32x8 (&k)[2], const uint32_t (&k_unit)[2]) const {
+    const auto term = [&](auto i, auto u, auto byte) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) add<decltype(i)::value, decltype(u)::value, decltype(byte)::value>(x[r][t], r, k[t], k_unit[t]);
+    };
+    // the smallest term first; products on one accumulator 2 RT apart
+    if constexpr (FOLD) {
+      term(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+      term(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    } else {
+      term(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+      term(std::integral_constant<int, 3>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 3>{});
+      term(std::integral_constant<int, 2>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 2>{});
+      term(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+      term(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    }
   }
 };
 
@@ -279,42 +346,26 @@ struct KvqRows {
 
 // A step added to a wave's RT row tiles.  The next one's codes (next < 0: there is none) are requested as soon as this one's have been made bf16.
 template <int HD, bool FOLD, int RT>
-__device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], KvqStep<HD>& st, const KvqQueries<HD, FOLD>& Q, const KvqRow& row, bool edge, int s,
+__device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], KvqStep<HD>& st, const KvqQueries<HD, FOLD, RT>& Q, const KvqRow& row, bool edge, int s,
                                          int next, const int (&seen)[RT], int len) {
-  constexpr int NKT = HD / 32, CPV = HD / 16, TERMS = KvqQueries<HD, FOLD>::TERMS;
+  constexpr int CPV = HD / 16, TERMS = FOLD ? 1 : 3;
   const int g = (threadIdx.x & 63) >> 4;
   f32x4 x[RT][2];
-  // queries are read from LDS at every step, which the compiler has to be kept from doing once: in registers they would leave no room for the results
-  int again = 0;
-  if (!FOLD) asm volatile("" : "+v"(again));
-u32x4 k[2][NKT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    // FOLD: the shift in the columns of one term, whose sum they become
+    const float start = !FOLD || (threadIdx.x & 12) == 0 ? R[r].shift : 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) x[r][t] = f32x4{start, start, start, start};
+  }
+  i32x8 k[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const float unit = unit_of(st.ks[t]);
-#pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) {
-      const uint32_t w = st.k[t][kt];
-      k[t][kt] = u32x4{bf16_pair<0>(w, unit), bf16_pair<1>(w, unit), bf16_pair<2>(w, unit), bf16_pair<3>(w, unit)};
-    }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      // FOLD: the shift in the columns of one term, whose sum they become
-      const float start = !FOLD || (threadIdx.x & 12) == 0 ? R[r].shift : 0.f;
-      x[r][t] = f32x4{start, start, start, start};
-    }
+    if constexpr (HD == 128) k[t] = i32x8{(int)st.k[t][0], (int)st.k[t][1], (int)st.k[t][2], (int)st.k[t][3]};
+    else k[t] = i32x8{(int)st.k[t][0], (int)st.k[t][1]};
   }
+  Q.scores(x, k, st.ks);
   if (next >= 0) st.load_k(row, next, len);
-  // the smallest term first; products on one accumulator 2 RT apart
-#pragma unroll
-  for (int i = TERMS - 1; i >= 0; --i)
-#pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const u32x4 q = Q.get(r, kt, i, again);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) mma<bf16_t>(x[r][t], k[t][kt], q);
-      }
   if constexpr (FOLD) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -384,11 +435,11 @@ u32x4 k[2][NKT];
 // (Two waves to a SIMD at least: otherwise the compiler keeps results in the other half of the registers and moves them to and fro.)
 template <int HD, bool FOLD, bool LIST, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
-  constexpr int ROWS = FOLD ? 4 : 16, CPV = HD / 16, NKT = HD / 32;
+  constexpr int ROWS = FOLD ? 4 : 16, CPV = HD / 16;
   __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
   __shared__ union Space {
     f32x4 o[NW][ROWS][HD / 4 + 1];  // a row's results four banks behind the last's: sixteen lanes store the same channels of sixteen rows
-    u32x4 q[FOLD ? 1 : RT * NKT * 3 * 64];
+    typename KvqQueries<HD, FOLD, RT>::Stage q;
     __device__ Space() {}
   } space;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -398,7 +449,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
   const size_t at_row = p.cache_row(a);
   const KvqRow row = {a.c.kc + at_row * (HD / 2), a.c.vc + at_row * (HD / 2), a.c.ks + at_row * (HD / 32), a.c.vs + at_row * (HD / 32)};
   KvqRows<HD, FOLD> R[RT];
-  KvqQueries<HD, FOLD> Q;
+  KvqQueries<HD, FOLD, RT> Q;
   KvqStep<HD> st;
   int seen[RT];
 #pragma unroll
@@ -503,7 +554,8 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
   }
 }
 
-// The pieces of a row joined: a wave to every (token, query head, layer), a lane HD / 64 channels... in order of the pieces.
+// The pieces of a row joined: a workgroup to every (token, query head, layer), of which HD / 4 threads stand side by side over the channels
+// and the groups of them take pieces in turn.  Sums have a fixed order.  4 us, most of it the launch and two chains of loads.
 template <int HD>
 __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   constexpr int C4 = HD / 4, PARTS = 256 / C4;  // threads side by side over the channels; pieces at a time

@@ -46,7 +46,9 @@ def attention_row(q, k, v):
     """One query head of one token over the slots it sees, float64: (result, bound on what fp32 arithmetic may be off by).  The bound:
     the scores' products and additions, (hd + 3) u sum|q||k| / sqrt(hd) (twice: numerator and sum), the exponential's argument
     and value, (range + 4) u (twice), the running sums and their rescalings, (slots + 32) u (twice); each relative to a weight, u = 2^-24.
-    The three bf16 terms of a query and of a probability leave 2^-24 of them: one u each, in the constants."""
+    The three bf16 terms of a probability leave 2^-24 of it: one u, in the constants.  The five 6-bit terms of a query leave 2^-24 of the largest
+    magnitude m of 32 neighbouring channels (scales 2^-5 apart, the first one's places worth a quarter where m is 2 .. 4: an eighth 2^-20 of the scale,
+    at most 2^-24 m): 2 u sum m |k| / sqrt(hd)."""
     hd, u = q.shape[0], 2.0 ** -24
     if k.shape[0] == 0:
         return np.zeros(hd), np.zeros(hd)
@@ -56,7 +58,9 @@ def attention_row(q, k, v):
         size = (np.abs(k) @ np.abs(q)).max() / math.sqrt(hd)
         e = np.exp(s - s.max())
         p = e / e.sum()
-        off = 2 * (hd + 3) * u * size + 2 * (s.max() - s.min() + 4) * u + 2 * (len(s) + 32) * u
+        most = np.repeat(np.abs(q).reshape(-1, 32).max(1), 32)
+        left = (np.abs(k) @ most).max() / math.sqrt(hd)
+        off = 2 * (hd + 3) * u * size + 2 * u * left + 2 * (s.max() - s.min() + 4) * u + 2 * (len(s) + 32) * u
         return p @ v, off * (p @ np.abs(v)) + 1e-37
 
 

@@ -152,6 +152,40 @@ def test_far_scores(es):
     K.check_attention(cache, zero, n, lens, K.attend(cache, zero, n, lens))
 
 
+@pytest.mark.parametrize("heads,hd", [((4, 1), 128), ((8, 1), 64), ((7, 1), 128), ((2, 1), 64)])
+def test_queries_of_every_size(es, heads, hd):
+    """Channels six decades apart in one query; queries far from 1 on keys as far on the other side; zeros but for one channel."""
+    g = np.random.default_rng(hd + heads[0])
+    n, lens = [5], [77]
+    for shift in (-90, -20, 0, 20, 90):
+        k = g.normal(0, 1, (1, 1, 1, 77, hd)) * 2.0 ** -shift
+        cache = K.Cache(es, 1, 1, 1, 77, hd).put(k, g.normal(0, 1, (1, 1, 1, 77, hd)))
+        q = g.normal(0, 2, (1, 5, heads[0], hd)) * 2.0 ** shift
+        q[:, 1] *= np.exp2(g.integers(-10, 11, hd))
+        q[:, 2] *= np.exp2(-g.integers(0, 60, hd))
+        q[:, 3, :, 1:] = 0
+        q[:, 4, :, :32] = 0
+        q = K.dev(q.astype(np.float32))
+        K.check_attention(cache, q, n, lens, K.attend(cache, q, n, lens))
+
+
+@pytest.mark.parametrize("heads,hd", [((4, 1), 128), ((8, 1), 64), ((7, 1), 128)])
+def test_queries_that_are_not_finite(es, heads, hd):
+    """A query with an infinity or NaN has no result; the others of its token and sequence are what they were."""
+    import torch
+    n, lens = [3], [130]
+    cache = K.random_cache(es, 21, 1, 1, 1, 130, hd)
+    q = K.dev(K.queries(21, 1, 3, heads[0], hd))
+    before = K.attend(cache, q, n, lens)
+    for value in (float("inf"), float("-inf"), float("nan")):
+        bad = q.clone()
+        bad[0, 1, 1, hd - 3] = value
+        after = K.attend(cache, bad, n, lens)
+        assert bool(after[0, 1, 1].isnan().all())
+        after[0, 1, 1] = before[0, 1, 1]
+        assert torch.equal(after, before)
+
+
 def test_stays_inside_its_arrays(es):
     import torch
     for heads, hd, n, lens, nb in (((8, 2), 128, [6, 16], [900, 2000], 0), ((4, 2), 64, [1, 1], [3000, 70], 0), ((28, 4), 128, [16, 2], [100, 90], 0), ((8, 2), 64, [3, 1], [700, 90], 11)):

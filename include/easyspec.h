@@ -435,6 +435,7 @@ int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layou
  *   out = sum over slots s of softmax_s(q . k_s / sqrt(head_dim)) v_s
  * The new tokens of sequence b, n_tokens[b] of them, are its last (their slots stored): token t sits in slot lens[b] - n_tokens[b] + t and
  * attends to the slots up to its own.  What a slot holds that a token does not see has no effect on it, values that are not finite among them.
+ * Everything is as exact as fp32 arithmetic (queries to 2^-24 of the largest magnitude of their 32 neighbouring channels).
  *   q            dev fp32 [n_layers][sum of n_tokens][n_q_heads][head_dim]  rotated queries, sequences in index order
  *   n_tokens     host [n_seqs]  0..EASYSPEC_MAX_CALIB_TOKENS
  *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots
@@ -443,7 +444,7 @@ int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layou
  *                a token reads, ascending: an entry that is not above the entry in front of it (the first: above -1), or that names a
  *                block without a slot that the token sees, is passed over.  As easyspec_kvq_select writes them.
  *   n_blocks     1..EASYSPEC_MAX_KVQ_SELECT; 0 without blocks
- *   out          dev fp32, the shape of q; zeros where a token sees no slot of its blocks
+ *   out          dev fp32, the shape of q; zeros where a token sees no slot of its blocks, or none whose score is above minus infinity
  *   workspace    dev, easyspec_kvq_attention_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
  * The same call gives the same bits; how contexts are cut goes by all sequences of the call, so that in the last bits a sequence's results
  * may differ with the others.  k_bounds is not read.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q, out and workspace may be NULL if no

@@ -53,8 +53,10 @@ __device__ __forceinline__ int entry_of(const KvqMoveArgs& a) {
 }
 
 // A workgroup: the slots of one block of kKvqBlock that a sequence stores, in one layer and KV head, of K (z = 0) or V.  A lane
-// takes eight channels of a slot.  K's bounds are taken from the values as they are held, from all slots of the block: those that were there
-// are read back, which a block's workgroup alone writes.
+// takes eight channels of a slot, the scale is the maximum over four lanes.  K's bounds are taken from the values as they are held, from all slots of
+// the block: those that were there are read back, which a block's workgroup alone writes.
+// Bound: memory.  2048 slots of bf16 in 32 layers of 8 KV heads of 128, 268 MB read and 73 written: 91 us behind other work, 73 called again
+// (3.7 .. 4.7 TB/s; a copy that moves as many bytes 65).  One slot of each: 4.6 us, a launch and three rounds through memory.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
   constexpr int kOcts = HD / 8, kUnits = kKvqBlock * kOcts, kTurns = kUnits / 256;
@@ -125,7 +127,8 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
   out[HD] = (uint16_t)(__float_as_uint(h4) >> 16);
 }
 
-// The way back: a lane takes eight channels of a slot.
+// The way back: a lane takes eight channels of a slot, four of them under way.  Bound: memory, by what it writes: the same 2048 slots
+// 57 us (5.9 TB/s of reads and writes).
 constexpr int kLoadTurns = 4;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_load_kernel(KvqMoveArgs a) {

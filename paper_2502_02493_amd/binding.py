@@ -151,16 +151,20 @@ def load_library():
 
 def _ptr(x):
     """Address of a torch tensor, numpy array, raw int or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    if isinstance(x, np.ndarray):
+    if type(x) is np.ndarray:
         assert x.flags["C_CONTIGUOUS"]
         return x.__array_interface__["data"][0]  # x.ctypes.data, at a third of its time
-    if hasattr(x, "data_ptr"):
+    try:  # a tensor, of which most calls have five to ten: asking for its kind first takes as long as its address
         assert x.is_contiguous()
         return x.data_ptr()
+    except AttributeError:
+        pass
+    if isinstance(x, np.ndarray):
+        return _ptr(x.view(np.ndarray))
+    if isinstance(x, int):
+        return x
     raise TypeError(type(x))
 
 
@@ -296,9 +300,12 @@ def easyspec_beam_select_workspace_bytes(groups: int, beams: int, vocab: int, n_
     return int(load_library().easyspec_beam_select_workspace_bytes(groups, beams, vocab, n_select))
 
 
+_INT32 = np.dtype(np.int32)
+
+
 def _host_ints(x, n):
     """An array of n host integers, all of which the library reads (n None: a handle that does not say how many)."""
-    a = np.ascontiguousarray(x, dtype=np.int32)
+    a = np.ascontiguousarray(x, _INT32)
     if n is not None and a.size != n:
         raise EasySpecError(EASYSPEC_EINVAL, f"an array of {a.size} entries where there are {n} sequences")
     return a

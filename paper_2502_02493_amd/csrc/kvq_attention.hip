@@ -17,8 +17,8 @@
 // the context is done.
 // Bound: a single token by the chain of one step a wave (2048 slots of 8 KV heads 6.5 us and 4 of the join; 0.3 us of bytes), long contexts with many
 // rows by the instructions of a step on two waves a SIMD: 48 products of 16 cycles, 20 of the other kind and some 230 vector instructions for 32 slots of 32 rows.
-// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 31 us in a graph (35 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
-// heads, 112 rows each, 18.8 (20.4); a large bf16 product's rate would allow 13 and 6.
+// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 30.6 us in a graph (34.6 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
+// heads, 112 rows each, 18.5 (20.3); a large bf16 product's rate would allow 13 and 6.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -436,9 +436,9 @@ __device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], KvqStep<HD>
 template <int HD, bool FOLD, bool LIST, int RT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
   constexpr int ROWS = FOLD ? 4 : 16, CPV = HD / 16;
-  __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+  __shared__ float s_m[RT][NW][ROWS], s_l[RT][NW][ROWS];
   __shared__ union Space {
-    f32x4 o[NW][ROWS][HD / 4 + 1];  // a row's results four banks behind the last's: sixteen lanes store the same channels of sixteen rows
+    f32x4 o[RT][NW][ROWS][HD / 4 + 1];  // all tiles at once (one after the other: 31.3 us for 30.6); a row's results four banks behind the last's: sixteen lanes store the same channels of sixteen rows
     typename KvqQueries<HD, FOLD, RT>::Stage q;
     __device__ Space() {}
   } space;
@@ -504,18 +504,19 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
   const size_t part = ((size_t)p.l * a.heads + p.h) * a.part_pitch + en.first_part;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    if (r > 0 && 16 * r >= p.rows) break;
     const float l = over_groups_sum(R[r].l);
-    if (!FOLD || r > 0) __syncthreads();  // queries and the last tile's shares have been read
     if (lane < ROWS) {
-      s_m[wave][lane] = R[r].m;
-      s_l[wave][lane] = l;
+      s_m[r][wave][lane] = R[r].m;
+      s_l[r][wave][lane] = l;
     }
-    __syncthreads();
+  }
+  __syncthreads();  // and queries have been read
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
     const int my_row = n % ROWS;
     float top = kLowest;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w][my_row]);
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[r][w][my_row]);
     const float f = pow2(R[r].m - top);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -524,32 +525,31 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
       for (int j = 0; j < CPV; ++j) x[j] = (FOLD ? fold_terms(R[r].o[j][i]) : R[r].o[j][i]) * f;
       if (!FOLD || n < 4)
 #pragma unroll
-        for (int j = 0; j < CPV; j += 4) space.o[wave][my_row][((4 * g + i) * CPV + j) / 4] = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+        for (int j = 0; j < CPV; j += 4) space.o[r][wave][my_row][((4 * g + i) * CPV + j) / 4] = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
     }
-    __syncthreads();
-    const int rows = min(ROWS, p.rows - 16 * r);
-    for (int u = threadIdx.x; u < rows * (HD / 4); u += NW * 64) {
-      const int k = u / (HD / 4), c = u % (HD / 4), ra = p.row0 + 16 * r + k;
-      f32x4 sum = space.o[0][k][c];
-      float m = s_m[0][k];
+  }
+  __syncthreads();
+  for (int u = threadIdx.x; u < p.rows * (HD / 4); u += NW * 64) {
+    const int row = u / (HD / 4), r = row / 16, k = row % 16, c = u % (HD / 4), ra = p.row0 + row;
+    f32x4 sum = space.o[r][0][k][c];
+    float m = s_m[r][0][k];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) {
-        sum += space.o[w][k][c];
-        m = fmaxf(m, s_m[w][k]);
-      }
-      float all = 0.f;
+    for (int w = 1; w < NW; ++w) {
+      sum += space.o[r][w][k][c];
+      m = fmaxf(m, s_m[r][w][k]);
+    }
+    float all = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) all += s_l[w][k] * pow2(s_m[w][k] - m);
-      if (en.chunks == 1) {
-        const int tok = p.token_of(a, ra);
-        f32x4* out = reinterpret_cast<f32x4*>(a.out + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(en.q_first + tok) * a.Hq + p.h * a.group + (ra - tok * a.group)) * HD);
-        const float inv = all == 0.f ? 0.f : 1.f / all;
-        out[c] = sum * inv;
-      } else {
-        const size_t at = part + (size_t)ra * en.chunks + p.c;
-        reinterpret_cast<f32x4*>(a.part)[at * (HD / 4) + c] = sum;
-        if (c == 0) a.part_ml[at] = make_float2(m, all);
-      }
+    for (int w = 0; w < NW; ++w) all += s_l[r][w][k] * pow2(s_m[r][w][k] - m);
+    if (en.chunks == 1) {
+      const int tok = p.token_of(a, ra);
+      f32x4* out = reinterpret_cast<f32x4*>(a.out + p.l * ((size_t)a.n_tokens * a.Hq * HD) + ((size_t)(en.q_first + tok) * a.Hq + p.h * a.group + (ra - tok * a.group)) * HD);
+      const float inv = all == 0.f ? 0.f : 1.f / all;
+      out[c] = sum * inv;
+    } else {
+      const size_t at = part + (size_t)ra * en.chunks + p.c;
+      reinterpret_cast<f32x4*>(a.part)[at * (HD / 4) + c] = sum;
+      if (c == 0) a.part_ml[at] = make_float2(m, all);
     }
   }
 }

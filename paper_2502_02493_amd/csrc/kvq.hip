@@ -10,6 +10,13 @@ template <typename T>
 struct Oct {  // eight neighbouring values
   u32x4 w[sizeof(T) / 2];
 };
+template <typename T>
+__device__ __forceinline__ Oct<T> fetch_oct(const T* p) {
+  Oct<T> o;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 2); ++i) o.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+  return o;
+}
 __device__ __forceinline__ void unpack_oct(const Oct<bf16_t>& o, float (&x)[8]) { unpack<bf16_t>(o.w[0], x); }
 __device__ __forceinline__ void unpack_oct(const Oct<float>& o, float (&x)[8]) {
 #pragma unroll
@@ -55,8 +62,9 @@ __device__ __forceinline__ int entry_of(const KvqMoveArgs& a) {
 // A workgroup: the slots of one block of kKvqBlock that a sequence stores, in one layer and KV head, of K (z = 0) or V.  A lane
 // takes eight channels of a slot, the scale is the maximum over four lanes.  K's bounds are taken from the values as they are held, from all slots of
 // the block: those that were there are read back, which a block's workgroup alone writes.
-// Bound: memory.  2048 slots of bf16 in 32 layers of 8 KV heads of 128, 268 MB read and 73 written: 91 us behind other work, 73 called again
-// (3.7 .. 4.7 TB/s; a copy that moves as many bytes 65).  One slot of each: 4.6 us, a launch and three rounds through memory.
+// Bound: memory.  2048 slots of bf16 in 32 layers of 8 KV heads of 128, 268 MB read and 73 written: 72 us (4.7 TB/s; a copy that moves as many bytes
+// 65), the bounds 8 of them.  What is read once goes past the caches (91 us otherwise), what is written, which the next attention reads, does not
+// (codes written past them too: 4 us more).  One slot of each of sixteen sequences: 4.6 us, a launch and three rounds through memory.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
   constexpr int kOcts = HD / 8, kUnits = kKvqBlock * kOcts, kTurns = kUnits / 256;
@@ -75,7 +83,7 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
 #pragma unroll
   for (int j = 0; j < kTurns; ++j) {
     const int u = j * 256 + tid, slot = slot0 + u / kOcts, i = slot - e.at4;
-    if (i >= 0 && i < e.n) x[j] = *reinterpret_cast<const Oct<T>*>(src + (size_t)(e.at + i) * HD + u % kOcts * 8);
+    if (i >= 0 && i < e.n) x[j] = fetch_oct(src + (size_t)(e.at + i) * HD + u % kOcts * 8);
   }
 #pragma unroll
   for (int j = 0; j < kTurns; ++j) {
@@ -127,9 +135,9 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
   out[HD] = (uint16_t)(__float_as_uint(h4) >> 16);
 }
 
-// The way back: a lane takes eight channels of a slot, four of them under way.  Bound: memory, by what it writes: the same 2048 slots
-// 57 us (5.9 TB/s of reads and writes).
-constexpr int kLoadTurns = 4;
+// The way back: a lane takes eight channels of a slot.  Bound: memory, by what it writes, past the caches: the same 2048 slots 49 us (6.9 TB/s
+// of reads and writes), 57 through them.  Both launches with one octet under way in a lane 141 us, two 116, four 118, eight 119.
+constexpr int kLoadTurns = 2;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_load_kernel(KvqMoveArgs a) {
   constexpr int kOcts = HD / 8;
@@ -154,10 +162,10 @@ __global__ __launch_bounds__(256) void kvq_load_kernel(KvqMoveArgs a) {
     const u32x4 b = decode(c[j], s[j]);
     u32x4* to = reinterpret_cast<u32x4*>(out + (size_t)u * 8);
     if constexpr (sizeof(T) == 2) {
-      to[0] = b;
+      __builtin_nontemporal_store(b, to);
     } else {
-      to[0] = u32x4{b[0] << 16, b[0] & 0xFFFF0000u, b[1] << 16, b[1] & 0xFFFF0000u};
-      to[1] = u32x4{b[2] << 16, b[2] & 0xFFFF0000u, b[3] << 16, b[3] & 0xFFFF0000u};
+      __builtin_nontemporal_store(u32x4{b[0] << 16, b[0] & 0xFFFF0000u, b[1] << 16, b[1] & 0xFFFF0000u}, to);
+      __builtin_nontemporal_store(u32x4{b[2] << 16, b[2] & 0xFFFF0000u, b[3] << 16, b[3] & 0xFFFF0000u}, to + 1);
     }
   }
 }

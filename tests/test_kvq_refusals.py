@@ -153,7 +153,7 @@ def test_nothing_to_do_needs_no_arrays():
 
 
 def test_arrays_that_touch_are_apart():
-    no_memory(store(k=far(5), v=far(5) + 81920, c=cache(k_scales=far(0) + 49152, v_scales=far(0) + 49152 + 3072)))
+    no_memory(store(k=far(5), v=far(5) + 81920, c=cache(k_scales=far(0) + 49152, v_scales=far(0) + 49152 + 49152 // 16)))
     no_memory(load(k_out=far(5), v_out=far(5) + 81920))
     no_memory(attend(out=far(5) + 46 * 1024))
     no_memory(select(blocks_out=far(6), workspace=far(6) + 23 * 2 * 2 * 4 * 4))

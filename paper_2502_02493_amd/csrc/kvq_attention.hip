@@ -558,7 +558,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
 // and the groups of them take pieces in turn.  Sums have a fixed order.  4 us, most of it the launch and two chains of loads.
 template <int HD>
 __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
-  constexpr int C4 = HD / 4, PARTS = 256 / C4;  // threads side by side over the channels; pieces at a time
+  constexpr int C4 = HD / 4, PARTS = 256 / C4, AHEAD = 4;  // threads side by side over the channels; pieces at a time; rounds of them requested first
   __shared__ float s_m[4], s_l[4];
   __shared__ f32x4 s_sum[PARTS][C4];
   const int t = blockIdx.x, j = blockIdx.y, l = blockIdx.z, tid = threadIdx.x, wave = tid >> 6;
@@ -569,6 +569,15 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   if (en.chunks == 1) return;
   const int h = j / a.group, row = (t - en.q_first) * a.group + j % a.group;
   const size_t at = ((size_t)l * a.heads + h) * a.part_pitch + en.first_part + (size_t)row * en.chunks;
+  const int c4 = tid % C4, c0 = tid / C4;
+  f32x4 x[AHEAD];
+  float xm[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int c = min(c0 + i * PARTS, en.chunks - 1);
+    x[i] = reinterpret_cast<const f32x4*>(a.part)[(at + c) * C4 + c4];
+    xm[i] = a.part_ml[at + c].x;
+  }
   float m = kLowest;
   for (int c = tid; c < en.chunks; c += 256) m = fmaxf(m, a.part_ml[at + c].x);
   m = lanes_max(m, 64);
@@ -582,10 +591,12 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   }
   sum = lanes_sum(sum, 64);
   if ((tid & 63) == 0) s_l[wave] = sum;
-  const int c4 = tid % C4;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int c = tid / C4; c < en.chunks; c += PARTS) o += reinterpret_cast<const f32x4*>(a.part)[(at + c) * C4 + c4] * pow2(a.part_ml[at + c].x - m);
-  s_sum[tid / C4][c4] = o;
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (c0 + i * PARTS < en.chunks) o += x[i] * pow2(xm[i] - m);
+  for (int c = c0 + AHEAD * PARTS; c < en.chunks; c += PARTS) o += reinterpret_cast<const f32x4*>(a.part)[(at + c) * C4 + c4] * pow2(a.part_ml[at + c].x - m);
+  s_sum[c0][c4] = o;
   __syncthreads();
   if (tid >= C4) return;
   const float all = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);

@@ -155,13 +155,18 @@ __device__ __forceinline__ u64 sum_all(u64 v, Sums* sh) {
   return all.weight;
 }
 
-// A row's bins in LDS: first their counts and weights, then those in front of each.
+// A row's bins in LDS: first their counts and weights, then, at(b), those in front of each, a place left out after every 32: threads step
+// over four bins each.
 template <int NT>
 struct Bins {
-  u64 weight[kBins + 1];
-  uint32_t count[kBins + 1];
+  static constexpr int kPlaces = kBins + kBins / 32 + 1;
+  u64 weight[kPlaces];
+  uint32_t count[kPlaces];
   Sums scan[NT / 64];
   int found[2];
+  static __device__ __forceinline__ int at(int b) { return b + (b >> 5); }
+  __device__ __forceinline__ u64 weight_before(int b) const { return weight[at(b)]; }
+  __device__ __forceinline__ uint32_t count_before(int b) const { return count[at(b)]; }
 };
 
 // The bins that matter, as up to four runs in ascending order, apart from each other: what is in front of a word is what its list has in
@@ -202,12 +207,12 @@ __device__ __forceinline__ void scan_bins(Bins<NT>& b, u64 (&w)[kBins / NT], uin
   Sums before = sums_before<NT>(own, b.scan, all);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    b.weight[tid * N + i] = before.weight;
-    b.count[tid * N + i] = (uint32_t)before.count;
+    b.weight[b.at(tid * N + i)] = before.weight;
+    b.count[b.at(tid * N + i)] = (uint32_t)before.count;
     before.weight += w[i];
     before.count += c[i];
   }
-  if (tid == 0) b.weight[kBins] = all.weight, b.count[kBins] = (uint32_t)all.count;
+  if (tid == 0) b.weight[b.at(kBins)] = all.weight, b.count[b.at(kBins)] = (uint32_t)all.count;
   __syncthreads();
 }
 
@@ -215,11 +220,11 @@ __device__ __forceinline__ void scan_bins(Bins<NT>& b, u64 (&w)[kBins / NT], uin
 template <int NT, class A>
 __device__ __forceinline__ void bins_that_reach(Bins<NT>& b, const A* run, u64 t0, u64 t1, int& b0, int& b1) {
   constexpr int N = kBins / NT;
-  u64 before = run[threadIdx.x * N];
+  u64 before = run[b.at(threadIdx.x * N)];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     const int i = threadIdx.x * N + j;
-    const u64 after = run[i + 1];
+    const u64 after = run[b.at(i + 1)];
     if (before < t0 && t0 <= after) b.found[0] = i;
     if (before < t1 && t1 <= after) b.found[1] = i;
     before = after;
@@ -250,11 +255,11 @@ __device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, 
     const bool any = n.lo[i] <= n.hi[i];
     n.weight[i] = n.count[i] = 0;
     if (any) {
-      const u64 w0 = b.weight[n.lo[i]], c0 = b.count[n.lo[i]];
+      const u64 w0 = b.weight_before(n.lo[i]), c0 = b.count_before(n.lo[i]);
       n.weight[i] = w0 - listed_w;
       n.count[i] = c0 - listed_c;
-      listed_w += b.weight[n.hi[i] + 1] - w0;
-      listed_c += b.count[n.hi[i] + 1] - c0;
+      listed_w += b.weight_before(n.hi[i] + 1) - w0;
+      listed_c += b.count_before(n.hi[i] + 1) - c0;
       end = n.hi[i];
       first = min(first, n.lo[i]);
     }
@@ -270,15 +275,15 @@ __device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w,
   int lo[4], hi[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) lo[i] = kBins, hi[i] = -1;
-  const u64 all = b.weight[kBins];
+  const u64 all = b.weight_before(kBins);
   u64 z0 = all, z1 = all;
   int cut0 = kBins, cut1 = kBins;
-  const bool k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count[kBins], p_on = a.top_p < 1.0, m_on = a.min_z > -INFINITY;
+  const bool k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count_before(kBins), p_on = a.top_p < 1.0, m_on = a.min_z > -INFINITY;
   if (k_on) {
     bins_that_reach(b, b.count, (u64)a.top_k, (u64)a.top_k, cut0, cut1);
     lo[0] = hi[0] = cut0;
-    z0 = b.weight[cut0];
-    z1 = b.weight[cut0 + 1];
+    z0 = b.weight_before(cut0);
+    z1 = b.weight_before(cut0 + 1);
   }
   if (p_on) {
     bins_that_reach(b, b.weight, top_p_target(a.top_p, z0), top_p_target(a.top_p, z1), lo[1], hi[1]);
@@ -291,7 +296,7 @@ __device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w,
     cut1 = min(cut1, hi[2]);
   }
   if (a.tokens) {
-    const u64 t0 = cut0 < kBins ? b.weight[cut0] : all, t1 = cut1 < kBins ? b.weight[cut1 + 1] : all;
+    const u64 t0 = cut0 < kBins ? b.weight_before(cut0) : all, t1 = cut1 < kBins ? b.weight_before(cut1 + 1) : all;
     bins_that_reach(b, b.weight, draw_target(u, t0), draw_target(u, t1), lo[3], hi[3]);
   }
   if (threadIdx.x < 64) {  // one wave: the same in all its lanes
@@ -303,7 +308,7 @@ __device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w,
     n.keep = cut0;
     n.stays = cut0 < kBins ? w.logit_at_bin(cut0, 1.0 - 1e-5) : -INFINITY;
     n.all = all;
-    n.m_front = m_on ? b.weight[lo[2]] : 0;
+    n.m_front = m_on ? b.weight_before(lo[2]) : 0;
     order_runs(w, b, lo, hi, n);
   }
   __syncthreads();

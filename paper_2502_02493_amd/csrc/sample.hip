@@ -155,15 +155,14 @@ __device__ __forceinline__ u64 sum_all(u64 v, Sums* sh) {
   return all.weight;
 }
 
-// A row's bins in LDS: first their counts and weights, then, at(b), those in front of each, a place left out after every 32: threads step
-// over four bins each.
+// A row's bins in LDS: first their counts and weights, then, at(b), those in front of each, a place left out after every 32, for steps
+// of several bins.
 template <int NT>
 struct Bins {
   static constexpr int kPlaces = kBins + kBins / 32 + 1;
   u64 weight[kPlaces];
   uint32_t count[kPlaces];
   Sums scan[NT / 64];
-  int found[2];
   static __device__ __forceinline__ int at(int b) { return b + (b >> 5); }
   __device__ __forceinline__ u64 weight_before(int b) const { return weight[at(b)]; }
   __device__ __forceinline__ uint32_t count_before(int b) const { return count[at(b)]; }
@@ -216,100 +215,97 @@ __device__ __forceinline__ void scan_bins(Bins<NT>& b, u64 (&w)[kBins / NT], uin
   __syncthreads();
 }
 
-// The bins that hold the words at which the running weight (count) reaches two targets, 1 or more and no more than there is.
+// The bin that holds the word at which the running weight (count) reaches a target, 1 or more and no more than there is: a wave's work, every
+// sixteenth sum first, then the sixteen between.
 template <int NT, class A>
-__device__ __forceinline__ void bins_that_reach(Bins<NT>& b, const A* run, u64 t0, u64 t1, int& b0, int& b1) {
-  constexpr int N = kBins / NT;
-  u64 before = run[b.at(threadIdx.x * N)];
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int i = threadIdx.x * N + j;
-    const u64 after = run[b.at(i + 1)];
-    if (before < t0 && t0 <= after) b.found[0] = i;
-    if (before < t1 && t1 <= after) b.found[1] = i;
-    before = after;
-  }
-  __syncthreads();
-  b0 = b.found[0];
-  b1 = b.found[1];
-  __syncthreads();
-}
-
-// Four runs of bins in ascending order, those that meet made one (the later of them empty), and what lies in front of each.
-template <int NT>
-__device__ __forceinline__ void order_runs(const Weigher& w, const Bins<NT>& b, int (&lo)[4], int (&hi)[4], NearBins& n) {
-  const auto order = [&](int i, int j) {
-    if (lo[j] < lo[i]) {
-      const int l = lo[i], h = hi[i];
-      lo[i] = lo[j]; hi[i] = hi[j];
-      lo[j] = l; hi[j] = h;
-    }
-  };
-  order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
-  int end = -1, first = kBins;  // of the runs so far
-  u64 listed_w = 0, listed_c = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    n.lo[i] = max(lo[i], end + 1);
-    n.hi[i] = lo[i] < kBins ? hi[i] : -1;
-    const bool any = n.lo[i] <= n.hi[i];
-    n.weight[i] = n.count[i] = 0;
-    if (any) {
-      const u64 w0 = b.weight_before(n.lo[i]), c0 = b.count_before(n.lo[i]);
-      n.weight[i] = w0 - listed_w;
-      n.count[i] = c0 - listed_c;
-      listed_w += b.weight_before(n.hi[i] + 1) - w0;
-      listed_c += b.count_before(n.hi[i] + 1) - c0;
-      end = n.hi[i];
-      first = min(first, n.lo[i]);
-    }
-  }
-  n.x0 = w.logit_at_bin(end + 1, 1.0 + 1e-5);
-  n.x1 = w.logit_at_bin(first, 1.0 - 1e-5);
+__device__ __forceinline__ int bin_that_reaches(const Bins<NT>& b, const A* run, u64 target) {
+  static_assert(kBins == 16 * 64, "sixteen bins to a lane");
+  const int lane = threadIdx.x & 63;
+  const int group = __popcll(__ballot(run[b.at(16 * lane + 16)] < target));
+  return 16 * group + __popcll(__ballot(lane < 16 && run[b.at(16 * group + (lane & 15) + 1)] < target));
 }
 
 // Which bins matter.  b: sums in front of the bins.  The weight of the first top_k words, and of all that stay, is known here up to the
-// words of one bin: whatever depends on it gets the bins between what either end asks for.
+// words of one bin: whatever depends on it gets the bins between what either end asks for.  One wave's work, with few instructions: executed once,
+// they take longer to arrive than to run (by all waves, with barriers at each search: 22.4 us a call for one row of 128 256, 32.7 for sixteen).
 template <int NT>
 __device__ __forceinline__ void near_bins(const SampleArgs& a, const Weigher& w, double u, Bins<NT>& b, NearBins& n) {
-  int lo[4], hi[4];
+  if (threadIdx.x < 64) {
+    int lo[4], hi[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) lo[i] = kBins, hi[i] = -1;
-  const u64 all = b.weight_before(kBins);
-  u64 z0 = all, z1 = all;
-  int cut0 = kBins, cut1 = kBins;
-  const bool k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count_before(kBins), p_on = a.top_p < 1.0, m_on = a.min_z > -INFINITY;
-  if (k_on) {
-    bins_that_reach(b, b.count, (u64)a.top_k, (u64)a.top_k, cut0, cut1);
-    lo[0] = hi[0] = cut0;
-    z0 = b.weight_before(cut0);
-    z1 = b.weight_before(cut0 + 1);
-  }
-  if (p_on) {
-    bins_that_reach(b, b.weight, top_p_target(a.top_p, z0), top_p_target(a.top_p, z1), lo[1], hi[1]);
-    cut0 = min(cut0, lo[1]);
-    cut1 = min(cut1, hi[1]);
-  }
-  if (m_on) {
-    lo[2] = hi[2] = w.bin(-a.min_z * w.log2e_T);
-    cut0 = min(cut0, lo[2]);
-    cut1 = min(cut1, hi[2]);
-  }
-  if (a.tokens) {
-    const u64 t0 = cut0 < kBins ? b.weight_before(cut0) : all, t1 = cut1 < kBins ? b.weight_before(cut1 + 1) : all;
-    bins_that_reach(b, b.weight, draw_target(u, t0), draw_target(u, t1), lo[3], hi[3]);
-  }
-  if (threadIdx.x < 64) {  // one wave: the same in all its lanes
-    n.k_on = k_on; n.p_on = p_on; n.m_on = m_on;
-    n.k_bin = lo[0];
-    n.p_bin = lo[1];
-    n.m_bin = m_on ? lo[2] : -1;
-    n.draw_bin = lo[3];
-    n.keep = cut0;
-    n.stays = cut0 < kBins ? w.logit_at_bin(cut0, 1.0 - 1e-5) : -INFINITY;
-    n.all = all;
-    n.m_front = m_on ? b.weight_before(lo[2]) : 0;
-    order_runs(w, b, lo, hi, n);
+    for (int i = 0; i < 4; ++i) lo[i] = kBins, hi[i] = -1;
+    const u64 all = b.weight_before(kBins);
+    u64 z0 = all, z1 = all;
+    int cut0 = kBins, cut1 = kBins;
+    const bool k_on = a.top_k > 0 && (uint32_t)a.top_k < b.count_before(kBins), p_on = a.top_p < 1.0, m_on = a.min_z > -INFINITY;
+    if (k_on) {
+      lo[0] = hi[0] = cut0 = cut1 = bin_that_reaches(b, b.count, (u64)a.top_k);
+      z0 = b.weight_before(cut0);
+      z1 = b.weight_before(cut0 + 1);
+    }
+    if (p_on) {
+      lo[1] = bin_that_reaches(b, b.weight, top_p_target(a.top_p, z0));
+      hi[1] = bin_that_reaches(b, b.weight, top_p_target(a.top_p, z1));
+      cut0 = min(cut0, lo[1]);
+      cut1 = min(cut1, hi[1]);
+    }
+    u64 m_front = 0;
+    if (m_on) {
+      lo[2] = hi[2] = w.bin(-a.min_z * w.log2e_T);
+      cut0 = min(cut0, lo[2]);
+      cut1 = min(cut1, hi[2]);
+      m_front = b.weight_before(lo[2]);
+    }
+    if (a.tokens) {
+      lo[3] = bin_that_reaches(b, b.weight, draw_target(u, cut0 < kBins ? b.weight_before(cut0) : all));
+      hi[3] = bin_that_reaches(b, b.weight, draw_target(u, cut1 < kBins ? b.weight_before(cut1 + 1) : all));
+    }
+    if (threadIdx.x == 0) {
+      n.k_on = k_on; n.p_on = p_on; n.m_on = m_on;
+      n.k_bin = lo[0];
+      n.p_bin = lo[1];
+      n.m_bin = m_on ? lo[2] : -1;
+      n.draw_bin = lo[3];
+      n.keep = cut0;
+      n.all = all;
+      n.m_front = m_front;
+    }
+    // in ascending order, those that meet made one (the later of them empty)
+    const auto order = [&](int i, int j) {
+      const bool swap = lo[j] < lo[i];
+      const int l = lo[i], h = hi[i];
+      lo[i] = swap ? lo[j] : l;
+      hi[i] = swap ? hi[j] : h;
+      lo[j] = swap ? l : lo[j];
+      hi[j] = swap ? h : hi[j];
+    };
+    order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
+    int end = -1, first = kBins;  // of the runs so far
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      hi[i] = lo[i] < kBins ? hi[i] : -1;
+      lo[i] = max(lo[i], end + 1);
+      const bool any = lo[i] <= hi[i];
+      end = any ? hi[i] : end;
+      first = any ? min(first, lo[i]) : first;
+    }
+    // a run to a lane: what lies in front of it, less what the runs before it list; then a border to a lane
+    const int lane = threadIdx.x, at = lane & 3;
+    const int my_lo = at == 0 ? lo[0] : at == 1 ? lo[1] : at == 2 ? lo[2] : lo[3], my_hi = at == 0 ? hi[0] : at == 1 ? hi[1] : at == 2 ? hi[2] : hi[3];
+    const bool any = lane < 4 && my_lo <= my_hi;
+    const u64 w0 = any ? b.weight_before(my_lo) : 0, w1 = any ? b.weight_before(my_hi + 1) - w0 : 0;
+    const u64 c0 = any ? b.count_before(my_lo) : 0, c1 = any ? b.count_before(my_hi + 1) - c0 : 0;
+    const u64 w_listed = running_sum(w1) - w1, c_listed = running_sum(c1) - c1;
+    if (lane < 4) {
+      n.lo[lane] = my_lo;
+      n.hi[lane] = my_hi;
+      n.weight[lane] = any ? w0 - w_listed : 0;
+      n.count[lane] = any ? c0 - c_listed : 0;
+    }
+    const float x = w.logit_at_bin(lane == 0 ? end + 1 : lane == 1 ? first : cut0, lane == 0 ? 1.0 + 1e-5 : 1.0 - 1e-5);
+    if (lane == 0) n.x0 = x;
+    if (lane == 1) n.x1 = x;
+    if (lane == 2) n.stays = cut0 < kBins ? x : -INFINITY;
   }
   __syncthreads();
 }

@@ -15,9 +15,9 @@
 //     hd / 16 (l % 16) .. of those slots, pairs of slots meeting in a register by one permutation.
 // The running maximum, sum and result of a row stay in the lanes of its column; nothing passes through LDS until a wave's share of
 // the context is done.
-// Bound: a single token by the chain of one step a wave (2048 slots of 8 KV heads 6.5 us and 4 of the join; 0.3 us of bytes), long contexts with many
+// Bound: a single token by the chain of one step a wave (2048 slots of 8 KV heads 6.9 us and 3.7 of the join; 0.3 us of bytes), long contexts with many
 // rows by the instructions of a step on two waves a SIMD: 48 products of 16 cycles, 20 of the other kind and some 230 vector instructions for 32 slots of 32 rows.
-// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 30.6 us in a graph (34.6 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
+// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 30 us in a graph (34 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
 // heads, 112 rows each, 18.5 (20.3); a large bf16 product's rate would allow 13 and 6.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
@@ -555,7 +555,8 @@ __global__ __launch_bounds__(NW * 64, 2) void kvq_attn_kernel(KvqArgs a) {
 }
 
 // The pieces of a row joined: a workgroup to every (token, query head, layer), of which HD / 4 threads stand side by side over the channels
-// and the groups of them take pieces in turn.  Sums have a fixed order.  4 us, most of it the launch and two chains of loads.
+// and the groups of them take pieces in turn.  Sums have a fixed order.  3.7 us, most of it the
+// launch and a round through memory: pieces are requested before their maximum is known (4.0 otherwise).
 template <int HD>
 __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
   constexpr int C4 = HD / 4, PARTS = 256 / C4, AHEAD = 4;  // threads side by side over the channels; pieces at a time; rounds of them requested first
@@ -611,6 +612,7 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
 // workgroups: one token at 32768 and 65536 slots of 8 KV heads 16.9 / 22.3 and 22.4 / 27.7, sixteen at 8192 35.1 / 42.0, six at 16384 17.9 / 24.2,
 // sixteen of 16 tokens at 512 .. 1067 on 4 heads 20.7 / 46.
 //   Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
+//   (Measured with K as bf16 and pieces requested late, which makes no difference to the comparisons.)
 //   Waves: eight, but four where a wave of eight would have a step or less.  four / eight: one token at 65536 slots 23.5 / 22.4, sixteen at
 //   8192 41.6 / 35.1, with seven heads to a KV head 25.9 / 23.4; at 16384 (2048 steps) 11.8 / 11.9.
 //   Contexts of two steps a wave are not cut: no second launch.  cut / whole, 32 query heads on 8 KV heads: one token at 256, 512, 768 slots 8.5 / 7.2,

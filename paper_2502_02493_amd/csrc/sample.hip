@@ -852,7 +852,7 @@ __global__ __launch_bounds__(kSliceNT) void sample_bins_kernel(SampleArgs a) {
   }
 }
 
-// grid (cuts, rows).  Reads and writes the row: 27.9 us (4.2 TB/s); of a single row of 128 256 9.5, of which 4 are the bins, which every
+// grid (cuts, rows).  Reads and writes the row: 27.2 us (4.3 TB/s); of a single row of 128 256 9.1, of which 2 to 3 are the bins, which every
 // workgroup sums up for itself.  Workgroups of 256 threads, 2048 of them at most: 1024 threads make the 71 us of all four launches 81, 1024
 // workgroups of 512 threads change nothing.
 __global__ __launch_bounds__(kCutNT) void sample_near_kernel(SampleArgs a) {

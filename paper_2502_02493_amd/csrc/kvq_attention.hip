@@ -608,16 +608,16 @@ __global__ __launch_bounds__(256) void kvq_join_kernel(KvqArgs a) {
 }
 
 // How a call is cut: into no more workgroups than CUs.  What one does before its first step and after its last (queries, results of its waves joined,
-// 5 us) costs as much as three to five steps of a wave, and a second round of workgroups adds it again.  us a call in a graph, with at most 256 / 512
-// workgroups: one token at 32768 and 65536 slots of 8 KV heads 16.9 / 22.3 and 22.4 / 27.7, sixteen at 8192 35.1 / 42.0, six at 16384 17.9 / 24.2,
-// sixteen of 16 tokens at 512 .. 1067 on 4 heads 20.7 / 46.
-//   Row tiles to a wave: one, or two where there are more than sixteen rows: a step's values are then made bf16 once for both.
-//   (Measured with K as bf16 and pieces requested late, which makes no difference to the comparisons.)
-//   Waves: eight, but four where a wave of eight would have a step or less.  four / eight: one token at 65536 slots 23.5 / 22.4, sixteen at
-//   8192 41.6 / 35.1, with seven heads to a KV head 25.9 / 23.4; at 16384 (2048 steps) 11.8 / 11.9.
-//   Contexts of two steps a wave are not cut: no second launch.  cut / whole, 32 query heads on 8 KV heads: one token at 256, 512, 768 slots 8.5 / 7.2,
-//   8.5 / 8.5, 8.7 / 9.7, six at 512 and 1024 11.9 / 11.2, 11.9 / 16.
-constexpr int kKvqCus = 256, kKvqFewSteps = 2048, kKvqWhole = 16;
+// 5 us) costs as much as three to five steps of a wave, and a second round of workgroups adds it again.  us a call in a graph, with at most 256 : 512
+// workgroups: one token at 32768 and 65536 slots of 8 KV heads 16.0 : 21.6 and 21.0 : 26.4, sixteen at 8192 35.6 : 41.1, six at 16384 16.9 : 24.1,
+// sixteen of 16 tokens at 512 .. 1067 on 4 heads 18.6 : 36.7; at 16384 slots of 4 heads 11.2 : 14.1.
+//   Row tiles to a wave: one, or two where there are more than sixteen rows: V of a step is then made bf16 once for both.
+//   Waves: eight, but four where a wave of eight would have two steps or less.  four : eight, one token: 2048 slots of 8 heads (512 steps) 9.2 : 10.5,
+//   16384 of 4 (2048) 11.2 : 11.7, sixteen lists of 24 blocks on 4 heads (3072) 24.7 : 25.4, 32768 of 8 (8192) 16.0 : 16.0, 65536 22.6 : 20.9, sixteen at
+//   8192 41.0 : 36.0.
+//   Contexts of two steps a wave are not cut: no second launch.  cut : whole, 8 KV heads: one token at 256, 512, 768, 1024 slots 8.9 : 7.2,
+//   8.9 : 8.3, 9.0 : 9.4, 9.0 : 10.6, six at 512 and 1024 12.0 : 10.8, 12.1 : 14.7.
+constexpr int kKvqCus = 256, kKvqFewSteps = 4096, kKvqWhole = 16;
 struct KvqCut {
   int rows, tiles, waves;  // rows of a sequence's (a token's) queries on a KV head; row tiles to a wave; waves of a workgroup
   bool whole;              // no context is cut
@@ -761,7 +761,8 @@ __device__ __forceinline__ uint64_t score_key(double s) {
 
 // A workgroup to every list; thread i holds blocks kSelectThreads j + i.  Bound: a chain of counts and barriers, two bits of the scores' upper
 // halves a round, from the first bit that differs until as many blocks reach the bound as shall stay: 32 of 512 blocks 6.9 us.  (One bit a
-// round, and queries requested one after the other: selection and attention of those sixteen sequences 27.1 us in a graph instead of 25.6.  A wave with all blocks in its registers: 10 us, much of which its instructions took to arrive, three thousand, each executed a few times.)
+// round, and queries requested one after the other: selection and attention of those sixteen sequences 27.1 us in a graph instead of 25.6.  A
+// wave with all blocks in its registers: 10 us, much of which its instructions took to arrive, three thousand, each executed a few times.)
 constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / 64, kSelectRegs = kMaxKvqSelect / kSelectThreads;
 struct SelectShared {
   int count[2][3][kSelectWaves];

@@ -445,7 +445,8 @@ int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layou
  *                block without a slot that the token sees, is passed over.  As easyspec_kvq_select writes them.
  *   n_blocks     1..EASYSPEC_MAX_KVQ_SELECT; 0 without blocks
  *   out          dev fp32, the shape of q; zeros where a token sees no slot of its blocks, or none whose score is above minus infinity
- *   workspace    dev, easyspec_kvq_attention_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ *   workspace    dev, easyspec_kvq_attention_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept; what a
+ *                call does not need of it is not looked at
  * The same call gives the same bits; how contexts are cut goes by all sequences of the call, so that in the last bits a sequence's results
  * may differ with the others.  k_bounds is not read.  Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q, out and workspace may be NULL if no
  * sequence has new tokens), a bad layout, counts or lengths, out or a workspace that overlaps another array, arrays that are not 16-byte aligned (scales: 1,
@@ -454,6 +455,10 @@ int easyspec_kvq_attention(const float *q, const easyspec_kvq *cache, const easy
                            int32_t n_q_heads, const int32_t *blocks, int32_t n_blocks, float *out, void *workspace, void *hip_stream);
 int64_t easyspec_kvq_attention_workspace_bytes(const easyspec_kv_layout *layout, const int32_t *n_tokens, const int32_t *lens, int32_t n_q_heads,
                                                int32_t n_blocks); /* -1 for bad arguments */
+/* A workspace of _workspace_bytes() for some lens and n_blocks holds every call with the same layout, n_tokens and n_q_heads whose lens are no
+ * longer, and n_blocks (if not 0) no more.  Across n_tokens, and between calls with and without lists, it may rise or fall: _workspace_limit() holds every
+ * call on the layout with up to max_tokens (1..EASYSPEC_MAX_CALIB_TOKENS) new tokens of a sequence, without lists or with lists of up to max_blocks (0: without only). */
+int64_t easyspec_kvq_attention_workspace_limit(const easyspec_kv_layout *layout, int32_t max_tokens, int32_t n_q_heads, int32_t max_blocks); /* -1 for bad arguments */
 
 /* The blocks that matter to a new token, for every layer and KV head: of the blocks that hold a slot it sees, the first keep_first, the last
  * keep_last and, of the others, those with the highest

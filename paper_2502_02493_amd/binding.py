@@ -31,7 +31,7 @@ EXPORTS = ["easyspec_create", "easyspec_destroy", "easyspec_load_weights", "easy
            "easyspec_attn_weights", "easyspec_attn_weights_workspace_bytes", "easyspec_kv_evict",
            "easyspec_beam_fork", "easyspec_beam_reorder", "easyspec_track_attention", "easyspec_evict", "easyspec_get_evicted",
            "easyspec_get_attn_weights",
-           "easyspec_kvq_store", "easyspec_kvq_load", "easyspec_kvq_attention", "easyspec_kvq_attention_workspace_bytes",
+           "easyspec_kvq_store", "easyspec_kvq_load", "easyspec_kvq_attention", "easyspec_kvq_attention_workspace_bytes", "easyspec_kvq_attention_workspace_limit",
            "easyspec_kvq_select", "easyspec_kvq_select_workspace_bytes", "easyspec_sample", "easyspec_sample_workspace_bytes",
            "easyspec_last_error"]
 EASYSPEC_OP_QKV, EASYSPEC_OP_ATTN, EASYSPEC_OP_OPROJ, EASYSPEC_OP_GATEUP, EASYSPEC_OP_DOWN, EASYSPEC_OP_HEAD, EASYSPEC_OP_ALL = range(7)
@@ -112,6 +112,8 @@ def load_library():
         L.easyspec_kvq_attention.argtypes = [vp, kvq, kvl, vp, vp, i32, vp, i32, vp, vp, vp]
         L.easyspec_kvq_attention_workspace_bytes.argtypes = [kvl, vp, vp, i32, i32]
         L.easyspec_kvq_attention_workspace_bytes.restype = C.c_int64
+        L.easyspec_kvq_attention_workspace_limit.argtypes = [kvl, i32, i32, i32]
+        L.easyspec_kvq_attention_workspace_limit.restype = C.c_int64
         L.easyspec_kvq_select.argtypes = [vp, vp, kvl, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         L.easyspec_kvq_select_workspace_bytes.argtypes = [kvl, vp, vp, i32, i32]
         L.easyspec_kvq_select_workspace_bytes.restype = C.c_int64
@@ -366,6 +368,10 @@ def easyspec_kvq_attention(q, cache: easyspec_kvq, layout: easyspec_kv_layout, n
 def easyspec_kvq_attention_workspace_bytes(layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, n_blocks) -> int:
     n, s = _int_bytes(n_tokens, layout.n_seqs), _int_bytes(lens, layout.n_seqs)
     return int(load_library().easyspec_kvq_attention_workspace_bytes(C.byref(layout), n, s, n_q_heads, n_blocks))
+
+
+def easyspec_kvq_attention_workspace_limit(layout: easyspec_kv_layout, max_tokens: int, n_q_heads: int, max_blocks: int) -> int:
+    return int(load_library().easyspec_kvq_attention_workspace_limit(C.byref(layout), max_tokens, n_q_heads, max_blocks))
 
 
 def easyspec_kvq_select(q, k_bounds, layout: easyspec_kv_layout, n_tokens, lens, n_q_heads, keep_first, keep_last, n_select, blocks_out, workspace,

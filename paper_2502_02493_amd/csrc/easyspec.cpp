@@ -1212,15 +1212,22 @@ extern "C" int easyspec_kvq_load(const easyspec_kvq* cache, const easyspec_kv_la
   return EASYSPEC_OK;
 }
 
+// Query heads of a KV head, or an error (negative).
+static int kvq_group(const char* what, const easyspec_kv_layout* g, int32_t n_q_heads) {
+  const int group = n_q_heads > 0 && n_q_heads % g->n_kv_heads == 0 ? n_q_heads / g->n_kv_heads : 0;
+  if ((group != 1 && group != 2 && group != 4 && group != 7 && group != 8) || n_q_heads > 65535)
+    return fail(nullptr, EASYSPEC_EINVAL, "%s: %d query heads on %d KV heads: not 1, 2, 4, 7 or 8 each, or more than 65535", what, n_q_heads, g->n_kv_heads);
+  return group;
+}
+
 // The sequences with new tokens, for attention and selection: returns their tokens, or an error.
 static int kvq_entries(const char* what, const easyspec_kv_layout* g, const int32_t* n_tokens, const int32_t* lens, int32_t n_q_heads, KvqEntry* entry,
                        int* n_entries, int* n_new) {
   const int rc = check_layout(what, g);
   if (rc != EASYSPEC_OK) return rc;
   if (!n_tokens || !lens) return fail(nullptr, EASYSPEC_EINVAL, "%s: NULL argument", what);
-  const int group = n_q_heads > 0 && n_q_heads % g->n_kv_heads == 0 ? n_q_heads / g->n_kv_heads : 0;
-  if ((group != 1 && group != 2 && group != 4 && group != 7 && group != 8) || n_q_heads > 65535)
-    return fail(nullptr, EASYSPEC_EINVAL, "%s: %d query heads on %d KV heads: not 1, 2, 4, 7 or 8 each, or more than 65535", what, n_q_heads, g->n_kv_heads);
+  const int group = kvq_group(what, g, n_q_heads);
+  if (group < 0) return group;
   *n_entries = *n_new = 0;
   for (int b = 0; b < g->n_seqs; ++b) {
     const int n = n_tokens[b];
@@ -1253,6 +1260,18 @@ extern "C" int64_t easyspec_kvq_attention_workspace_bytes(const easyspec_kv_layo
   return (int64_t)kvq_workspace_bytes(a, layout->n_layers, layout->head_dim);
 }
 
+extern "C" int64_t easyspec_kvq_attention_workspace_limit(const easyspec_kv_layout* layout, int32_t max_tokens, int32_t n_q_heads, int32_t max_blocks) {
+  const char* what = "kvq_attention_workspace_limit";
+  if (check_layout(what, layout) != EASYSPEC_OK) return -1;
+  const int group = kvq_group(what, layout, n_q_heads);
+  if (group < 0) return -1;
+  if (max_tokens < 1 || max_tokens > EASYSPEC_MAX_CALIB_TOKENS || max_blocks < 0 || max_blocks > kMaxKvqSelect) {
+    fail(nullptr, EASYSPEC_EINVAL, "%s: up to %d tokens (1..%d) and lists of up to %d blocks (0..%d)", what, max_tokens, EASYSPEC_MAX_CALIB_TOKENS, max_blocks, kMaxKvqSelect);
+    return -1;
+  }
+  return (int64_t)kvq_workspace_limit(layout->n_seqs, layout->n_kv_heads, group, layout->n_layers, layout->head_dim, max_tokens, layout->max_slots, max_blocks);
+}
+
 extern "C" int easyspec_kvq_attention(const float* q, const easyspec_kvq* cache, const easyspec_kv_layout* layout, const int32_t* n_tokens, const int32_t* lens,
                                       int32_t n_q_heads, const int32_t* blocks, int32_t n_blocks, float* out, void* workspace, void* hip_stream) {
   if (!cache || !cache->k_codes || !cache->v_codes || !cache->k_scales || !cache->v_scales) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: NULL argument");
@@ -1262,7 +1281,7 @@ extern "C" int easyspec_kvq_attention(const float* q, const easyspec_kvq* cache,
   if (!blocks != !n_blocks) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: lists of %d blocks, and %s", n_blocks, blocks ? "an array of them" : "no array");
   if (a.n_entries == 0) return EASYSPEC_OK;
   const KvqExtents x = kvq_extents(cache, layout);
-  const size_t bytes = (size_t)layout->n_layers * a.n_tokens * n_q_heads * layout->head_dim * sizeof(float), ws = kvq_workspace_bytes(a, layout->n_layers, layout->head_dim);
+  const size_t bytes = (size_t)layout->n_layers * a.n_tokens * n_q_heads * layout->head_dim * sizeof(float), ws = kvq_bytes_used(a, layout->n_layers, layout->head_dim);
   if (!q || !out || (ws && !workspace)) return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: NULL argument");
   if (misaligned({q, out, workspace, x.kc.p, x.vc.p}, 16) || misaligned({blocks}, 4))
     return fail(nullptr, EASYSPEC_EINVAL, "kvq_attention: q, out, workspace and codes must be 16-byte aligned, blocks 4-byte");

@@ -339,7 +339,9 @@ struct KvqArgs {
   KvqEntry entry[kMaxCols];
 };
 void kvq_plan(KvqArgs& a, int n_layers);
-size_t kvq_workspace_bytes(const KvqArgs& a, int n_layers, int hd);
+size_t kvq_bytes_used(const KvqArgs& a, int n_layers, int hd);       // by this call
+size_t kvq_workspace_bytes(const KvqArgs& a, int n_layers, int hd);  // by it and those of shorter contexts or lists
+size_t kvq_workspace_limit(int n_seqs, int heads, int group, int n_layers, int hd, int max_tokens, int max_slots, int max_blocks);
 void launch_kvq_attention(const KvqArgs& a, int n_layers, int hd, hipStream_t st);
 struct KvqSelectArgs {
   const float* q;

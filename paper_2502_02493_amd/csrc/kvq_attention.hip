@@ -679,8 +679,48 @@ static bool kvq_joined(const KvqArgs& a) {
     if (a.entry[i].chunks > 1) return true;
   return false;
 }
+static size_t kvq_part_bytes(int hd) { return hd * sizeof(float) + sizeof(float2); }
+size_t kvq_bytes_used(const KvqArgs& a, int n_layers, int hd) { return kvq_joined(a) ? a.part_pitch * a.heads * n_layers * kvq_part_bytes(hd) : 0; }
+
+// Workgroups that a call may have beyond one chunk of everything.  A chunk either leaves no more workgroups than CUs, or it is twice what a CU has to
+// do on average, with which all pieces are kKvqCus / 2 chunks and a part of one more to each; rounded to `least` pieces, four or more (lists: two),
+// it may come out short by a part in least + 1.
+static long kvq_more_wgs(long once, bool lists) { return std::max<long>(kKvqCus - once, kKvqCus / 2 * (lists ? 3 : 5) / (lists ? 2 : 4)); }
+
+// What holds this call and every one like it whose contexts, or lists, are shorter: of those it is often a shorter one that has most pieces.
 size_t kvq_workspace_bytes(const KvqArgs& a, int n_layers, int hd) {
-  return kvq_joined(a) ? a.part_pitch * a.heads * n_layers * (hd * sizeof(float) + sizeof(float2)) : 0;
+  const KvqCut cut = kvq_cut(a, n_layers);
+  if (cut.whole) return 0;
+  const long hl = (long)a.heads * n_layers;
+  long wgs = 0, rows = 0;  // of a (layer, KV head), one chunk of everything
+  for (int i = 0; i < a.n_entries; ++i) {
+    wgs += a.n_blocks ? a.entry[i].n : a.entry[i].tiles;
+    rows += a.entry[i].n * a.group;
+  }
+  const long more = kvq_more_wgs(wgs * hl, a.n_blocks) / hl;
+  long parts = 0;
+  bool joined = false;
+  for (int i = 0; i < a.n_entries; ++i) {
+    const KvqEntry& e = a.entry[i];
+    // lists are all cut alike, into chunks of 64 entries at most
+    const long chunks = a.n_blocks ? std::min<long>(a.n_blocks, std::max<long>(1 + more / wgs, (a.n_blocks + 63) / 64))
+                                   : std::min<long>((e.len + kStep - 1) / kStep, 1 + more / e.tiles);
+    joined = joined || chunks > 1;
+    parts += e.n * a.group * chunks;
+  }
+  if (!a.n_blocks) parts = std::min(parts, rows + more * std::min(16 * cut.tiles, cut.rows));
+  return joined ? (size_t)(parts * hl) * kvq_part_bytes(hd) : 0;
+}
+
+// ... and every call of up to max_tokens new tokens of a sequence and lists of up to max_blocks.
+size_t kvq_workspace_limit(int n_seqs, int heads, int group, int n_layers, int hd, int max_tokens, int max_slots, int max_blocks) {
+  const long hl = (long)heads * n_layers, rows = (long)n_seqs * max_tokens * group * hl, tokens = (long)n_seqs * max_tokens * hl;
+  const long steps = (max_slots + kStep - 1) / kStep;
+  long parts = 0;
+  if (steps > kKvqWhole) parts = std::min(rows * steps, rows + kKvqCus * std::min(32, max_tokens * group));
+  if (2 * max_blocks > kKvqWhole)
+    parts = std::max(parts, std::min(rows * max_blocks, group * std::max({(long)kKvqCus, tokens + kvq_more_wgs(tokens, true), tokens * ((max_blocks + 63) / 64)})));
+  return (size_t)parts * kvq_part_bytes(hd);
 }
 
 void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t st) {

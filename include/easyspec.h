@@ -495,7 +495,8 @@ int64_t easyspec_kvq_select_workspace_bytes(const easyspec_kv_layout *layout, co
  *   logits_out  dev [rows][vocab] or NULL: the logits that stay, minus infinity for the others (all of them in a row without a token); may be
  *               logits.  softmax(logits_out / temperature) is what the token was drawn from: what easyspec_accept takes as draft_logits
  *               and, of the target's logits filtered alike, as target_logits
- *   workspace   dev, easyspec_sample_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ *   workspace   dev, easyspec_sample_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept.  Fewer rows or words
+ *               never need more
  *   hip_stream  the hipStream_t to launch on (NULL = the null stream); nothing is synchronised
  * Weights are worked out in double precision (to 2.2e-13) and kept as whole multiples of 2^-s, s = 62 - ceil(log2(vocab)) and 51 at most (45 at
  * 128 256 words), below 2^-48 as 0: sums of them are exact, so results do not depend on their order, and a decision can differ from that of the real numbers only

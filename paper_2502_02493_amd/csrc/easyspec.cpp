@@ -1355,7 +1355,7 @@ extern "C" int easyspec_sample(const float* logits, const float* u, int32_t rows
   if (misaligned({workspace}, 16) || misaligned({logits, u, tokens_out, logits_out}, 4)) return fail(nullptr, EASYSPEC_EINVAL, "sample: workspace must be 16-byte aligned, the other arrays 4-byte");
   const size_t words = (size_t)rows * vocab * sizeof(float);
   const Extent in = {logits, words}, us = {tokens_out ? u : nullptr, rows * sizeof(float)}, tokens = {tokens_out, rows * sizeof(int32_t)};
-  const Extent left = {logits_out, words}, ws = {workspace, sample_workspace_bytes(rows, vocab)};
+  const Extent left = {logits_out, words}, ws = {workspace, sample_bytes_used(rows, vocab)};
   if (writes_into({tokens, left, ws}, {us}) || writes_into({tokens, ws}, {in}) || (logits_out != logits && writes_into({left}, {in})))
     return fail(nullptr, EASYSPEC_EINVAL, "sample: arrays overlap (logits_out may be logits)");
   const int rc = check_arrays(nullptr, "sample", {tokens_out, logits_out, workspace}, {logits, us.p});

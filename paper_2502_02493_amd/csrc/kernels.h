@@ -358,7 +358,8 @@ void launch_kvq_select(const KvqSelectArgs& a, int n_layers, int hd, hipStream_t
 
 // Sampling; ws: sample_workspace_bytes() of scratch, 16-byte aligned.
 constexpr int kMaxSampleVocab = 1 << 20;
-size_t sample_workspace_bytes(int rows, int V);
+size_t sample_bytes_used(int rows, int V);
+size_t sample_workspace_bytes(int rows, int V);  // what holds calls of fewer rows or words too
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
                    float* logits_out, void* ws, hipStream_t st);
 

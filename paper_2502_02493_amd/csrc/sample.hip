@@ -915,7 +915,9 @@ __global__ __launch_bounds__(kFinishNT) void sample_finish_kernel(SampleArgs a) 
 // 152 064 502 : 403.  Rows that fill the chip by themselves gain little: 1200 of 152 064 849 : 792, with top_k 676 : 715.
 static bool whole_rows(int rows, int V) { return V <= kRowWords || rows > kMaxSlicedRows; }
 static size_t sample_row_bytes() { return kMaxSlices * sizeof(float2) + kBins * sizeof(u64) + (kBins + 1) * sizeof(uint32_t) + kNear * sizeof(u64) + sizeof(NearBins); }
-size_t sample_workspace_bytes(int rows, int V) { return whole_rows(rows, V) ? 16 : rows * sample_row_bytes(); }
+size_t sample_bytes_used(int rows, int V) { return whole_rows(rows, V) ? 16 : rows * sample_row_bytes(); }
+// ... and by any call of fewer rows or words: more than kMaxSlicedRows rows need none, but a call of some of them may follow.
+size_t sample_workspace_bytes(int rows, int V) { return sample_bytes_used(std::min(rows, kMaxSlicedRows), V); }
 
 void launch_sample(const float* logits, const float* u, int rows, int V, double T, int top_k, double top_p, double min_p, int32_t* tokens_out,
                    float* logits_out, void* ws, hipStream_t st) {

@@ -462,8 +462,9 @@ int64_t easyspec_kvq_attention_workspace_limit(const easyspec_kv_layout *layout,
 
 /* The blocks that matter to a new token, for every layer and KV head: of the blocks that hold a slot it sees, the first keep_first, the last
  * keep_last and, of the others, those with the highest
- *   score(j) = max over the query heads of the KV head of  sum over channels d of max(q_d lo_jd, q_d hi_jd),
- * which no q . k_s of the block exceeds: n_select in all, or all there are.  Of equal scores the lowest block goes first, a score of NaN (passed
+ *   score(j) = max over the query heads of the KV head of  sum over channels d of  q_d hi_jd where q_d > 0, q_d lo_jd elsewhere,
+ * which no q . k_s of the block exceeds: n_select in all, or all there are.  A block without a number in some channel (lo plus, hi minus infinity: every
+ * q . k_s is NaN) thus has a score of minus infinity or NaN and goes behind all others.  Of equal scores the lowest block goes first, a score of NaN (passed
  * over where another query head has a number) last; scores are compared in double precision.  If n_select < keep_first + keep_last the
  * lowest of those stay.
  *   k_bounds     dev       as easyspec_kvq_store keeps them

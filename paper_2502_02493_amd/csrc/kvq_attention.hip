@@ -753,7 +753,8 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
 // ------------------------------------------------------------------------------------------
 // grid (groups of blocks of all entries, KV heads, layers).  G: query heads of a KV head, or one more: their queries are requested together.
 // Products and sums are fp64, whose operands are exact: blocks are compared with each other, and a
-// rounding that went one way for one and the other way for its neighbour would show as another list.  Bound: the chain of two loads, and eight products a lane
+// rounding that went one way for one and the other way for its neighbour would show as another list.  The bound that a channel takes goes by q's sign: where a
+// block has no number (plus, minus infinity), the larger of both products would be plus infinity, and NaN be read first.  Bound: the chain of two loads, and eight products a lane
 // and query; 512 blocks of 8 KV heads, one token 3.6 us (0.3 of bytes), sixteen sequences of 63 .. 250 blocks with seven heads to a KV head 5.9.
 template <int HD, int G>
 __global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {

@@ -282,7 +282,7 @@ constexpr float kHeadroom = 8.f;
 template <int HD, bool FOLD>
 struct KvqRows {
   static constexpr int CPV = HD / 16;  // channels of V that a lane takes
-  float m = kLowest, shift = 0.f;      // shift: -m, 0 while there is none; where the first product's accumulator starts
+  float m = kLowest, shift = 0.f;      // shift: -m, 0 while there is none
   float l = 0.f;                       // sum of the lane's own slots' weights
   f32x4 o[CPV];                        // o[j][i]: channel (4 (l / 16) + i) CPV + j (FOLD: term l % 16 / 4 of it)
 
@@ -290,8 +290,9 @@ struct KvqRows {
 #pragma unroll
     for (int j = 0; j < CPV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // Scores, shifted, -> weights, as the fragments of the second product.  edge: some row does not see all of the step's slots; seen: how many the
-  // lane's does.
+  // Scores -> weights, as the fragments of the second product.  edge: some row does not see all of the step's slots; seen: how many the
+  // lane's does.  The shift is added to whole scores: an accumulator that started from it would round them to the last place of a reference that may lie
+  // far below, of a step of slots that hardly count.  (Four sequences of 6 tokens at 4096 .. 32768 slots 30.4 us, 30.0 that way; others within 1%.)
   __device__ __forceinline__ void weigh(f32x4 (&x)[2], bool edge, int s, int seen, u32x4 (&pf)[FOLD ? 1 : 3]) {
     const int lane = threadIdx.x & 63, g = lane >> 4;
     if (edge) {
@@ -301,27 +302,23 @@ struct KvqRows {
         for (int i = 0; i < 4; ++i) x[t][i] = s + 16 * t + 4 * g + i < seen ? x[t][i] : -INFINITY;
     }
     float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-    if (__any(top > kHeadroom || m == kLowest)) {
-      top = fmaxf(m, over_groups_max(top - shift));
-      const float f = pow2(m - top), back = top == kLowest ? 0.f : -top - shift;
+    if (__any(top + shift > kHeadroom || m == kLowest)) {
+      top = fmaxf(m, over_groups_max(top));
+      const float f = pow2(m - top);
       l *= f;
 #pragma unroll
       for (int j = 0; j < CPV; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[j][i] *= f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[t][i] += back;
       m = top;
-      shift += back;
+      shift = top == kLowest ? 0.f : -top;
     }
     float p[8];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[4 * t + i] = pow2(x[t][i]);
+        p[4 * t + i] = pow2(x[t][i] + shift);
         l += p[4 * t + i];
       }
     // in three terms (FOLD: the lane's column takes its own)
@@ -352,12 +349,9 @@ __device__ __forceinline__ void add_step(KvqRows<HD, FOLD> (&R)[RT], KvqStep<HD>
   const int g = (threadIdx.x & 63) >> 4;
   f32x4 x[RT][2];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    // FOLD: the shift in the columns of one term, whose sum they become
-    const float start = !FOLD || (threadIdx.x & 12) == 0 ? R[r].shift : 0.f;
+  for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) x[r][t] = f32x4{start, start, start, start};
-  }
+    for (int t = 0; t < 2; ++t) x[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   i32x8 k[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {

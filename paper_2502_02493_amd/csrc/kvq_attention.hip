@@ -303,15 +303,15 @@ struct KvqRows {
     }
     float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
     if (__any(top + shift > kHeadroom || m == kLowest)) {
-      top = fmaxf(m, over_groups_max(top));
-      const float f = pow2(m - top);
+      // by the row's own scores: a row that others' moves moved would have bits that go by slots it does not see
+      const float highest = over_groups_max(top), to = highest + shift > kHeadroom || m == kLowest ? fmaxf(m, highest) : m, f = pow2(m - to);
       l *= f;
 #pragma unroll
       for (int j = 0; j < CPV; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[j][i] *= f;
-      m = top;
-      shift = top == kLowest ? 0.f : -top;
+      m = to;
+      shift = to == kLowest ? 0.f : -to;
     }
     float p[8];
 #pragma unroll

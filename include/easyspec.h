@@ -435,7 +435,9 @@ int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layou
  *   out = sum over slots s of softmax_s(q . k_s / sqrt(head_dim)) v_s
  * The new tokens of sequence b, n_tokens[b] of them, are its last (their slots stored): token t sits in slot lens[b] - n_tokens[b] + t and
  * attends to the slots up to its own.  What a slot holds that a token does not see has no effect on it, values that are not finite among them.
- * Everything is as exact as fp32 arithmetic (queries to 2^-24 of the largest magnitude of their 32 neighbouring channels).
+ * Everything is as exact as fp32 arithmetic (queries to 2^-24 of the largest magnitude of their 32 neighbouring channels) while the largest magnitude of V
+ * times the slots that a token sees is below 2^119 (V below 2^103: whatever the length); beyond that a result may be infinite or NaN.  Weights below 2^-126 of the highest
+ * may count as 0.  A query with a channel that is not finite has NaN as its results.
  *   q            dev fp32 [n_layers][sum of n_tokens][n_q_heads][head_dim]  rotated queries, sequences in index order
  *   n_tokens     host [n_seqs]  0..EASYSPEC_MAX_CALIB_TOKENS
  *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots

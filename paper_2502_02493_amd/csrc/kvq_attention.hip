@@ -277,7 +277,8 @@ __device__ __forceinline__ float over_groups_sum(float x) {
 
 // The running softmax of a wave's share of a row tile: row l % 16 (FOLD: l % 4) in lane l.  Weights are taken relative to a reference m, a score that
 // was the highest once: it moves only when one lies more than kHeadroom above it, since every move multiplies the results, and 2^kHeadroom times too
-// large a weight is as exact.
+// large a weight is as exact.  What is added up of V is that much larger too: it stays finite while slots times the largest V are below 2^119.  (A reference
+// that starts kHeadroom above the score would lose weights below 2^-118 of the highest instead of those below 2^-126.)
 constexpr float kHeadroom = 8.f;
 template <int HD, bool FOLD>
 struct KvqRows {

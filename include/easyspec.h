@@ -415,7 +415,8 @@ typedef struct easyspec_kvq { /* a host struct of dev arrays, contiguous, for an
 /* Slots brought into such a cache: of sequence b, slots src_from[b] .. src_from[b] + n_slots[b] - 1 of k, v become its slots from to[b] on.
  *   k, v      dev  [n_layers][n_seqs][n_kv_heads][src_slots][head_dim] in layout->dtype, 16-byte aligned: a cache, one that
  *                  easyspec_kv_export filled (n_seqs = 1, src_slots its n_slots), or the new tokens' keys and values
- *   src_from, n_slots, to   host [n_seqs]; n_slots[b] = 0: the sequence is left alone
+ *   src_from, n_slots, to   host [n_seqs]; n_slots[b] = 0: the sequence is left alone, its entries of the other arrays
+ *                  (lens too) are not looked at
  *   lens      host [n_seqs]  slots that the sequence holds after the call, to[b] + n_slots[b] .. max_slots
  * k_bounds: those of every block that receives a slot become the bounds of its slots below lens[b], those that were there among
  * them (NaN is passed over; plus and minus infinity where nothing else is).  A sequence that is cut back keeps, in the block that the cut is in, bounds that cover the slots
@@ -440,8 +441,8 @@ int easyspec_kvq_load(const easyspec_kvq *cache, const easyspec_kv_layout *layou
  * may count as 0.  A query with a channel that is not finite has NaN as its results.
  *   q            dev fp32 [n_layers][sum of n_tokens][n_q_heads][head_dim]  rotated queries, sequences in index order
  *   n_tokens     host [n_seqs]  0..EASYSPEC_MAX_CALIB_TOKENS
- *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots
- *   n_q_heads    n_kv_heads times 1, 2, 4, 7 or 8
+ *   lens         host [n_seqs]  slots with the new tokens', n_tokens..max_slots; not looked at where n_tokens is 0
+ *   n_q_heads    n_kv_heads times 1, 2, 4, 7 or 8, 65535 at most
  *   blocks       dev [n_layers][sum of n_tokens][n_kv_heads][n_blocks], or NULL: every slot.  The blocks of EASYSPEC_KVQ_BLOCK slots that
  *                a token reads, ascending: an entry that is not above the entry in front of it (the first: above -1), or that names a
  *                block without a slot that the token sees, is passed over.  As easyspec_kvq_select writes them.

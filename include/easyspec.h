@@ -279,7 +279,8 @@ int64_t easyspec_accept_static_max_bytes(void);
  *   tokens_out  dev [groups][n_select]      the token; -1 where a group has fewer continuations than n_select
  *   parents_out dev [groups][n_select]      the beam it continues, 0..beams-1, or -1
  *   scores_out  dev [groups][n_select]      fp32, or minus infinity; may be `scores` if n_select == beams
- *   workspace   dev, easyspec_beam_select_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept
+ *   workspace   dev, easyspec_beam_select_workspace_bytes() bytes, 16-byte aligned; one call at a time; contents need not be kept.  A call of
+ *               other sizes, smaller ones among them, may need more
  *   hip_stream  the hipStream_t to launch on (NULL = the null stream); nothing is synchronised
  * Logits of minus infinity and NaN are no continuations and add nothing to the sum; a beam with a logit of plus infinity, or
  * with none that is finite, offers nothing.  A beam selection over sequences 0..beams-1 of a context takes the logits of a
@@ -342,7 +343,8 @@ int easyspec_beam_reorder(easyspec_ctx *ctx, int32_t first, int32_t count, const
  *   weights_in   dev fp32 [n_layers][n_seqs][n_kv_heads][max_slots], read up to the new tokens' slots, which start from zero;
  *                NULL: zeros
  *   weights_out  dev, the same shape; slots from lens[b] on are left as they were; may be weights_in
- *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time
+ *   workspace    dev, easyspec_attn_weights_workspace_bytes() bytes, 16-byte aligned; one call at a time.  That is what this call needs: a
+ *                call with other n_tokens or lens, shorter ones among them, may need more
  * The same call gives the same bits.  How the contexts are cut goes by the longest of the call and by its most query rows, so in the
  * last bits a sequence's weights may differ with the other sequences of the call.
  * Launched on hip_stream, nothing is synchronised.  EASYSPEC_EINVAL for NULL pointers (q and workspace may be NULL if no sequence

@@ -64,7 +64,7 @@ __device__ __forceinline__ int entry_of(const KvqMoveArgs& a) {
 // the block: those that were there are read back, which a block's workgroup alone writes.
 // Bound: memory.  2048 slots of bf16 in 32 layers of 8 KV heads of 128, 268 MB read and 73 written: 72 us (4.7 TB/s; a copy that moves as many bytes
 // 65), the bounds 8 of them.  What is read once goes past the caches (91 us otherwise), what is written, which the next attention reads, does not
-// (codes written past them too: 4 us more).  One slot of each of sixteen sequences: 4.6 us, a launch and three rounds through memory.
+// (codes written past them too: 4 us more).  Of fp32, 537 MB read and 73 written, 114 us (5.3 TB/s).  One slot of each of sixteen sequences: 4.6 us, a launch and three rounds through memory.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
   constexpr int kOcts = HD / 8, kUnits = kKvqBlock * kOcts, kTurns = kUnits / 256;
@@ -137,6 +137,8 @@ __global__ __launch_bounds__(256) void kvq_store_kernel(KvqMoveArgs a) {
 
 // The way back: a lane takes eight channels of a slot.  Bound: memory, by what it writes, past the caches: the same 2048 slots 49 us (6.9 TB/s
 // of reads and writes), 57 through them.  Both launches with one octet under way in a lane 141 us, two 116, four 118, eight 119.
+// Into fp32, 73 MB read and 537 written, 249 us (2.4 TB/s): a lane writes two pieces of 16 bytes, so that a store of the wave leaves every other piece out;
+// how much of the time that is has not been measured apart.
 constexpr int kLoadTurns = 2;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kvq_load_kernel(KvqMoveArgs a) {

@@ -16,9 +16,11 @@
 // The running maximum, sum and result of a row stay in the lanes of its column; nothing passes through LDS until a wave's share of
 // the context is done.
 // Bound: a single token by the chain of one step a wave (2048 slots of 8 KV heads 6.9 us and 3.7 of the join; 0.3 us of bytes), long contexts with many
-// rows by the instructions of a step on two waves a SIMD: 48 products of 16 cycles, 20 of the other kind and some 230 vector instructions for 32 slots of 32 rows.
-// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 30 us in a graph (34 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
-// heads, 112 rows each, 18.5 (20.3); a large bf16 product's rate would allow 13 and 6.
+// rows by the instructions of a step on two waves a SIMD: 48 products of 16 cycles, 20 of the other kind and some 240 vector instructions for 32 slots of 32 rows.
+// Four sequences of 6 tokens at 4096 .. 32768 slots of 8 KV heads 30.6 us in a graph (34 with K as bf16 too, in three terms), sixteen of 16 tokens at 512 .. 1067 on 4
+// heads, 112 rows each, 18.9 (20.3); a large bf16 product's rate would allow 13 and 6.  Over lists every token has workgroups of its own, which read and convert a
+// block again that several tokens list: 32 blocks for each of those four sequences' tokens 24.3 us, 24 for each of sixteen sequences' 16 tokens, seven heads to a KV
+// head, 69.
 #include "launch_common.hpp"
 #include "lane_ops.hpp"
 
@@ -750,7 +752,8 @@ void launch_kvq_attention(const KvqArgs& args, int n_layers, int hd, hipStream_t
 // Products and sums are fp64, whose operands are exact: blocks are compared with each other, and a
 // rounding that went one way for one and the other way for its neighbour would show as another list.  The bound that a channel takes goes by q's sign: where a
 // block has no number (plus, minus infinity), the larger of both products would be plus infinity, and NaN be read first.  Bound: the chain of two loads, and eight products a lane
-// and query; 512 blocks of 8 KV heads, one token 3.6 us (0.3 of bytes), sixteen sequences of 63 .. 250 blocks with seven heads to a KV head 5.9.
+// and query; 512 blocks of 8 KV heads, one token 3.6 us (0.3 of bytes), sixteen sequences of 63 .. 250 blocks with seven heads to a KV head 5.9;
+// several tokens one after the other: four sequences of 6 tokens at 64 .. 512 blocks 9.3, sixteen of 16 at 63 .. 180 on 4 heads 33.7.
 template <int HD, int G>
 __global__ __launch_bounds__(256) void kvq_score_kernel(KvqSelectArgs a) {
   constexpr int LANES = HD / 8, BLOCKS = 256 / LANES;  // lanes to a block: eight channels each
